@@ -4,7 +4,8 @@ One step of serving over the paged cache is: page assignment and slot map (plan)
 (append), attention of the new tokens over the cache (attention), verification of drafted tokens (verify).  Training
 takes the same norm + rotation between the QKV projection and the attention (rope_fwd, rope_bwd).
 
-`run` computes an operator in elementary torch operations, or through the package's entry points where `own` is true.
+`run` computes an operator in elementary torch operations, or through the package's entry points where `own` is true.  A
+serving loop keeps the buffers of its step's outputs, as its captured graph needs; a training step allocates them.
 """
 import math
 import random
@@ -159,6 +160,7 @@ def prepare(case, seed):
         if own:
             from paper_2609_13141_gb300 import sas
             s["chunk"] = sas.SasChunk(case["seqs"], 1, 1, 64, case["max_blocks"], P, s["T"])
+            s["out"] = s["chunk"].plan_buffers(case["seqs"], s["T"], DEV)
     elif kind == "append":
         cached, new = lengths(case)
         T, H = sum(new), case["Hq"] + 2 * case["Hkv"]
@@ -178,6 +180,7 @@ def prepare(case, seed):
         if own:
             from paper_2609_13141_gb300 import sas
             s["chunk"] = sas.SasChunk(len(new), case["Hq"], case["Hkv"], case["d"], table.shape[1], touched.numel(), T)
+            s["out"] = torch.empty(T, case["Hq"], case["d"], dtype=torch.bfloat16, device=DEV)
     elif kind in ("rope_fwd", "rope_bwd"):
         B, N, Hq, Hkv, d = (case[k] for k in ("B", "N", "Hq", "Hkv", "d"))
         cos, sin = _tables(N, case["rot"])
@@ -202,6 +205,7 @@ def prepare(case, seed):
         if own:
             from paper_2609_13141_gb300 import sas
             s["chunk"] = sas.SasChunk(len(new), case["Hq"], case["Hkv"], d, table.shape[1], P, T)
+            s["out"] = torch.empty_like(s["Q"]), torch.empty(T, case["Hq"], device=DEV)
     else:
         counts, V = draft_counts(case), case["V"]
         B, Td = case["seqs"], sum(counts)
@@ -222,6 +226,7 @@ def prepare(case, seed):
         if own:
             from paper_2609_13141_gb300 import sas
             s["chunk"] = sas.SasChunk(B, 1, 1, 64, 1, 1, max(1, Td))
+            s["out"] = _ints([0] * B), _ints([[0] * (case["drafts"] + 1)] * B)
     return s
 
 
@@ -365,12 +370,12 @@ def run(s):
     if not own:
         return PLAIN[kind](s)
     if kind == "plan":
-        p = s["chunk"].plan(s["seq_lens"], s["new_lens"], s["free_pages"], s["free_begin"], s["table"], s["T"])
+        p = s["chunk"].plan(s["seq_lens"], s["new_lens"], s["free_pages"], s["free_begin"], s["table"], s["T"], out=s["out"])
         return dict(kv_lens=p.kv_lens, cu=p.cu_new, positions=p.positions, slots=p.slots, free_end=p.free_end,
                     table=s["table"])
     if kind == "append":
         Q = s["chunk"].append(s["qkv"], s["wq"], s["wk"], s["cos"], s["sin"], s["positions"], s["slots"], s["K_cache"],
-                              s["V_cache"], eps=EPS, interleaved=s["inter"])
+                              s["V_cache"], eps=EPS, interleaved=s["inter"], out=s["out"])
         return dict(Q=Q, K_cache=s["K_cache"], V_cache=s["V_cache"])
     if kind == "rope_fwd":
         Q, K, V = s["layer"].qk_norm_rope(s["qkv"], s["wq"], s["wk"], s["cos"], s["sin"], eps=EPS, interleaved=s["inter"])
@@ -380,9 +385,10 @@ def run(s):
                                                      s["dV"], eps=EPS, interleaved=s["inter"])
         return dict(dqkv=dqkv, dwq=dwq, dwk=dwk)
     if kind == "attention":
-        O, LSE = s["chunk"].attention(s["Q"], s["K_cache"], s["V_cache"], s["table"], s["cu"], s["kv_lens"])
+        O, LSE = s["chunk"].attention(s["Q"], s["K_cache"], s["V_cache"], s["table"], s["cu"], s["kv_lens"], out=s["out"])
         return dict(O=O, LSE=LSE)
-    accepted, tokens = s["chunk"].verify(s["tokens"], s["cu"], s["target"], s["draft"], s["u"], s["noise"], s["drafts"])
+    accepted, tokens = s["chunk"].verify(s["tokens"], s["cu"], s["target"], s["draft"], s["u"], s["noise"], s["drafts"],
+                                         out=s["out"])
     return dict(accepted=accepted, tokens=tokens)
 
 
