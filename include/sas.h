@@ -300,6 +300,53 @@ sas_status sas_attention_fwd_varlen(sas_handle* h, const int32_t* cu_seqlens, in
                                     const void* Wq, const void* Wk,
                                     void* O, float* LSE, int32_t* sel_idx, float* sel_logg, void* stream);
 
+/* Per-head RMS norm of queries and keys with the rotary position rotation, in
+ * one pass from a layer's fused projection to the layouts sas_attention_fwd
+ * reads, and its gradient.  (The paper has no counterpart: its backbones'
+ * attention layers, e.g. Qwen3's, compute it between the projection and the
+ * attention.)
+ *
+ * For a head row x of a query or key at position p, with the norm weight w:
+ *   xh = x / sqrt(mean(x^2) + eps),  z = w xh,  y = R_p z,
+ * R_p rotating pair i of the first `rot` dims, y_a = z_a c - z_b s, y_b = z_b c
+ * + z_a s with c = cos[p][i], s = sin[p][i]; pair i is (i, i + rot / 2), or (2i,
+ * 2i + 1) when interleaved; dims past rot pass.  Value rows pass unchanged.
+ * fp32 arithmetic, one rounding to bf16. */
+typedef struct {
+    int32_t rot;          /* rotated dims of a head: a multiple of 16, 16 .. d            */
+    int32_t interleaved;  /* pairs: 0 (i, i + rot / 2), 1 (2i, 2i + 1)                   */
+    int32_t max_pos;      /* rows of the cos and sin tables                              */
+    float eps;            /* >= 0, added to the mean square                              */
+} sas_rope_config;
+
+/*   qkv        bf16, token (b, n) at row b N + n: H query heads, then Hkv key
+ *              heads, then Hkv value heads of d elements each; rows `ld`
+ *              elements apart (ld >= (H + 2 Hkv) d, a multiple of 8)         (in)
+ *   wq, wk     bf16 [d] norm weights of queries and keys                   (in)
+ *   cos, sin   fp32 [max_pos, rot / 2], 16-byte aligned                    (in)
+ *   positions  int32 [B, N], or NULL for position n of token (b, n) (then
+ *              max_pos >= N).  Read on the device: a token whose position is
+ *              outside the tables is skipped (its outputs are not written) and
+ *              the device status word becomes SAS_ERR_INVALID_ARG           (in)
+ *   Q, K, V    bf16 [B, H, N, d], [B, Hkv, N, d], [B, Hkv, N, d]           (out)
+ * Packed-sequence handles (B = 1): give each token's position in its sequence.
+ * Outputs must not overlap inputs. */
+sas_status sas_qk_norm_rope_fwd(sas_handle* h, const sas_rope_config* rope, const void* qkv, int64_t ld,
+                                const void* wq, const void* wk, const float* cos, const float* sin,
+                                const int32_t* positions, void* Q, void* K, void* V, void* stream);
+
+/* Gradient of sas_qk_norm_rope_fwd, from its inputs (nothing is kept between
+ * the two calls): dz = R_p^T dy, u = w dz, dx = (u - xh mean(u xh)) / sqrt(mean(
+ * x^2) + eps), dw = sum of dz xh over all tokens and heads.
+ *   dQ, dK, dV  bf16, the layouts of Q, K, V                                (in)
+ *   dqkv        bf16, the layout of qkv with row stride ld_d               (out)
+ *   dwq, dwk    fp32 [d]; summed in a fixed order                          (out)
+ * One launch, no allocation, no synchronisation. */
+sas_status sas_qk_norm_rope_bwd(sas_handle* h, const sas_rope_config* rope, const void* qkv, int64_t ld,
+                                const void* wq, const void* wk, const float* cos, const float* sin,
+                                const int32_t* positions, const void* dQ, const void* dK, const void* dV, void* dqkv,
+                                int64_t ld_d, float* dwq, float* dwk, void* stream);
+
 /* Dense MLP sublayer Y = GELU(X W1^T + b1) W2^T + b2 with the exact (erf)
  * GELU.  SAS itself does not define or change the MLP; this is the plain
  * transformer MLP that completes a layer.
@@ -375,9 +422,9 @@ sas_status sas_get_device_status(sas_handle* h, int32_t* out_status);
  * the number of launches and the summed milliseconds.  Kinds, in order:
  * 0 block summaries, 1 (unused: the selector's query projection runs inside
  * the selection kernel), 2 selection, 3 attention, 4 MLP up-projection +
- * GELU, 5 MLP down-projection, 6 attention backward (all its kernels).
- * n_kinds <= 7. */
-#define SAS_NUM_KERNEL_KINDS 7
+ * GELU, 5 MLP down-projection, 6 attention backward (all its kernels), 7 norm +
+ * rotation and its gradient.  n_kinds <= 8. */
+#define SAS_NUM_KERNEL_KINDS 8
 sas_status sas_set_timing(sas_handle* h, int32_t enable);
 sas_status sas_get_timings(sas_handle* h, int64_t* launches, double* total_ms, int32_t n_kinds);
 
@@ -530,6 +577,140 @@ sas_status sas_decode_get_timings(sas_decode_handle* h, int64_t* launches, doubl
 
 /* Kernels this handle has launched since creation. */
 int64_t sas_decode_launch_count(const sas_decode_handle* h);
+
+/* ================================================================ serving step
+ *
+ * One step of serving over the paged cache of the decode section, for sequences
+ * that each get any number of new tokens (a prompt chunk, a few drafted tokens, a
+ * single token, none): page plan, norm + rotation + append, dense causal attention
+ * of the new tokens over the cache, verification of drafted tokens.  (The paper
+ * prefills before it decodes and has no counterpart of these.)  After a prompt is
+ * in the cache, sas_decode_summarize and sas_decode_step continue on the same
+ * cache, block table and lengths.
+ *
+ * Lengths, offsets, slots, page and token indices are read on the device: nothing
+ * here synchronises or allocates after sas_chunk_create, and a captured step can be
+ * replayed while they change.  An index out of range is never used as an address;
+ * each entry point says what happens instead, and the device status word tells. */
+
+typedef struct {
+    int32_t max_seqs;     /* sequences of a call, at most (1 .. 8192)                       */
+    int32_t Hq, Hkv;      /* query heads and KV heads; Hq / Hkv in {1, 2, 4, 8}             */
+    int32_t d;            /* head dim, 64 or 128                                           */
+    int32_t block;        /* tokens of a page; must be 64                                  */
+    int32_t max_blocks;   /* block-table width, <= 32768                                   */
+    int32_t num_pages;    /* pages in K_cache / V_cache (num_pages * Hkv < 2^31)            */
+    int32_t max_tokens;   /* new tokens of a call, at most (1 .. 2^26)                      */
+    float sm_scale;       /* scale on q.k; 0 selects 1/sqrt(d)                             */
+} sas_chunk_config;
+
+typedef struct sas_chunk_handle sas_chunk_handle;
+
+/* Validates cfg and allocates the handle's workspace on the current device (the
+ * one its calls must run on): the attention's work list and split results (80 MB at
+ * d = 128) and small arrays.  Synchronous. */
+sas_status sas_chunk_create(const sas_chunk_config* cfg, sas_chunk_handle** out);
+void sas_chunk_destroy(sas_chunk_handle* h);
+
+/* Page plan of a step: gives every request the pages its new tokens need and maps
+ * the new tokens to cache slots.  With s = seq_lens[b], n = new_lens[b], request b
+ * goes from ceil(s / 64) to ceil((s + n) / 64) pages; new pages are taken from
+ * free_pages in request order, starting at free_pages[*free_begin].
+ *   num_seqs     requests, 1 .. max_seqs
+ *   T            capacity of positions and slots, 1 .. max_tokens
+ *   seq_lens     int32 [num_seqs] tokens in the cache                          (in)
+ *   new_lens     int32 [num_seqs] new tokens, 0 allowed                        (in)
+ *   free_pages   int32 [num_free] unused pages, taken front to back            (in)
+ *   free_begin   int32 [1] first one not yet taken                             (in)
+ *   block_table  int32 [num_seqs, max_blocks]: entries of the new pages written (in/out)
+ *   kv_lens      int32 [num_seqs] s + n                                       (out)
+ *   cu_new       int32 [num_seqs + 1] first new token of each request         (out)
+ *   positions    int32 [T] position of each new token in its request, -1 past
+ *                cu_new[num_seqs]                                             (out)
+ *   slots        int64 [T] page * 64 + position % 64, -1 past the end         (out)
+ *   free_end     int32 [1] *free_begin + pages taken                          (out)
+ * All or nothing: if a length is negative or passes 64 max_blocks, more than T new
+ * tokens or free_begin out of 0 .. num_free (status SAS_ERR_INVALID_ARG), or too
+ * few pages are left (SAS_ERR_OOM), nobody gets anything: the table is not written,
+ * kv_lens = seq_lens, cu_new = 0, positions and slots -1, free_end = free_begin.  A
+ * page index outside the cache, from the list or of a held partly filled page,
+ * makes its tokens' position and slot -1 (a new one's table entry too) and sets
+ * SAS_ERR_INVALID_ARG.  kv_lens and free_end must not be the inputs' memory.
+ * One launch. */
+sas_status sas_chunk_plan(sas_chunk_handle* h, int32_t num_seqs, int32_t T, const int32_t* seq_lens,
+                          const int32_t* new_lens, const int32_t* free_pages, int32_t num_free,
+                          const int32_t* free_begin, int32_t* block_table, int32_t* kv_lens, int32_t* cu_new,
+                          int32_t* positions, int64_t* slots, int32_t* free_end, void* stream);
+
+/* Norm + rotation of the new tokens' queries and keys (as sas_qk_norm_rope_fwd, heads
+ * Hq and Hkv), keys and values written into the cache.
+ *   qkv        bf16 [T] rows, `ld` elements apart, as in sas_qk_norm_rope_fwd  (in)
+ *   positions  int32 [T]; slots int64 [T] (as sas_chunk_plan writes them; no slot
+ *              twice)                                                        (in)
+ *   Q          bf16 [T, Hq, d]                                               (out)
+ *   K_cache, V_cache  bf16 [num_pages, Hkv, 64, d]                        (in/out)
+ * A token of slot -1 is skipped: nothing of it is written.  So is one whose slot is
+ * outside the cache or position outside the tables, with status
+ * SAS_ERR_INVALID_ARG.  One launch. */
+sas_status sas_chunk_append(sas_chunk_handle* h, const sas_rope_config* rope, int32_t T, const void* qkv, int64_t ld,
+                            const void* wq, const void* wk, const float* cos, const float* sin,
+                            const int32_t* positions, const int64_t* slots, void* Q, void* K_cache, void* V_cache,
+                            void* stream);
+
+/* Dense causal attention of the new tokens over the paged cache, which holds them
+ * already: token i of request b (i = 0 .. n - 1, n = cu_new[b + 1] - cu_new[b]) has
+ * position kv_lens[b] - n + i and attends to every token of its request up to itself.
+ *   Q            bf16 [T, Hq, d], request b's tokens at rows cu_new[b] ..       (in)
+ *   K_cache, V_cache  bf16 [num_pages, Hkv, 64, d]                            (in)
+ *   block_table  int32 [num_seqs, max_blocks]                                 (in)
+ *   cu_new       int32 [num_seqs + 1]; kv_lens int32 [num_seqs]               (in)
+ *   O            bf16 [T, Hq, d]; LSE fp32 [T, Hq] natural log, or NULL       (out)
+ * Rows past cu_new[num_seqs] are not written; requests without new tokens cost
+ * nothing.  What a page holds past a request's end does not matter.  Offsets that
+ * decrease or leave 0 .. T: nothing is computed; n > kv_lens[b] or kv_lens[b] > 64
+ * max_blocks: that request is skipped; a page index outside the cache reads as zero
+ * keys and values; each with status SAS_ERR_INVALID_ARG.  Two launches. */
+sas_status sas_chunk_attention(sas_chunk_handle* h, int32_t num_seqs, int32_t T, const void* Q, const void* K_cache,
+                               const void* V_cache, const int32_t* block_table, const int32_t* cu_new,
+                               const int32_t* kv_lens, void* O, float* LSE, void* stream);
+
+/* Verification of drafted tokens.  Request b drafted x_0 .. x_{n-1} (n = cu_draft[b +
+ * 1] - cu_draft[b]), x_j drawn from q_j; the target model's distributions are p_0 ..
+ * p_n.  x_j is accepted while u_j q_j(x_j) < p_j(x_j).  The next token after the a
+ * accepted ones is argmax_v w_v / e_v (the lowest v of equal ones) over v with w_v >
+ * 0 and e_v > 0, w = max(p_a - q_a, 0) after a rejection, or p_a where that is zero
+ * everywhere or all drafts were accepted.  With u uniform on [0, 1) and e exponential
+ * (Exp(1)) the tokens are distributed as the target's own.
+ *   num_drafts  drafts of all requests; max_draft: columns of out_tokens - 1
+ *   tokens      int32 [num_drafts]; cu_draft int32 [num_seqs + 1]               (in)
+ *   target      fp32 [num_drafts + num_seqs] rows of V, ld_target apart: request
+ *               b's rows p_0 .. p_n start at row cu_draft[b] + b                (in)
+ *   draft       fp32 [num_drafts] rows of V, ld_draft apart, or NULL: the drafts
+ *               were certain (q = 1 at the drafted token)                       (in)
+ *   u           fp32 [num_drafts]; noise fp32 [num_seqs] rows of V, ld_noise apart (in)
+ *   accepted    int32 [num_seqs]                                               (out)
+ *   out_tokens  int32 [num_seqs, max_draft + 1]: the accepted drafts, the next
+ *               token, then -1                                                 (out)
+ * tokens, u and draft may be NULL when num_drafts is 0.  Offsets that decrease, leave 0
+ * .. num_drafts or give a request more than max_draft drafts: that request gets 0
+ * accepted and all -1; a drafted token outside 0 .. V - 1 is rejected; a row without
+ * a positive weight gives the token -1; each with status SAS_ERR_INVALID_ARG.
+ * One launch. */
+sas_status sas_chunk_verify(sas_chunk_handle* h, int32_t num_seqs, int32_t num_drafts, int32_t max_draft, int32_t V,
+                            const int32_t* tokens, const int32_t* cu_draft, const float* target, int64_t ld_target,
+                            const float* draft, int64_t ld_draft, const float* u, const float* noise, int64_t ld_noise,
+                            int32_t* accepted, int32_t* out_tokens, void* stream);
+
+/* As their sas_decode_ counterparts.  Kinds: 0 plan, 1 append, 2 attention (both its
+ * kernels), 3 verification.  n_kinds <= 4. */
+const char* sas_chunk_last_error(const sas_chunk_handle* h);
+sas_status sas_chunk_get_device_status(sas_chunk_handle* h, int32_t* out_status);
+#define SAS_CHUNK_NUM_KERNEL_KINDS 4
+sas_status sas_chunk_set_timing(sas_chunk_handle* h, int32_t enable);
+sas_status sas_chunk_get_timings(sas_chunk_handle* h, int64_t* launches, double* total_ms, int32_t n_kinds);
+int64_t sas_chunk_launch_count(const sas_chunk_handle* h);
+/* Failure-path diagnostics of the attention's waits, as sas_set_wait_limit. */
+sas_status sas_chunk_set_wait_limit(sas_chunk_handle* h, int64_t cycles);
 
 #ifdef __cplusplus
 }

@@ -36,11 +36,16 @@ void resolve_encode() {
 
 int make_tmap_bf16_3d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t outer,
                       uint32_t box_inner, uint32_t box_rows) {
+    return make_tmap_bf16_box(map, base, inner, rows, outer, box_inner, box_rows, 1);
+}
+
+int make_tmap_bf16_box(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t outer,
+                       uint32_t box_inner, uint32_t box_rows, uint32_t box_outer) {
     std::call_once(g_encode_once, resolve_encode);
     if (g_encode == nullptr) return -1;
     cuuint64_t dims[3] = {inner, rows, outer};
     cuuint64_t strides[2] = {inner * 2, inner * rows * 2};
-    cuuint32_t box[3] = {box_inner, box_rows, 1};
+    cuuint32_t box[3] = {box_inner, box_rows, box_outer};
     cuuint32_t estr[3] = {1, 1, 1};
     CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -165,6 +170,9 @@ struct sas_handle {
     float* dense_lse = nullptr;     // [BHkv][N] soft normalisers of the given scores (hard-STE)
     size_t bwd_offs_bytes = 0;
     bool bwd_offs_bound = false;    // sized for the upper bound: no per-call read-back
+    // gradient of the norm + rotation: weight sums of each block, arrival counter
+    float* rope_part = nullptr;
+    int* rope_count = nullptr;
     // timing
     bool timing = false;
     std::vector<TimeRec> recs;
@@ -353,6 +361,9 @@ sas_status sas_create(const sas_config* cfg, sas_handle** out) {
     if (e == cudaSuccess) e = cudaMemset(h->status, 0, 16);
     if (e == cudaSuccess) e = alloc(&h->sched, 16);
     if (e == cudaSuccess) e = cudaMemset(h->sched, 0, 16);
+    if (e == cudaSuccess) e = alloc(&h->rope_part, static_cast<size_t>(sas::rope_bwd_max_blocks()) * 2 * c.d * 4);
+    if (e == cudaSuccess) e = alloc(&h->rope_count, 16);
+    if (e == cudaSuccess) e = cudaMemset(h->rope_count, 0, 16);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) {
         sas_status s = e == cudaErrorMemoryAllocation ? SAS_ERR_OOM : SAS_ERR_CUDA;
@@ -376,6 +387,8 @@ void sas_destroy(sas_handle* h) {
     cudaFree(h->tile_off);
     cudaFree(h->status);
     cudaFree(h->sched);
+    cudaFree(h->rope_part);
+    cudaFree(h->rope_count);
     cudaFree(h->full_lse);
     cudaFree(h->full_table);
     cudaFree(h->seg_union_idx);
@@ -840,6 +853,82 @@ sas_status sas_attention_bwd(sas_handle* h, const void* Q, const void* K, const 
                        ((ag.ds != nullptr && ag.scores != nullptr && ag.topk > 0) ? 1 : 0);
     }
     return SAS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// Checks and arguments common to the norm + rotation and its gradient.
+sas_status rope_args(sas_handle* h, const sas_rope_config* rope, const void* qkv, int64_t ld, const void* wq,
+                     const void* wk, const float* cos, const float* sin, const int32_t* positions, sas::RopeArgs& a) {
+    const sas_config& c = h->cfg;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return fail(h, SAS_ERR_CUDA, "cudaGetDevice");
+    if (dev != h->device) return fail(h, SAS_ERR_INVALID_ARG, "the current device is not the handle's");
+    if (!rope || !qkv || !wq || !wk || !cos || !sin) return fail(h, SAS_ERR_INVALID_ARG, "a required argument is NULL");
+    if (!aligned16(qkv) || !aligned16(wq) || !aligned16(wk) || !aligned16(cos) || !aligned16(sin) || !aligned4(positions))
+        return fail(h, SAS_ERR_INVALID_ARG, "misaligned pointer");
+    if (const char* why = sas::rope_check(rope->rot, rope->interleaved, rope->max_pos, rope->eps, c.H + 2LL * h->Hkv, c.d, ld))
+        return fail(h, SAS_ERR_INVALID_ARG, why);
+    if (positions == nullptr && rope->max_pos < c.N)
+        return fail(h, SAS_ERR_INVALID_ARG, "max_pos must be at least N when positions are not given");
+    a.qkv = static_cast<const sas::bf16*>(qkv); a.ld = ld;
+    a.wq = static_cast<const sas::bf16*>(wq); a.wk = static_cast<const sas::bf16*>(wk);
+    a.cos = cos; a.sin = sin; a.pos = positions;
+    a.max_pos = rope->max_pos; a.rot = rope->rot; a.interleaved = rope->interleaved; a.eps = rope->eps;
+    a.Hq = c.H; a.Hkv = h->Hkv; a.T = static_cast<long long>(c.B) * c.N; a.N = c.N;
+    a.status = h->status;
+    if (!sas::rope_supported(a, c.d)) return fail(h, SAS_ERR_UNSUPPORTED, "too many rows for one launch");
+    return SAS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+sas_status sas_qk_norm_rope_fwd(sas_handle* h, const sas_rope_config* rope, const void* qkv, int64_t ld,
+                                const void* wq, const void* wk, const float* cos, const float* sin,
+                                const int32_t* positions, void* Q, void* K, void* V, void* stream) try {
+    if (h == nullptr) return SAS_ERR_INVALID_ARG;
+    sas::RopeArgs a{};
+    if (sas_status st = rope_args(h, rope, qkv, ld, wq, wk, cos, sin, positions, a); st != SAS_OK) return st;
+    if (!Q || !K || !V) return fail(h, SAS_ERR_INVALID_ARG, "Q, K and V are required");
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(V)) return fail(h, SAS_ERR_INVALID_ARG, "misaligned pointer");
+    a.Q = static_cast<sas::bf16*>(Q); a.K = static_cast<sas::bf16*>(K); a.V = static_cast<sas::bf16*>(V);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const sas::KernelEnv env{s, h->status, h->limit};
+    const cudaError_t e = timed_launch(h, 7, s, [&] { return sas::launch_rope_fwd(a, h->cfg.d, env); });
+    return e == cudaSuccess ? SAS_OK : cuda_fail(h, e, "norm + rotation");
+} catch (...) {
+    return SAS_ERR_OOM;   // only the host's own bookkeeping throws
+}
+
+sas_status sas_qk_norm_rope_bwd(sas_handle* h, const sas_rope_config* rope, const void* qkv, int64_t ld,
+                                const void* wq, const void* wk, const float* cos, const float* sin,
+                                const int32_t* positions, const void* dQ, const void* dK, const void* dV, void* dqkv,
+                                int64_t ld_d, float* dwq, float* dwk, void* stream) try {
+    if (h == nullptr) return SAS_ERR_INVALID_ARG;
+    sas::RopeArgs a{};
+    if (sas_status st = rope_args(h, rope, qkv, ld, wq, wk, cos, sin, positions, a); st != SAS_OK) return st;
+    if (!dQ || !dK || !dV || !dqkv || !dwq || !dwk) return fail(h, SAS_ERR_INVALID_ARG, "a required argument is NULL");
+    if (!aligned16(dQ) || !aligned16(dK) || !aligned16(dV) || !aligned16(dqkv) || !aligned4(dwq) || !aligned4(dwk))
+        return fail(h, SAS_ERR_INVALID_ARG, "misaligned pointer");
+    if (const char* why = sas::rope_check(rope->rot, rope->interleaved, rope->max_pos, rope->eps,
+                                          h->cfg.H + 2LL * h->Hkv, h->cfg.d, ld_d))
+        return fail(h, SAS_ERR_INVALID_ARG, why);
+    // read here, written nowhere
+    a.Q = static_cast<sas::bf16*>(const_cast<void*>(dQ));
+    a.K = static_cast<sas::bf16*>(const_cast<void*>(dK));
+    a.V = static_cast<sas::bf16*>(const_cast<void*>(dV));
+    a.dqkv = static_cast<sas::bf16*>(dqkv); a.ld_d = ld_d; a.dwq = dwq; a.dwk = dwk;
+    a.part = h->rope_part; a.counter = h->rope_count;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const sas::KernelEnv env{s, h->status, h->limit};
+    const cudaError_t e = timed_launch(h, 7, s, [&] { return sas::launch_rope_bwd(a, h->cfg.d, env); });
+    return e == cudaSuccess ? SAS_OK : cuda_fail(h, e, "gradient of norm + rotation");
+} catch (...) {
+    return SAS_ERR_OOM;   // only the host's own bookkeeping throws
 }
 
 sas_status sas_get_device_status(sas_handle* h, int32_t* out_status) {

@@ -8,6 +8,8 @@ the calls raise.
 """
 from __future__ import annotations
 
+import collections
+import contextlib
 import ctypes
 import os
 import re
@@ -35,9 +37,9 @@ SAS_GATE_INNER = 0
 SAS_GATE_OUTER = 1
 SAS_SCOPE_SPARSE = 0
 SAS_SCOPE_FULL = 1
-SAS_NUM_KERNEL_KINDS = 7
+SAS_NUM_KERNEL_KINDS = 8
 KERNEL_KINDS = ["block_summaries", "query_projection", "selection", "attention", "mlp_up_gelu", "mlp_down",
-                "attention_bwd"]
+                "attention_bwd", "qk_norm_rope"]
 
 HEADER = os.path.join(_build.ROOT, "include", "sas.h")
 
@@ -57,8 +59,21 @@ class SasDecodeConfig(ctypes.Structure):
                 ("dense", ctypes.c_int32)]
 
 
+class SasRopeConfig(ctypes.Structure):
+    _fields_ = [("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("max_pos", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+
+class SasChunkConfig(ctypes.Structure):
+    _fields_ = [("max_seqs", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("block", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("max_tokens", ctypes.c_int32), ("sm_scale", ctypes.c_float)]
+
+
 SAS_DECODE_NUM_KERNEL_KINDS = 4
 DECODE_KERNEL_KINDS = ["prep", "select", "attention", "summarize"]
+SAS_CHUNK_NUM_KERNEL_KINDS = 4
+CHUNK_KERNEL_KINDS = ["plan", "append", "attention", "verify"]
 
 
 class SasError(RuntimeError):
@@ -135,6 +150,35 @@ def lib():
     L.sas_decode_get_timings.restype = i32
     L.sas_decode_launch_count.argtypes = [vp]
     L.sas_decode_launch_count.restype = i64
+    rope = ctypes.POINTER(SasRopeConfig)
+    L.sas_qk_norm_rope_fwd.argtypes = [vp, rope, vp, i64] + [vp] * 9
+    L.sas_qk_norm_rope_fwd.restype = i32
+    L.sas_qk_norm_rope_bwd.argtypes = [vp, rope, vp, i64] + [vp] * 9 + [i64] + [vp] * 3
+    L.sas_qk_norm_rope_bwd.restype = i32
+    L.sas_chunk_create.argtypes = [ctypes.POINTER(SasChunkConfig), ctypes.POINTER(vp)]
+    L.sas_chunk_create.restype = i32
+    L.sas_chunk_destroy.argtypes = [vp]
+    L.sas_chunk_destroy.restype = None
+    L.sas_chunk_plan.argtypes = [vp, i32, i32, vp, vp, vp, i32] + [vp] * 8
+    L.sas_chunk_plan.restype = i32
+    L.sas_chunk_append.argtypes = [vp, rope, i32, vp, i64] + [vp] * 10
+    L.sas_chunk_append.restype = i32
+    L.sas_chunk_attention.argtypes = [vp, i32, i32] + [vp] * 9
+    L.sas_chunk_attention.restype = i32
+    L.sas_chunk_verify.argtypes = [vp] + [i32] * 4 + [vp, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp]
+    L.sas_chunk_verify.restype = i32
+    L.sas_chunk_last_error.argtypes = [vp]
+    L.sas_chunk_last_error.restype = ctypes.c_char_p
+    L.sas_chunk_get_device_status.argtypes = [vp, ctypes.POINTER(i32)]
+    L.sas_chunk_get_device_status.restype = i32
+    L.sas_chunk_set_timing.argtypes = [vp, i32]
+    L.sas_chunk_set_timing.restype = i32
+    L.sas_chunk_get_timings.argtypes = [vp, ctypes.POINTER(i64), ctypes.POINTER(ctypes.c_double), i32]
+    L.sas_chunk_get_timings.restype = i32
+    L.sas_chunk_launch_count.argtypes = [vp]
+    L.sas_chunk_launch_count.restype = i64
+    L.sas_chunk_set_wait_limit.argtypes = [vp, i64]
+    L.sas_chunk_set_wait_limit.restype = i32
     _lib = L
     return L
 
@@ -158,6 +202,64 @@ def _ptr(t, dtype, name, required=True):
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _arg(t, dtype, name, shape=None, dev=None):
+    """Device address of a contiguous tensor: like _ptr, with its shape and device checked, and a plain
+    integer, for the entry points whose time is mostly the call's."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if dev is not None and t.get_device() != dev:
+        raise ValueError(f"{name} must be on device {dev}")
+    return t.data_ptr()
+
+
+def _rows(t, dtype, name, shape, dev):
+    """Device address of a tensor of any strides (its caller checks those)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on device {dev}")
+    return t.data_ptr()
+
+
+def _token_stride(t, name, lead):
+    """Elements between two tokens of a [tokens.., heads, d] tensor (lead token axes): the heads of a token are
+    contiguous, and all tokens evenly spaced."""
+    st, sh = t.stride(), t.shape
+    if (sh[-1] > 1 and st[-1] != 1) or (sh[-2] > 1 and st[-2] != sh[-1]):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    if lead == 1:
+        return st[0] if sh[0] > 1 else sh[1] * sh[2]
+    ld = st[1] if sh[1] > 1 else (st[0] if sh[0] > 1 else sh[2] * sh[3])
+    if sh[0] > 1 and st[0] != sh[1] * ld:
+        raise ValueError(f"{name}: the tokens of all batch rows must be evenly spaced")
+    return ld
+
+
+def _raw_stream(stream):
+    if stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _on(stream):
+    """Context in which outputs are allocated: the stream the call runs on, whose pool then owns them."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream))
+    return torch.cuda.stream(stream)
 
 
 def _stream(stream):
@@ -251,6 +353,38 @@ def sas_attention_bwd(h, Q, K, V, O, LSE, dO, dQ, dK, dV, scores=None, sel_idx=N
         _ptr(sel_logg, f32, "sel_logg", False), _ptr(dQ, bf, "dQ"), _ptr(dK, bf, "dK"), _ptr(dV, bf, "dV"),
         _ptr(dlogg, f32, "dlogg", False), _ptr(dscores, f32, "dscores", False), _stream(stream))
     _check(st, h, "sas_attention_bwd")
+
+
+def sas_qk_norm_rope_fwd(h, qkv, wq, wk, cos, sin, Q, K, V, positions=None, eps=1e-6, interleaved=False, stream=None):
+    """qkv [B, N, H + 2 Hkv, d] (tokens evenly spaced, any distance) to Q [B, H, N, d], K and V [B, Hkv, N, d]."""
+    B, H, N, d = Q.shape
+    Hkv, dev, bf, f32 = K.shape[1], Q.get_device(), torch.bfloat16, torch.float32
+    cfg = SasRopeConfig(2 * cos.shape[-1], 1 if interleaved else 0, cos.shape[0], eps)
+    st = lib().sas_qk_norm_rope_fwd(
+        h, cfg, _rows(qkv, bf, "qkv", (B, N, H + 2 * Hkv, d), dev), _token_stride(qkv, "qkv", 2), _arg(wq, bf, "wq", (d,), dev),
+        _arg(wk, bf, "wk", (d,), dev), _arg(cos, f32, "cos", None, dev), _arg(sin, f32, "sin", cos.shape, dev),
+        None if positions is None else _arg(positions, torch.int32, "positions", (B, N), dev), _arg(Q, bf, "Q"),
+        _arg(K, bf, "K", (B, Hkv, N, d), dev), _arg(V, bf, "V", (B, Hkv, N, d), dev), _raw_stream(stream))
+    if st != SAS_OK:
+        _check(st, h, "sas_qk_norm_rope_fwd")
+
+
+def sas_qk_norm_rope_bwd(h, qkv, wq, wk, cos, sin, dQ, dK, dV, dqkv, dwq, dwk, positions=None, eps=1e-6,
+                         interleaved=False, stream=None):
+    """Gradients of sas_qk_norm_rope_fwd: dqkv like qkv, dwq and dwk fp32 [d]."""
+    B, H, N, d = dQ.shape
+    Hkv, dev, bf, f32 = dK.shape[1], dQ.get_device(), torch.bfloat16, torch.float32
+    rows = (B, N, H + 2 * Hkv, d)
+    cfg = SasRopeConfig(2 * cos.shape[-1], 1 if interleaved else 0, cos.shape[0], eps)
+    st = lib().sas_qk_norm_rope_bwd(
+        h, cfg, _rows(qkv, bf, "qkv", rows, dev), _token_stride(qkv, "qkv", 2), _arg(wq, bf, "wq", (d,), dev),
+        _arg(wk, bf, "wk", (d,), dev), _arg(cos, f32, "cos", None, dev), _arg(sin, f32, "sin", cos.shape, dev),
+        None if positions is None else _arg(positions, torch.int32, "positions", (B, N), dev), _arg(dQ, bf, "dQ"),
+        _arg(dK, bf, "dK", (B, Hkv, N, d), dev), _arg(dV, bf, "dV", (B, Hkv, N, d), dev), _rows(dqkv, bf, "dqkv", rows, dev),
+        _token_stride(dqkv, "dqkv", 2), _arg(dwq, f32, "dwq", (d,), dev), _arg(dwk, f32, "dwk", (d,), dev),
+        _raw_stream(stream))
+    if st != SAS_OK:
+        _check(st, h, "sas_qk_norm_rope_bwd")
 
 
 def sas_mlp_fwd(h, X, W1, W2, Y, b1=None, b2=None, stream=None):
@@ -419,6 +553,30 @@ class SasLayer:
         sas_attention_bwd(self.h, Q, K, V, O, LSE, dO, dQ, dK, dV, scores, sel_idx, sel_logg, dlogg, ds, stream)
         return dQ, dK, dV, dlogg, ds
 
+    def qk_norm_rope(self, qkv, wq, wk, cos, sin, positions=None, eps=1e-6, interleaved=False, stream=None):
+        """Per-head norm of queries and keys and the rotary rotation: the fused projection qkv
+        [B, N, H + 2 Hkv, d] to (Q [B, H, N, d], K, V [B, Hkv, N, d]), as attention() takes them."""
+        with _on(stream):
+            Q = torch.empty(self.B, self.H, self.N, self.d, device=qkv.device, dtype=torch.bfloat16)
+            K = torch.empty(self.B, self.Hkv, self.N, self.d, device=qkv.device, dtype=torch.bfloat16)
+            V = torch.empty_like(K)
+        sas_qk_norm_rope_fwd(self.h, qkv, wq, wk, cos, sin, Q, K, V, positions, eps, interleaved, stream)
+        return Q, K, V
+
+    def qk_norm_rope_bwd(self, qkv, wq, wk, cos, sin, dQ, dK, dV, positions=None, eps=1e-6, interleaved=False,
+                         stream=None):
+        """Returns (dqkv [B, N, H + 2 Hkv, d] bf16, dwq, dwk fp32 [d])."""
+        shape = {"dQ": (dQ, self.H), "dK": (dK, self.Hkv)}
+        for name, (t, heads) in shape.items():
+            if t.shape != (self.B, heads, self.N, self.d):
+                raise ValueError(f"{name} must have shape {(self.B, heads, self.N, self.d)}, got {tuple(t.shape)}")
+        with _on(stream):
+            dqkv = torch.empty(qkv.shape, device=qkv.device, dtype=torch.bfloat16)
+            dwq = torch.empty(self.d, device=qkv.device, dtype=torch.float32)
+            dwk = torch.empty_like(dwq)
+        sas_qk_norm_rope_bwd(self.h, qkv, wq, wk, cos, sin, dQ, dK, dV, dqkv, dwq, dwk, positions, eps, interleaved, stream)
+        return dqkv, dwq, dwk
+
     def mlp(self, X, W1, W2, b1=None, b2=None, stream=None):
         Y = torch.empty(X.shape[0], W2.shape[0], device=X.device, dtype=torch.bfloat16)
         sas_mlp_fwd(self.h, X, W1, W2, Y, b1, b2, stream)
@@ -542,6 +700,229 @@ class SasDecoder:
     def close(self):
         if self.h is not None:
             sas_decode_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ------------------------------------------------------------------ serving step
+
+
+def _ccheck(status, handle, what):
+    if status != SAS_OK:
+        L = lib()
+        msg = L.sas_status_str(status).decode()
+        if handle is not None:
+            detail = L.sas_chunk_last_error(handle).decode()
+            if detail:
+                msg += ": " + detail
+        raise SasError(status, f"{what}: {msg}")
+
+
+def sas_chunk_create(max_seqs, Hq, Hkv, d, max_blocks, num_pages, max_tokens, sm_scale=0.0, block=64):
+    cfg = SasChunkConfig(max_seqs, Hq, Hkv, d, block, max_blocks, num_pages, max_tokens, sm_scale)
+    h = ctypes.c_void_p()
+    _ccheck(lib().sas_chunk_create(ctypes.byref(cfg), ctypes.byref(h)), None, "sas_chunk_create")
+    return h
+
+
+def sas_chunk_create_status(max_seqs, Hq, Hkv, d, max_blocks, num_pages, max_tokens, sm_scale=0.0, block=64):
+    """Raw status of sas_chunk_create (argument-check tests); destroys the handle on success."""
+    cfg = SasChunkConfig(max_seqs, Hq, Hkv, d, block, max_blocks, num_pages, max_tokens, sm_scale)
+    h = ctypes.c_void_p()
+    st = lib().sas_chunk_create(ctypes.byref(cfg), ctypes.byref(h))
+    if st == SAS_OK:
+        lib().sas_chunk_destroy(h)
+    return st
+
+
+def sas_chunk_destroy(h):
+    lib().sas_chunk_destroy(h)
+
+
+def sas_chunk_plan(h, seq_lens, new_lens, free_pages, free_begin, block_table, kv_lens, cu_new, positions, slots,
+                   free_end, stream=None):
+    i32, B, T, dev = torch.int32, seq_lens.shape[0], positions.shape[0], seq_lens.get_device()
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError(f"block_table must have {B} rows")
+    st = lib().sas_chunk_plan(
+        h, B, T, _arg(seq_lens, i32, "seq_lens", (B,)), _arg(new_lens, i32, "new_lens", (B,), dev),
+        _arg(free_pages, i32, "free_pages", None, dev), free_pages.numel(), _arg(free_begin, i32, "free_begin", (1,), dev),
+        _arg(block_table, i32, "block_table", None, dev), _arg(kv_lens, i32, "kv_lens", (B,), dev),
+        _arg(cu_new, i32, "cu_new", (B + 1,), dev), _arg(positions, i32, "positions", (T,), dev),
+        _arg(slots, torch.int64, "slots", (T,), dev), _arg(free_end, i32, "free_end", (1,), dev), _raw_stream(stream))
+    if st != SAS_OK:
+        _ccheck(st, h, "sas_chunk_plan")
+
+
+def sas_chunk_append(h, qkv, wq, wk, cos, sin, positions, slots, Q, K_cache, V_cache, eps=1e-6, interleaved=False,
+                     stream=None):
+    """qkv [T, Hq + 2 Hkv, d] (tokens evenly spaced, any distance)."""
+    T, Hq, d = Q.shape
+    Hkv, dev, bf, f32 = K_cache.shape[1], Q.get_device(), torch.bfloat16, torch.float32
+    cfg = SasRopeConfig(2 * cos.shape[-1], 1 if interleaved else 0, cos.shape[0], eps)
+    st = lib().sas_chunk_append(
+        h, cfg, T, _rows(qkv, bf, "qkv", (T, Hq + 2 * Hkv, d), dev), _token_stride(qkv, "qkv", 1), _arg(wq, bf, "wq", (d,), dev),
+        _arg(wk, bf, "wk", (d,), dev), _arg(cos, f32, "cos", None, dev), _arg(sin, f32, "sin", cos.shape, dev),
+        _arg(positions, torch.int32, "positions", (T,), dev), _arg(slots, torch.int64, "slots", (T,), dev), _arg(Q, bf, "Q"),
+        _arg(K_cache, bf, "K_cache", None, dev), _arg(V_cache, bf, "V_cache", K_cache.shape, dev), _raw_stream(stream))
+    if st != SAS_OK:
+        _ccheck(st, h, "sas_chunk_append")
+
+
+def sas_chunk_attention(h, Q, K_cache, V_cache, block_table, cu_new, kv_lens, O, LSE=None, stream=None):
+    i32, bf, B, dev = torch.int32, torch.bfloat16, kv_lens.shape[0], Q.get_device()
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError(f"block_table must have {B} rows")
+    st = lib().sas_chunk_attention(
+        h, B, Q.shape[0], _arg(Q, bf, "Q"), _arg(K_cache, bf, "K_cache", None, dev),
+        _arg(V_cache, bf, "V_cache", K_cache.shape, dev), _arg(block_table, i32, "block_table", None, dev),
+        _arg(cu_new, i32, "cu_new", (B + 1,), dev), _arg(kv_lens, i32, "kv_lens", (B,), dev), _arg(O, bf, "O", Q.shape, dev),
+        None if LSE is None else _arg(LSE, torch.float32, "LSE", Q.shape[:2], dev), _raw_stream(stream))
+    if st != SAS_OK:
+        _ccheck(st, h, "sas_chunk_attention")
+
+
+def _prob_rows(t, name, rows, V, dev):
+    """Address and row stride of an fp32 [rows, V] tensor with contiguous columns."""
+    at = _rows(t, torch.float32, name, (rows, V), dev)
+    st = t.stride()
+    if V > 1 and st[1] != 1:
+        raise ValueError(f"{name} must have contiguous columns")
+    return at, st[0] if rows > 1 else max(st[0], V)
+
+
+def sas_chunk_verify(h, tokens, cu_draft, target, draft, u, noise, accepted, out_tokens, stream=None):
+    """draft None: the drafts were certain."""
+    i32, B, n, V, dev = torch.int32, cu_draft.shape[0] - 1, tokens.shape[0], target.shape[1], target.get_device()
+    p, ldp = _prob_rows(target, "target", n + B, V, dev)
+    q, ldq = (None, V) if draft is None else _prob_rows(draft, "draft", n, V, dev)
+    e, lde = _prob_rows(noise, "noise", B, V, dev)
+    if out_tokens.dim() != 2 or out_tokens.shape[0] != B or out_tokens.shape[1] < 1:
+        raise ValueError(f"out_tokens must have {B} rows and at least one column")
+    st = lib().sas_chunk_verify(
+        h, B, n, out_tokens.shape[1] - 1, V, _arg(tokens, i32, "tokens", (n,), dev), _arg(cu_draft, i32, "cu_draft", None, dev), p,
+        ldp, q, ldq, _arg(u, torch.float32, "u", (n,), dev), e, lde, _arg(accepted, i32, "accepted", (B,), dev),
+        _arg(out_tokens, i32, "out_tokens", None, dev), _raw_stream(stream))
+    if st != SAS_OK:
+        _ccheck(st, h, "sas_chunk_verify")
+
+
+def sas_chunk_get_device_status(h):
+    v = ctypes.c_int32(0)
+    _ccheck(lib().sas_chunk_get_device_status(h, ctypes.byref(v)), h, "sas_chunk_get_device_status")
+    return v.value
+
+
+def sas_chunk_set_timing(h, enable):
+    _ccheck(lib().sas_chunk_set_timing(h, 1 if enable else 0), h, "sas_chunk_set_timing")
+
+
+def sas_chunk_get_timings(h):
+    n = SAS_CHUNK_NUM_KERNEL_KINDS
+    launches = (ctypes.c_int64 * n)()
+    ms = (ctypes.c_double * n)()
+    _ccheck(lib().sas_chunk_get_timings(h, launches, ms, n), h, "sas_chunk_get_timings")
+    return {CHUNK_KERNEL_KINDS[k]: (launches[k], ms[k]) for k in range(n)}
+
+
+def sas_chunk_launch_count(h):
+    return lib().sas_chunk_launch_count(h)
+
+
+def sas_chunk_set_wait_limit(h, cycles):
+    """Failure-path diagnostics: wait budget of the attention in SM cycles (0: default)."""
+    _ccheck(lib().sas_chunk_set_wait_limit(h, int(cycles)), h, "sas_chunk_set_wait_limit")
+
+
+# Outputs of a page plan (see sas_chunk_plan in sas.h).
+ChunkPlan = collections.namedtuple("ChunkPlan", "kv_lens cu_new positions slots free_end")
+
+
+class SasChunk:
+    """One serving step over a paged cache: plan -> append -> attention (-> verify).
+
+    Owns one handle; allocates the outputs (on the stream the call runs on) unless the caller
+    passes its own, as a captured graph needs.  K_cache, V_cache [num_pages, Hkv, 64, d] and
+    block_table [requests, max_blocks] are those of SasDecoder."""
+
+    def __init__(self, max_seqs, Hq, Hkv, d, max_blocks, num_pages, max_tokens, sm_scale=0.0):
+        self.Hq, self.Hkv, self.d, self.max_blocks = Hq, Hkv, d, max_blocks
+        self.cache_shape = (num_pages, Hkv, 64, d)
+        self.h = sas_chunk_create(max_seqs, Hq, Hkv, d, max_blocks, num_pages, max_tokens, sm_scale)
+
+    def plan_buffers(self, num_seqs, T, device):
+        i32 = torch.int32
+        return ChunkPlan(torch.empty(num_seqs, device=device, dtype=i32), torch.empty(num_seqs + 1, device=device, dtype=i32),
+                         torch.empty(T, device=device, dtype=i32), torch.empty(T, device=device, dtype=torch.int64),
+                         torch.empty(1, device=device, dtype=i32))
+
+    def _table(self, block_table):
+        if block_table.dim() != 2 or block_table.shape[1] != self.max_blocks:
+            raise ValueError(f"block_table must have {self.max_blocks} columns")
+
+    def _caches(self, K_cache):
+        if K_cache.shape != self.cache_shape:
+            raise ValueError(f"K_cache must have shape {self.cache_shape}, got {tuple(K_cache.shape)}")
+
+    def plan(self, seq_lens, new_lens, free_pages, free_begin, block_table, T, out=None, stream=None):
+        """Pages and slots of the new tokens: a ChunkPlan; block_table gets the new pages.  T: capacity for new
+        tokens (positions and slots are -1 past their number)."""
+        self._table(block_table)
+        if out is None:
+            with _on(stream):
+                out = self.plan_buffers(seq_lens.shape[0], T, seq_lens.device)
+        elif out.positions.shape[0] != T:
+            raise ValueError(f"out.positions must have {T} entries")
+        sas_chunk_plan(self.h, seq_lens, new_lens, free_pages, free_begin, block_table, *out, stream=stream)
+        return out
+
+    def append(self, qkv, wq, wk, cos, sin, positions, slots, K_cache, V_cache, eps=1e-6, interleaved=False, out=None,
+               stream=None):
+        """Norm + rotation of the new tokens' queries and keys; keys and values into the cache.  Returns Q
+        [T, Hq, d] (rows of slot -1 are not written)."""
+        self._caches(K_cache)
+        if out is None:
+            with _on(stream):
+                out = torch.empty(qkv.shape[0], self.Hq, self.d, device=qkv.device, dtype=torch.bfloat16)
+        elif out.dim() != 3 or out.shape[1] != self.Hq or out.shape[2] != self.d:
+            raise ValueError(f"out must have shape [T, {self.Hq}, {self.d}]")
+        sas_chunk_append(self.h, qkv, wq, wk, cos, sin, positions, slots, out, K_cache, V_cache, eps, interleaved, stream)
+        return out
+
+    def attention(self, Q, K_cache, V_cache, block_table, cu_new, kv_lens, out=None, stream=None):
+        """Dense causal attention of the new tokens.  Returns (O [T, Hq, d], LSE [T, Hq]); out = (O, LSE) reuses
+        caller buffers (LSE may be None)."""
+        self._table(block_table)
+        self._caches(K_cache)
+        if Q.dim() != 3 or Q.shape[1] != self.Hq or Q.shape[2] != self.d:
+            raise ValueError(f"Q must have shape [T, {self.Hq}, {self.d}]")
+        if out is None:
+            with _on(stream):
+                out = (torch.empty_like(Q), torch.empty(Q.shape[:2], device=Q.device, dtype=torch.float32))
+        sas_chunk_attention(self.h, Q, K_cache, V_cache, block_table, cu_new, kv_lens, out[0], out[1], stream)
+        return out
+
+    def verify(self, tokens, cu_draft, target, draft, u, noise, max_draft, out=None, stream=None):
+        """Accepted drafts and the next token of every request: (accepted [requests], tokens [requests, max_draft + 1]
+        padded with -1)."""
+        B = cu_draft.shape[0] - 1
+        if out is None:
+            with _on(stream):
+                out = (torch.empty(B, device=target.device, dtype=torch.int32),
+                       torch.empty(B, max_draft + 1, device=target.device, dtype=torch.int32))
+        elif out[1].dim() != 2 or out[1].shape[1] != max_draft + 1:
+            raise ValueError(f"out[1] must have {max_draft + 1} columns")
+        sas_chunk_verify(self.h, tokens, cu_draft, target, draft, u, noise, out[0], out[1], stream)
+        return out
+
+    def close(self):
+        if self.h is not None:
+            sas_chunk_destroy(self.h)
             self.h = None
 
     def __del__(self):
