@@ -41,6 +41,7 @@ constexpr int kItemSlots = 4;     // work items in flight between warp 0 and the
 constexpr int kItemReaders = 7;   // V producer, two MMA issuers, four softmax warps
 constexpr int kStatusBadInput = 1;
 constexpr int kStatusLayout = 3;
+constexpr int kJoin = 8;          // rows of a warp in flight when splits are joined
 constexpr int kPlanThreads = 1024;
 constexpr int kBuckets = 64;
 
@@ -222,7 +223,7 @@ static_assert(sizeof(Ctl) <= 512, "control block");
 
 __device__ __forceinline__ bool read_item(Ctl& ctl, int r, const WaitCtl& wc, Item& x) {
     const int slot = r % kItemSlots;
-    if (!mbar_wait_warp(&ctl.item_full[slot], (r / kItemSlots) & 1, wc)) return false;
+    if (!mbar_poll_warp(&ctl.item_full[slot], (r / kItemSlots) & 1, wc)) return false;
     x = ctl.item[slot];
     __syncwarp();
     if (lane_id() == 0) mbar_arrive(&ctl.item_empty[slot]);
@@ -626,53 +627,82 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
             ++np;
             if (*reinterpret_cast<volatile int*>(&ctl.last) == 0) continue;
             __threadfence();
-            // join the splits: a warp per row, D / 32 columns a lane
+            // join the splits: a warp takes kJoin rows at a time (their loads in flight
+            // together), D / 32 columns a lane
             constexpr int CPL = D / 32;
             const size_t stride = static_cast<size_t>(a.Hkv) * kBM;   // rows between the splits of a tile
             const int rows = x.ntok * a.G;
-            for (int rr = q; rr < rows; rr += 4) {
-                const size_t base = (static_cast<size_t>(x.part) * a.Hkv + x.head) * kBM + rr;
-                float M = -CUDART_INF_F;
-                for (int s = lane; s < x.ns; s += 32) M = fmaxf(M, __ldcg(a.part_ml + base + s * stride).x);
+            const size_t base = (static_cast<size_t>(x.part) * a.Hkv + x.head) * kBM;
+            for (int r0 = q; r0 < rows; r0 += 4 * kJoin) {
+                float M[kJoin], L[kJoin], acc[kJoin][CPL];
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-                float L = 0.f, acc[CPL];
+                for (int k = 0; k < kJoin; ++k) {
+                    M[k] = -CUDART_INF_F;
+                    L[k] = 0.f;
 #pragma unroll
-                for (int e = 0; e < CPL; ++e) acc[e] = 0.f;
+                    for (int e = 0; e < CPL; ++e) acc[k][e] = 0.f;
+                }
+                // rows past the last repeat it: loaded, not stored
+                for (int s = lane; s < x.ns; s += 32) {
+#pragma unroll
+                    for (int k = 0; k < kJoin; ++k)
+                        M[k] = fmaxf(M[k], __ldcg(a.part_ml + base + min(r0 + 4 * k, rows - 1) + s * stride).x);
+                }
+#pragma unroll
+                for (int k = 0; k < kJoin; ++k)
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) M[k] = fmaxf(M[k], __shfl_xor_sync(0xffffffffu, M[k], o));
                 for (int s0 = 0; s0 < x.ns; s0 += 32) {
-                    float wgt = 0.f;
-                    if (s0 + static_cast<int>(lane) < x.ns) {
-                        const float2 ml = __ldcg(a.part_ml + base + (s0 + lane) * stride);
-                        wgt = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - M);
-                        L = fmaf(wgt, ml.y, L);
+                    float wgt[kJoin];
+#pragma unroll
+                    for (int k = 0; k < kJoin; ++k) {
+                        wgt[k] = 0.f;
+                        if (s0 + static_cast<int>(lane) < x.ns) {
+                            const float2 ml = __ldcg(a.part_ml + base + min(r0 + 4 * k, rows - 1) + (s0 + lane) * stride);
+                            wgt[k] = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - M[k]);
+                            L[k] = fmaf(wgt[k], ml.y, L[k]);
+                        }
                     }
                     const int cnt = min(32, x.ns - s0);
-#pragma unroll 4
+#pragma unroll 1
                     for (int s = 0; s < cnt; ++s) {
-                        const float ws = __shfl_sync(0xffffffffu, wgt, s);
                         const float* src = a.part_o + (base + (s0 + s) * stride) * D + lane * CPL;
-                        if constexpr (CPL == 4) {
-                            const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
-                            acc[0] = fmaf(ws, v.x, acc[0]);
-                            acc[1] = fmaf(ws, v.y, acc[1]);
-                            acc[2] = fmaf(ws, v.z, acc[2]);
-                            acc[3] = fmaf(ws, v.w, acc[3]);
-                        } else {
-                            const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
-                            acc[0] = fmaf(ws, v.x, acc[0]);
-                            acc[1] = fmaf(ws, v.y, acc[1]);
+                        float v[kJoin][CPL];
+#pragma unroll
+                        for (int k = 0; k < kJoin; ++k) {
+                            const float* at = src + static_cast<size_t>(min(r0 + 4 * k, rows - 1)) * D;
+                            if constexpr (CPL == 4) {
+                                const float4 f = __ldcg(reinterpret_cast<const float4*>(at));
+                                v[k][0] = f.x; v[k][1] = f.y; v[k][2] = f.z; v[k][3] = f.w;
+                            } else {
+                                const float2 f = __ldcg(reinterpret_cast<const float2*>(at));
+                                v[k][0] = f.x; v[k][1] = f.y;
+                            }
+                        }
+#pragma unroll
+                        for (int k = 0; k < kJoin; ++k) {
+                            const float ws = __shfl_sync(0xffffffffu, wgt[k], s);
+                            if (ws != 0.f) {   // (a split in which the row sees no key does not count, whatever it holds)
+#pragma unroll
+                                for (int e = 0; e < CPL; ++e) acc[k][e] = fmaf(ws, v[k][e], acc[k][e]);
+                            }
                         }
                     }
                 }
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
-                const float inv = 1.f / L;
-                const int tk = rr / a.G, h = rr - tk * a.G;
-                const size_t at = (static_cast<size_t>(x.tok0) + tk) * a.Hq + static_cast<size_t>(x.head) * a.G + h;
-                uint32_t* dst = reinterpret_cast<uint32_t*>(a.O + at * D) + lane * (CPL / 2);
+                for (int k = 0; k < kJoin; ++k) {
 #pragma unroll
-                for (int e = 0; e < CPL / 2; ++e) dst[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-                if (lane == 0 && a.LSE != nullptr) a.LSE[at] = M * kLn2 + logf(L);
+                    for (int o = 16; o > 0; o >>= 1) L[k] += __shfl_xor_sync(0xffffffffu, L[k], o);
+                    const int rr = r0 + 4 * k;
+                    if (rr >= rows) continue;
+                    const float inv = 1.f / L[k];
+                    const int tk = rr / a.G, h = rr - tk * a.G;
+                    const size_t at = (static_cast<size_t>(x.tok0) + tk) * a.Hq + static_cast<size_t>(x.head) * a.G + h;
+                    uint32_t* dst = reinterpret_cast<uint32_t*>(a.O + at * D) + lane * (CPL / 2);
+#pragma unroll
+                    for (int e = 0; e < CPL / 2; ++e) dst[e] = pack_bf16x2(acc[k][2 * e] * inv, acc[k][2 * e + 1] * inv);
+                    if (lane == 0 && a.LSE != nullptr) a.LSE[at] = M[k] * kLn2 + logf(L[k]);
+                }
             }
         }
     }

@@ -224,11 +224,10 @@ def test_bad_lengths_and_pages_are_reported_and_contained():
 
 
 def test_timeouts_are_reported_and_the_handle_recovers():
-    # a budget of one cycle makes the waits give up: a status, no hang, and the right result afterwards.
-    # (A wait of a few microseconds may end within one try of the barrier: items of hundreds of pages
-    # make the roles wait long, and the single token's pages are split)
-    Q, K, V, table, cu, kv = _case([(3000, 1), (20000, 3000)], 32, 8, 128, poison=False)
-    ch = sas.SasChunk(2, 32, 8, 128, table.shape[1], K.shape[0], 3001)
+    # a budget of one cycle makes the waits for the first work item give up: a status, no hang, and the
+    # right result afterwards
+    Q, K, V, table, cu, kv = _case([(3000, 1), (2000, 200)], 8, 2, 128, poison=False)
+    ch = sas.SasChunk(2, 8, 2, 128, table.shape[1], K.shape[0], 201)
     want = ch.attention(Q, K, V, table, cu, kv)
     sas.sas_chunk_set_wait_limit(ch.h, 1)
     ch.attention(Q, K, V, table, cu, kv)
