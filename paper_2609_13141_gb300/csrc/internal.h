@@ -279,7 +279,7 @@ struct RopeArgs {
 };
 // What is wrong with a rotation of rows of `heads` heads, ld elements apart, or null.
 const char* rope_check(int rot, int interleaved, int max_pos, float eps, long long heads, int d, long long ld);
-bool rope_supported(const RopeArgs& a, int d);   // the launch grid holds this many rows
+bool rope_supported(const RopeArgs& a);   // the kernels can count this many tokens
 int rope_bwd_max_blocks();
 cudaError_t launch_rope_fwd(const RopeArgs& a, int d, const KernelEnv& env);
 cudaError_t launch_rope_bwd(const RopeArgs& a, int d, const KernelEnv& env);

@@ -13,9 +13,11 @@
 // Value rows pass through, so that the fused projection [token][Hq + 2 Hkv][d] is
 // read once and leaves in the attention's layouts.
 //
-// Bound: HBM.  A row is a group of d / 8 lanes with 8 elements each; a warp takes
-// kRows rows per group of one token, all in flight before any is used, and reads the
-// table's row once.
+// Bound: HBM, and close behind it the issue slots (a row of d = 128 is 256 bytes and
+// some 110 instructions of 16 lanes).  So: both kernels are persistent, a warp keeps
+// the same heads for all its tokens (their kinds, weights and addresses are then
+// fixed), rows stream through a ring in shared memory (cp.async, no registers held
+// while they are in flight), and the arithmetic runs on packed fp32 pairs.
 #include "internal.h"
 #include "ptx.cuh"
 
@@ -24,10 +26,16 @@ namespace {
 
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
-constexpr int kRows = 4;          // rows in flight per lane group
 constexpr int kStatusBadInput = 1;   // == SAS_ERR_INVALID_ARG
 
-// A lane's 8 elements of a head row, as two quads (bf16 in memory).
+__device__ __forceinline__ uint64_t dup2(float v) { return f32x2(v, v); }
+__device__ __forceinline__ float sum2(uint64_t v) {
+    float lo, hi;
+    f32x2_split(v, lo, hi);
+    return lo + hi;
+}
+
+// A lane's 8 elements of a head row: two quads in memory (bf16), four fp32 pairs.
 struct Quads {
     uint2 a, b;
     __device__ __forceinline__ void load(const bf16* row, int ia, int ib) {
@@ -42,253 +50,398 @@ struct Quads {
         *reinterpret_cast<uint2*>(row + ia) = a;
         *reinterpret_cast<uint2*>(row + ib) = b;
     }
-    __device__ __forceinline__ void unpack(float (&f)[8]) const {
+    __device__ __forceinline__ void unpack(uint64_t (&f)[4]) const {
         const uint32_t w[4] = {a.x, a.y, b.x, b.y};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] = __uint_as_float(w[i] << 16);
-            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
+        for (int i = 0; i < 4; ++i) f[i] = f32x2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
     }
-    __device__ __forceinline__ void pack(const float (&f)[8]) {
-        a = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
-        b = make_uint2(pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+    __device__ __forceinline__ void pack(const uint64_t (&f)[4]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float lo, hi;
+            f32x2_split(f[i], lo, hi);
+            w[i] = pack_bf16x2(lo, hi);
+        }
+        a = make_uint2(w[0], w[1]);
+        b = make_uint2(w[2], w[3]);
     }
 };
-
-// Sum over the LPR lanes of a row.
-template <int LPR>
-__device__ __forceinline__ float row_sum(float v) {
-#pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
 
 // Where a lane's two quads sit in a row, and its share of the rotation at one
 // position.  A lane always holds whole pairs, so the rotation needs no exchange:
 // half-split pairs put the second quad R / 2 past the first; interleaved pairs, and
 // dims past R, take 8 neighbours.  Either way the lane's four pairs are 4 l .. 4 l + 3.
 template <bool INTER>
-struct Turn {
+struct Place {
     int ia, ib;
-    float c[4], s[4];
-
-    __device__ __forceinline__ void place(const RopeArgs& a, int l) {
+    __device__ __forceinline__ Place(const RopeArgs& a, int l) {
         const bool split = !INTER && l < (a.rot >> 3);
         ia = split ? 4 * l : 8 * l;
         ib = split ? 4 * l + (a.rot >> 1) : 8 * l + 4;
     }
-    __device__ __forceinline__ void load(const RopeArgs& a, int pos, int l) {
-        float4 cv = make_float4(1.f, 1.f, 1.f, 1.f), sv = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (l < (a.rot >> 3)) {
-            const size_t at = static_cast<size_t>(pos) * (a.rot >> 1) + 4 * l;
-            cv = __ldg(reinterpret_cast<const float4*>(a.cos + at));
-            sv = __ldg(reinterpret_cast<const float4*>(a.sin + at));
-        }
-        c[0] = cv.x; c[1] = cv.y; c[2] = cv.z; c[3] = cv.w;
-        s[0] = sv.x; s[1] = sv.y; s[2] = sv.z; s[3] = sv.w;
+};
+
+// The cosines and sines of a token, 16 bytes a lane each, in a ring stage.  Lanes past
+// the rotated dims keep (1, 0), set once.
+template <int D>
+struct Table {
+    static constexpr int BYTES = 2 * (D / 8) * 16;
+    __device__ __forceinline__ static void clear(uint8_t* at, int l) {
+        *reinterpret_cast<float4*>(at + l * 16) = make_float4(1.f, 1.f, 1.f, 1.f);
+        *reinterpret_cast<float4*>(at + BYTES / 2 + l * 16) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    // BACK: the transposed rotation (the sine's sign flips).
-    template <bool BACK>
-    __device__ __forceinline__ void apply(float (&z)[8]) const {
+    __device__ __forceinline__ static void fetch(uint8_t* at, const RopeArgs& a, int pos, int l) {
+        if (l >= (a.rot >> 3)) return;
+        const size_t from = static_cast<size_t>(pos) * (a.rot >> 1) + 4 * l;
+        cp_async16(at + l * 16, a.cos + from);
+        cp_async16(at + BYTES / 2 + l * 16, a.sin + from);
+    }
+};
+
+// BACK: the transposed rotation (the sine's sign flips).
+template <bool INTER, bool BACK>
+struct Turn {
+    uint64_t c[INTER ? 4 : 2], s[INTER ? 4 : 2], t[INTER ? 1 : 2];
+    __device__ __forceinline__ Turn(const uint8_t* cos, const uint8_t* sin) {
+        const struct { float4 c, s; } g{*reinterpret_cast<const float4*>(cos), *reinterpret_cast<const float4*>(sin)};
+        if constexpr (INTER) {   // per pair (c, c) and (-s, s)
+            const float cs[4] = {g.c.x, g.c.y, g.c.z, g.c.w}, sn[4] = {g.s.x, g.s.y, g.s.z, g.s.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int p = INTER ? 2 * i : i, q = INTER ? 2 * i + 1 : i + 4;
-            const float za = z[p], zb = z[q], sn = BACK ? -s[i] : s[i];
-            z[p] = fmaf(-zb, sn, za * c[i]);
-            z[q] = fmaf(za, sn, zb * c[i]);
+            for (int i = 0; i < 4; ++i) {
+                c[i] = dup2(cs[i]);
+                s[i] = BACK ? f32x2(sn[i], -sn[i]) : f32x2(-sn[i], sn[i]);
+            }
+        } else {   // first quad: a c + b s', second: b c + a t'
+            c[0] = f32x2(g.c.x, g.c.y);
+            c[1] = f32x2(g.c.z, g.c.w);
+            const uint64_t p0 = f32x2(g.s.x, g.s.y), p1 = f32x2(g.s.z, g.s.w);
+            const uint64_t n0 = f32x2(-g.s.x, -g.s.y), n1 = f32x2(-g.s.z, -g.s.w);
+            s[0] = BACK ? p0 : n0;
+            s[1] = BACK ? p1 : n1;
+            t[0] = BACK ? n0 : p0;
+            t[1] = BACK ? n1 : p1;
+        }
+    }
+    __device__ __forceinline__ void apply(uint64_t (&z)[4]) const {
+        if constexpr (INTER) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float lo, hi;
+                f32x2_split(z[i], lo, hi);
+                z[i] = fma_f32x2(f32x2(hi, lo), s[i], mul_f32x2(z[i], c[i]));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint64_t x = z[i], y = z[i + 2];
+                z[i] = fma_f32x2(y, s[i], mul_f32x2(x, c[i]));
+                z[i + 2] = fma_f32x2(x, t[i], mul_f32x2(y, c[i]));
+            }
         }
     }
 };
 
-// A warp's unit: RPU = kRows rows per lane group of one token, any kinds (queries,
-// keys, values).  Row u of group g is head part * RPU + u * groups + g, so that one
-// load of the warp covers neighbouring rows.
-template <int D>
-struct Unit {
-    static constexpr int LPR = D / 8, GPW = 32 / LPR, RPU = kRows * GPW;
+// kRows: rows of a lane group per token.
+template <int D, int kRows>
+struct Rows {
+    static constexpr int LPR = D / 8, GPW = 32 / LPR, RPU = kRows * GPW;   // lanes a row, groups and rows a warp
     __host__ __device__ __forceinline__ static int parts(const RopeArgs& a) { return (a.Hq + 2 * a.Hkv + RPU - 1) / RPU; }
-    unsigned t, b, n;   // token, its batch row, its index there
-    int h0;             // the group's first head
-    __device__ __forceinline__ Unit(const RopeArgs& a, unsigned unit, int parts, int g) {
-        t = unit / parts;
-        h0 = (unit - t * parts) * RPU + g;
-        b = t / static_cast<unsigned>(a.N);
-        n = t - b * a.N;
+    // Sum over the lanes of a row (groups may be in different branches).
+    __device__ __forceinline__ static float sum(float v, unsigned group) {
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(group, v, o);
+        return v;
     }
-    __device__ __forceinline__ int head(int u) const { return h0 + u * GPW; }
+    __device__ __forceinline__ static unsigned group_mask(int g) {
+        return (LPR == 32 ? 0xffffffffu : (1u << LPR) - 1u) << (g * LPR);
+    }
+};
+
+// How the warps share the work: a part (RPU neighbouring heads of the fused row) per
+// warp, tokens t0, t0 + step, ...  With more parts than warps a warp takes several.
+struct Share {
+    int part, part_step;
+    long long t0, step;
+    __device__ __forceinline__ Share(int parts) {
+        const int warps = gridDim.x * kWarps, w = blockIdx.x * kWarps + warp_id();
+        part_step = min(parts, warps);
+        part = w % part_step;
+        step = warps / part_step;
+        t0 = w / part_step;
+        if (t0 >= step) part = parts;   // left over: nothing
+    }
+};
+
+// A token's place: batch row b and index n there.
+struct Where {
+    long long b;
+    int n;
+    __device__ __forceinline__ Where(const RopeArgs& a, long long t) {
+        b = 0;
+        n = static_cast<int>(t);
+        if (a.T != a.N) {   // batches: 32-bit division (T <= 2^31)
+            const unsigned q = static_cast<unsigned>(t) / static_cast<unsigned>(a.N);
+            b = q;
+            n = static_cast<int>(static_cast<unsigned>(t) - q * static_cast<unsigned>(a.N));
+        }
+    }
 };
 
 // PAGED: keys and values go to the cache pages that `slots` names and the queries
 // to [token][Hq][d]; else all three go to [batch][head][N][d].
+constexpr int kFwdRows = 4, kFwdStages = 2, kFwdBlocks = 2;   // blocks: per multiprocessor
+template <int D>
+constexpr int rope_fwd_unit() { return kFwdRows * 32 * 16 + Table<D>::BYTES; }   // bytes of a token in a warp's ring
+template <int D>
+constexpr int rope_fwd_smem() { return kWarps * kFwdStages * rope_fwd_unit<D>(); }
+
 template <int D, bool INTER, bool PAGED>
-__global__ void __launch_bounds__(kThreads) rope_fwd_kernel(RopeArgs a, unsigned units) {
-    using U = Unit<D>;
-    const unsigned unit = blockIdx.x * kWarps + warp_id();
-    if (unit >= units) return;
-    const int lane = lane_id(), l = lane % U::LPR;
-    const U w(a, unit, U::parts(a), lane / U::LPR);
-    const int H = a.Hq + 2 * a.Hkv;
-    Turn<INTER> turn;
-    turn.place(a, l);
-    Quads x[kRows];
-    const bf16* const xrow = a.qkv + static_cast<long long>(w.t) * a.ld;
+__global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs a) {
+    constexpr int kRows = kFwdRows;
+    using R = Rows<D, kRows>;
+    constexpr int UNIT = rope_fwd_unit<D>(), TAB = kRows * 512;
+    extern __shared__ __align__(16) uint8_t sm[];
+    const int lane = lane_id(), l = lane % R::LPR, g = lane / R::LPR;
+    const unsigned group = R::group_mask(g);
+    const int H = a.Hq + 2 * a.Hkv, HN = a.Hq + a.Hkv, parts = R::parts(a);
+    uint8_t* const ring = sm + warp_id() * kFwdStages * UNIT;
+    const int mine = g * (R::LPR * 16);   // the group's row within 512 bytes
+    const Place<INTER> pl(a, l);
+    const Share sh(parts);
+    if (g == 0)
+        for (int i = 0; i < kFwdStages; ++i) Table<D>::clear(ring + i * UNIT + TAB, l);
+    for (int part = sh.part; part < parts; part += sh.part_step) {
+        const int h0 = part * R::RPU + g;   // row u of the group is head h0 + u GPW
+        bf16* out[kRows];
+        Quads w[kRows];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) x[u].load(xrow + min(w.head(u), H - 1) * D, turn.ia, turn.ib);   // past the last: unused
-    const int pos = a.pos != nullptr ? __ldg(a.pos + w.t) : static_cast<int>(w.n);
-    long long slot = 0;
-    if constexpr (PAGED) {
-        slot = __ldg(a.slots + w.t);
-        if (slot == -1) return;   // padding
-    }
-    if (pos < 0 || pos >= a.max_pos || (PAGED && (slot < 0 || slot >= a.n_slots))) {
-        if (lane == 0) atomicExch(a.status, kStatusBadInput);
-        return;
-    }
-    turn.load(a, pos, l);
-    Quads wq, wk;
-    wq.load(a.wq, turn.ia, turn.ib);
-    wk.load(a.wk, turn.ia, turn.ib);
+        for (int u = 0; u < kRows; ++u) {
+            const int h = h0 + u * R::GPW;
+            const bool isq = h < a.Hq, isv = h >= HN;
+            const int hk = isq ? h : (isv ? h - HN : h - a.Hq);
+            const long long rows = PAGED ? (isq ? 1 : 64) : a.N;   // rows of a head before the next head's
+            out[u] = (isq ? a.Q : (isv ? a.V : a.K)) + hk * rows * D;
+            w[u].load(isq ? a.wq : a.wk, pl.ia, pl.ib);
+        }
+        // the next token to fetch, its position and slot (read a token early)
+        long long tf = sh.t0, slot_f = 0, slot = 0, slot1 = 0;
+        int pos_f = 0;
+        unsigned good = 0;   // per fetched token, the latest in bit 0: it has outputs
+        auto locate = [&] {
+            if (tf >= a.T) return;
+            pos_f = a.pos != nullptr ? __ldg(a.pos + tf) : Where(a, tf).n;
+            if constexpr (PAGED) slot_f = __ldg(a.slots + tf);
+        };
+        auto fetch = [&](int st) {
+            good <<= 1;
+            if (tf < a.T) {
+                uint8_t* const dst = ring + st * UNIT;
+                const bf16* const src = a.qkv + tf * a.ld + h0 * D + l * 8;
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-        const int h = w.head(u);
-        const bool isq = h < a.Hq, isv = h >= a.Hq + a.Hkv;
-        float z[8], wf[8];
-        x[u].unpack(z);
-        (isq ? wq : wk).unpack(wf);
-        float ss = 0.f;
+                for (int u = 0; u < kRows; ++u)
+                    if (h0 + u * R::GPW < H) cp_async16(dst + u * 512 + mine + l * 16, src + u * R::GPW * D);
+                const bool ok = pos_f >= 0 && pos_f < a.max_pos && (!PAGED || (slot_f >= 0 && slot_f < a.n_slots));
+                if (ok && g == 0) Table<D>::fetch(dst + TAB, a, pos_f, l);
+                if (!ok && !(PAGED && slot_f == -1) && lane == 0) atomicExch(a.status, kStatusBadInput);   // -1: padding
+                good |= ok;
+            }
+            cp_async_commit();
+            tf += sh.step;
+            locate();
+        };
+        locate();
+        for (int i = 0; i < kFwdStages - 1; ++i) fetch(i);
+        if constexpr (PAGED) slot1 = __ldg(a.slots + sh.t0);
+        int st = 0;
+        for (long long t = sh.t0; t < a.T; t += sh.step) {
+            slot = slot1;
+            if (PAGED && t + sh.step < a.T) slot1 = __ldg(a.slots + t + sh.step);
+            cp_async_wait<kFwdStages - 2>();
+            __syncwarp();   // the lanes' copies of this token have landed; the stage refilled next has been read
+            fetch(st == 0 ? kFwdStages - 1 : st - 1);
+            const uint8_t* const stage = ring + st * UNIT;
+            st = st + 1 == kFwdStages ? 0 : st + 1;
+            if (!((good >> (kFwdStages - 1)) & 1u)) continue;
+            const Turn<INTER, false> turn(stage + TAB + l * 16, stage + TAB + Table<D>::BYTES / 2 + l * 16);
+            long long at_q, at_kv;   // the token's offset in Q, and in K and V
+            if constexpr (PAGED) {
+                at_q = t * a.Hq * D;
+                at_kv = ((slot >> 6) * a.Hkv * 64 + (slot & 63)) * D;
+            } else {
+                const Where at(a, t);
+                at_q = (at.b * a.Hq * a.N + at.n) * D;
+                at_kv = (at.b * a.Hkv * a.N + at.n) * D;
+            }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(z[e], z[e], ss);
-        const float r = rsqrtf(row_sum<U::LPR>(ss) * (1.f / D) + a.eps);
+            for (int u = 0; u < kRows; ++u) {
+                const int h = h0 + u * R::GPW;
+                const uint8_t* const row = stage + u * 512 + mine;
+                if (h < HN) {
+                    Quads q;
+                    uint64_t z[4], wf[4];
+                    q.read(row, pl.ia, pl.ib);
+                    q.unpack(z);
+                    w[u].unpack(wf);
+                    uint64_t ss = mul_f32x2(z[0], z[0]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = z[e] * r * wf[e];
-        turn.template apply<false>(z);
-        if (h >= H) continue;
-        if (!isv) x[u].pack(z);   // values pass through
-        const int hk = isq ? h : (isv ? h - a.Hq - a.Hkv : h - a.Hq);
-        bf16* dst;
-        if constexpr (PAGED)
-            dst = isq ? a.Q + (static_cast<size_t>(w.t) * a.Hq + hk) * D
-                      : (isv ? a.V : a.K) + ((static_cast<size_t>(slot >> 6) * a.Hkv + hk) * 64 + (slot & 63)) * D;
-        else
-            dst = (isq ? a.Q : (isv ? a.V : a.K)) + ((static_cast<size_t>(w.b) * (isq ? a.Hq : a.Hkv) + hk) * a.N + w.n) * D;
-        x[u].store(dst, turn.ia, turn.ib);
+                    for (int i = 1; i < 4; ++i) ss = fma_f32x2(z[i], z[i], ss);
+                    const uint64_t r = dup2(rsqrtf(R::sum(sum2(ss), group) * (1.f / D) + a.eps));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[i] = mul_f32x2(mul_f32x2(z[i], r), wf[i]);
+                    turn.apply(z);
+                    q.pack(z);
+                    q.store(out[u] + (h < a.Hq ? at_q : at_kv), pl.ia, pl.ib);
+                } else if (h < H) {   // values pass through
+                    *reinterpret_cast<uint4*>(out[u] + at_kv + l * 8) = *reinterpret_cast<const uint4*>(row + l * 16);
+                }
+            }
+        }
+        cp_async_wait<0>();
+        __syncwarp();
     }
 }
 
-// Persistent.  A warp streams its units through its own ring in shared memory
-// (cp.async of 16 bytes a lane, kStages - 1 units ahead, no registers held) and keeps
-// its lanes' columns of dwq and dwk in registers.  A block adds its warps' sums into
-// one row of `part`, and the last block to finish adds those in their order: equal
-// inputs give equal sums.
-constexpr int kStages = 3;
+// A lane keeps its columns of dw in registers, per row of its group, and adds them to
+// its warp's sums at the end; a block adds its warps' sums into one row of `part`,
+// and the last block to finish adds those in their order: equal inputs give equal
+// sums.
+constexpr int kBwdRows = 2, kBwdStages = 3, kBwdBlocks = 2;
 template <int D>
-constexpr int rope_bwd_smem() { return kWarps * (kStages * 2 * kRows * 32 * 16 + 2 * D * 4); }
+constexpr int rope_bwd_unit() { return 2 * kBwdRows * 32 * 16 + Table<D>::BYTES; }
+template <int D>
+constexpr int rope_bwd_smem() { return kWarps * (kBwdStages * rope_bwd_unit<D>() + 2 * D * 4); }
 
 template <int D, bool INTER>
-__global__ void __launch_bounds__(kThreads, 2) rope_bwd_kernel(RopeArgs a, unsigned units) {
-    using U = Unit<D>;
-    constexpr int LPR = U::LPR;
-    constexpr int UNIT = 2 * kRows * 32 * 16;   // bytes: kRows rows of x and of dy per group
+__global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs a) {
+    constexpr int kRows = kBwdRows;
+    using R = Rows<D, kRows>;
+    constexpr int UNIT = rope_bwd_unit<D>(), DY = kRows * 512, TAB = 2 * DY;   // rows of x, rows of dy, the table's row
     extern __shared__ __align__(16) uint8_t sm[];
     __shared__ int last;
-    const int lane = lane_id(), warp = warp_id(), l = lane % LPR, g = lane / LPR;
-    const int H = a.Hq + 2 * a.Hkv, HN = a.Hq + a.Hkv, parts = U::parts(a);
-    uint8_t* const ring = sm + warp * kStages * UNIT;
-    float* const sums = reinterpret_cast<float*>(sm + kWarps * kStages * UNIT);   // [kWarps][2 D]
-    const unsigned step = gridDim.x * kWarps;
-    unsigned long long next = blockIdx.x * kWarps + warp;
-
-    // row u of the lane's group, x (0) or dy (1), in stage st
-    auto slot = [&](int st, int which, int u) { return ring + st * UNIT + ((which * kRows + u) * 32 + g * LPR) * 16; };
-    auto fetch = [&](int st) {
-        if (next < units) {
-            const U w(a, static_cast<unsigned>(next), parts, g);
+    const int lane = lane_id(), warp = warp_id(), l = lane % R::LPR, g = lane / R::LPR;
+    const unsigned group = R::group_mask(g);
+    const int H = a.Hq + 2 * a.Hkv, HN = a.Hq + a.Hkv, parts = R::parts(a);
+    uint8_t* const ring = sm + warp * kBwdStages * UNIT;
+    const int mine = g * (R::LPR * 16);
+    float* const sums = reinterpret_cast<float*>(sm + kWarps * kBwdStages * UNIT);   // [kWarps][2 D]
+    float* const sum = sums + warp * 2 * D;
+    for (int i = lane; i < 2 * D; i += 32) sum[i] = 0.f;
+    if (g == 0)
+        for (int i = 0; i < kBwdStages; ++i) Table<D>::clear(ring + i * UNIT + TAB, l);
+    const Place<INTER> pl(a, l);
+    const Share sh(parts);
+    for (int part = sh.part; part < parts; part += sh.part_step) {
+        const int h0 = part * R::RPU + g;
+        const bf16* grad[kRows];
+        Quads w[kRows];
+        uint64_t acc[kRows][4];
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+            const int h = h0 + u * R::GPW;
+            const bool isq = h < a.Hq, isv = h >= HN;
+            const int hk = isq ? h : (isv ? h - HN : h - a.Hq);
+            grad[u] = (isq ? a.Q : (isv ? a.V : a.K)) + static_cast<long long>(hk) * a.N * D + l * 8;
+            w[u].load(isq ? a.wq : a.wk, pl.ia, pl.ib);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[u][i] = 0;
+        }
+        long long tf = sh.t0;   // the next token to fetch and its position (read a token early)
+        int pos_f = 0;
+        unsigned good = 0;      // per fetched token, the latest in bit 0: its position is in the tables
+        auto locate = [&] {
+            if (tf < a.T) pos_f = a.pos != nullptr ? __ldg(a.pos + tf) : Where(a, tf).n;
+        };
+        auto fetch = [&](int st) {
+            good <<= 1;
+            if (tf < a.T) {
+                const bf16* const src = a.qkv + tf * a.ld + h0 * D + l * 8;
+                const Where at(a, tf);
+                const long long at_q = (at.b * a.Hq * a.N + at.n) * D, at_kv = (at.b * a.Hkv * a.N + at.n) * D;
+                uint8_t* const dst = ring + st * UNIT;
+#pragma unroll
+                for (int u = 0; u < kRows; ++u) {
+                    const int h = h0 + u * R::GPW;
+                    if (h < HN) cp_async16(dst + u * 512 + mine + l * 16, src + u * R::GPW * D);
+                    if (h < H) cp_async16(dst + DY + u * 512 + mine + l * 16, grad[u] + (h < a.Hq ? at_q : at_kv));
+                }
+                const bool ok = pos_f >= 0 && pos_f < a.max_pos;
+                if (ok && g == 0) Table<D>::fetch(dst + TAB, a, pos_f, l);
+                if (!ok && lane == 0) atomicExch(a.status, kStatusBadInput);
+                good |= ok;
+            }
+            cp_async_commit();
+            tf += sh.step;
+            locate();
+        };
+        locate();
+        for (int i = 0; i < kBwdStages - 1; ++i) fetch(i);
+        int st = 0;
+        for (long long t = sh.t0; t < a.T; t += sh.step) {
+            cp_async_wait<kBwdStages - 2>();
+            __syncwarp();   // the lanes' copies of this token have landed; the stage refilled next has been read
+            fetch(st == 0 ? kBwdStages - 1 : st - 1);
+            const uint8_t* const stage = ring + st * UNIT;
+            st = st + 1 == kBwdStages ? 0 : st + 1;
+            if (!((good >> (kBwdStages - 1)) & 1u)) continue;
+            const Turn<INTER, true> turn(stage + TAB + l * 16, stage + TAB + Table<D>::BYTES / 2 + l * 16);
+            bf16* const dst = a.dqkv + t * a.ld_d + h0 * D;
 #pragma unroll
             for (int u = 0; u < kRows; ++u) {
-                const int h = w.head(u);
-                if (h < H) {
-                    const bool isq = h < a.Hq, isv = h >= HN;
-                    const int hk = isq ? h : (isv ? h - HN : h - a.Hq);
-                    if (!isv) cp_async16(slot(st, 0, u) + l * 16, a.qkv + static_cast<long long>(w.t) * a.ld + h * D + l * 8);
-                    cp_async16(slot(st, 1, u) + l * 16,
-                               (isq ? a.Q : (isv ? a.V : a.K)) +
-                                   ((static_cast<size_t>(w.b) * (isq ? a.Hq : a.Hkv) + hk) * a.N + w.n) * D + l * 8);
+                const int h = h0 + u * R::GPW;
+                const uint8_t* const row = stage + u * 512 + mine;
+                if (h < HN) {
+                    Quads q;
+                    uint64_t xf[4], z[4], wf[4];
+                    q.read(row, pl.ia, pl.ib);
+                    q.unpack(xf);
+                    q.read(row + DY, pl.ia, pl.ib);
+                    q.unpack(z);
+                    w[u].unpack(wf);
+                    uint64_t ss = mul_f32x2(xf[0], xf[0]);
+#pragma unroll
+                    for (int i = 1; i < 4; ++i) ss = fma_f32x2(xf[i], xf[i], ss);
+                    const uint64_t r = dup2(rsqrtf(R::sum(sum2(ss), group) * (1.f / D) + a.eps));
+                    turn.apply(z);
+                    uint64_t dot = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        xf[i] = mul_f32x2(xf[i], r);   // xh
+                        const uint64_t p = mul_f32x2(z[i], xf[i]);
+                        acc[u][i] = add_f32x2(acc[u][i], p);
+                        dot = fma_f32x2(p, wf[i], dot);
+                    }
+                    const uint64_t m = dup2(R::sum(sum2(dot), group) * (-1.f / D));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[i] = mul_f32x2(r, fma_f32x2(m, xf[i], mul_f32x2(z[i], wf[i])));
+                    q.pack(z);
+                    q.store(dst + u * R::GPW * D, pl.ia, pl.ib);
+                } else if (h < H) {   // values pass through
+                    *reinterpret_cast<uint4*>(dst + u * R::GPW * D + l * 8) = *reinterpret_cast<const uint4*>(row + DY + l * 16);
                 }
             }
         }
-        cp_async_commit();
-        next += step;
-    };
-    for (int i = 0; i < kStages - 1; ++i) fetch(i);
-
-    Turn<INTER> turn;
-    turn.place(a, l);
-    Quads wq, wk;
-    wq.load(a.wq, turn.ia, turn.ib);
-    wk.load(a.wk, turn.ia, turn.ib);
-    float aq[8], ak[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) aq[e] = ak[e] = 0.f;
-    int st = 0;
-    for (unsigned long long unit = blockIdx.x * kWarps + warp; unit < units; unit += step) {
-        const U w(a, static_cast<unsigned>(unit), parts, g);
-        const int pos = a.pos != nullptr ? __ldg(a.pos + w.t) : static_cast<int>(w.n);
-        const bool ok = pos >= 0 && pos < a.max_pos;
-        if (ok) turn.load(a, pos, l);
-        else if (lane == 0) atomicExch(a.status, kStatusBadInput);
-        cp_async_wait<kStages - 2>();
-        __syncwarp();   // the lanes' copies of this unit have landed; the stage refilled next has been read
-        fetch(st == 0 ? kStages - 1 : st - 1);
-        if (ok) {
+        cp_async_wait<0>();
+        // the part's sums, one lane group after the other
+        for (int gg = 0; gg < R::GPW; ++gg) {
+            __syncwarp();
+            if (g != gg) continue;
 #pragma unroll
             for (int u = 0; u < kRows; ++u) {
-                const int h = w.head(u);
-                const bool isq = h < a.Hq, isk = !isq && h < HN;
-                Quads q;
-                float xf[8], z[8], wf[8];
-                q.read(slot(st, 0, u), turn.ia, turn.ib);
-                q.unpack(xf);
-                q.read(slot(st, 1, u), turn.ia, turn.ib);
-                q.unpack(z);
-                (isq ? wq : wk).unpack(wf);
-                float ss = 0.f;
+                const int h = h0 + u * R::GPW;
+                if (h >= HN) continue;
+                float* const col = sum + (h < a.Hq ? 0 : D);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ss = fmaf(xf[e], xf[e], ss);
-                const float r = rsqrtf(row_sum<LPR>(ss) * (1.f / D) + a.eps);
-                turn.template apply<true>(z);
-                float dot = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    xf[e] *= r;   // xh
-                    const float p = z[e] * xf[e];
-                    if (isq) aq[e] += p;
-                    if (isk) ak[e] += p;
-                    dot = fmaf(p, wf[e], dot);
+                for (int i = 0; i < 4; ++i) {
+                    float lo, hi;
+                    f32x2_split(acc[u][i], lo, hi);
+                    const int at = i < 2 ? pl.ia + 2 * i : pl.ib + 2 * (i - 2);
+                    col[at] += lo;
+                    col[at + 1] += hi;
                 }
-                const float m = row_sum<LPR>(dot) * (1.f / D);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] = r * fmaf(-m, xf[e], z[e] * wf[e]);
-                if (isq || isk) q.pack(z);   // values pass through
-                if (h < H) q.store(a.dqkv + static_cast<long long>(w.t) * a.ld_d + h * D, turn.ia, turn.ib);
             }
         }
-        st = st + 1 == kStages ? 0 : st + 1;
-    }
-    cp_async_wait<0>();
-    // the warp's groups, then the block's warps
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-#pragma unroll
-        for (int o = LPR; o < 32; o <<= 1) {
-            aq[e] += __shfl_xor_sync(0xffffffffu, aq[e], o);
-            ak[e] += __shfl_xor_sync(0xffffffffu, ak[e], o);
-        }
-        if (g == 0) {
-            const int at = warp * 2 * D + (e < 4 ? turn.ia + e : turn.ib + e - 4);
-            sums[at] = aq[e];
-            sums[at + D] = ak[e];
-        }
+        __syncwarp();
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
@@ -323,14 +476,19 @@ __global__ void __launch_bounds__(kThreads, 2) rope_bwd_kernel(RopeArgs a, unsig
     }
 }
 
-template <int D>
-long long units_of(const RopeArgs& a) { return a.T * Unit<D>::parts(a); }
+// Blocks for all (token, part) pairs at `tokens` a warp, at most `most` (the kernels are
+// persistent).
+template <int D, int kRows>
+int blocks_for(const RopeArgs& a, int most, int tokens) {
+    const long long need = (a.T * Rows<D, kRows>::parts(a) + kWarps * tokens - 1) / (kWarps * tokens);
+    return static_cast<int>(need < most ? need : most);
+}
 
-template <int D, bool INTER>
+template <int D, bool INTER, bool PAGED>
 cudaError_t launch_fwd(const RopeArgs& a, const KernelEnv& env) {
-    const unsigned units = static_cast<unsigned>(units_of<D>(a)), blocks = (units + kWarps - 1) / kWarps;
-    if (a.slots != nullptr) rope_fwd_kernel<D, INTER, true><<<blocks, kThreads, 0, env.stream>>>(a, units);
-    else rope_fwd_kernel<D, INTER, false><<<blocks, kThreads, 0, env.stream>>>(a, units);
+    const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(rope_fwd_kernel<D, INTER, PAGED>), rope_fwd_smem<D>(), true);
+    if (e != cudaSuccess) return e;
+    rope_fwd_kernel<D, INTER, PAGED><<<blocks_for<D, kFwdRows>(a, kFwdBlocks * device_sm_count(), 1), kThreads, rope_fwd_smem<D>(), env.stream>>>(a);
     return cudaGetLastError();
 }
 
@@ -338,11 +496,13 @@ template <int D, bool INTER>
 cudaError_t launch_bwd(const RopeArgs& a, const KernelEnv& env) {
     const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(rope_bwd_kernel<D, INTER>), rope_bwd_smem<D>(), true);
     if (e != cudaSuccess) return e;
-    const unsigned units = static_cast<unsigned>(units_of<D>(a));
-    const long long need = (static_cast<long long>(units) + kWarps - 1) / kWarps;
-    const int blocks = static_cast<int>(need < rope_bwd_max_blocks() ? need : rope_bwd_max_blocks());
-    rope_bwd_kernel<D, INTER><<<blocks, kThreads, rope_bwd_smem<D>(), env.stream>>>(a, units);
+    rope_bwd_kernel<D, INTER><<<blocks_for<D, kBwdRows>(a, rope_bwd_max_blocks(), 4), kThreads, rope_bwd_smem<D>(), env.stream>>>(a);
     return cudaGetLastError();
+}
+
+template <int D, bool INTER>
+cudaError_t launch_any_fwd(const RopeArgs& a, const KernelEnv& env) {
+    return a.slots != nullptr ? launch_fwd<D, INTER, true>(a, env) : launch_fwd<D, INTER, false>(a, env);
 }
 
 }  // namespace
@@ -356,14 +516,14 @@ const char* rope_check(int rot, int interleaved, int max_pos, float eps, long lo
     return nullptr;
 }
 
-// Units are counted in 32 bits, so that the kernels divide 32-bit numbers.
-bool rope_supported(const RopeArgs& a, int d) { return (d == 128 ? units_of<128>(a) : units_of<64>(a)) <= 0x7fffffffLL; }
+// Tokens are counted in 32 bits where a batch row is found by division.
+bool rope_supported(const RopeArgs& a) { return a.T <= 0x7fffffffLL; }
 
-int rope_bwd_max_blocks() { return 2 * device_sm_count(); }   // two a multiprocessor, all resident
+int rope_bwd_max_blocks() { return kBwdBlocks * device_sm_count(); }   // all resident
 
 cudaError_t launch_rope_fwd(const RopeArgs& a, int d, const KernelEnv& env) {
-    if (d == 128) return a.interleaved ? launch_fwd<128, true>(a, env) : launch_fwd<128, false>(a, env);
-    if (d == 64) return a.interleaved ? launch_fwd<64, true>(a, env) : launch_fwd<64, false>(a, env);
+    if (d == 128) return a.interleaved ? launch_any_fwd<128, true>(a, env) : launch_any_fwd<128, false>(a, env);
+    if (d == 64) return a.interleaved ? launch_any_fwd<64, true>(a, env) : launch_any_fwd<64, false>(a, env);
     return cudaErrorInvalidValue;
 }
 

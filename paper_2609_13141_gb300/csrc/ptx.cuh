@@ -380,6 +380,11 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 // One to the shared word at saddr when u >= lo (false for a NaN u), the
 // comparison inside the predicated block.
 __device__ __forceinline__ void red_shared_inc_if_ge(float u, float lo, uint32_t saddr) {

@@ -879,7 +879,7 @@ sas_status rope_args(sas_handle* h, const sas_rope_config* rope, const void* qkv
     a.max_pos = rope->max_pos; a.rot = rope->rot; a.interleaved = rope->interleaved; a.eps = rope->eps;
     a.Hq = c.H; a.Hkv = h->Hkv; a.T = static_cast<long long>(c.B) * c.N; a.N = c.N;
     a.status = h->status;
-    if (!sas::rope_supported(a, c.d)) return fail(h, SAS_ERR_UNSUPPORTED, "too many rows for one launch");
+    if (!sas::rope_supported(a)) return fail(h, SAS_ERR_UNSUPPORTED, "too many tokens");
     return SAS_OK;
 }
 

@@ -268,7 +268,7 @@ sas_status sas_chunk_append(sas_chunk_handle* h, const sas_rope_config* rope, in
         a.Hq = c.Hq; a.Hkv = c.Hkv; a.T = T; a.N = T;
         a.Q = static_cast<sas::bf16*>(Q); a.K = static_cast<sas::bf16*>(K_cache); a.V = static_cast<sas::bf16*>(V_cache);
         a.slots = slots; a.n_slots = 64LL * c.num_pages; a.status = h->status;
-        if (!sas::rope_supported(a, c.d)) return cfail(h, SAS_ERR_UNSUPPORTED, "too many rows for one launch");
+        if (!sas::rope_supported(a)) return cfail(h, SAS_ERR_UNSUPPORTED, "too many tokens");
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         const sas::KernelEnv env{s, h->status, h->limit};
         const cudaError_t e = ctimed(h, 1, 1, s, [&] { return sas::launch_rope_fwd(a, c.d, env); });
