@@ -607,8 +607,8 @@ typedef struct {
 typedef struct sas_chunk_handle sas_chunk_handle;
 
 /* Validates cfg and allocates the handle's workspace on the current device (the
- * one its calls must run on): the attention's work list and split results (80 MB at
- * d = 128) and small arrays.  Synchronous. */
+ * one its calls must run on): the attention's split results (40 MB at d = 128) and
+ * small arrays.  Synchronous. */
 sas_status sas_chunk_create(const sas_chunk_config* cfg, sas_chunk_handle** out);
 void sas_chunk_destroy(sas_chunk_handle* h);
 

@@ -334,24 +334,14 @@ struct ChunkArgs {
     const int32_t* kv_lens;     // [B] tokens of each sequence, the new ones included
     bf16* O;                    // [T][Hq][d]
     float* LSE;                 // [T][Hq] or null
-    // workspace (sizes: chunk_* below)
-    int target;                 // items to split the work into
-    int32_t* tile_off;          // [B] first tile of each sequence
-    int4* tiles;                // [tiles] {sequence, first token, tokens, first position}
-    int4* items;                // [items][2] the tile, then {first page, end page, first partial, split << 16 | splits}
-    int* nitems;                // items per KV group
-    int* sched;                 // items handed out past each block's first
-    int* counts;                // [partials][Hkv] splits done of each tile
-    float* part_o;              // [partials][Hkv][128][d]
-    float2* part_ml;            // [partials][Hkv][128] (max, sum)
+    // workspace
+    int blocks;                 // chunk_blocks()
+    int4* splits;               // [2 blocks][2] {KV group, first token, tokens, used}, {first page, end page, unit's pages, 0}
+    float* part_o;              // [2 blocks][d / 4][128][4]
+    float2* part_ml;            // [2 blocks][128] (max, sum)
     int* status;
 };
-constexpr int kChunkMinSplit = 4;   // pages
-// Items aimed at when tiles are split.  With W pages over all tiles and heads, a
-// split takes len = max(kChunkMinSplit, W / target) pages, so per KV group there are at
-// most target / Hkv items more than tiles, and at most 2 target / Hkv partials (only
-// tiles of more than len pages have any).
-int chunk_target_items();
+int chunk_blocks();             // blocks of the attention; each writes at most two splits
 cudaError_t chunk_attn_prepare(int d);   // shared-memory limit (before any capture)
 cudaError_t launch_chunk_attn(const ChunkArgs& a, const KernelEnv& env, const char** err);
 

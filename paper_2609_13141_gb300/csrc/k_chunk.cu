@@ -14,10 +14,14 @@
 //     bf16 pairs into TMEM, O rescaled only when the maximum grows by 2^8.
 // P is rounded to bf16 for the tensor core (its row sum is taken before, in fp32).
 //
-// Few new tokens over a long cache leave few tiles: a tile's pages are then split
-// over several items (chunk_tiles_kernel), each writing its (max, sum, O) in fp32,
-// and the last item of a tile to finish joins them in the order of the splits, so
-// equal inputs give equal outputs.
+// Work: a unit is one tile of one KV group, its cost its pages and a constant.  All
+// units, in the order (sequence, tile, group), are cut into equal ranges, one per block: no
+// scheduling at run time, every block ends at about the same time however long the
+// units are, and a block splits at most the first and the last unit of its range.  A
+// split writes its (max, sum, O) in fp32, and chunk_join_kernel joins the splits of
+// a unit in their order, so equal inputs give equal outputs.  A block takes its whole
+// units first: units of one sequence then walk the same pages at about the same time
+// on many blocks, out of L2.
 //
 // Keys past a sequence's end in its last page may hold anything: scores there are
 // replaced, not weighted by zero, and values past the tile's last position are
@@ -41,145 +45,146 @@ constexpr int kItemSlots = 4;     // work items in flight between warp 0 and the
 constexpr int kItemReaders = 7;   // V producer, two MMA issuers, four softmax warps
 constexpr int kStatusBadInput = 1;
 constexpr int kStatusLayout = 3;
-constexpr int kJoin = 8;          // rows of a warp in flight when splits are joined
-constexpr int kPlanThreads = 1024;
-constexpr int kBuckets = 64;
+constexpr int kUnitCost = 3;      // what a unit costs beside its pages (its Q tile, its epilogue), in pages
+constexpr int kSnap = 4;          // pages: ranges do not cut this close to a unit's ends
+constexpr int kMinShare = 4;      // pages of a block's range, at least
+constexpr int kJoinThreads = 256;
 
 __device__ __forceinline__ void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
-// ------------------------------------------------------------------ work list
-//
-// One block: tiles of every sequence (prefix sum over sequences), the total number
-// of pages they walk, from it the split length that gives about `target` items, and
-// the items, longest first (64 classes of length; the order within a class does not
-// change any result).
+// ------------------------------------------------------------------ shares
 
-__global__ void __launch_bounds__(kPlanThreads) chunk_tiles_kernel(ChunkArgs a, int R) {
-    __shared__ int wsum[32];
-    __shared__ int hist[kBuckets], carry, npart, maxlen;
-    __shared__ unsigned long long work;
-    grid_dep_launch();
+// Sequence b: its new tokens and its length, no new tokens if the length is wrong.
+struct Seq {
+    int c0, n, L;
+    __device__ __forceinline__ Seq(const ChunkArgs& a, int b) {
+        c0 = __ldg(a.cu + b);
+        n = __ldg(a.cu + b + 1) - c0;
+        L = __ldg(a.kv_lens + b);
+        if (L < n || L > 64LL * a.max_blocks) n = 0;
+    }
+    __device__ __forceinline__ int tiles(int R) const { return (n + R - 1) / R; }
+    // pages of tile t
+    __device__ __forceinline__ int pages(int t, int R) const { return ((L - n + min(n, (t + 1) * R) - 1) >> 6) + 1; }
+    // cost of tiles 0 .. m - 1, all full: their pages are the sum over t = 1 .. m of floor((p + t R) / 64)
+    // + 1, p = L - n - 1
+    __device__ __forceinline__ long long before(int m, int R) const {
+        const int p = L - n - 1;
+        const long long M = m;
+        if (R >= 64) return M * (p >> 6) + (R >> 6) * (M * (M + 1) / 2) + M * (1 + kUnitCost);
+        const int k = 64 / R;   // tiles of a page's length: t = k s + j gives floor((p + j R) / 64) + s
+        long long sum = M * (1 + kUnitCost);
+        for (int j = 0; j < k; ++j) {
+            const long long cnt = j == 0 ? m / k : (m >= j ? (m - j) / k + 1 : 0);
+            sum += cnt * ((p + j * R) >> 6) + (j == 0 ? cnt * (cnt + 1) : cnt * (cnt - 1)) / 2;
+        }
+        return sum;
+    }
+    __device__ __forceinline__ long long all(int R) const {
+        const int nt = tiles(R);
+        return nt == 0 ? 0 : before(nt - 1, R) + pages(nt - 1, R) + kUnitCost;
+    }
+};
+
+// A boundary between two ranges: page `page` of unit (seq, tile, head) of nb pages.
+struct Bound {
+    int seq, tile, head, page, nb;
+};
+
+// Scratch of the block that finds its range.
+struct Shares {
+    long long sum[kThreads / 32];
+    int units[kThreads / 32];
+    Bound at[2];
+};
+
+// The block's range [at[0], at[1]); false if it has none.  All threads call it.  Every
+// block sums up all sequences itself (12 bytes each, from L2): no launch before this
+// one, nothing to wait for.
+__device__ __forceinline__ bool find_range(const ChunkArgs& a, int R, Shares& sh) {
     const int t = threadIdx.x, lane = lane_id(), warp = warp_id();
-    if (t == 0) {
-        carry = 0;
-        npart = 0;
-        maxlen = 1;
-        work = 0;
-        a.sched[0] = 0;
-    }
-    if (t < kBuckets) hist[t] = 0;
-    int bad = 0;
-    for (int b = t; b < a.B; b += kPlanThreads) {
+    const int per = (a.B + kThreads - 1) / kThreads;   // neighbouring sequences of a thread
+    const int b0 = min(a.B, t * per), b1 = min(a.B, b0 + per);
+    long long cost = 0;
+    int units = 0, bad = 0;
+    for (int b = b0; b < b1; ++b) {
         const int c0 = __ldg(a.cu + b), c1 = __ldg(a.cu + b + 1);
+        const Seq x(a, b);
         bad |= c0 < 0 || c1 < c0 || c1 > a.T;
+        if (x.n != c1 - c0 && blockIdx.x == 0) atomicExch(a.status, kStatusBadInput);
+        cost += x.all(R);
+        units += x.tiles(R);
     }
-    bad = __syncthreads_or(bad);
-    if (bad) {   // offsets that overlap could ask for more tiles than there is room for
-        if (t == 0) {
-            atomicExch(a.status, kStatusBadInput);
-            *a.nitems = 0;
-        }
-        return;
-    }
-    for (int base = 0; base < a.B; base += kPlanThreads) {
-        const int b = base + t;
-        int nt = 0;
-        if (b < a.B) {
-            const int n = __ldg(a.cu + b + 1) - __ldg(a.cu + b), L = __ldg(a.kv_lens + b);
-            if (L < n || L > 64LL * a.max_blocks) atomicExch(a.status, kStatusBadInput);
-            else nt = (n + R - 1) / R;
-        }
-        int inc = nt;
+    long long inc = cost;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += x;
-        }
-        if (lane == 31) wsum[warp] = inc;
-        __syncthreads();
-        if (warp == 0) {
-            int v = wsum[lane];
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += x;
+    }
+    units = __reduce_add_sync(0xffffffffu, units);
+    if (lane == 31) {
+        sh.sum[warp] = inc;
+        sh.units[warp] = units;
+    }
+    if (__syncthreads_or(bad)) {
+        if (blockIdx.x == 0 && t == 0) atomicExch(a.status, kStatusBadInput);
+        return false;
+    }
+    long long base = 0, total = 0, all_units = 0;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int x = __shfl_up_sync(0xffffffffu, v, o);
-                if (lane >= o) v += x;
-            }
-            wsum[lane] = v;
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w == warp) base = total;
+        total += sh.sum[w];
+        all_units += sh.units[w];
+    }
+    total *= a.Hkv;
+    all_units *= a.Hkv;
+    if (total == 0) return false;
+    // as many ranges as blocks, fewer where they would be under kMinShare pages or a unit
+    const long long want = max(all_units, (total - all_units * kUnitCost + kMinShare - 1) / kMinShare);
+    const int ranges = static_cast<int>(min(static_cast<long long>(gridDim.x), want));
+    if (static_cast<int>(blockIdx.x) >= ranges) return false;
+    // boundary k at k share + min(k, rest): ranges differ by one at most
+    const long long share = total / ranges;
+    const int rest = static_cast<int>(total - share * ranges);
+    const long long lo = (base + inc - cost) * a.Hkv, hi = (base + inc) * a.Hkv;   // this thread's sequences
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+        const int c = blockIdx.x + k;
+        const long long p = c * share + min(c, rest);
+        // the end of the last range is the end of the last unit
+        const long long q = p < total ? p : total - 1;
+        if (q < lo || q >= hi) continue;
+        long long off = q - lo;
+        int b = b0;
+        Seq x(a, b);
+        while (b + 1 < b1) {
+            const long long y = x.all(R) * a.Hkv;
+            if (off < y) break;
+            off -= y;
+            x = Seq(a, ++b);
         }
-        __syncthreads();
-        if (b < a.B) a.tile_off[b] = carry + (warp > 0 ? wsum[warp - 1] : 0) + inc - nt;
-        __syncthreads();
-        if (t == 0) carry += wsum[31];
-        __syncthreads();
-    }
-    const int ntiles = carry;
-    unsigned long long mine = 0;
-    int longest = 1;
-    for (int i = t; i < ntiles; i += kPlanThreads) {
-        int lo = 0, hi = a.B;   // the last sequence whose first tile is <= i (empty ones share theirs with the next)
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (a.tile_off[mid] <= i) lo = mid;
-            else hi = mid;
+        int tl = 0, th = x.tiles(R);   // the last tile that starts at or before off
+        while (th - tl > 1) {
+            const int mid = (tl + th) >> 1;
+            if (x.before(mid, R) * a.Hkv <= off) tl = mid;
+            else th = mid;
         }
-        const int c0 = __ldg(a.cu + lo), n = __ldg(a.cu + lo + 1) - c0, L = __ldg(a.kv_lens + lo);
-        const int k = (i - a.tile_off[lo]) * R;
-        const int nt = min(R, n - k), pos0 = L - n + k;
-        a.tiles[i] = make_int4(lo, c0 + k, nt, pos0);
-        const int nb = ((pos0 + nt - 1) >> 6) + 1;
-        mine += nb;
-        longest = max(longest, nb);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        mine += __shfl_xor_sync(0xffffffffu, mine, o);
-        longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
-    }
-    if (lane == 0) {
-        atomicAdd(&work, mine);
-        atomicMax(&maxlen, longest);
+        off -= x.before(tl, R) * a.Hkv;
+        // off < Hkv (pages + kUnitCost) < 2^32
+        Bound y;
+        y.seq = b;
+        y.tile = tl;
+        y.nb = x.pages(tl, R);
+        y.head = static_cast<unsigned>(off) / static_cast<unsigned>(y.nb + kUnitCost);
+        const int page = static_cast<int>(off - static_cast<long long>(y.head) * (y.nb + kUnitCost)) - kUnitCost;
+        y.page = page < kSnap ? 0 : (y.nb - page < kSnap ? y.nb : page);
+        if (p >= total) y.page = y.nb;
+        sh.at[k] = y;
     }
     __syncthreads();
-    const unsigned long long per_item = (work * a.Hkv + a.target - 1) / a.target;
-    const int len = per_item < kChunkMinSplit ? kChunkMinSplit
-                                              : (per_item < (1u << 20) ? static_cast<int>(per_item) : (1 << 20));
-    const int top = min(maxlen, len);
-    // longest first: class of a split length
-    auto cls = [&](int per) { return kBuckets - 1 - static_cast<int>(static_cast<long long>(per) * (kBuckets - 1) / top); };
-    for (int pass = 0; pass < 2; ++pass) {
-        for (int i = t; i < ntiles; i += kPlanThreads) {
-            const int4 x = a.tiles[i];
-            const int nb = ((x.w + x.z - 1) >> 6) + 1;
-            const int want = (nb + len - 1) / len;
-            const int per = (nb + want - 1) / want, ns = (nb + per - 1) / per;
-            const int c = max(0, min(kBuckets - 1, cls(per)));
-            const int at = atomicAdd(&hist[c], ns);
-            if (pass == 0) continue;
-            int part = -1;
-            if (ns > 1) {
-                part = atomicAdd(&npart, ns);
-                for (int h = 0; h < a.Hkv; ++h) a.counts[static_cast<size_t>(part) * a.Hkv + h] = 0;
-            }
-            for (int s = 0; s < ns; ++s) {
-                a.items[2 * (at + s)] = x;
-                a.items[2 * (at + s) + 1] = make_int4(s * per, min(nb, (s + 1) * per), part, (s << 16) | ns);
-            }
-        }
-        __syncthreads();
-        if (pass == 0) {
-            if (t == 0) {
-                int sum = 0;
-                for (int c = 0; c < kBuckets; ++c) {
-                    const int x = hist[c];
-                    hist[c] = sum;
-                    sum += x;
-                }
-                *a.nitems = sum;
-            }
-            __syncthreads();
-        }
-    }
+    return true;
 }
 
 // ------------------------------------------------------------------ attention
@@ -193,7 +198,7 @@ struct Cfg {
     static constexpr int OFF_K = Q_BYTES;
     static constexpr int OFF_V = OFF_K + KST * KV_BYTES;
     static constexpr int OFF_CTL = OFF_V + VST * KV_BYTES;
-    static constexpr int SMEM = OFF_CTL + 512;
+    static constexpr int SMEM = OFF_CTL + 768;   // barriers and items, then Shares
     static constexpr int TMEM_COLS = 256;    // O [0,D)  S [128,192)  P0 [192,224)  P1 [224,256)
     static constexpr int TMEM_O = 0;
     static constexpr int TMEM_S = 128;
@@ -202,24 +207,23 @@ struct Cfg {
     static constexpr uint32_t IDESC_O = idesc_bf16(kBM, D, 0, 1);
 };
 
-// A work item as the roles read it: one split of one tile of one KV group.
+// A work item as the roles read it: a unit, or a split of one.
 struct Item {
     int head;                 // KV group, or -1: no more work
     int seq, tok0, ntok, pos0;
-    int blk0, blk1;           // its pages
-    int part, split, ns;      // partial results (part < 0: the whole tile)
+    int blk0, blk1, nb;       // its pages, of the unit's nb
+    int part;                 // where a split's results go (-1: the whole unit)
 };
 
 struct Ctl {
     uint64_t q_full, q_empty, k_full[4], k_empty[4], v_full[4], v_empty[4];
     uint64_t s_full, s_free, p_full[2], pv_done[2], drain_bar;
-    uint64_t part_done, last_known;   // a split's results written by the four softmax warps; ctl.last set
     uint64_t item_full[kItemSlots], item_empty[kItemSlots];
     Item item[kItemSlots];
     uint32_t tmem_base;
-    int abort_flag, last;
+    int abort_flag;
 };
-static_assert(sizeof(Ctl) <= 512, "control block");
+static_assert(sizeof(Ctl) <= 512 && sizeof(Shares) <= 256, "control block");
 
 __device__ __forceinline__ bool read_item(Ctl& ctl, int r, const WaitCtl& wc, Item& x) {
     const int slot = r % kItemSlots;
@@ -266,8 +270,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
             mbar_init(&ctl.p_full[s], 4);
         }
         mbar_init(&ctl.drain_bar, 2);
-        mbar_init(&ctl.part_done, 4);
-        mbar_init(&ctl.last_known, 1);
         for (int s = 0; s < kItemSlots; ++s) {
             mbar_init(&ctl.item_full[s], 1);
             mbar_init(&ctl.item_empty[s], kItemReaders);
@@ -283,33 +285,74 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
     tc_fence_after();
     const uint32_t tmem_base = ctl.tmem_base;
     const WaitCtl wc{&ctl.abort_flag, a.status, limit};
-    grid_dep_wait();   // the work list, and through its kernel everything before it
+    Shares& sh = *reinterpret_cast<Shares*>(smem + C::OFF_CTL + 512);
+    grid_dep_wait();   // whatever the stream ran before: lengths, table, cache
+    const int R = kBM / a.G;
+    const bool any = find_range(a, R, sh);
+    grid_dep_launch();   // the join's blocks may take the places that open up (they wait for this grid's end)
 
     // Every role walks the same items and counts pages over all of them (g): ring
     // slots, score buffers and barrier phases follow g across item boundaries.
     if (warp == 0) {
         // ---------------- items and K pages
         if (lane == 0) tma_prefetch_desc(&mapK);
-        const long long W = static_cast<long long>(*a.nitems) * a.Hkv;
-        long long w = blockIdx.x;
+        const Bound from = sh.at[0], to = sh.at[1];
+        int seq = from.seq, tile = from.tile, head = from.head;   // the unit to look at next
+        bool more = any, first = true;
+        int late_lo = 0, late_hi = 0;   // the split of the first unit, left for the end
+        unsigned used = 0;              // partial results written: slots 2 block + 0, + 1
         int g = 0;
         bool ok = true;
         for (int r = 0; ok; ++r) {
-            const int slot = r % kItemSlots;
-            if (!mbar_wait_warp(&ctl.item_empty[slot], ((r / kItemSlots) & 1) ^ 1u, wc)) { ok = false; break; }
             Item x;
             x.head = -1;
             x.blk0 = x.blk1 = 0;
-            int next = 0;
-            if (w < W) {
-                if (lane == 0) next = atomicAdd(a.sched, 1);   // used when this item's pages are issued
-                const long long e = w / a.Hkv;
-                const int4 v0 = a.items[2 * e], v1 = a.items[2 * e + 1];
-                x = Item{static_cast<int>(w - e * a.Hkv), v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w >> 16, v1.w & 0xffff};
+            while (more && x.head < 0) {
+                const Seq q(a, seq);
+                const int nb = q.pages(tile, R);
+                const bool last = seq == to.seq && tile == to.tile && head == to.head;
+                const int lo = first ? from.page : 0, hi = last ? to.page : nb;
+                if (first && lo < hi && (lo > 0 || hi < nb)) {
+                    late_lo = lo;
+                    late_hi = hi;
+                } else if (lo < hi) {
+                    x = Item{head, seq, q.c0 + tile * R, min(R, q.n - tile * R), q.L - q.n + tile * R, lo, hi, nb,
+                             hi < nb ? static_cast<int>(2 * blockIdx.x + 1) : -1};
+                }
+                first = false;
+                more = !last;
+                if (more && ++head == a.Hkv) {
+                    head = 0;
+                    if (++tile >= q.tiles(R)) {
+                        // the next sequence with new tokens; the range's end lies in one
+                        tile = 0;
+                        for (int b = seq + 1;; b += 32) {
+                            const int y = b + static_cast<int>(lane);
+                            const unsigned has = __ballot_sync(0xffffffffu, y <= to.seq && Seq(a, min(y, to.seq)).n > 0);
+                            if (has != 0 || b >= to.seq) {
+                                seq = has != 0 ? b + __ffs(has) - 1 : to.seq;
+                                break;
+                            }
+                        }
+                    }
+                }
             }
+            if (x.head < 0 && late_lo < late_hi) {
+                const Seq q(a, from.seq);
+                x = Item{from.head, from.seq, q.c0 + from.tile * R, min(R, q.n - from.tile * R), q.L - q.n + from.tile * R,
+                         late_lo, late_hi, from.nb, static_cast<int>(2 * blockIdx.x)};
+                late_hi = 0;
+            }
+            const int slot = r % kItemSlots;
+            if (!mbar_wait_warp(&ctl.item_empty[slot], ((r / kItemSlots) & 1) ^ 1u, wc)) { ok = false; break; }
             if (lane == 0) {
                 ctl.item[slot] = x;
                 mbar_arrive(&ctl.item_full[slot]);
+                if (x.part >= 0 && x.head >= 0) {   // what the join has to know
+                    a.splits[2 * x.part] = make_int4(x.head, x.tok0, x.ntok, 1);
+                    a.splits[2 * x.part + 1] = make_int4(x.blk0, x.blk1, x.nb, 0);
+                    used |= 1u << (x.part & 1);
+                }
             }
             __syncwarp();
             if (x.head < 0) break;
@@ -328,7 +371,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 }
                 __syncwarp();
             }
-            w = gridDim.x + static_cast<long long>(__shfl_sync(0xffffffffu, next, 0));
+        }
+        if (lane == 0) {
+            for (int k = 0; k < 2; ++k)
+                if (!((used >> k) & 1u)) a.splits[2 * (2 * blockIdx.x + k)] = make_int4(0, 0, 0, 0);
         }
         if (!ok && lane == 0) {   // the last KST loads may be in flight
             for (int q = g - 1; q >= 0 && q >= g - C::KST; --q)
@@ -462,7 +508,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
         const int tok = row / a.G, hq = row - tok * a.G;
         const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
         const uint64_t scale2 = f32x2(scale_log2, scale_log2);
-        int g = 0, np = 0;   // pages and splits over all items
+        int g = 0;
         bool ok = true;
         for (int r = 0; ok; ++r) {
             Item x;
@@ -591,10 +637,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 tc_fence_before();
                 continue;
             }
-            // ---- a split: (max, sum) and the unnormalised O of every row in fp32
-            const size_t pslot = (static_cast<size_t>(x.part) + x.split) * a.Hkv + x.head;
+            // ---- a split: (max, sum) and the unnormalised O of every row in fp32, laid out
+            // [quad of columns][row], so that a warp's 32 rows write 512 bytes at a time
             if (warp_rows) {
-                float* po = a.part_o + (pslot * kBM + row) * D;
+                float4* po = reinterpret_cast<float4*>(a.part_o) + static_cast<size_t>(x.part) * (D / 4) * kBM + row;
 #pragma unroll 1
                 for (int cc = 0; cc < D / 32; ++cc) {
                     uint32_t o[32];
@@ -603,107 +649,13 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                     if (valid) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
-                            reinterpret_cast<uint4*>(po + cc * 32)[e] =
-                                make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                            po[(cc * 8 + e) * kBM] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]),
+                                                                 __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
                     }
                 }
-                if (valid) a.part_ml[pslot * kBM + row] = make_float2(m_use, l);
+                if (valid) a.part_ml[static_cast<size_t>(x.part) * kBM + row] = make_float2(m_use, l);
             }
             tc_fence_before();
-            // (barriers with a bounded wait: a warp that gave up must not leave the others waiting)
-            __threadfence();
-            mbar_arrive_warp(&ctl.part_done);
-            if (q == 0) {
-                if (!mbar_wait_warp(&ctl.part_done, np & 1, wc)) { ok = false; break; }
-                if (lane == 0) {
-                    *reinterpret_cast<volatile int*>(&ctl.last) =
-                        atomicAdd(a.counts + static_cast<size_t>(x.part) * a.Hkv + x.head, 1) == x.ns - 1;
-                    mbar_arrive(&ctl.last_known);
-                }
-                __syncwarp();
-            }
-            // the flag is set again only after all four warps' next arrival on part_done
-            if (!mbar_wait_warp(&ctl.last_known, np & 1, wc)) { ok = false; break; }
-            ++np;
-            if (*reinterpret_cast<volatile int*>(&ctl.last) == 0) continue;
-            __threadfence();
-            // join the splits: a warp takes kJoin rows at a time (their loads in flight
-            // together), D / 32 columns a lane
-            constexpr int CPL = D / 32;
-            const size_t stride = static_cast<size_t>(a.Hkv) * kBM;   // rows between the splits of a tile
-            const int rows = x.ntok * a.G;
-            const size_t base = (static_cast<size_t>(x.part) * a.Hkv + x.head) * kBM;
-            for (int r0 = q; r0 < rows; r0 += 4 * kJoin) {
-                float M[kJoin], L[kJoin], acc[kJoin][CPL];
-#pragma unroll
-                for (int k = 0; k < kJoin; ++k) {
-                    M[k] = -CUDART_INF_F;
-                    L[k] = 0.f;
-#pragma unroll
-                    for (int e = 0; e < CPL; ++e) acc[k][e] = 0.f;
-                }
-                // rows past the last repeat it: loaded, not stored
-                for (int s = lane; s < x.ns; s += 32) {
-#pragma unroll
-                    for (int k = 0; k < kJoin; ++k)
-                        M[k] = fmaxf(M[k], __ldcg(a.part_ml + base + min(r0 + 4 * k, rows - 1) + s * stride).x);
-                }
-#pragma unroll
-                for (int k = 0; k < kJoin; ++k)
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) M[k] = fmaxf(M[k], __shfl_xor_sync(0xffffffffu, M[k], o));
-                for (int s0 = 0; s0 < x.ns; s0 += 32) {
-                    float wgt[kJoin];
-#pragma unroll
-                    for (int k = 0; k < kJoin; ++k) {
-                        wgt[k] = 0.f;
-                        if (s0 + static_cast<int>(lane) < x.ns) {
-                            const float2 ml = __ldcg(a.part_ml + base + min(r0 + 4 * k, rows - 1) + (s0 + lane) * stride);
-                            wgt[k] = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - M[k]);
-                            L[k] = fmaf(wgt[k], ml.y, L[k]);
-                        }
-                    }
-                    const int cnt = min(32, x.ns - s0);
-#pragma unroll 1
-                    for (int s = 0; s < cnt; ++s) {
-                        const float* src = a.part_o + (base + (s0 + s) * stride) * D + lane * CPL;
-                        float v[kJoin][CPL];
-#pragma unroll
-                        for (int k = 0; k < kJoin; ++k) {
-                            const float* at = src + static_cast<size_t>(min(r0 + 4 * k, rows - 1)) * D;
-                            if constexpr (CPL == 4) {
-                                const float4 f = __ldcg(reinterpret_cast<const float4*>(at));
-                                v[k][0] = f.x; v[k][1] = f.y; v[k][2] = f.z; v[k][3] = f.w;
-                            } else {
-                                const float2 f = __ldcg(reinterpret_cast<const float2*>(at));
-                                v[k][0] = f.x; v[k][1] = f.y;
-                            }
-                        }
-#pragma unroll
-                        for (int k = 0; k < kJoin; ++k) {
-                            const float ws = __shfl_sync(0xffffffffu, wgt[k], s);
-                            if (ws != 0.f) {   // (a split in which the row sees no key does not count, whatever it holds)
-#pragma unroll
-                                for (int e = 0; e < CPL; ++e) acc[k][e] = fmaf(ws, v[k][e], acc[k][e]);
-                            }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < kJoin; ++k) {
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) L[k] += __shfl_xor_sync(0xffffffffu, L[k], o);
-                    const int rr = r0 + 4 * k;
-                    if (rr >= rows) continue;
-                    const float inv = 1.f / L[k];
-                    const int tk = rr / a.G, h = rr - tk * a.G;
-                    const size_t at = (static_cast<size_t>(x.tok0) + tk) * a.Hq + static_cast<size_t>(x.head) * a.G + h;
-                    uint32_t* dst = reinterpret_cast<uint32_t*>(a.O + at * D) + lane * (CPL / 2);
-#pragma unroll
-                    for (int e = 0; e < CPL / 2; ++e) dst[e] = pack_bf16x2(acc[k][2 * e] * inv, acc[k][2 * e + 1] * inv);
-                    if (lane == 0 && a.LSE != nullptr) a.LSE[at] = M[k] * kLn2 + logf(L[k]);
-                }
-            }
         }
     }
     __syncthreads();
@@ -713,41 +665,177 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
     }
 }
 
+// ------------------------------------------------------------------ join
+
+// Block c joins the unit whose first split is block c's of the attention: that split
+// and the following blocks' first ones, up to the unit's last page; blockIdx.y takes a
+// slice of the columns.  Threads are (row, columns, share of the splits): few rows
+// leave many threads for the splits of a row.  Latency-bound: all that can be loaded
+// without knowing the rest is loaded together.
+constexpr int kJoinSlices = 4;
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
+    constexpr int ALL = D / 4, QUADS = ALL / kJoinSlices;   // quads of columns: of a row, of this block
+    constexpr int QB = 4, U = 4;                            // quads and splits of a thread in flight together
+    __shared__ float top[kJoinThreads], len[kJoinThreads];
+    __shared__ float4 part[kJoinThreads];
+    __shared__ int ends;
+    const int t = threadIdx.x, c = blockIdx.x;
+    if (t == 0) ends = a.blocks;
+    grid_dep_wait();   // the splits
+    const int4 u1 = a.splits[4 * c + 2], u0 = a.splits[4 * c], v0 = a.splits[4 * c + 1];
+    int4 w = make_int4(0, 0, 0, 0), wv = w;
+    if (c + 1 + t < a.blocks) {
+        w = a.splits[4 * (c + 1 + t)];
+        wv = a.splits[4 * (c + 1 + t) + 1];
+    }
+    const bool second = u1.w != 0;
+    if (!second && (u0.w == 0 || v0.x != 0)) return;   // no unit starts here
+    const int4 u = second ? u1 : u0;
+    __syncthreads();
+    // the unit ends in the first following block whose first split reaches its unit's end
+    if (w.w != 0 && wv.y == wv.z) atomicMin(&ends, c + 1 + t);
+    for (int k = c + 1 + t + kJoinThreads; k < a.blocks; k += kJoinThreads) {
+        const int4 y = a.splits[4 * k + 1];
+        if (a.splits[4 * k].w != 0 && y.y == y.z) atomicMin(&ends, k);
+    }
+    __syncthreads();
+    const int ns = ends < a.blocks ? ends - c + 1 : 1, rows = u.z * a.G;
+    // split s: the first in its slot, the others in slot 0 of the following blocks
+    const int first = 2 * c + (second ? 1 : 0);
+    auto slot = [&](int s) { return static_cast<size_t>(s == 0 ? first : 2 * (c + s)); };
+    int rp = 4;
+    while (rp < rows) rp *= 2;                          // rows, to a power of two
+    const int groups = min(QUADS, kJoinThreads / rp);   // column groups, of `per` quads each
+    const int per = QUADS / groups, span = rp * groups;
+    const int shares = kJoinThreads / span;             // of the splits; more than one only where per = 1
+    const int row = t % rp, cg = t / rp % groups, mine = t / span;
+    const bool live = row < rows;
+    const int at = live ? row : 0;
+    const int tok = at / a.G, h = at - tok * a.G;
+    const size_t orow = (static_cast<size_t>(u.y) + tok) * a.Hq + static_cast<size_t>(u.x) * a.G + h;
+    const float4* const po = reinterpret_cast<const float4*>(a.part_o) + at;
+    for (int q0 = 0; q0 < per; q0 += QB) {
+        const int quad = blockIdx.y * QUADS + cg * per + q0;
+        float M = -CUDART_INF_F, L = 0.f;
+        float4 o[QB];
+#pragma unroll
+        for (int k = 0; k < QB; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s0 = mine; s0 < ns; s0 += U * shares) {
+            float2 ml[U];
+            float4 x[U][QB];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int s = s0 + i * shares;
+                ml[i] = make_float2(-CUDART_INF_F, 0.f);
+                if (s < ns) {
+                    ml[i] = __ldcg(a.part_ml + slot(s) * kBM + at);
+#pragma unroll
+                    for (int k = 0; k < QB; ++k)
+                        if (k < per) x[i][k] = __ldcg(po + (slot(s) * ALL + quad + k) * kBM);
+                }
+            }
+            float m2 = M;
+#pragma unroll
+            for (int i = 0; i < U; ++i) m2 = fmaxf(m2, ml[i].x);
+            const float f = M == -CUDART_INF_F ? 0.f : fast_exp2(M - m2);
+            M = m2;
+            L *= f;
+#pragma unroll
+            for (int k = 0; k < QB; ++k) {
+                o[k].x *= f; o[k].y *= f; o[k].z *= f; o[k].w *= f;
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                // a split in which the row sees no key does not count, whatever it holds
+                if (ml[i].x == -CUDART_INF_F) continue;
+                const float g = fast_exp2(ml[i].x - M);
+                L = fmaf(g, ml[i].y, L);
+#pragma unroll
+                for (int k = 0; k < QB; ++k) {
+                    if (k < per) {
+                        o[k].x = fmaf(g, x[i][k].x, o[k].x);
+                        o[k].y = fmaf(g, x[i][k].y, o[k].y);
+                        o[k].z = fmaf(g, x[i][k].z, o[k].z);
+                        o[k].w = fmaf(g, x[i][k].w, o[k].w);
+                    }
+                }
+            }
+        }
+        if (shares > 1) {
+            top[t] = M;
+            len[t] = L;
+            part[t] = o[0];
+            __syncthreads();
+            if (mine != 0) return;
+            float m2 = M;
+            for (int k = 1; k < shares; ++k) m2 = fmaxf(m2, top[k * span + t]);
+            const float f = M == -CUDART_INF_F ? 0.f : fast_exp2(M - m2);
+            L *= f;
+            o[0].x *= f; o[0].y *= f; o[0].z *= f; o[0].w *= f;
+            for (int k = 1; k < shares; ++k) {
+                const float mk = top[k * span + t];
+                if (mk == -CUDART_INF_F) continue;
+                const float g = fast_exp2(mk - m2);
+                const float4 x = part[k * span + t];
+                L = fmaf(g, len[k * span + t], L);
+                o[0].x = fmaf(g, x.x, o[0].x);
+                o[0].y = fmaf(g, x.y, o[0].y);
+                o[0].z = fmaf(g, x.z, o[0].z);
+                o[0].w = fmaf(g, x.w, o[0].w);
+            }
+            M = m2;
+        }
+        if (!live) continue;
+        const float inv = 1.f / L;
+#pragma unroll
+        for (int k = 0; k < QB; ++k)
+            if (k < per)
+                *reinterpret_cast<uint2*>(a.O + orow * D + (quad + k) * 4) =
+                    make_uint2(pack_bf16x2(o[k].x * inv, o[k].y * inv), pack_bf16x2(o[k].z * inv, o[k].w * inv));
+        if (quad == 0 && a.LSE != nullptr) a.LSE[orow] = M * kLn2 + logf(L);
+    }
+}
+
 template <int D>
 cudaError_t launch_d(const ChunkArgs& a, const KernelEnv& env, const char** err) {
     using C = Cfg<D>;
     cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(chunk_attn_kernel<D>), C::SMEM);
     if (e != cudaSuccess) { *err = "cudaFuncSetAttribute(chunk attention)"; return e; }
-    const int R = kBM / a.G;
     CUtensorMap mq, mk, mv;
     const uint64_t rows = static_cast<uint64_t>(a.num_pages) * a.Hkv;
-    if (make_tmap_bf16_box(&mq, a.Q, D, a.Hq, a.T, 64, a.G, R) != 0 ||
+    if (make_tmap_bf16_box(&mq, a.Q, D, a.Hq, a.T, 64, a.G, kBM / a.G) != 0 ||
         make_tmap_bf16_3d(&mk, a.K_cache, D, kBN, rows, 64, kBN) != 0 ||
         make_tmap_bf16_3d(&mv, a.V_cache, D, kBN, rows, 64, kBN) != 0) {
         *err = "tensor map";
         return cudaErrorInvalidValue;
     }
-    chunk_tiles_kernel<<<1, kPlanThreads, 0, env.stream>>>(a, R);
-    e = cudaGetLastError();
-    if (e != cudaSuccess) { *err = "chunk work list launch"; return e; }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * device_sm_count());
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = C::SMEM;
-    cfg.stream = env.stream;
+    // Two blocks a multiprocessor: their shared memory and tensor memory both fit twice.
+    // Both launches may set up before the kernel ahead of them has ended (they wait for it
+    // themselves, griddepcontrol).
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.stream = env.stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    cfg.gridDim = dim3(a.blocks);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = C::SMEM;
     e = cudaLaunchKernelEx(&cfg, chunk_attn_kernel<D>, mq, mk, mv, a, a.sm_scale * kLog2e, env.limit);
-    if (e != cudaSuccess) *err = "chunk attention launch";
+    if (e != cudaSuccess) { *err = "chunk attention launch"; return e; }
+    cfg.gridDim = dim3(a.blocks, kJoinSlices);
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.dynamicSmemBytes = 0;
+    e = cudaLaunchKernelEx(&cfg, chunk_join_kernel<D>, a);
+    if (e != cudaSuccess) *err = "chunk join launch";
     return e;
 }
 
 }  // namespace
 
-int chunk_target_items() { return 4 * device_sm_count(); }
+int chunk_blocks() { return 2 * device_sm_count(); }
 
 cudaError_t chunk_attn_prepare(int d) {
     return d == 128 ? ensure_smem_attr(reinterpret_cast<const void*>(chunk_attn_kernel<128>), Cfg<128>::SMEM)

@@ -25,13 +25,9 @@ struct sas_chunk_handle {
     sas_chunk_config cfg;
     int G = 1, device = 0;
     float sm_scale = 0.f;
-    int target = 0;
+    int blocks = 0;
     // workspace
-    int32_t* tile_off = nullptr;
-    int4* tiles = nullptr;
-    int4* items = nullptr;
-    int* words = nullptr;      // nitems, sched
-    int* counts = nullptr;
+    int4* splits = nullptr;
     float* part_o = nullptr;
     float2* part_ml = nullptr;
     unsigned long long* vkey = nullptr;
@@ -153,30 +149,20 @@ sas_status sas_chunk_create(const sas_chunk_config* cfg, sas_chunk_handle** out)
         cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
         return SAS_ERR_CUDA;
     if (major != 10 || minor != 3) return SAS_ERR_UNSUPPORTED;
-    const int R = 128 / G, target = sas::chunk_target_items();
-    const long long tiles = c.max_tokens / R + c.max_seqs;      // every sequence ends in one part tile at most
-    const long long items = tiles + target / c.Hkv + 1;
-    const long long parts = 2LL * target + 2LL * c.Hkv;         // over the KV heads together
-    if (items * c.Hkv > (1 << 30)) return SAS_ERR_UNSUPPORTED;  // the work counter is 32 bits
-
     sas_chunk_handle* h = new (std::nothrow) sas_chunk_handle();
     if (h == nullptr) return SAS_ERR_OOM;
     h->cfg = c;
     h->G = G;
     h->device = dev;
-    h->target = target;
+    h->blocks = sas::chunk_blocks();
     h->sm_scale = c.sm_scale > 0.f ? c.sm_scale : 1.0f / std::sqrt(static_cast<float>(c.d));
-    cudaError_t e = calloc_dev(&h->tile_off, c.max_seqs);
-    if (e == cudaSuccess) e = calloc_dev(&h->tiles, tiles);
-    if (e == cudaSuccess) e = calloc_dev(&h->items, 2 * items);
-    if (e == cudaSuccess) e = calloc_dev(&h->words, 4);
-    if (e == cudaSuccess) e = calloc_dev(&h->counts, parts);
+    const size_t parts = 2 * static_cast<size_t>(h->blocks);
+    cudaError_t e = calloc_dev(&h->splits, 2 * parts);
     if (e == cudaSuccess) e = calloc_dev(&h->part_o, parts * 128 * c.d);
     if (e == cudaSuccess) e = calloc_dev(&h->part_ml, parts * 128);
     if (e == cudaSuccess) e = calloc_dev(&h->vkey, c.max_seqs);
     if (e == cudaSuccess) e = calloc_dev(&h->vcount, c.max_seqs);
     if (e == cudaSuccess) e = calloc_dev(&h->status, 4);
-    if (e == cudaSuccess) e = cudaMemset(h->words, 0, 16);
     if (e == cudaSuccess) e = cudaMemset(h->vkey, 0, static_cast<size_t>(c.max_seqs) * 8);
     if (e == cudaSuccess) e = cudaMemset(h->vcount, 0, static_cast<size_t>(c.max_seqs) * 4);
     if (e == cudaSuccess) e = cudaMemset(h->status, 0, 16);
@@ -196,11 +182,7 @@ sas_status sas_chunk_create(const sas_chunk_config* cfg, sas_chunk_handle** out)
 void sas_chunk_destroy(sas_chunk_handle* h) {
     if (h == nullptr) return;
     cudaDeviceSynchronize();
-    cudaFree(h->tile_off);
-    cudaFree(h->tiles);
-    cudaFree(h->items);
-    cudaFree(h->words);
-    cudaFree(h->counts);
+    cudaFree(h->splits);
     cudaFree(h->part_o);
     cudaFree(h->part_ml);
     cudaFree(h->vkey);
@@ -298,8 +280,7 @@ sas_status sas_chunk_attention(sas_chunk_handle* h, int32_t num_seqs, int32_t T,
         a.K_cache = static_cast<const sas::bf16*>(K_cache); a.V_cache = static_cast<const sas::bf16*>(V_cache);
         a.block_table = block_table; a.cu = cu_new; a.kv_lens = kv_lens;
         a.O = static_cast<sas::bf16*>(O); a.LSE = LSE;
-        a.target = h->target; a.tile_off = h->tile_off; a.tiles = h->tiles; a.items = h->items;
-        a.nitems = h->words; a.sched = h->words + 1; a.counts = h->counts; a.part_o = h->part_o; a.part_ml = h->part_ml;
+        a.blocks = h->blocks; a.splits = h->splits; a.part_o = h->part_o; a.part_ml = h->part_ml;
         a.status = h->status;
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         const sas::KernelEnv env{s, h->status, h->limit};
