@@ -48,7 +48,7 @@ constexpr int kStatusLayout = 3;
 constexpr int kUnitCost = 3;      // what a unit costs beside its pages (its Q tile, its epilogue), in pages
 constexpr int kSnap = 4;          // pages: ranges do not cut this close to a unit's ends
 constexpr int kMinShare = 4;      // pages of a block's range, at least
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 512;
 
 __device__ __forceinline__ void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -668,15 +668,14 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
 // ------------------------------------------------------------------ join
 
 // Block c joins the unit whose first split is block c's of the attention: that split
-// and the following blocks' first ones, up to the unit's last page; blockIdx.y takes a
-// slice of the columns.  Threads are (row, columns, share of the splits): few rows
-// leave many threads for the splits of a row.  Latency-bound: all that can be loaded
-// without knowing the rest is loaded together.
-constexpr int kJoinSlices = 4;
+// and the following blocks' first ones, up to the unit's last page.  Threads are (row,
+// columns, share of the splits): few rows leave many threads for the splits of a row.
+// Latency-bound: what can be loaded without knowing the rest is loaded together, and
+// two blocks fit a multiprocessor, so that all run at once.
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
-    constexpr int ALL = D / 4, QUADS = ALL / kJoinSlices;   // quads of columns: of a row, of this block
-    constexpr int QB = 4, U = 4;                            // quads and splits of a thread in flight together
+__global__ void __launch_bounds__(kJoinThreads, 2) chunk_join_kernel(ChunkArgs a) {
+    constexpr int QUADS = D / 4;      // of columns
+    constexpr int QB = 2, U = 4;      // quads and splits of a thread in flight together
     __shared__ float top[kJoinThreads], len[kJoinThreads];
     __shared__ float4 part[kJoinThreads];
     __shared__ int ends;
@@ -716,7 +715,7 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
     const size_t orow = (static_cast<size_t>(u.y) + tok) * a.Hq + static_cast<size_t>(u.x) * a.G + h;
     const float4* const po = reinterpret_cast<const float4*>(a.part_o) + at;
     for (int q0 = 0; q0 < per; q0 += QB) {
-        const int quad = blockIdx.y * QUADS + cg * per + q0;
+        const int quad = cg * per + q0;
         float M = -CUDART_INF_F, L = 0.f;
         float4 o[QB];
 #pragma unroll
@@ -732,7 +731,7 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
                     ml[i] = __ldcg(a.part_ml + slot(s) * kBM + at);
 #pragma unroll
                     for (int k = 0; k < QB; ++k)
-                        if (k < per) x[i][k] = __ldcg(po + (slot(s) * ALL + quad + k) * kBM);
+                        if (k < per) x[i][k] = __ldcg(po + (slot(s) * QUADS + quad + k) * kBM);
                 }
             }
             float m2 = M;
@@ -825,7 +824,6 @@ cudaError_t launch_d(const ChunkArgs& a, const KernelEnv& env, const char** err)
     cfg.dynamicSmemBytes = C::SMEM;
     e = cudaLaunchKernelEx(&cfg, chunk_attn_kernel<D>, mq, mk, mv, a, a.sm_scale * kLog2e, env.limit);
     if (e != cudaSuccess) { *err = "chunk attention launch"; return e; }
-    cfg.gridDim = dim3(a.blocks, kJoinSlices);
     cfg.blockDim = dim3(kJoinThreads);
     cfg.dynamicSmemBytes = 0;
     e = cudaLaunchKernelEx(&cfg, chunk_join_kernel<D>, a);
