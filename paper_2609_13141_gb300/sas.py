@@ -207,30 +207,30 @@ def _ptr(t, dtype, name, required=True):
 def _arg(t, dtype, name, shape=None, dev=None):
     """Device address of a contiguous tensor: like _ptr, with its shape and device checked, and a plain
     integer, for the entry points whose time is mostly the call's."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if dev is not None and t.get_device() != dev:
-        raise ValueError(f"{name} must be on device {dev}")
-    return t.data_ptr()
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_contiguous() and (dev is None or t.get_device() == dev) and
+            (shape is None or t.shape == shape) and t.is_cuda):
+        return t.data_ptr()
+    _refuse(t, dtype, name, shape, dev)
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _rows(t, dtype, name, shape, dev):
     """Device address of a tensor of any strides (its caller checks those)."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_cuda:
+        return t.data_ptr()
+    _refuse(t, dtype, name, shape, dev)
+
+
+def _refuse(t, dtype, name, shape, dev):
+    """Raises for what is wrong with a tensor argument, if it is not its strides."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dtype is not dtype:
+    if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.get_device() != dev:
+    if dev is not None and t.get_device() != dev:
         raise ValueError(f"{name} must be on device {dev}")
-    return t.data_ptr()
 
 
 def _token_stride(t, name, lead):
@@ -247,16 +247,19 @@ def _token_stride(t, name, lead):
     return ld
 
 
-def _raw_stream(stream):
+def _raw_stream(stream, dev):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(dev)   # current_stream(dev).cuda_stream without the object
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+_HERE = contextlib.nullcontext()
 
 
 def _on(stream):
     """Context in which outputs are allocated: the stream the call runs on, whose pool then owns them."""
     if stream is None:
-        return contextlib.nullcontext()
+        return _HERE
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream))
     return torch.cuda.stream(stream)
@@ -364,7 +367,7 @@ def sas_qk_norm_rope_fwd(h, qkv, wq, wk, cos, sin, Q, K, V, positions=None, eps=
         h, cfg, _rows(qkv, bf, "qkv", (B, N, H + 2 * Hkv, d), dev), _token_stride(qkv, "qkv", 2), _arg(wq, bf, "wq", (d,), dev),
         _arg(wk, bf, "wk", (d,), dev), _arg(cos, f32, "cos", None, dev), _arg(sin, f32, "sin", cos.shape, dev),
         None if positions is None else _arg(positions, torch.int32, "positions", (B, N), dev), _arg(Q, bf, "Q"),
-        _arg(K, bf, "K", (B, Hkv, N, d), dev), _arg(V, bf, "V", (B, Hkv, N, d), dev), _raw_stream(stream))
+        _arg(K, bf, "K", (B, Hkv, N, d), dev), _arg(V, bf, "V", (B, Hkv, N, d), dev), _raw_stream(stream, dev))
     if st != SAS_OK:
         _check(st, h, "sas_qk_norm_rope_fwd")
 
@@ -382,7 +385,7 @@ def sas_qk_norm_rope_bwd(h, qkv, wq, wk, cos, sin, dQ, dK, dV, dqkv, dwq, dwk, p
         None if positions is None else _arg(positions, torch.int32, "positions", (B, N), dev), _arg(dQ, bf, "dQ"),
         _arg(dK, bf, "dK", (B, Hkv, N, d), dev), _arg(dV, bf, "dV", (B, Hkv, N, d), dev), _rows(dqkv, bf, "dqkv", rows, dev),
         _token_stride(dqkv, "dqkv", 2), _arg(dwq, f32, "dwq", (d,), dev), _arg(dwk, f32, "dwk", (d,), dev),
-        _raw_stream(stream))
+        _raw_stream(stream, dev))
     if st != SAS_OK:
         _check(st, h, "sas_qk_norm_rope_bwd")
 
@@ -754,7 +757,7 @@ def sas_chunk_plan(h, seq_lens, new_lens, free_pages, free_begin, block_table, k
         _arg(free_pages, i32, "free_pages", None, dev), free_pages.numel(), _arg(free_begin, i32, "free_begin", (1,), dev),
         _arg(block_table, i32, "block_table", None, dev), _arg(kv_lens, i32, "kv_lens", (B,), dev),
         _arg(cu_new, i32, "cu_new", (B + 1,), dev), _arg(positions, i32, "positions", (T,), dev),
-        _arg(slots, torch.int64, "slots", (T,), dev), _arg(free_end, i32, "free_end", (1,), dev), _raw_stream(stream))
+        _arg(slots, torch.int64, "slots", (T,), dev), _arg(free_end, i32, "free_end", (1,), dev), _raw_stream(stream, dev))
     if st != SAS_OK:
         _ccheck(st, h, "sas_chunk_plan")
 
@@ -769,7 +772,7 @@ def sas_chunk_append(h, qkv, wq, wk, cos, sin, positions, slots, Q, K_cache, V_c
         h, cfg, T, _rows(qkv, bf, "qkv", (T, Hq + 2 * Hkv, d), dev), _token_stride(qkv, "qkv", 1), _arg(wq, bf, "wq", (d,), dev),
         _arg(wk, bf, "wk", (d,), dev), _arg(cos, f32, "cos", None, dev), _arg(sin, f32, "sin", cos.shape, dev),
         _arg(positions, torch.int32, "positions", (T,), dev), _arg(slots, torch.int64, "slots", (T,), dev), _arg(Q, bf, "Q"),
-        _arg(K_cache, bf, "K_cache", None, dev), _arg(V_cache, bf, "V_cache", K_cache.shape, dev), _raw_stream(stream))
+        _arg(K_cache, bf, "K_cache", None, dev), _arg(V_cache, bf, "V_cache", K_cache.shape, dev), _raw_stream(stream, dev))
     if st != SAS_OK:
         _ccheck(st, h, "sas_chunk_append")
 
@@ -782,7 +785,7 @@ def sas_chunk_attention(h, Q, K_cache, V_cache, block_table, cu_new, kv_lens, O,
         h, B, Q.shape[0], _arg(Q, bf, "Q"), _arg(K_cache, bf, "K_cache", None, dev),
         _arg(V_cache, bf, "V_cache", K_cache.shape, dev), _arg(block_table, i32, "block_table", None, dev),
         _arg(cu_new, i32, "cu_new", (B + 1,), dev), _arg(kv_lens, i32, "kv_lens", (B,), dev), _arg(O, bf, "O", Q.shape, dev),
-        None if LSE is None else _arg(LSE, torch.float32, "LSE", Q.shape[:2], dev), _raw_stream(stream))
+        None if LSE is None else _arg(LSE, torch.float32, "LSE", Q.shape[:2], dev), _raw_stream(stream, dev))
     if st != SAS_OK:
         _ccheck(st, h, "sas_chunk_attention")
 
@@ -807,7 +810,7 @@ def sas_chunk_verify(h, tokens, cu_draft, target, draft, u, noise, accepted, out
     st = lib().sas_chunk_verify(
         h, B, n, out_tokens.shape[1] - 1, V, _arg(tokens, i32, "tokens", (n,), dev), _arg(cu_draft, i32, "cu_draft", None, dev), p,
         ldp, q, ldq, _arg(u, torch.float32, "u", (n,), dev), e, lde, _arg(accepted, i32, "accepted", (B,), dev),
-        _arg(out_tokens, i32, "out_tokens", None, dev), _raw_stream(stream))
+        _arg(out_tokens, i32, "out_tokens", None, dev), _raw_stream(stream, dev))
     if st != SAS_OK:
         _ccheck(st, h, "sas_chunk_verify")
 
