@@ -189,23 +189,45 @@ __device__ __forceinline__ bool find_range(const ChunkArgs& a, int R, Shares& sh
 
 // ------------------------------------------------------------------ attention
 
+// A step is KPS pages: their scores, softmax and product go through the pipeline together.
+// Each step costs the softmax warps some 400 cycles of waits, tensor-memory loads and
+// stores beside its arithmetic.  At d = 128 two blocks' products (1024 cycles a page
+// pair) cover that, and tensor memory holds no more: O 128 + S 64 + two P of 32
+// columns.  At d = 64 the products are half as long and nothing covers it: two pages
+// a step, O 64 + S 128 + one P of 64 columns, with the score rows in registers (184 a
+// softmax thread, 64 for the others, of the 128 the block is launched with).
 template <int D>
 struct Cfg {
+    static constexpr int KPS = D == 64 ? 2 : 1;
+    static constexpr int NPB = D == 64 ? 1 : 2;     // P buffers
+    static constexpr int QST = D == 64 ? 2 : 1;     // Q tiles (of the item at work, and the next one's)
     static constexpr int Q_BYTES = kBM * D * 2;
     static constexpr int KV_BYTES = kBN * D * 2;
-    static constexpr int KST = 2;
-    static constexpr int VST = 2;
-    static constexpr int OFF_K = Q_BYTES;
+    static constexpr int KST = D == 64 ? 4 : 2;     // pages of the rings
+    static constexpr int VST = KST;
+    static constexpr int OFF_K = QST * Q_BYTES;
     static constexpr int OFF_V = OFF_K + KST * KV_BYTES;
     static constexpr int OFF_CTL = OFF_V + VST * KV_BYTES;
     static constexpr int SMEM = OFF_CTL + 768;   // barriers and items, then Shares
-    static constexpr int TMEM_COLS = 256;    // O [0,D)  S [128,192)  P0 [192,224)  P1 [224,256)
+    static constexpr int TMEM_COLS = 256;
     static constexpr int TMEM_O = 0;
-    static constexpr int TMEM_S = 128;
-    static constexpr int TMEM_P = 192;
+    static constexpr int TMEM_S = D;
+    static constexpr int TMEM_P = TMEM_S + KPS * kBN;   // buffer b at + 32 KPS b (keys packed in pairs)
+    static_assert(TMEM_P + NPB * 32 * KPS <= TMEM_COLS, "tensor memory");
     static constexpr uint32_t IDESC_S = idesc_bf16(kBM, kBN, 0, 0);
     static constexpr uint32_t IDESC_O = idesc_bf16(kBM, D, 0, 1);
 };
+
+// Moves registers between the block's two warpgroups (the sum stays within what it was
+// launched with: 128 threads x (64 + 184) <= 256 x 128).
+template <int D>
+__device__ __forceinline__ void give_registers() {
+    if constexpr (Cfg<D>::KPS == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+}
+template <int D>
+__device__ __forceinline__ void take_registers() {
+    if constexpr (Cfg<D>::KPS == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+}
 
 // A work item as the roles read it: a unit, or a split of one.
 struct Item {
@@ -216,7 +238,7 @@ struct Item {
 };
 
 struct Ctl {
-    uint64_t q_full, q_empty, k_full[4], k_empty[4], v_full[4], v_empty[4];
+    uint64_t q_full[2], q_empty[2], k_full[4], k_empty[4], v_full[4], v_empty[4];
     uint64_t s_full, s_free, p_full[2], pv_done[2], drain_bar;
     uint64_t item_full[kItemSlots], item_empty[kItemSlots];
     Item item[kItemSlots];
@@ -259,8 +281,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
     Ctl& ctl = *reinterpret_cast<Ctl*>(smem + C::OFF_CTL);
     const uint32_t warp = warp_id(), lane = lane_id();
     if (threadIdx.x == 0) {
-        mbar_init(&ctl.q_full, 1);
-        mbar_init(&ctl.q_empty, 1);
+        for (int s = 0; s < C::QST; ++s) { mbar_init(&ctl.q_full[s], 1); mbar_init(&ctl.q_empty[s], 1); }
         for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.k_full[s], 1); mbar_init(&ctl.k_empty[s], 1); }
         for (int s = 0; s < C::VST; ++s) { mbar_init(&ctl.v_full[s], 1); mbar_init(&ctl.v_empty[s], 1); }
         mbar_init(&ctl.s_full, 1);
@@ -293,216 +314,242 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
 
     // Every role walks the same items and counts pages over all of them (g): ring
     // slots, score buffers and barrier phases follow g across item boundaries.
-    if (warp == 0) {
-        // ---------------- items and K pages
-        if (lane == 0) tma_prefetch_desc(&mapK);
-        const Bound from = sh.at[0], to = sh.at[1];
-        int seq = from.seq, tile = from.tile, head = from.head;   // the unit to look at next
-        bool more = any, first = true;
-        int late_lo = 0, late_hi = 0;   // the split of the first unit, left for the end
-        unsigned used = 0;              // partial results written: slots 2 block + 0, + 1
-        int g = 0;
-        bool ok = true;
-        for (int r = 0; ok; ++r) {
-            Item x;
-            x.head = -1;
-            x.blk0 = x.blk1 = 0;
-            while (more && x.head < 0) {
-                const Seq q(a, seq);
-                const int nb = q.pages(tile, R);
-                const bool last = seq == to.seq && tile == to.tile && head == to.head;
-                const int lo = first ? from.page : 0, hi = last ? to.page : nb;
-                if (first && lo < hi && (lo > 0 || hi < nb)) {
-                    late_lo = lo;
-                    late_hi = hi;
-                } else if (lo < hi) {
-                    x = Item{head, seq, q.c0 + tile * R, min(R, q.n - tile * R), q.L - q.n + tile * R, lo, hi, nb,
-                             hi < nb ? static_cast<int>(2 * blockIdx.x + 1) : -1};
-                }
-                first = false;
-                more = !last;
-                if (more && ++head == a.Hkv) {
-                    head = 0;
-                    if (++tile >= q.tiles(R)) {
-                        // the next sequence with new tokens; the range's end lies in one
-                        tile = 0;
-                        for (int b = seq + 1;; b += 32) {
-                            const int y = b + static_cast<int>(lane);
-                            const unsigned has = __ballot_sync(0xffffffffu, y <= to.seq && Seq(a, min(y, to.seq)).n > 0);
-                            if (has != 0 || b >= to.seq) {
-                                seq = has != 0 ? b + __ffs(has) - 1 : to.seq;
-                                break;
+    if (warp < 4) {
+        give_registers<D>();
+        if (warp == 0) {
+            // ---------------- items and K pages
+            if (lane == 0) tma_prefetch_desc(&mapK);
+            const Bound from = sh.at[0], to = sh.at[1];
+            int seq = from.seq, tile = from.tile, head = from.head;   // the unit to look at next
+            bool more = any, first = true;
+            int late_lo = 0, late_hi = 0;   // the split of the first unit, left for the end
+            unsigned used = 0;              // partial results written: slots 2 block + 0, + 1
+            int g = 0;
+            bool ok = true;
+            for (int r = 0; ok; ++r) {
+                Item x;
+                x.head = -1;
+                x.blk0 = x.blk1 = 0;
+                while (more && x.head < 0) {
+                    const Seq q(a, seq);
+                    const int nb = q.pages(tile, R);
+                    const bool last = seq == to.seq && tile == to.tile && head == to.head;
+                    const int lo = first ? from.page : 0, hi = last ? to.page : nb;
+                    if (first && lo < hi && (lo > 0 || hi < nb)) {
+                        late_lo = lo;
+                        late_hi = hi;
+                    } else if (lo < hi) {
+                        x = Item{head, seq, q.c0 + tile * R, min(R, q.n - tile * R), q.L - q.n + tile * R, lo, hi, nb,
+                                 hi < nb ? static_cast<int>(2 * blockIdx.x + 1) : -1};
+                    }
+                    first = false;
+                    more = !last;
+                    if (more && ++head == a.Hkv) {
+                        head = 0;
+                        if (++tile >= q.tiles(R)) {
+                            // the next sequence with new tokens; the range's end lies in one
+                            tile = 0;
+                            for (int b = seq + 1;; b += 32) {
+                                const int y = b + static_cast<int>(lane);
+                                const unsigned has = __ballot_sync(0xffffffffu, y <= to.seq && Seq(a, min(y, to.seq)).n > 0);
+                                if (has != 0 || b >= to.seq) {
+                                    seq = has != 0 ? b + __ffs(has) - 1 : to.seq;
+                                    break;
+                                }
                             }
                         }
                     }
                 }
-            }
-            if (x.head < 0 && late_lo < late_hi) {
-                const Seq q(a, from.seq);
-                x = Item{from.head, from.seq, q.c0 + from.tile * R, min(R, q.n - from.tile * R), q.L - q.n + from.tile * R,
-                         late_lo, late_hi, from.nb, static_cast<int>(2 * blockIdx.x)};
-                late_hi = 0;
-            }
-            const int slot = r % kItemSlots;
-            if (!mbar_wait_warp(&ctl.item_empty[slot], ((r / kItemSlots) & 1) ^ 1u, wc)) { ok = false; break; }
-            if (lane == 0) {
-                ctl.item[slot] = x;
-                mbar_arrive(&ctl.item_full[slot]);
-                if (x.part >= 0 && x.head >= 0) {   // what the join has to know
-                    a.splits[2 * x.part] = make_int4(x.head, x.tok0, x.ntok, 1);
-                    a.splits[2 * x.part + 1] = make_int4(x.blk0, x.blk1, x.nb, 0);
-                    used |= 1u << (x.part & 1);
+                if (x.head < 0 && late_lo < late_hi) {
+                    const Seq q(a, from.seq);
+                    x = Item{from.head, from.seq, q.c0 + from.tile * R, min(R, q.n - from.tile * R), q.L - q.n + from.tile * R,
+                             late_lo, late_hi, from.nb, static_cast<int>(2 * blockIdx.x)};
+                    late_hi = 0;
                 }
-            }
-            __syncwarp();
-            if (x.head < 0) break;
-            int rows = 0;
-            for (int m = x.blk0; m < x.blk1; ++m, ++g) {
-                const int j = (m - x.blk0) & 31;
-                if (j == 0) rows = page_row(a, x, m, lane);
-                const int row = __shfl_sync(0xffffffffu, rows, j);
-                const int s = g % C::KST;
-                if (!mbar_wait_warp(&ctl.k_empty[s], ((g / C::KST) & 1) ^ 1u, wc)) { ok = false; break; }
+                const int slot = r % kItemSlots;
+                if (!mbar_wait_warp(&ctl.item_empty[slot], ((r / kItemSlots) & 1) ^ 1u, wc)) { ok = false; break; }
                 if (lane == 0) {
-                    uint8_t* dst = smem + C::OFF_K + s * C::KV_BYTES;
-                    mbar_arrive_expect_tx(&ctl.k_full[s], C::KV_BYTES);
+                    ctl.item[slot] = x;
+                    mbar_arrive(&ctl.item_full[slot]);
+                    if (x.head >= 0) {   // its Q tile is loaded when the item before is done with its own: into L2 now
 #pragma unroll
-                    for (int h = 0; h < D / 64; ++h) tma_load_3d(dst + h * (kBN * 128), &mapK, &ctl.k_full[s], h * 64, 0, row);
-                }
-                __syncwarp();
-            }
-        }
-        if (lane == 0) {
-            for (int k = 0; k < 2; ++k)
-                if (!((used >> k) & 1u)) a.splits[2 * (2 * blockIdx.x + k)] = make_int4(0, 0, 0, 0);
-        }
-        if (!ok && lane == 0) {   // the last KST loads may be in flight
-            for (int q = g - 1; q >= 0 && q >= g - C::KST; --q)
-                mbar_wait_drain(&ctl.k_full[q % C::KST], (q / C::KST) & 1, limit, a.status);
-        }
-    } else if (warp == 1) {
-        // ---------------- V pages and the Q tile
-        if (lane == 0) {
-            tma_prefetch_desc(&mapQ);
-            tma_prefetch_desc(&mapV);
-        }
-        int g = 0, nq = 0;
-        bool ok = true;
-        for (int r = 0; ok; ++r) {
-            Item x;
-            if (!read_item(ctl, r, wc, x)) { ok = false; break; }
-            if (x.head < 0) break;
-            if (!mbar_wait_warp(&ctl.q_empty, (nq & 1) ^ 1u, wc)) { ok = false; break; }
-            if (lane == 0) {
-                mbar_arrive_expect_tx(&ctl.q_full, C::Q_BYTES);
-#pragma unroll
-                for (int h = 0; h < D / 64; ++h)
-                    tma_load_3d(smem + h * (kBM * 128), &mapQ, &ctl.q_full, h * 64, x.head * a.G, x.tok0);
-            }
-            ++nq;
-            int rows = 0;
-            for (int m = x.blk0; m < x.blk1; ++m, ++g) {
-                const int j = (m - x.blk0) & 31;
-                if (j == 0) rows = page_row(a, x, m, lane);
-                const int row = __shfl_sync(0xffffffffu, rows, j);
-                const int s = g % C::VST;
-                if (!mbar_wait_warp(&ctl.v_empty[s], ((g / C::VST) & 1) ^ 1u, wc)) { ok = false; break; }
-                if (lane == 0) {
-                    uint8_t* dst = smem + C::OFF_V + s * C::KV_BYTES;
-                    mbar_arrive_expect_tx(&ctl.v_full[s], C::KV_BYTES);
-#pragma unroll
-                    for (int h = 0; h < D / 64; ++h) tma_load_3d(dst + h * (kBN * 128), &mapV, &ctl.v_full[s], h * 64, 0, row);
-                }
-                __syncwarp();
-            }
-        }
-        if (!ok && lane == 0) {
-            if (nq > 0) mbar_wait_drain(&ctl.q_full, (nq - 1) & 1, limit, a.status);
-            for (int q = g - 1; q >= 0 && q >= g - C::VST; --q)
-                mbar_wait_drain(&ctl.v_full[q % C::VST], (q / C::VST) & 1, limit, a.status);
-        }
-    } else if (warp == 2) {
-        // ---------------- S = Q K_g^T, once the softmax warps have loaded S_{g-1}
-        const uint64_t dq0 = smem_desc_sw128(smem_u32(smem), 16, 1024);
-        const uint64_t dk0 = smem_desc_sw128(smem_u32(smem + C::OFF_K), 16, 1024);
-        int g = 0, tc = 0;
-        bool ok = true;
-        for (int r = 0; ok; ++r, ++tc) {
-            Item x;
-            if (!read_item(ctl, r, wc, x)) { ok = false; break; }
-            if (x.head < 0) break;
-            if (!mbar_wait_warp(&ctl.q_full, tc & 1, wc)) { ok = false; break; }
-            for (int m = x.blk0; m < x.blk1; ++m, ++g) {
-                const int s = g % C::KST;
-                if (!mbar_wait_warp(&ctl.k_full[s], (g / C::KST) & 1, wc)) { ok = false; break; }
-                if (g >= 1 && !mbar_wait_warp(&ctl.s_free, (g - 1) & 1, wc)) { ok = false; break; }
-                tc_fence_after();
-                const uint64_t dk = dk0 + static_cast<uint64_t>((s * C::KV_BYTES) >> 4);
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t off_q = (k >> 2) * (kBM * 128) + (k & 3) * 32;
-                        const uint32_t off_k = (k >> 2) * (kBN * 128) + (k & 3) * 32;
-                        umma_bf16(tmem_base + C::TMEM_S, dq0 + (off_q >> 4), dk + (off_k >> 4), C::IDESC_S, k > 0);
+                        for (int h = 0; h < D / 64; ++h) tma_prefetch_3d(&mapQ, h * 64, x.head * a.G, x.tok0);
                     }
-                    umma_commit(&ctl.s_full);
-                    umma_commit(&ctl.k_empty[s]);
-                    if (m == x.blk1 - 1) umma_commit(&ctl.q_empty);
+                    if (x.part >= 0 && x.head >= 0) {   // what the join has to know
+                        a.splits[2 * x.part] = make_int4(x.head, x.tok0, x.ntok, 1);
+                        a.splits[2 * x.part + 1] = make_int4(x.blk0, x.blk1, x.nb, 0);
+                        used |= 1u << (x.part & 1);
+                    }
                 }
                 __syncwarp();
-            }
-        }
-        if (elect_one()) {
-            umma_commit(&ctl.drain_bar);
-            mbar_wait_drain(&ctl.drain_bar, 0, limit, a.status);
-        }
-        __syncwarp();
-    } else if (warp == 3) {
-        // ---------------- O += P_g V_g; an item's first page starts a new accumulator
-        const uint64_t dv0 = smem_desc_sw128(smem_u32(smem + C::OFF_V), kBN * 128, 1024);
-        int g = 0;
-        bool ok = true;
-        for (int r = 0; ok; ++r) {
-            Item x;
-            if (!read_item(ctl, r, wc, x)) { ok = false; break; }
-            if (x.head < 0) break;
-            const int end = x.pos0 + x.ntok;   // keys from here on belong to no row of the tile
-            for (int m = x.blk0; m < x.blk1; ++m, ++g) {
-                const int vs = g % C::VST;
-                if (!mbar_wait_warp(&ctl.v_full[vs], (g / C::VST) & 1, wc)) { ok = false; break; }
-                if (end < (m + 1) * kBN) {
-                    // zero value rows: P is 0 there, and 0 times a stale infinity or NaN is NaN
-                    const int r0 = max(0, end - m * kBN);
-                    uint8_t* v = smem + C::OFF_V + vs * C::KV_BYTES;
-                    for (int i = r0 * 8 + lane; i < kBN * 8; i += 32) {
+                if (x.head < 0) break;
+                int rows = 0;
+                for (int m = x.blk0; m < x.blk1; ++m, ++g) {
+                    const int j = (m - x.blk0) & 31;
+                    if (j == 0) rows = page_row(a, x, m, lane);
+                    const int row = __shfl_sync(0xffffffffu, rows, j);
+                    const int s = g % C::KST;
+                    if (!mbar_wait_warp(&ctl.k_empty[s], ((g / C::KST) & 1) ^ 1u, wc)) { ok = false; break; }
+                    if (lane == 0) {
+                        uint8_t* dst = smem + C::OFF_K + s * C::KV_BYTES;
+                        mbar_arrive_expect_tx(&ctl.k_full[s], C::KV_BYTES);
 #pragma unroll
-                        for (int h = 0; h < D / 64; ++h)
-                            *reinterpret_cast<uint4*>(v + h * (kBN * 128) + i * 16) = make_uint4(0, 0, 0, 0);
+                        for (int h = 0; h < D / 64; ++h) tma_load_3d(dst + h * (kBN * 128), &mapK, &ctl.k_full[s], h * 64, 0, row);
                     }
-                    fence_proxy_async_smem();
                     __syncwarp();
                 }
-                if (!mbar_wait_warp(&ctl.p_full[g & 1], (g >> 1) & 1, wc)) { ok = false; break; }
-                tc_fence_after();
-                const uint64_t dv = dv0 + static_cast<uint64_t>((vs * C::KV_BYTES) >> 4);
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < kBN / 16; ++k)
-                        umma_bf16_ta(tmem_base + C::TMEM_O, tmem_base + C::TMEM_P + (g & 1) * 32 + k * 8,
-                                     dv + ((k * 2048) >> 4), C::IDESC_O, (m > x.blk0 || k > 0) ? 1u : 0u);
-                    umma_commit(&ctl.pv_done[g & 1]);
-                    umma_commit(&ctl.v_empty[vs]);
-                }
-                __syncwarp();
             }
+            if (lane == 0) {
+                for (int k = 0; k < 2; ++k)
+                    if (!((used >> k) & 1u)) a.splits[2 * (2 * blockIdx.x + k)] = make_int4(0, 0, 0, 0);
+            }
+            if (!ok && lane == 0) {   // the last KST loads may be in flight
+                for (int q = g - 1; q >= 0 && q >= g - C::KST; --q)
+                    mbar_wait_drain(&ctl.k_full[q % C::KST], (q / C::KST) & 1, limit, a.status);
+            }
+        } else if (warp == 1) {
+            // ---------------- V pages and the Q tile
+            if (lane == 0) {
+                tma_prefetch_desc(&mapQ);
+                tma_prefetch_desc(&mapV);
+            }
+            int g = 0, nq = 0;
+            bool ok = true;
+            for (int r = 0; ok; ++r) {
+                Item x;
+                if (!read_item(ctl, r, wc, x)) { ok = false; break; }
+                if (x.head < 0) break;
+                const int qs = nq % C::QST;
+                if (!mbar_wait_warp(&ctl.q_empty[qs], ((nq / C::QST) & 1) ^ 1u, wc)) { ok = false; break; }
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(&ctl.q_full[qs], C::Q_BYTES);
+#pragma unroll
+                    for (int h = 0; h < D / 64; ++h)
+                        tma_load_3d(smem + qs * C::Q_BYTES + h * (kBM * 128), &mapQ, &ctl.q_full[qs], h * 64, x.head * a.G, x.tok0);
+                }
+                ++nq;
+                int rows = 0;
+                for (int m = x.blk0; m < x.blk1; ++m, ++g) {
+                    const int j = (m - x.blk0) & 31;
+                    if (j == 0) rows = page_row(a, x, m, lane);
+                    const int row = __shfl_sync(0xffffffffu, rows, j);
+                    const int s = g % C::VST;
+                    if (!mbar_wait_warp(&ctl.v_empty[s], ((g / C::VST) & 1) ^ 1u, wc)) { ok = false; break; }
+                    if (lane == 0) {
+                        uint8_t* dst = smem + C::OFF_V + s * C::KV_BYTES;
+                        mbar_arrive_expect_tx(&ctl.v_full[s], C::KV_BYTES);
+#pragma unroll
+                        for (int h = 0; h < D / 64; ++h) tma_load_3d(dst + h * (kBN * 128), &mapV, &ctl.v_full[s], h * 64, 0, row);
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!ok && lane == 0) {
+                for (int q = nq - 1; q >= 0 && q >= nq - C::QST; --q)
+                    mbar_wait_drain(&ctl.q_full[q % C::QST], (q / C::QST) & 1, limit, a.status);
+                for (int q = g - 1; q >= 0 && q >= g - C::VST; --q)
+                    mbar_wait_drain(&ctl.v_full[q % C::VST], (q / C::VST) & 1, limit, a.status);
+            }
+        } else if (warp == 2) {
+            // ---------------- S = Q K^T of step g, once the softmax warps have loaded S of step g - 1
+            const uint64_t dq0 = smem_desc_sw128(smem_u32(smem), 16, 1024);
+            const uint64_t dk0 = smem_desc_sw128(smem_u32(smem + C::OFF_K), 16, 1024);
+            int g = 0, gp = 0, tc = 0;   // steps, pages, items
+            bool ok = true;
+            for (int r = 0; ok; ++r, ++tc) {
+                Item x;
+                if (!read_item(ctl, r, wc, x)) { ok = false; break; }
+                if (x.head < 0) break;
+                const int qs = tc % C::QST;
+                const uint64_t dq = dq0 + static_cast<uint64_t>((qs * C::Q_BYTES) >> 4);
+                if (!mbar_wait_warp(&ctl.q_full[qs], (tc / C::QST) & 1, wc)) { ok = false; break; }
+                for (int m = x.blk0; ok && m < x.blk1; m += C::KPS, ++g) {
+                    if (g >= 1 && !mbar_wait_warp(&ctl.s_free, (g - 1) & 1, wc)) { ok = false; break; }
+                    for (int i = 0; i < C::KPS && m + i < x.blk1; ++i, ++gp) {
+                        const int s = gp % C::KST;
+                        if (!mbar_wait_warp(&ctl.k_full[s], (gp / C::KST) & 1, wc)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint64_t dk = dk0 + static_cast<uint64_t>((s * C::KV_BYTES) >> 4);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < D / 16; ++k) {
+                                const uint32_t off_q = (k >> 2) * (kBM * 128) + (k & 3) * 32;
+                                const uint32_t off_k = (k >> 2) * (kBN * 128) + (k & 3) * 32;
+                                umma_bf16(tmem_base + C::TMEM_S + i * kBN, dq + (off_q >> 4), dk + (off_k >> 4), C::IDESC_S, k > 0);
+                            }
+                            umma_commit(&ctl.k_empty[s]);
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+                    if (elect_one()) {
+                        umma_commit(&ctl.s_full);
+                        if (m + C::KPS >= x.blk1) umma_commit(&ctl.q_empty[qs]);
+                    }
+                    __syncwarp();
+                }
+            }
+            if (elect_one()) {
+                umma_commit(&ctl.drain_bar);
+                mbar_wait_drain(&ctl.drain_bar, 0, limit, a.status);
+            }
+            __syncwarp();
+        } else if (warp == 3) {
+            // ---------------- O += P V of step g; an item's first page starts a new accumulator
+            const uint64_t dv0 = smem_desc_sw128(smem_u32(smem + C::OFF_V), kBN * 128, 1024);
+            int g = 0, gp = 0;
+            bool ok = true;
+            for (int r = 0; ok; ++r) {
+                Item x;
+                if (!read_item(ctl, r, wc, x)) { ok = false; break; }
+                if (x.head < 0) break;
+                const int end = x.pos0 + x.ntok;   // keys from here on belong to no row of the tile
+                for (int m0 = x.blk0; ok && m0 < x.blk1; m0 += C::KPS, ++g) {
+                    const int pb = g % C::NPB;
+                    for (int i = 0; i < C::KPS && m0 + i < x.blk1; ++i, ++gp) {
+                        const int m = m0 + i;
+                        const int vs = gp % C::VST;
+                        if (!mbar_wait_warp(&ctl.v_full[vs], (gp / C::VST) & 1, wc)) { ok = false; break; }
+                        if (end < (m + 1) * kBN) {
+                            // zero value rows: P is 0 there, and 0 times a stale infinity or NaN is NaN
+                            const int r0 = max(0, end - m * kBN);
+                            uint8_t* v = smem + C::OFF_V + vs * C::KV_BYTES;
+                            for (int j = r0 * 8 + lane; j < kBN * 8; j += 32) {
+#pragma unroll
+                                for (int h = 0; h < D / 64; ++h)
+                                    *reinterpret_cast<uint4*>(v + h * (kBN * 128) + j * 16) = make_uint4(0, 0, 0, 0);
+                            }
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                        }
+                        if (i == 0 && !mbar_wait_warp(&ctl.p_full[pb], (g / C::NPB) & 1, wc)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint64_t dv = dv0 + static_cast<uint64_t>((vs * C::KV_BYTES) >> 4);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < kBN / 16; ++k)
+                                umma_bf16_ta(tmem_base + C::TMEM_O,
+                                             tmem_base + C::TMEM_P + pb * (32 * C::KPS) + i * 32 + k * 8,
+                                             dv + ((k * 2048) >> 4), C::IDESC_O, (m > x.blk0 || k > 0) ? 1u : 0u);
+                            umma_commit(&ctl.v_empty[vs]);
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+                    if (elect_one()) umma_commit(&ctl.pv_done[pb]);
+                    __syncwarp();
+                }
+            }
+            if (elect_one()) {
+                umma_commit(&ctl.drain_bar);
+                mbar_wait_drain(&ctl.drain_bar, 0, limit, a.status);
+            }
+            __syncwarp();
         }
-        if (elect_one()) {
-            umma_commit(&ctl.drain_bar);
-            mbar_wait_drain(&ctl.drain_bar, 0, limit, a.status);
-        }
-        __syncwarp();
     } else {
         // ---------------- softmax, one thread per row
+        take_registers<D>();
+        constexpr int NK = C::KPS * kBN;   // keys of a step
         const int q = warp - 4;
         const int row = q * 32 + lane;
         const int tok = row / a.G, hq = row - tok * a.G;
@@ -518,60 +565,56 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
             const bool warp_rows = q * 32 < x.ntok * a.G;   // else nothing of this warp is ever read
             const int pos = x.pos0 + tok;
             float m_use = -CUDART_INF_F, l = 0.f;
-            for (int m = x.blk0; m < x.blk1; ++m, ++g) {
-                const int pb = g & 1;
-                // last key column of page m that this row sees (< 0: none)
-                const int lim = valid ? min(kBN - 1, pos - m * kBN) : -1;
+            for (int m = x.blk0; m < x.blk1; m += C::KPS, ++g) {
+                const int pb = g % C::NPB;
+                // last key column of the step that this row sees (< 0: none; none of a page that is not
+                // there).  Rows of no token are never read: they go unmasked.
+                const int lim = valid ? min(min(NK - 1, pos - m * kBN), (x.blk1 - m) * kBN - 1) : NK - 1;
                 if (!mbar_wait_warp(&ctl.s_full, g & 1, wc)) { ok = false; break; }
-                if (g >= 2 && !mbar_wait_warp(&ctl.pv_done[pb], ((g - 2) >> 1) & 1, wc)) { ok = false; break; }
                 if (!warp_rows) {
-                    if (lane == 0) {
-                        mbar_arrive(&ctl.s_free);
-                        mbar_arrive(&ctl.p_full[pb]);
-                    }
+                    if (lane == 0) mbar_arrive(&ctl.s_free);
+                    if (g >= C::NPB && !mbar_wait_warp(&ctl.pv_done[pb], (g / C::NPB - 1) & 1, wc)) { ok = false; break; }
+                    if (lane == 0) mbar_arrive(&ctl.p_full[pb]);
                     __syncwarp();
                     continue;
                 }
                 tc_fence_after();
-                float xs[64];
+                float xs[NK];
                 {
-                    uint32_t u0[32], u1[32];
-                    tmem_ld32(lane_addr + C::TMEM_S, u0);
-                    tmem_ld32(lane_addr + C::TMEM_S + 32, u1);
+                    uint32_t u[NK / 32][32];
+#pragma unroll
+                    for (int c = 0; c < NK / 32; ++c) tmem_ld32(lane_addr + C::TMEM_S + c * 32, u[c]);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        xs[k] = __uint_as_float(u0[k]);
-                        xs[k + 32] = __uint_as_float(u1[k]);
-                    }
+                    for (int k = 0; k < NK; ++k) xs[k] = __uint_as_float(u[k / 32][k % 32]);
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&ctl.s_free);
-                if (__any_sync(0xffffffffu, lim < kBN - 1)) {
+                if (__any_sync(0xffffffffu, lim < NK - 1)) {
 #pragma unroll
-                    for (int k = 0; k < 64; ++k) xs[k] = k <= lim ? xs[k] : -CUDART_INF_F;
+                    for (int k = 0; k < NK; ++k) xs[k] = k <= lim ? xs[k] : -CUDART_INF_F;
                 }
-                float mx0 = -CUDART_INF_F, mx1 = -CUDART_INF_F;
+                float mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-                for (int k = 0; k < 64; k += 4) {
-                    mx0 = max3f(mx0, xs[k], xs[k + 1]);
-                    mx1 = max3f(mx1, xs[k + 2], xs[k + 3]);
+                for (int k = 0; k < NK; k += 8) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) mx[j] = max3f(mx[j], xs[k + 2 * j], xs[k + 2 * j + 1]);
                 }
-                const float mb = fmaxf(mx0, mx1) * scale_log2;
-                const bool need = mb > m_use + kRescaleThreshold;
+                const float mb = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale_log2;
+                const bool need = valid && mb > m_use + kRescaleThreshold;
                 const float m_new = need ? mb : m_use;
                 const float off = m_new == -CUDART_INF_F ? 0.f : -m_new;
                 const uint64_t off2 = f32x2(off, off);
                 uint64_t acc[4] = {0, 0, 0, 0};
-                uint32_t pk[32];
+                uint32_t pk[C::KPS][32];
 #pragma unroll
-                for (int k = 0; k < 64; k += 2) {
+                for (int k = 0; k < NK; k += 2) {
                     float a0, a1;
                     f32x2_split(fma_f32x2(f32x2(xs[k], xs[k + 1]), scale2, off2), a0, a1);
                     const float e0 = fast_exp2(a0), e1 = fast_exp2(a1);
                     acc[(k >> 1) & 3] = add_f32x2(acc[(k >> 1) & 3], f32x2(e0, e1));
-                    pk[k >> 1] = pack_bf16x2(e0, e1);
+                    pk[k / 64][(k % 64) >> 1] = pack_bf16x2(e0, e1);
                 }
                 float s0, s1, s2, s3, s4, s5, s6, s7;
                 f32x2_split(acc[0], s0, s1);
@@ -582,8 +625,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 float factor = 1.f;
                 if (need) factor = m_use == -CUDART_INF_F ? 0.f : fast_exp2(m_use - m_new);
                 if (m > x.blk0 && __any_sync(0xffffffffu, need)) {
-                    // rescaling O needs the previous page's PV done
-                    if (!mbar_wait_warp(&ctl.pv_done[(g - 1) & 1], ((g - 1) >> 1) & 1, wc)) { ok = false; break; }
+                    // rescaling O needs the previous step's PV done
+                    if (!mbar_wait_warp(&ctl.pv_done[(g - 1) % C::NPB], ((g - 1) / C::NPB) & 1, wc)) { ok = false; break; }
                     tc_fence_after();
 #pragma unroll 1
                     for (int cc = 0; cc < D / 32; ++cc) {
@@ -598,7 +641,11 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 }
                 l = l * factor + rs;
                 m_use = m_new;
-                tmem_st32(lane_addr + C::TMEM_P + pb * 32, pk);
+                // P buffer pb is free once the PV of step g - NPB has read it
+                if (g >= C::NPB && !mbar_wait_warp(&ctl.pv_done[pb], (g / C::NPB - 1) & 1, wc)) { ok = false; break; }
+                tc_fence_after();
+#pragma unroll
+                for (int i = 0; i < C::KPS; ++i) tmem_st32(lane_addr + C::TMEM_P + pb * (32 * C::KPS) + i * 32, pk[i]);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -608,7 +655,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
             // The next item's first PV overwrites O only after this warp's next arrival on
             // p_full, which follows the reads below.
             const int gl = g - 1;
-            if (!mbar_wait_warp(&ctl.pv_done[gl & 1], (gl >> 1) & 1, wc)) { ok = false; break; }
+            if (!mbar_wait_warp(&ctl.pv_done[gl % C::NPB], (gl / C::NPB) & 1, wc)) { ok = false; break; }
             tc_fence_after();
             const size_t orow = (static_cast<size_t>(x.tok0) + tok) * a.Hq + static_cast<size_t>(x.head) * a.G + hq;
             if (x.part < 0) {
