@@ -584,9 +584,10 @@ int64_t sas_decode_launch_count(const sas_decode_handle* h);
  * that each get any number of new tokens (a prompt chunk, a few drafted tokens, a
  * single token, none): page plan, norm + rotation + append, dense causal attention
  * of the new tokens over the cache, verification of drafted tokens.  (The paper
- * prefills before it decodes and has no counterpart of these.)  After a prompt is
- * in the cache, sas_decode_summarize and sas_decode_step continue on the same
- * cache, block table and lengths.
+ * prefills before it decodes and has no counterpart of these.)  After a prompt or
+ * accepted drafts are in the cache, sas_decode_summarize makes the summaries of the
+ * blocks they filled, and sas_decode_step continues on the same cache, block table
+ * and lengths.
  *
  * Lengths, offsets, slots, page and token indices are read on the device: nothing
  * here synchronises or allocates after sas_chunk_create, and a captured step can be
@@ -614,12 +615,15 @@ void sas_chunk_destroy(sas_chunk_handle* h);
 
 /* Page plan of a step: gives every request the pages its new tokens need and maps
  * the new tokens to cache slots.  With s = seq_lens[b], n = new_lens[b], request b
- * goes from ceil(s / 64) to ceil((s + n) / 64) pages; new pages are taken from
- * free_pages in request order, starting at free_pages[*free_begin].
+ * goes from ceil(h / 64) to ceil((s + n) / 64) pages, h = max(s, held_lens[b]); new
+ * pages are taken from free_pages in request order, starting at
+ * free_pages[*free_begin].
  *   num_seqs     requests, 1 .. max_seqs
  *   T            capacity of positions and slots, 1 .. max_tokens
  *   seq_lens     int32 [num_seqs] tokens in the cache                          (in)
  *   new_lens     int32 [num_seqs] new tokens, 0 allowed                        (in)
+ *   held_lens    int32 [num_seqs] tokens whose pages a request holds (more than s
+ *                after a step whose drafts were rejected), or NULL: seq_lens     (in)
  *   free_pages   int32 [num_free] unused pages, taken front to back            (in)
  *   free_begin   int32 [1] first one not yet taken                             (in)
  *   block_table  int32 [num_seqs, max_blocks]: entries of the new pages written (in/out)
@@ -638,7 +642,7 @@ void sas_chunk_destroy(sas_chunk_handle* h);
  * SAS_ERR_INVALID_ARG.  kv_lens and free_end must not be the inputs' memory.
  * One launch. */
 sas_status sas_chunk_plan(sas_chunk_handle* h, int32_t num_seqs, int32_t T, const int32_t* seq_lens,
-                          const int32_t* new_lens, const int32_t* free_pages, int32_t num_free,
+                          const int32_t* new_lens, const int32_t* held_lens, const int32_t* free_pages, int32_t num_free,
                           const int32_t* free_begin, int32_t* block_table, int32_t* kv_lens, int32_t* cu_new,
                           int32_t* positions, int64_t* slots, int32_t* free_end, void* stream);
 

@@ -61,14 +61,14 @@ def qk_norm_rope_grad(qkv, wq, wk, cos, sin, positions, Hq, eps, interleaved, dY
     return dx, dw[0], dw[1]
 
 
-def plan(seq_lens, new_lens, free_pages, free_begin, table, T):
+def plan(seq_lens, new_lens, free_pages, free_begin, table, T, held_lens=None):
     """(kv_lens, cu, positions, slots, free_end, table) of a plan that fits."""
     table = np.array(table)
     at = free_begin
     cu, positions, slots = [0], [], []
     for b, (s, n) in enumerate(zip(seq_lens, new_lens)):
         for p in range(s, s + n):
-            if p % PAGE == 0:
+            if p % PAGE == 0 and (held_lens is None or p >= held_lens[b]):   # a block no held page covers
                 table[b, p // PAGE] = free_pages[at]
                 at += 1
             positions.append(p)

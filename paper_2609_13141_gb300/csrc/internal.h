@@ -289,6 +289,7 @@ struct PlanArgs {
     int B, T, max_blocks, num_pages, num_free;
     const int32_t* seq_lens;    // [B]
     const int32_t* new_lens;    // [B]
+    const int32_t* held_lens;   // [B] tokens whose pages are held, or null (seq_lens)
     const int32_t* free_pages;  // [num_free]
     const int32_t* free_begin;  // [1]
     int32_t* block_table;       // [B][max_blocks]

@@ -10,7 +10,7 @@ constexpr int kStatusNoPages = 5;    // == SAS_ERR_OOM
 
 // ------------------------------------------------------------------ page plan
 //
-// Request b holds s tokens and gets n more: its pages grow from ceil(s / 64) to
+// Request b has s tokens and gets n more: its pages grow from ceil(max(s, held) / 64) to
 // ceil((s + n) / 64), the new ones taken from the free list in request order, and
 // new token i sits at position s + i, slot page * 64 + (s + i) % 64.
 //
@@ -70,6 +70,11 @@ __device__ __forceinline__ int owner(const int* sums, int n, int v) {
     return lo;
 }
 
+// Pages request b holds.
+__device__ __forceinline__ int pages_held(const PlanArgs& a, int b, int s) {
+    return ((a.held_lens != nullptr ? max(s, __ldg(a.held_lens + b)) : s) + 63) / 64;
+}
+
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
     extern __shared__ int sm[];
     int* cu = sm;              // [B] first new token of each request
@@ -79,10 +84,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
     int bad = 0;
     for (int b = t; b < a.B; b += kPlanThreads) {
         const int s = __ldg(a.seq_lens + b), n = __ldg(a.new_lens + b);
-        const bool wrong = s < 0 || n < 0 || static_cast<long long>(s) + n > cap;
+        const int held = a.held_lens != nullptr ? __ldg(a.held_lens + b) : 0;
+        const bool wrong = s < 0 || n < 0 || static_cast<long long>(s) + n > cap || held < 0 || held > cap;
         bad |= wrong;
         cu[b] = wrong ? 0 : n;
-        off[b] = wrong ? 0 : (s + n + 63) / 64 - (s + 63) / 64;
+        off[b] = wrong ? 0 : max(0, (s + n + 63) / 64 - (max(s, held) + 63) / 64);
     }
     bad = __syncthreads_or(bad);
     const int per = (a.B + kPlanThreads - 1) / kPlanThreads;
@@ -119,7 +125,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
     }
     for (int p = at; p < pages; p += step) {
         const int b = owner(off, a.B, p);
-        const int blk = (__ldg(a.seq_lens + b) + 63) / 64 + p - off[b];
+        const int blk = pages_held(a, b, __ldg(a.seq_lens + b)) + p - off[b];
         int page = __ldg(a.free_pages + begin + p);
         if (page < 0 || page >= a.num_pages) {
             atomicExch(a.status, kStatusBadInput);
@@ -134,7 +140,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
             const int b = owner(cu, a.B, i);
             const int s = __ldg(a.seq_lens + b);
             pos = s + i - cu[b];
-            const int blk = pos >> 6, have = (s + 63) / 64;
+            const int blk = pos >> 6, have = pages_held(a, b, s);
             // a page of this call comes from the free list: its table entry may not be written yet
             const int page = blk < have ? a.block_table[static_cast<size_t>(b) * a.max_blocks + blk]
                                         : __ldg(a.free_pages + begin + off[b] + blk - have);

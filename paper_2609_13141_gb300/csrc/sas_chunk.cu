@@ -193,7 +193,7 @@ void sas_chunk_destroy(sas_chunk_handle* h) {
 }
 
 sas_status sas_chunk_plan(sas_chunk_handle* h, int32_t num_seqs, int32_t T, const int32_t* seq_lens,
-                          const int32_t* new_lens, const int32_t* free_pages, int32_t num_free,
+                          const int32_t* new_lens, const int32_t* held_lens, const int32_t* free_pages, int32_t num_free,
                           const int32_t* free_begin, int32_t* block_table, int32_t* kv_lens, int32_t* cu_new,
                           int32_t* positions, int64_t* slots, int32_t* free_end, void* stream) {
     if (h == nullptr) return SAS_ERR_INVALID_ARG;
@@ -207,15 +207,15 @@ sas_status sas_chunk_plan(sas_chunk_handle* h, int32_t num_seqs, int32_t T, cons
         if (!seq_lens || !new_lens || (!free_pages && num_free > 0) || !free_begin || !block_table || !kv_lens || !cu_new ||
             !positions || !slots || !free_end)
             return cfail(h, SAS_ERR_INVALID_ARG, "a required argument is NULL");
-        if (!al4(seq_lens) || !al4(new_lens) || !al4(free_pages) || !al4(free_begin) || !al4(block_table) ||
+        if (!al4(seq_lens) || !al4(new_lens) || !al4(held_lens) || !al4(free_pages) || !al4(free_begin) || !al4(block_table) ||
             !al4(kv_lens) || !al4(cu_new) || !al4(positions) || !al8(slots) || !al4(free_end))
             return cfail(h, SAS_ERR_INVALID_ARG, "misaligned pointer");
         // every block reads the inputs while others write
-        if (kv_lens == seq_lens || kv_lens == new_lens || free_end == free_begin)
+        if (kv_lens == seq_lens || kv_lens == new_lens || kv_lens == held_lens || free_end == free_begin)
             return cfail(h, SAS_ERR_INVALID_ARG, "outputs must not be the inputs' memory");
         sas::PlanArgs a{};
         a.B = num_seqs; a.T = T; a.max_blocks = c.max_blocks; a.num_pages = c.num_pages; a.num_free = num_free;
-        a.seq_lens = seq_lens; a.new_lens = new_lens; a.free_pages = free_pages; a.free_begin = free_begin;
+        a.seq_lens = seq_lens; a.new_lens = new_lens; a.held_lens = held_lens; a.free_pages = free_pages; a.free_begin = free_begin;
         a.block_table = block_table; a.kv_lens = kv_lens; a.cu_new = cu_new; a.positions = positions; a.slots = slots;
         a.free_end = free_end; a.status = h->status;
         cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -159,7 +159,7 @@ def lib():
     L.sas_chunk_create.restype = i32
     L.sas_chunk_destroy.argtypes = [vp]
     L.sas_chunk_destroy.restype = None
-    L.sas_chunk_plan.argtypes = [vp, i32, i32, vp, vp, vp, i32] + [vp] * 8
+    L.sas_chunk_plan.argtypes = [vp, i32, i32, vp, vp, vp, vp, i32] + [vp] * 8
     L.sas_chunk_plan.restype = i32
     L.sas_chunk_append.argtypes = [vp, rope, i32, vp, i64] + [vp] * 10
     L.sas_chunk_append.restype = i32
@@ -748,12 +748,13 @@ def sas_chunk_destroy(h):
 
 
 def sas_chunk_plan(h, seq_lens, new_lens, free_pages, free_begin, block_table, kv_lens, cu_new, positions, slots,
-                   free_end, stream=None):
+                   free_end, held_lens=None, stream=None):
     i32, B, T, dev = torch.int32, seq_lens.shape[0], positions.shape[0], seq_lens.get_device()
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError(f"block_table must have {B} rows")
     st = lib().sas_chunk_plan(
         h, B, T, _arg(seq_lens, i32, "seq_lens", (B,)), _arg(new_lens, i32, "new_lens", (B,), dev),
+        None if held_lens is None else _arg(held_lens, i32, "held_lens", (B,), dev),
         _arg(free_pages, i32, "free_pages", None, dev), free_pages.numel(), _arg(free_begin, i32, "free_begin", (1,), dev),
         _arg(block_table, i32, "block_table", None, dev), _arg(kv_lens, i32, "kv_lens", (B,), dev),
         _arg(cu_new, i32, "cu_new", (B + 1,), dev), _arg(positions, i32, "positions", (T,), dev),
@@ -872,16 +873,17 @@ class SasChunk:
         if K_cache.shape != self.cache_shape:
             raise ValueError(f"K_cache must have shape {self.cache_shape}, got {tuple(K_cache.shape)}")
 
-    def plan(self, seq_lens, new_lens, free_pages, free_begin, block_table, T, out=None, stream=None):
+    def plan(self, seq_lens, new_lens, free_pages, free_begin, block_table, T, held_lens=None, out=None, stream=None):
         """Pages and slots of the new tokens: a ChunkPlan; block_table gets the new pages.  T: capacity for new
-        tokens (positions and slots are -1 past their number)."""
+        tokens (positions and slots are -1 past their number).  held_lens: tokens whose pages each request holds
+        (seq_lens if not given)."""
         self._table(block_table)
         if out is None:
             with _on(stream):
                 out = self.plan_buffers(seq_lens.shape[0], T, seq_lens.device)
         elif out.positions.shape[0] != T:
             raise ValueError(f"out.positions must have {T} entries")
-        sas_chunk_plan(self.h, seq_lens, new_lens, free_pages, free_begin, block_table, *out, stream=stream)
+        sas_chunk_plan(self.h, seq_lens, new_lens, free_pages, free_begin, block_table, *out, held_lens, stream)
         return out
 
     def append(self, qkv, wq, wk, cos, sin, positions, slots, K_cache, V_cache, eps=1e-6, interleaved=False, out=None,

@@ -152,3 +152,29 @@ def test_no_free_pages_needed():
     assert sas.sas_chunk_get_device_status(ch.h) == sas.SAS_OK
     assert p.slots.tolist() == [7 * 64 + 3 + i for i in range(8)]
     ch.close()
+
+
+@pytest.mark.parametrize("seq,held,new", [
+    ([62, 10, 130], [66, 10, 200], [3, 60, 62]),        # a held page opened by rejected drafts is used, not replaced
+    ([1, 64, 0], [300, 64, 65], [5, 64, 200]),           # held far past the new tokens; exactly at a boundary
+    ([70, 5], [0, 3], [10, 70]),                         # held below the length counts as the length
+])
+def test_held_pages_are_used_before_free_ones(seq, held, new):
+    T = sum(new)
+    top = [max(s, h) for s, h in zip(seq, held)]
+    need = sum(max(0, -(-(s + n) // 64) - -(-h // 64)) for s, n, h in zip(seq, new, top))
+    table, free, P = _state(top, 8, need)
+    ch = sas.SasChunk(len(seq), 1, 1, 64, 8, P, T)
+    tab = _t(table)
+    p = ch.plan(_t(seq), _t(new), _t(free), _t([0]), tab, T, held_lens=_t(held))
+    assert sas.sas_chunk_get_device_status(ch.h) == sas.SAS_OK
+    kv, cu, pos, slots, end, want = S.plan(seq, new, free, 0, table, T, top)
+    assert p.kv_lens.tolist() == kv and p.cu_new.tolist() == cu and p.positions.tolist() == pos
+    assert p.slots.tolist() == slots and p.free_end.tolist() == [end] == [need] and np.array_equal(tab.cpu().numpy(), want)
+    for bad in (-1, 64 * 8 + 1):
+        p = ch.plan(_t(seq), _t(new), _t(free), _t([0]), tab, T, held_lens=_t([bad] + held[1:]))
+        assert sas.sas_chunk_get_device_status(ch.h) == sas.SAS_ERR_INVALID_ARG and p.cu_new.tolist() == [0] * (len(seq) + 1)
+    with pytest.raises(sas.SasError, match="inputs"):
+        h = _t(held)
+        ch.plan(_t(seq), _t(new), _t(free), _t([0]), tab, T, held_lens=h, out=p._replace(kv_lens=h))
+    ch.close()

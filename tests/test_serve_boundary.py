@@ -44,7 +44,7 @@ def test_chunk_create_without_gpu_fails_cleanly(lib):
 
 def test_serving_null_handles(lib):
     null, rope = ctypes.c_void_p(), sas.SasRopeConfig(64, 0, 8, 1e-6)
-    assert lib.sas_chunk_plan(null, 1, 1, None, None, None, 0, *([None] * 8)) == sas.SAS_ERR_INVALID_ARG
+    assert lib.sas_chunk_plan(null, 1, 1, None, None, None, None, 0, *([None] * 8)) == sas.SAS_ERR_INVALID_ARG
     assert lib.sas_chunk_append(null, rope, 1, None, 64, *([None] * 10)) == sas.SAS_ERR_INVALID_ARG
     assert lib.sas_chunk_attention(null, 1, 1, *([None] * 9)) == sas.SAS_ERR_INVALID_ARG
     assert lib.sas_chunk_verify(null, 1, 0, 0, 8, None, None, None, 8, None, 8, None, None, 8, None, None, None) == \
