@@ -29,8 +29,8 @@
 // used as an address: it becomes the row past the cache, which TMA reads as zero.
 #include <math_constants.h>
 
-#include "internal.h"
-#include "ptx.cuh"
+#include "serve.h"
+#include "serve_ptx.cuh"
 
 namespace sas {
 namespace {

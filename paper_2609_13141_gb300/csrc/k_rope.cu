@@ -18,8 +18,8 @@
 // the same heads for all its tokens (their kinds, weights and addresses are then
 // fixed), rows stream through a ring in shared memory (cp.async, no registers held
 // while they are in flight), and the arithmetic runs on packed fp32 pairs.
-#include "internal.h"
-#include "ptx.cuh"
+#include "serve.h"
+#include "serve_ptx.cuh"
 
 namespace sas {
 namespace {

@@ -1,6 +1,6 @@
 // Bookkeeping of a serving step: the page plan and the verification of drafts.
-#include "internal.h"
-#include "ptx.cuh"
+#include "serve.h"
+#include "serve_ptx.cuh"
 
 namespace sas {
 namespace {

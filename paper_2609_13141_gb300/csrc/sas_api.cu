@@ -13,7 +13,7 @@
 #include <cudaTypedefs.h>
 
 #include "../../include/sas.h"
-#include "internal.h"
+#include "serve.h"
 #include "ptx.cuh"
 
 namespace sas {

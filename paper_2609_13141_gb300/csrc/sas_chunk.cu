@@ -8,7 +8,7 @@
 #include <vector>
 
 #include "../../include/sas.h"
-#include "internal.h"
+#include "serve.h"
 
 namespace {
 
