@@ -191,15 +191,18 @@ __device__ __forceinline__ bool find_range(const ChunkArgs& a, int R, Shares& sh
 
 // A step is KPS pages: their scores, softmax and product go through the pipeline together.
 // Each step costs the softmax warps some 400 cycles of waits, tensor-memory loads and
-// stores beside its arithmetic.  At d = 128 two blocks' products (1024 cycles a page
-// pair) cover that, and tensor memory holds no more: O 128 + S 64 + two P of 32
-// columns.  At d = 64 the products are half as long and nothing covers it: two pages
-// a step, O 64 + S 128 + one P of 64 columns, with the score rows in registers (184 a
-// softmax thread, 64 for the others, of the 128 the block is launched with).
+// stores beside its arithmetic.  At d = 128 the products of the multiprocessor's two
+// blocks cover that.  They are bound by the operands' way out of shared memory: with 64
+// keys a product step reads 4 KB of Q and 2 KB of K in 48 cycles, for 32 of arithmetic.
+// With the first half of Q in tensor memory (O 128 + S 64 + P 32 + Q 32 columns: no room
+// for more) a page takes 571 cycles of the tensor pipe instead of 618.  At d = 64 the
+// products are half as long and nothing covers the waits: two pages a step, O 64 + S
+// 128 + P 64 columns, with the score rows in registers (184 a softmax thread, 64 for the
+// others, of the 128 the block is launched with).
 template <int D>
 struct Cfg {
     static constexpr int KPS = D == 64 ? 2 : 1;
-    static constexpr int NPB = D == 64 ? 1 : 2;     // P buffers
+    static constexpr bool QT = D == 128;            // half of Q in tensor memory
     static constexpr int QST = D == 64 ? 2 : 1;     // Q tiles (of the item at work, and the next one's)
     static constexpr int Q_BYTES = kBM * D * 2;
     static constexpr int KV_BYTES = kBN * D * 2;
@@ -212,8 +215,9 @@ struct Cfg {
     static constexpr int TMEM_COLS = 256;
     static constexpr int TMEM_O = 0;
     static constexpr int TMEM_S = D;
-    static constexpr int TMEM_P = TMEM_S + KPS * kBN;   // buffer b at + 32 KPS b (keys packed in pairs)
-    static_assert(TMEM_P + NPB * 32 * KPS <= TMEM_COLS, "tensor memory");
+    static constexpr int TMEM_P = TMEM_S + KPS * kBN;   // keys packed in pairs
+    static constexpr int TMEM_Q = TMEM_P + 32 * KPS;    // the row's first 64 dims packed in pairs
+    static_assert(TMEM_Q + (QT ? 32 : 0) <= TMEM_COLS, "tensor memory");
     static constexpr uint32_t IDESC_S = idesc_bf16(kBM, kBN, 0, 0);
     static constexpr uint32_t IDESC_O = idesc_bf16(kBM, D, 0, 1);
 };
@@ -239,7 +243,7 @@ struct Item {
 
 struct Ctl {
     uint64_t q_full[2], q_empty[2], k_full[4], k_empty[4], v_full[4], v_empty[4];
-    uint64_t s_full, s_free, p_full[2], pv_done[2], drain_bar;
+    uint64_t s_full, s_free, p_full, pv_done, q_ready, drain_bar;
     uint64_t item_full[kItemSlots], item_empty[kItemSlots];
     Item item[kItemSlots];
     uint32_t tmem_base;
@@ -286,10 +290,9 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
         for (int s = 0; s < C::VST; ++s) { mbar_init(&ctl.v_full[s], 1); mbar_init(&ctl.v_empty[s], 1); }
         mbar_init(&ctl.s_full, 1);
         mbar_init(&ctl.s_free, 4);
-        for (int s = 0; s < 2; ++s) {
-            mbar_init(&ctl.pv_done[s], 1);
-            mbar_init(&ctl.p_full[s], 4);
-        }
+        mbar_init(&ctl.pv_done, 1);
+        mbar_init(&ctl.p_full, 4);
+        mbar_init(&ctl.q_ready, 4);
         mbar_init(&ctl.drain_bar, 2);
         for (int s = 0; s < kItemSlots; ++s) {
             mbar_init(&ctl.item_full[s], 1);
@@ -463,6 +466,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 const int qs = tc % C::QST;
                 const uint64_t dq = dq0 + static_cast<uint64_t>((qs * C::Q_BYTES) >> 4);
                 if (!mbar_wait_warp(&ctl.q_full[qs], (tc / C::QST) & 1, wc)) { ok = false; break; }
+                if (C::QT && !mbar_wait_warp(&ctl.q_ready, tc & 1, wc)) { ok = false; break; }
                 for (int m = x.blk0; ok && m < x.blk1; m += C::KPS, ++g) {
                     if (g >= 1 && !mbar_wait_warp(&ctl.s_free, (g - 1) & 1, wc)) { ok = false; break; }
                     for (int i = 0; i < C::KPS && m + i < x.blk1; ++i, ++gp) {
@@ -475,7 +479,12 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                             for (int k = 0; k < D / 16; ++k) {
                                 const uint32_t off_q = (k >> 2) * (kBM * 128) + (k & 3) * 32;
                                 const uint32_t off_k = (k >> 2) * (kBN * 128) + (k & 3) * 32;
-                                umma_bf16(tmem_base + C::TMEM_S + i * kBN, dq + (off_q >> 4), dk + (off_k >> 4), C::IDESC_S, k > 0);
+                                if (C::QT && k < 4)
+                                    umma_bf16_ta(tmem_base + C::TMEM_S, tmem_base + C::TMEM_Q + k * 8, dk + (off_k >> 4),
+                                                 C::IDESC_S, k > 0);
+                                else
+                                    umma_bf16(tmem_base + C::TMEM_S + i * kBN, dq + (off_q >> 4), dk + (off_k >> 4),
+                                              C::IDESC_S, k > 0);
                             }
                             umma_commit(&ctl.k_empty[s]);
                         }
@@ -505,7 +514,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 if (x.head < 0) break;
                 const int end = x.pos0 + x.ntok;   // keys from here on belong to no row of the tile
                 for (int m0 = x.blk0; ok && m0 < x.blk1; m0 += C::KPS, ++g) {
-                    const int pb = g % C::NPB;
                     for (int i = 0; i < C::KPS && m0 + i < x.blk1; ++i, ++gp) {
                         const int m = m0 + i;
                         const int vs = gp % C::VST;
@@ -522,21 +530,21 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                             fence_proxy_async_smem();
                             __syncwarp();
                         }
-                        if (i == 0 && !mbar_wait_warp(&ctl.p_full[pb], (g / C::NPB) & 1, wc)) { ok = false; break; }
+                        if (i == 0 && !mbar_wait_warp(&ctl.p_full, g & 1, wc)) { ok = false; break; }
                         tc_fence_after();
                         const uint64_t dv = dv0 + static_cast<uint64_t>((vs * C::KV_BYTES) >> 4);
                         if (elect_one()) {
 #pragma unroll
                             for (int k = 0; k < kBN / 16; ++k)
                                 umma_bf16_ta(tmem_base + C::TMEM_O,
-                                             tmem_base + C::TMEM_P + pb * (32 * C::KPS) + i * 32 + k * 8,
+                                             tmem_base + C::TMEM_P + i * 32 + k * 8,
                                              dv + ((k * 2048) >> 4), C::IDESC_O, (m > x.blk0 || k > 0) ? 1u : 0u);
                             umma_commit(&ctl.v_empty[vs]);
                         }
                         __syncwarp();
                     }
                     if (!ok) break;
-                    if (elect_one()) umma_commit(&ctl.pv_done[pb]);
+                    if (elect_one()) umma_commit(&ctl.pv_done);
                     __syncwarp();
                 }
             }
@@ -555,26 +563,47 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
         const int tok = row / a.G, hq = row - tok * a.G;
         const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
         const uint64_t scale2 = f32x2(scale_log2, scale_log2);
+        // the r-th item, and its rows' first 64 dims from shared into tensor memory (the products of
+        // the item before, which read the ones there, are done: this warp has seen their scores)
+        auto take_item = [&](int r, Item& x) {
+            if (!read_item(ctl, r, wc, x)) return false;
+            if (!C::QT || x.head < 0) return true;
+            if (!mbar_wait_warp(&ctl.q_full[0], r & 1, wc)) return false;
+            if (q * 32 < x.ntok * a.G) {
+                uint32_t w[32];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {   // 16-byte chunks, swizzled within the 128-byte row
+                    const uint4 v = *reinterpret_cast<const uint4*>(smem + row * 128 + ((c ^ (row & 7)) << 4));
+                    w[4 * c] = v.x;
+                    w[4 * c + 1] = v.y;
+                    w[4 * c + 2] = v.z;
+                    w[4 * c + 3] = v.w;
+                }
+                tmem_st32(lane_addr + C::TMEM_Q, w);
+                tmem_wait_st();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.q_ready);
+            return true;
+        };
         int g = 0;
-        bool ok = true;
-        for (int r = 0; ok; ++r) {
-            Item x;
-            if (!read_item(ctl, r, wc, x)) { ok = false; break; }
-            if (x.head < 0) break;
+        Item x, nx;
+        bool ok = take_item(0, x);
+        for (int r = 1; ok && x.head >= 0; x = nx, ++r) {
             const bool valid = tok < x.ntok;
             const bool warp_rows = q * 32 < x.ntok * a.G;   // else nothing of this warp is ever read
             const int pos = x.pos0 + tok;
             float m_use = -CUDART_INF_F, l = 0.f;
             for (int m = x.blk0; m < x.blk1; m += C::KPS, ++g) {
-                const int pb = g % C::NPB;
                 // last key column of the step that this row sees (< 0: none; none of a page that is not
                 // there).  Rows of no token are never read: they go unmasked.
                 const int lim = valid ? min(min(NK - 1, pos - m * kBN), (x.blk1 - m) * kBN - 1) : NK - 1;
                 if (!mbar_wait_warp(&ctl.s_full, g & 1, wc)) { ok = false; break; }
                 if (!warp_rows) {
                     if (lane == 0) mbar_arrive(&ctl.s_free);
-                    if (g >= C::NPB && !mbar_wait_warp(&ctl.pv_done[pb], (g / C::NPB - 1) & 1, wc)) { ok = false; break; }
-                    if (lane == 0) mbar_arrive(&ctl.p_full[pb]);
+                    if (g >= 1 && !mbar_wait_warp(&ctl.pv_done, (g - 1) & 1, wc)) { ok = false; break; }
+                    if (lane == 0) mbar_arrive(&ctl.p_full);
                     __syncwarp();
                     continue;
                 }
@@ -626,7 +655,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 if (need) factor = m_use == -CUDART_INF_F ? 0.f : fast_exp2(m_use - m_new);
                 if (m > x.blk0 && __any_sync(0xffffffffu, need)) {
                     // rescaling O needs the previous step's PV done
-                    if (!mbar_wait_warp(&ctl.pv_done[(g - 1) % C::NPB], ((g - 1) / C::NPB) & 1, wc)) { ok = false; break; }
+                    if (!mbar_wait_warp(&ctl.pv_done, (g - 1) & 1, wc)) { ok = false; break; }
                     tc_fence_after();
 #pragma unroll 1
                     for (int cc = 0; cc < D / 32; ++cc) {
@@ -641,21 +670,21 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 }
                 l = l * factor + rs;
                 m_use = m_new;
-                // P buffer pb is free once the PV of step g - NPB has read it
-                if (g >= C::NPB && !mbar_wait_warp(&ctl.pv_done[pb], (g / C::NPB - 1) & 1, wc)) { ok = false; break; }
+                // P is free once the PV of step g - 1 has read it
+                if (g >= 1 && !mbar_wait_warp(&ctl.pv_done, (g - 1) & 1, wc)) { ok = false; break; }
                 tc_fence_after();
 #pragma unroll
-                for (int i = 0; i < C::KPS; ++i) tmem_st32(lane_addr + C::TMEM_P + pb * (32 * C::KPS) + i * 32, pk[i]);
+                for (int i = 0; i < C::KPS; ++i) tmem_st32(lane_addr + C::TMEM_P + i * 32, pk[i]);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&ctl.p_full[pb]);
+                if (lane == 0) mbar_arrive(&ctl.p_full);
             }
-            if (!ok) break;
+            // the next item's Q goes ahead of this one's epilogue: its first product runs during it
+            if (!ok || !take_item(r, nx)) { ok = false; break; }
             // The next item's first PV overwrites O only after this warp's next arrival on
             // p_full, which follows the reads below.
-            const int gl = g - 1;
-            if (!mbar_wait_warp(&ctl.pv_done[gl % C::NPB], (gl / C::NPB) & 1, wc)) { ok = false; break; }
+            if (!mbar_wait_warp(&ctl.pv_done, (g - 1) & 1, wc)) { ok = false; break; }
             tc_fence_after();
             const size_t orow = (static_cast<size_t>(x.tok0) + tok) * a.Hq + static_cast<size_t>(x.head) * a.G + hq;
             if (x.part < 0) {
