@@ -204,24 +204,29 @@ def _ptr(t, dtype, name, required=True):
     return ctypes.c_void_p(t.data_ptr())
 
 
-def _arg(t, dtype, name, shape=None, dev=None):
-    """Device address of a contiguous tensor: like _ptr, with its shape and device checked, and a plain
-    integer, for the entry points whose time is mostly the call's."""
-    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_contiguous() and (dev is None or t.get_device() == dev) and
-            (shape is None or t.shape == shape) and t.is_cuda):
-        return t.data_ptr()
-    _refuse(t, dtype, name, shape, dev)
+def _arg(t, dtype, name, dev, shape=None):
+    """Device address of a contiguous tensor on device `dev` (its index): like _ptr, with its shape and device checked,
+    and a plain integer, for the entry points whose time is mostly the call's."""
+    try:
+        if t.dtype is dtype and t.get_device() == dev >= 0 and t.is_contiguous() and (shape is None or t.shape == shape):
+            return t.data_ptr()
+    except AttributeError:   # not a tensor
+        pass
+    _refuse(t, dtype, name, dev, shape)
     raise ValueError(f"{name} must be contiguous")
 
 
-def _rows(t, dtype, name, shape, dev):
+def _rows(t, dtype, name, dev, shape):
     """Device address of a tensor of any strides (its caller checks those)."""
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_cuda:
-        return t.data_ptr()
-    _refuse(t, dtype, name, shape, dev)
+    try:
+        if t.dtype is dtype and t.get_device() == dev >= 0 and t.shape == shape:
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(t, dtype, name, dev, shape)
 
 
-def _refuse(t, dtype, name, shape, dev):
+def _refuse(t, dtype, name, dev, shape):
     """Raises for what is wrong with a tensor argument, if it is not its strides."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
@@ -229,8 +234,16 @@ def _refuse(t, dtype, name, shape, dev):
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if dev is not None and t.get_device() != dev:
+    if t.get_device() != dev:
         raise ValueError(f"{name} must be on device {dev}")
+
+
+def _rope_config(cos, eps, interleaved):
+    try:
+        max_pos, half = cos.shape
+    except (AttributeError, ValueError):
+        raise ValueError("cos must be a [max_pos, rot / 2] tensor") from None
+    return SasRopeConfig(2 * half, 1 if interleaved else 0, max_pos, eps)
 
 
 def _token_stride(t, name, lead):
@@ -362,12 +375,12 @@ def sas_qk_norm_rope_fwd(h, qkv, wq, wk, cos, sin, Q, K, V, positions=None, eps=
     """qkv [B, N, H + 2 Hkv, d] (tokens evenly spaced, any distance) to Q [B, H, N, d], K and V [B, Hkv, N, d]."""
     B, H, N, d = Q.shape
     Hkv, dev, bf, f32 = K.shape[1], Q.get_device(), torch.bfloat16, torch.float32
-    cfg = SasRopeConfig(2 * cos.shape[-1], 1 if interleaved else 0, cos.shape[0], eps)
+    cfg = _rope_config(cos, eps, interleaved)
     st = lib().sas_qk_norm_rope_fwd(
-        h, cfg, _rows(qkv, bf, "qkv", (B, N, H + 2 * Hkv, d), dev), _token_stride(qkv, "qkv", 2), _arg(wq, bf, "wq", (d,), dev),
-        _arg(wk, bf, "wk", (d,), dev), _arg(cos, f32, "cos", None, dev), _arg(sin, f32, "sin", cos.shape, dev),
-        None if positions is None else _arg(positions, torch.int32, "positions", (B, N), dev), _arg(Q, bf, "Q"),
-        _arg(K, bf, "K", (B, Hkv, N, d), dev), _arg(V, bf, "V", (B, Hkv, N, d), dev), _raw_stream(stream, dev))
+        h, cfg, _rows(qkv, bf, "qkv", dev, (B, N, H + 2 * Hkv, d)), _token_stride(qkv, "qkv", 2),
+        _arg(wq, bf, "wq", dev, (d,)), _arg(wk, bf, "wk", dev, (d,)), _arg(cos, f32, "cos", dev), _arg(sin, f32, "sin", dev, cos.shape),
+        None if positions is None else _arg(positions, torch.int32, "positions", dev, (B, N)), _arg(Q, bf, "Q", dev),
+        _arg(K, bf, "K", dev, (B, Hkv, N, d)), _arg(V, bf, "V", dev, (B, Hkv, N, d)), _raw_stream(stream, dev))
     if st != SAS_OK:
         _check(st, h, "sas_qk_norm_rope_fwd")
 
@@ -378,13 +391,13 @@ def sas_qk_norm_rope_bwd(h, qkv, wq, wk, cos, sin, dQ, dK, dV, dqkv, dwq, dwk, p
     B, H, N, d = dQ.shape
     Hkv, dev, bf, f32 = dK.shape[1], dQ.get_device(), torch.bfloat16, torch.float32
     rows = (B, N, H + 2 * Hkv, d)
-    cfg = SasRopeConfig(2 * cos.shape[-1], 1 if interleaved else 0, cos.shape[0], eps)
+    cfg = _rope_config(cos, eps, interleaved)
     st = lib().sas_qk_norm_rope_bwd(
-        h, cfg, _rows(qkv, bf, "qkv", rows, dev), _token_stride(qkv, "qkv", 2), _arg(wq, bf, "wq", (d,), dev),
-        _arg(wk, bf, "wk", (d,), dev), _arg(cos, f32, "cos", None, dev), _arg(sin, f32, "sin", cos.shape, dev),
-        None if positions is None else _arg(positions, torch.int32, "positions", (B, N), dev), _arg(dQ, bf, "dQ"),
-        _arg(dK, bf, "dK", (B, Hkv, N, d), dev), _arg(dV, bf, "dV", (B, Hkv, N, d), dev), _rows(dqkv, bf, "dqkv", rows, dev),
-        _token_stride(dqkv, "dqkv", 2), _arg(dwq, f32, "dwq", (d,), dev), _arg(dwk, f32, "dwk", (d,), dev),
+        h, cfg, _rows(qkv, bf, "qkv", dev, rows), _token_stride(qkv, "qkv", 2), _arg(wq, bf, "wq", dev, (d,)),
+        _arg(wk, bf, "wk", dev, (d,)), _arg(cos, f32, "cos", dev), _arg(sin, f32, "sin", dev, cos.shape),
+        None if positions is None else _arg(positions, torch.int32, "positions", dev, (B, N)), _arg(dQ, bf, "dQ", dev),
+        _arg(dK, bf, "dK", dev, (B, Hkv, N, d)), _arg(dV, bf, "dV", dev, (B, Hkv, N, d)), _rows(dqkv, bf, "dqkv", dev, rows),
+        _token_stride(dqkv, "dqkv", 2), _arg(dwq, f32, "dwq", dev, (d,)), _arg(dwk, f32, "dwk", dev, (d,)),
         _raw_stream(stream, dev))
     if st != SAS_OK:
         _check(st, h, "sas_qk_norm_rope_bwd")
@@ -753,12 +766,12 @@ def sas_chunk_plan(h, seq_lens, new_lens, free_pages, free_begin, block_table, k
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError(f"block_table must have {B} rows")
     st = lib().sas_chunk_plan(
-        h, B, T, _arg(seq_lens, i32, "seq_lens", (B,)), _arg(new_lens, i32, "new_lens", (B,), dev),
-        None if held_lens is None else _arg(held_lens, i32, "held_lens", (B,), dev),
-        _arg(free_pages, i32, "free_pages", None, dev), free_pages.numel(), _arg(free_begin, i32, "free_begin", (1,), dev),
-        _arg(block_table, i32, "block_table", None, dev), _arg(kv_lens, i32, "kv_lens", (B,), dev),
-        _arg(cu_new, i32, "cu_new", (B + 1,), dev), _arg(positions, i32, "positions", (T,), dev),
-        _arg(slots, torch.int64, "slots", (T,), dev), _arg(free_end, i32, "free_end", (1,), dev), _raw_stream(stream, dev))
+        h, B, T, _arg(seq_lens, i32, "seq_lens", dev, (B,)), _arg(new_lens, i32, "new_lens", dev, (B,)),
+        None if held_lens is None else _arg(held_lens, i32, "held_lens", dev, (B,)),
+        _arg(free_pages, i32, "free_pages", dev), free_pages.numel(), _arg(free_begin, i32, "free_begin", dev, (1,)),
+        _arg(block_table, i32, "block_table", dev), _arg(kv_lens, i32, "kv_lens", dev, (B,)),
+        _arg(cu_new, i32, "cu_new", dev, (B + 1,)), _arg(positions, i32, "positions", dev, (T,)),
+        _arg(slots, torch.int64, "slots", dev, (T,)), _arg(free_end, i32, "free_end", dev, (1,)), _raw_stream(stream, dev))
     if st != SAS_OK:
         _ccheck(st, h, "sas_chunk_plan")
 
@@ -768,12 +781,12 @@ def sas_chunk_append(h, qkv, wq, wk, cos, sin, positions, slots, Q, K_cache, V_c
     """qkv [T, Hq + 2 Hkv, d] (tokens evenly spaced, any distance)."""
     T, Hq, d = Q.shape
     Hkv, dev, bf, f32 = K_cache.shape[1], Q.get_device(), torch.bfloat16, torch.float32
-    cfg = SasRopeConfig(2 * cos.shape[-1], 1 if interleaved else 0, cos.shape[0], eps)
+    cfg = _rope_config(cos, eps, interleaved)
     st = lib().sas_chunk_append(
-        h, cfg, T, _rows(qkv, bf, "qkv", (T, Hq + 2 * Hkv, d), dev), _token_stride(qkv, "qkv", 1), _arg(wq, bf, "wq", (d,), dev),
-        _arg(wk, bf, "wk", (d,), dev), _arg(cos, f32, "cos", None, dev), _arg(sin, f32, "sin", cos.shape, dev),
-        _arg(positions, torch.int32, "positions", (T,), dev), _arg(slots, torch.int64, "slots", (T,), dev), _arg(Q, bf, "Q"),
-        _arg(K_cache, bf, "K_cache", None, dev), _arg(V_cache, bf, "V_cache", K_cache.shape, dev), _raw_stream(stream, dev))
+        h, cfg, T, _rows(qkv, bf, "qkv", dev, (T, Hq + 2 * Hkv, d)), _token_stride(qkv, "qkv", 1),
+        _arg(wq, bf, "wq", dev, (d,)), _arg(wk, bf, "wk", dev, (d,)), _arg(cos, f32, "cos", dev), _arg(sin, f32, "sin", dev, cos.shape),
+        _arg(positions, torch.int32, "positions", dev, (T,)), _arg(slots, torch.int64, "slots", dev, (T,)),
+        _arg(Q, bf, "Q", dev), _arg(K_cache, bf, "K_cache", dev), _arg(V_cache, bf, "V_cache", dev, K_cache.shape), _raw_stream(stream, dev))
     if st != SAS_OK:
         _ccheck(st, h, "sas_chunk_append")
 
@@ -783,17 +796,17 @@ def sas_chunk_attention(h, Q, K_cache, V_cache, block_table, cu_new, kv_lens, O,
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError(f"block_table must have {B} rows")
     st = lib().sas_chunk_attention(
-        h, B, Q.shape[0], _arg(Q, bf, "Q"), _arg(K_cache, bf, "K_cache", None, dev),
-        _arg(V_cache, bf, "V_cache", K_cache.shape, dev), _arg(block_table, i32, "block_table", None, dev),
-        _arg(cu_new, i32, "cu_new", (B + 1,), dev), _arg(kv_lens, i32, "kv_lens", (B,), dev), _arg(O, bf, "O", Q.shape, dev),
-        None if LSE is None else _arg(LSE, torch.float32, "LSE", Q.shape[:2], dev), _raw_stream(stream, dev))
+        h, B, Q.shape[0], _arg(Q, bf, "Q", dev), _arg(K_cache, bf, "K_cache", dev),
+        _arg(V_cache, bf, "V_cache", dev, K_cache.shape), _arg(block_table, i32, "block_table", dev),
+        _arg(cu_new, i32, "cu_new", dev, (B + 1,)), _arg(kv_lens, i32, "kv_lens", dev, (B,)), _arg(O, bf, "O", dev, Q.shape),
+        None if LSE is None else _arg(LSE, torch.float32, "LSE", dev, Q.shape[:2]), _raw_stream(stream, dev))
     if st != SAS_OK:
         _ccheck(st, h, "sas_chunk_attention")
 
 
-def _prob_rows(t, name, rows, V, dev):
+def _prob_rows(t, name, rows, dev, V):
     """Address and row stride of an fp32 [rows, V] tensor with contiguous columns."""
-    at = _rows(t, torch.float32, name, (rows, V), dev)
+    at = _rows(t, torch.float32, name, dev, (rows, V))
     st = t.stride()
     if V > 1 and st[1] != 1:
         raise ValueError(f"{name} must have contiguous columns")
@@ -803,15 +816,15 @@ def _prob_rows(t, name, rows, V, dev):
 def sas_chunk_verify(h, tokens, cu_draft, target, draft, u, noise, accepted, out_tokens, stream=None):
     """draft None: the drafts were certain."""
     i32, B, n, V, dev = torch.int32, cu_draft.shape[0] - 1, tokens.shape[0], target.shape[1], target.get_device()
-    p, ldp = _prob_rows(target, "target", n + B, V, dev)
-    q, ldq = (None, V) if draft is None else _prob_rows(draft, "draft", n, V, dev)
-    e, lde = _prob_rows(noise, "noise", B, V, dev)
+    p, ldp = _prob_rows(target, "target", n + B, dev, V)
+    q, ldq = (None, V) if draft is None else _prob_rows(draft, "draft", n, dev, V)
+    e, lde = _prob_rows(noise, "noise", B, dev, V)
     if out_tokens.dim() != 2 or out_tokens.shape[0] != B or out_tokens.shape[1] < 1:
         raise ValueError(f"out_tokens must have {B} rows and at least one column")
     st = lib().sas_chunk_verify(
-        h, B, n, out_tokens.shape[1] - 1, V, _arg(tokens, i32, "tokens", (n,), dev), _arg(cu_draft, i32, "cu_draft", None, dev), p,
-        ldp, q, ldq, _arg(u, torch.float32, "u", (n,), dev), e, lde, _arg(accepted, i32, "accepted", (B,), dev),
-        _arg(out_tokens, i32, "out_tokens", None, dev), _raw_stream(stream, dev))
+        h, B, n, out_tokens.shape[1] - 1, V, _arg(tokens, i32, "tokens", dev, (n,)), _arg(cu_draft, i32, "cu_draft", dev, (B + 1,)), p,
+        ldp, q, ldq, _arg(u, torch.float32, "u", dev, (n,)), e, lde, _arg(accepted, i32, "accepted", dev, (B,)),
+        _arg(out_tokens, i32, "out_tokens", dev), _raw_stream(stream, dev))
     if st != SAS_OK:
         _ccheck(st, h, "sas_chunk_verify")
 
