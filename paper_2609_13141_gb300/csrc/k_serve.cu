@@ -20,6 +20,7 @@ constexpr int kStatusNoPages = 5;    // == SAS_ERR_OOM
 // tokens, the new pages and the requests.
 
 constexpr int kPlanThreads = 512;
+constexpr int kTokens = 4;   // of a thread
 
 // Exclusive sums over the block's threads of (x, y), and the totals.
 __device__ __forceinline__ void block_scan2(long long& x, int& y, long long& tx, int& ty) {
@@ -133,26 +134,58 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
         }
         a.block_table[static_cast<size_t>(b) * a.max_blocks + blk] = page;
     }
-    for (int i = at; i < a.T; i += step) {
-        int pos = -1;
-        long long slot = -1;
-        if (i < total) {
-            const int b = owner(cu, a.B, i);
-            const int s = __ldg(a.seq_lens + b);
-            pos = s + i - cu[b];
-            const int blk = pos >> 6, have = pages_held(a, b, s);
-            // a page of this call comes from the free list: its table entry may not be written yet
-            const int page = blk < have ? a.block_table[static_cast<size_t>(b) * a.max_blocks + blk]
-                                        : __ldg(a.free_pages + begin + off[b] + blk - have);
-            if (page < 0 || page >= a.num_pages) {
-                atomicExch(a.status, kStatusBadInput);
-                pos = -1;
-            } else {
-                slot = static_cast<long long>(page) * 64 + (pos & 63);
+    // kTokens neighbouring tokens a thread: one search, and a page looked up once, for most
+    const bool wide = ((reinterpret_cast<uintptr_t>(a.positions) | reinterpret_cast<uintptr_t>(a.slots)) & 15u) == 0;
+    for (long long i0 = static_cast<long long>(at) * kTokens; i0 < a.T; i0 += static_cast<long long>(step) * kTokens) {
+        int pos[kTokens];
+        long long slot[kTokens];
+        int b = i0 < total ? owner(cu, a.B, static_cast<int>(i0)) : 0, s = 0, have = 0, last = -1, page = -1;
+        bool fresh = true;
+#pragma unroll
+        for (int j = 0; j < kTokens; ++j) {
+            const int i = static_cast<int>(i0) + j;
+            pos[j] = -1;
+            slot[j] = -1;
+            if (i0 + j >= total) continue;
+            while (b + 1 < a.B && cu[b + 1] <= i) {
+                ++b;
+                fresh = true;
+            }
+            if (fresh) {
+                s = __ldg(a.seq_lens + b);
+                have = pages_held(a, b, s);
+                last = -1;
+                fresh = false;
+            }
+            const int p = s + i - cu[b], blk = p >> 6;
+            if (blk != last) {
+                // a page of this call comes from the free list: its table entry may not be written yet
+                page = blk < have ? a.block_table[static_cast<size_t>(b) * a.max_blocks + blk]
+                                  : __ldg(a.free_pages + begin + off[b] + blk - have);
+                last = blk;
+                if (page < 0 || page >= a.num_pages) {
+                    atomicExch(a.status, kStatusBadInput);
+                    page = -1;
+                }
+            }
+            if (page >= 0) {
+                pos[j] = p;
+                slot[j] = static_cast<long long>(page) * 64 + (p & 63);
             }
         }
-        a.positions[i] = pos;
-        a.slots[i] = slot;
+        if (wide && i0 + kTokens <= a.T) {
+            *reinterpret_cast<int4*>(a.positions + i0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+            *reinterpret_cast<longlong2*>(a.slots + i0) = make_longlong2(slot[0], slot[1]);
+            *reinterpret_cast<longlong2*>(a.slots + i0 + 2) = make_longlong2(slot[2], slot[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kTokens; ++j) {
+                if (i0 + j < a.T) {
+                    a.positions[i0 + j] = pos[j];
+                    a.slots[i0 + j] = slot[j];
+                }
+            }
+        }
     }
 }
 
@@ -368,8 +401,8 @@ cudaError_t plan_prepare(int max_seqs) {
 }
 
 cudaError_t launch_plan(const PlanArgs& a, const KernelEnv& env) {
-    const int most = device_sm_count();
-    const int need = (max(a.T, a.B) + kPlanThreads - 1) / kPlanThreads;
+    const int most = 2 * device_sm_count();
+    const int need = (max((a.T + kTokens - 1) / kTokens, a.B) + kPlanThreads - 1) / kPlanThreads;
     plan_kernel<<<need < most ? need : most, kPlanThreads, plan_smem(a.B), env.stream>>>(a);
     return cudaGetLastError();
 }

@@ -178,3 +178,23 @@ def test_held_pages_are_used_before_free_ones(seq, held, new):
         h = _t(held)
         ch.plan(_t(seq), _t(new), _t(free), _t([0]), tab, T, held_lens=h, out=p._replace(kv_lens=h))
     ch.close()
+
+
+@pytest.mark.parametrize("off", [0, 1, 2])
+def test_outputs_of_any_alignment(off):
+    # capacity and addresses that four-token stores do not fit, with a canary behind each output
+    seq, new, T = [60, 0, 130, 5], [7, 1, 66, 0], 77
+    need = sum(-(-(s + n) // 64) - -(-s // 64) for s, n in zip(seq, new))
+    table, free, P = _state(seq, 8, need)
+    ch = sas.SasChunk(4, 1, 1, 64, 8, P, T)
+    out = ch.plan_buffers(4, T, DEV)
+    pos = torch.full((T + off + 8,), 77, dtype=I32, device=DEV)
+    slots = torch.full((T + off + 8,), 77, dtype=torch.int64, device=DEV)
+    out = out._replace(positions=pos[off:off + T], slots=slots[off:off + T])
+    p = ch.plan(_t(seq), _t(new), _t(free), _t([0]), _t(table), T, out=out)
+    assert sas.sas_chunk_get_device_status(ch.h) == sas.SAS_OK
+    _, _, want_pos, want_slots, _, _ = S.plan(seq, new, free, 0, table, T)
+    assert p.positions.tolist() == want_pos and p.slots.tolist() == want_slots
+    assert bool((pos[:off] == 77).all()) and bool((pos[off + T:] == 77).all())
+    assert bool((slots[:off] == 77).all()) and bool((slots[off + T:] == 77).all())
+    ch.close()
