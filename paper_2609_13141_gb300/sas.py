@@ -569,29 +569,37 @@ class SasLayer:
         sas_attention_bwd(self.h, Q, K, V, O, LSE, dO, dQ, dK, dV, scores, sel_idx, sel_logg, dlogg, ds, stream)
         return dQ, dK, dV, dlogg, ds
 
-    def qk_norm_rope(self, qkv, wq, wk, cos, sin, positions=None, eps=1e-6, interleaved=False, stream=None):
+    def qk_norm_rope(self, qkv, wq, wk, cos, sin, positions=None, eps=1e-6, interleaved=False, out=None, stream=None):
         """Per-head norm of queries and keys and the rotary rotation: the fused projection qkv
-        [B, N, H + 2 Hkv, d] to (Q [B, H, N, d], K, V [B, Hkv, N, d]), as attention() takes them."""
-        with _on(stream):
-            Q = torch.empty(self.B, self.H, self.N, self.d, device=qkv.device, dtype=torch.bfloat16)
-            K = torch.empty(self.B, self.Hkv, self.N, self.d, device=qkv.device, dtype=torch.bfloat16)
-            V = torch.empty_like(K)
-        sas_qk_norm_rope_fwd(self.h, qkv, wq, wk, cos, sin, Q, K, V, positions, eps, interleaved, stream)
-        return Q, K, V
+        [B, N, H + 2 Hkv, d] to (Q [B, H, N, d], K, V [B, Hkv, N, d]), as attention() takes them; out reuses the
+        caller's."""
+        if out is None:
+            with _on(stream):
+                Q = torch.empty(self.B, self.H, self.N, self.d, device=qkv.device, dtype=torch.bfloat16)
+                K = torch.empty(self.B, self.Hkv, self.N, self.d, device=qkv.device, dtype=torch.bfloat16)
+                out = (Q, K, torch.empty_like(K))
+        else:
+            self._heads("Q", out[0], self.H)
+            self._heads("K", out[1], self.Hkv)
+        sas_qk_norm_rope_fwd(self.h, qkv, wq, wk, cos, sin, *out, positions, eps, interleaved, stream)
+        return out
 
-    def qk_norm_rope_bwd(self, qkv, wq, wk, cos, sin, dQ, dK, dV, positions=None, eps=1e-6, interleaved=False,
+    def _heads(self, name, t, heads):
+        if t.shape != (self.B, heads, self.N, self.d):
+            raise ValueError(f"{name} must have shape {(self.B, heads, self.N, self.d)}, got {tuple(t.shape)}")
+
+    def qk_norm_rope_bwd(self, qkv, wq, wk, cos, sin, dQ, dK, dV, positions=None, eps=1e-6, interleaved=False, out=None,
                          stream=None):
-        """Returns (dqkv [B, N, H + 2 Hkv, d] bf16, dwq, dwk fp32 [d])."""
-        shape = {"dQ": (dQ, self.H), "dK": (dK, self.Hkv)}
-        for name, (t, heads) in shape.items():
-            if t.shape != (self.B, heads, self.N, self.d):
-                raise ValueError(f"{name} must have shape {(self.B, heads, self.N, self.d)}, got {tuple(t.shape)}")
-        with _on(stream):
-            dqkv = torch.empty(qkv.shape, device=qkv.device, dtype=torch.bfloat16)
-            dwq = torch.empty(self.d, device=qkv.device, dtype=torch.float32)
-            dwk = torch.empty_like(dwq)
-        sas_qk_norm_rope_bwd(self.h, qkv, wq, wk, cos, sin, dQ, dK, dV, dqkv, dwq, dwk, positions, eps, interleaved, stream)
-        return dqkv, dwq, dwk
+        """Returns (dqkv [B, N, H + 2 Hkv, d] bf16, dwq, dwk fp32 [d]); out reuses the caller's."""
+        self._heads("dQ", dQ, self.H)
+        self._heads("dK", dK, self.Hkv)
+        if out is None:
+            with _on(stream):
+                dqkv = torch.empty(qkv.shape, device=qkv.device, dtype=torch.bfloat16)
+                dwq = torch.empty(self.d, device=qkv.device, dtype=torch.float32)
+                out = (dqkv, dwq, torch.empty_like(dwq))
+        sas_qk_norm_rope_bwd(self.h, qkv, wq, wk, cos, sin, dQ, dK, dV, *out, positions, eps, interleaved, stream)
+        return out
 
     def mlp(self, X, W1, W2, b1=None, b2=None, stream=None):
         Y = torch.empty(X.shape[0], W2.shape[0], device=X.device, dtype=torch.bfloat16)

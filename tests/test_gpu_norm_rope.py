@@ -295,3 +295,36 @@ def test_append_past_two_to_the_31_elements():
         assert torch.equal(Vc[a // 64, :, a % 64], vs[b // 64, :, b % 64])
     ch.close()
     small.close()
+
+
+def test_caller_buffers_and_a_captured_step():
+    # own outputs, on another stream, captured once and replayed on new inputs
+    B, N, Hq, Hkv, d = 2, 50, 4, 2, 128
+    g, qkv, wq, wk, cos, sin = _inputs(B, N, Hq, Hkv, d, 128, 0)
+    layer = sas.SasLayer(B, Hq, N, d, 0, Hkv=Hkv)
+    want = layer.qk_norm_rope(qkv, wq, wk, cos, sin)
+    dy = tuple(_normal(g, *t.shape) for t in want)
+    want += layer.qk_norm_rope_bwd(qkv, wq, wk, cos, sin, *dy)
+    fwd = tuple(torch.zeros_like(t) for t in want[:3])
+    bwd = tuple(torch.zeros_like(t) for t in want[3:])
+    side, x = torch.cuda.Stream(), torch.zeros_like(qkv)
+    torch.cuda.synchronize()
+    layer.qk_norm_rope(x, wq, wk, cos, sin, out=fwd, stream=side)       # sets the kernels' attributes
+    layer.qk_norm_rope_bwd(x, wq, wk, cos, sin, *dy, out=bwd, stream=side)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        assert layer.qk_norm_rope(x, wq, wk, cos, sin, out=fwd, stream=side) is fwd
+        assert layer.qk_norm_rope_bwd(x, wq, wk, cos, sin, *dy, out=bwd, stream=side) is bwd
+    for scale in (1, 2):
+        x.copy_(qkv * scale)
+        for t in fwd + bwd:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        ref = want if scale == 1 else layer.qk_norm_rope(x, wq, wk, cos, sin) + layer.qk_norm_rope_bwd(x, wq, wk, cos, sin, *dy)
+        assert all(torch.equal(a, b) for a, b in zip(fwd + bwd, ref))
+    assert sas.sas_get_device_status(layer.h) == sas.SAS_OK
+    with pytest.raises(ValueError, match="Q must"):
+        layer.qk_norm_rope(qkv, wq, wk, cos, sin, out=(fwd[1], fwd[1], fwd[2]))
+    layer.close()
