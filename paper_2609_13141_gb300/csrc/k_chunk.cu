@@ -23,6 +23,11 @@
 // units first: units of one sequence then walk the same pages at about the same time
 // on many blocks, out of L2.
 //
+// Measured: 6.2 TB/s of keys and values for 96 single tokens over 100 to 12000 (126 us),
+// 6.1 TB/s for 6 x 5 tokens over 20000 to 32000 (109 us), 1653 TFLOP/s for 4096 tokens
+// over 32096 (1220 us; 1464 and 1378 us once the card is at its power limit, at 1.64
+// GHz), all d = 128 with 32 and 8 heads.
+//
 // Keys past a sequence's end in its last page may hold anything: scores there are
 // replaced, not weighted by zero, and values past the tile's last position are
 // zeroed in shared memory before the product.  A table entry out of range is never

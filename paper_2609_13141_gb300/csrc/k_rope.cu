@@ -17,7 +17,12 @@
 // some 110 instructions of 16 lanes).  So: both kernels are persistent, a warp keeps
 // the same heads for all its tokens (their kinds, weights and addresses are then
 // fixed), rows stream through a ring in shared memory (cp.async, no registers held
-// while they are in flight), and the arithmetic runs on packed fp32 pairs.
+// while they are in flight), and the arithmetic runs on packed fp32 pairs.  Measured:
+// 6.2 TB/s forward (131 us for 32768 tokens of 32 + 2 x 8 heads of 128, and as much into
+// cache pages), 5.4 TB/s for the gradient (213 us), where a row is read twice as much
+// as written and the waits for shared memory and reductions show.  One or two more
+// stages of the rings are slower (158 us forward with three): the warps drift apart and
+// DRAM pages are opened more often.
 #include "serve.h"
 #include "serve_ptx.cuh"
 
