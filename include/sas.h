@@ -330,7 +330,8 @@ typedef struct {
  *              the device status word becomes SAS_ERR_INVALID_ARG           (in)
  *   Q, K, V    bf16 [B, H, N, d], [B, Hkv, N, d], [B, Hkv, N, d]           (out)
  * Packed-sequence handles (B = 1): give each token's position in its sequence.
- * Outputs must not overlap inputs. */
+ * Outputs must not overlap inputs.  One launch, no allocation, no synchronisation;
+ * the first call of a kind loads its kernel, so make it before a capture. */
 sas_status sas_qk_norm_rope_fwd(sas_handle* h, const sas_rope_config* rope, const void* qkv, int64_t ld,
                                 const void* wq, const void* wk, const float* cos, const float* sin,
                                 const int32_t* positions, void* Q, void* K, void* V, void* stream);
@@ -341,7 +342,7 @@ sas_status sas_qk_norm_rope_fwd(sas_handle* h, const sas_rope_config* rope, cons
  *   dQ, dK, dV  bf16, the layouts of Q, K, V                                (in)
  *   dqkv        bf16, the layout of qkv with row stride ld_d               (out)
  *   dwq, dwk    fp32 [d]; summed in a fixed order                          (out)
- * One launch, no allocation, no synchronisation. */
+ * One launch, as above. */
 sas_status sas_qk_norm_rope_bwd(sas_handle* h, const sas_rope_config* rope, const void* qkv, int64_t ld,
                                 const void* wq, const void* wk, const float* cos, const float* sin,
                                 const int32_t* positions, const void* dQ, const void* dK, const void* dV, void* dqkv,
@@ -596,7 +597,7 @@ int64_t sas_decode_launch_count(const sas_decode_handle* h);
 
 typedef struct {
     int32_t max_seqs;     /* sequences of a call, at most (1 .. 8192)                       */
-    int32_t Hq, Hkv;      /* query heads and KV heads; Hq / Hkv in {1, 2, 4, 8}             */
+    int32_t Hq, Hkv;      /* query heads (<= 65536) and KV heads; Hq / Hkv in {1, 2, 4, 8}   */
     int32_t d;            /* head dim, 64 or 128                                           */
     int32_t block;        /* tokens of a page; must be 64                                  */
     int32_t max_blocks;   /* block-table width, <= 32768                                   */
@@ -609,7 +610,8 @@ typedef struct sas_chunk_handle sas_chunk_handle;
 
 /* Validates cfg and allocates the handle's workspace on the current device (the
  * one its calls must run on): the attention's split results (40 MB at d = 128) and
- * small arrays.  Synchronous. */
+ * small arrays.  Calls on one handle share them and must not overlap on the GPU: one
+ * stream at a time, or streams ordered by events.  Synchronous. */
 sas_status sas_chunk_create(const sas_chunk_config* cfg, sas_chunk_handle** out);
 void sas_chunk_destroy(sas_chunk_handle* h);
 

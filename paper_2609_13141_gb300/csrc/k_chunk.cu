@@ -284,7 +284,12 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
     using C = Cfg<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     if ((smem_u32(smem) & 1023u) != 0) {
-        if (threadIdx.x == 0) atomicExch(a.status, kStatusLayout);
+        grid_dep_wait();
+        if (threadIdx.x == 0) {
+            atomicExch(a.status, kStatusLayout);
+            // no splits, rather than the last call's
+            a.splits[4 * blockIdx.x] = a.splits[4 * blockIdx.x + 2] = make_int4(0, 0, 0, 0);
+        }
         return;
     }
     Ctl& ctl = *reinterpret_cast<Ctl*>(smem + C::OFF_CTL);

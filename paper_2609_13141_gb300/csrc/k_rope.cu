@@ -516,6 +516,7 @@ const char* rope_check(int rot, int interleaved, int max_pos, float eps, long lo
     if (rot < 16 || rot > d || rot % 16 != 0) return "rot must be a multiple of 16 from 16 to d";
     if (interleaved != 0 && interleaved != 1) return "interleaved must be 0 or 1";
     if (max_pos < 1) return "max_pos must be positive";
+    if (heads * d > (1 << 30)) return "a token's heads must not exceed 2^30 elements";
     if (!(eps >= 0.f) || eps > 3.0e38f) return "eps must be finite and not negative";
     if (ld < heads * d || ld % 8 != 0) return "a token's row stride must hold all its heads and be a multiple of 8";
     return nullptr;
@@ -525,6 +526,19 @@ const char* rope_check(int rot, int interleaved, int max_pos, float eps, long lo
 bool rope_supported(const RopeArgs& a) { return a.T <= 0x7fffffffLL; }
 
 int rope_bwd_max_blocks() { return kBwdBlocks * device_sm_count(); }   // all resident
+
+cudaError_t rope_paged_prepare(int d) {
+    auto set = [](const void* f, int smem) { return ensure_smem_attr(f, smem, true); };
+    cudaError_t e = cudaSuccess;
+    if (d == 128) {
+        e = set(reinterpret_cast<const void*>(rope_fwd_kernel<128, true, true>), rope_fwd_smem<128>());
+        if (e == cudaSuccess) e = set(reinterpret_cast<const void*>(rope_fwd_kernel<128, false, true>), rope_fwd_smem<128>());
+    } else {
+        e = set(reinterpret_cast<const void*>(rope_fwd_kernel<64, true, true>), rope_fwd_smem<64>());
+        if (e == cudaSuccess) e = set(reinterpret_cast<const void*>(rope_fwd_kernel<64, false, true>), rope_fwd_smem<64>());
+    }
+    return e;
+}
 
 cudaError_t launch_rope_fwd(const RopeArgs& a, int d, const KernelEnv& env) {
     if (d == 128) return a.interleaved ? launch_any_fwd<128, true>(a, env) : launch_any_fwd<128, false>(a, env);

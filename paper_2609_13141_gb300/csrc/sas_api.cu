@@ -921,6 +921,7 @@ sas_status sas_qk_norm_rope_bwd(sas_handle* h, const sas_rope_config* rope, cons
     a.Q = static_cast<sas::bf16*>(const_cast<void*>(dQ));
     a.K = static_cast<sas::bf16*>(const_cast<void*>(dK));
     a.V = static_cast<sas::bf16*>(const_cast<void*>(dV));
+    if (dqkv == qkv) return fail(h, SAS_ERR_INVALID_ARG, "dqkv must not be qkv's memory");
     a.dqkv = static_cast<sas::bf16*>(dqkv); a.ld_d = ld_d; a.dwq = dwq; a.dwk = dwk;
     a.part = h->rope_part; a.counter = h->rope_count;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

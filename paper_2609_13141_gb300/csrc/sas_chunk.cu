@@ -139,7 +139,7 @@ sas_status sas_chunk_create(const sas_chunk_config* cfg, sas_chunk_handle** out)
     if (G != 1 && G != 2 && G != 4 && G != 8) return SAS_ERR_UNSUPPORTED;
     if (c.block != 64) return SAS_ERR_UNSUPPORTED;
     if (c.d != 64 && c.d != 128) return SAS_ERR_UNSUPPORTED;
-    if (c.max_seqs > 8192 || c.max_blocks > 32768 || c.max_tokens > (1 << 26)) return SAS_ERR_UNSUPPORTED;
+    if (c.Hq > 65536 || c.max_seqs > 8192 || c.max_blocks > 32768 || c.max_tokens > (1 << 26)) return SAS_ERR_UNSUPPORTED;
     if (!(c.sm_scale >= 0.f) || !std::isfinite(c.sm_scale)) return SAS_ERR_INVALID_ARG;
     // (page, KV head) pairs are TMA coordinates, one past the last included
     if (static_cast<long long>(c.num_pages) * c.Hkv > 0x7fffffffLL) return SAS_ERR_UNSUPPORTED;
@@ -168,6 +168,7 @@ sas_status sas_chunk_create(const sas_chunk_config* cfg, sas_chunk_handle** out)
     if (e == cudaSuccess) e = cudaMemset(h->status, 0, 16);
     // shared-memory limits now, so that a captured call sets nothing
     if (e == cudaSuccess) e = sas::plan_prepare(c.max_seqs);
+    if (e == cudaSuccess) e = sas::rope_paged_prepare(c.d);
     if (e == cudaSuccess) e = sas::chunk_attn_prepare(c.d);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) {

@@ -42,6 +42,7 @@ struct RopeArgs {
 const char* rope_check(int rot, int interleaved, int max_pos, float eps, long long heads, int d, long long ld);
 bool rope_supported(const RopeArgs& a);   // the kernels can count this many tokens
 int rope_bwd_max_blocks();
+cudaError_t rope_paged_prepare(int d);    // shared-memory limit of the form into cache pages (before any capture)
 cudaError_t launch_rope_fwd(const RopeArgs& a, int d, const KernelEnv& env);
 cudaError_t launch_rope_bwd(const RopeArgs& a, int d, const KernelEnv& env);
 

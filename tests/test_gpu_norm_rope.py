@@ -210,6 +210,9 @@ def test_refusals():
         layer.qk_norm_rope(qkv, wq.float(), wk, cos, sin)
     with pytest.raises(ValueError, match="dQ"):
         layer.qk_norm_rope_bwd(*good, qkv, qkv, qkv)
+    dq, dk = torch.zeros(B, Hq, N, d, device=DEV, dtype=torch.bfloat16), torch.zeros(B, Hkv, N, d, device=DEV, dtype=torch.bfloat16)
+    with pytest.raises(sas.SasError, match="dqkv"):
+        layer.qk_norm_rope_bwd(*good, dq, dk, dk, out=(qkv, torch.zeros(d, device=DEV), torch.zeros(d, device=DEV)))
     assert sas.sas_launch_count(layer.h) == before
     layer.close()
 

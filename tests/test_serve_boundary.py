@@ -20,6 +20,7 @@ def lib():
     (dict(Hq=12, Hkv=8), sas.SAS_ERR_INVALID_ARG),
     (dict(Hq=6, Hkv=2), sas.SAS_ERR_UNSUPPORTED),
     (dict(Hkv=0), sas.SAS_ERR_INVALID_ARG),
+    (dict(Hq=131072, Hkv=65536), sas.SAS_ERR_UNSUPPORTED),
     (dict(d=96), sas.SAS_ERR_UNSUPPORTED),
     (dict(block=32), sas.SAS_ERR_UNSUPPORTED),
     (dict(max_blocks=0), sas.SAS_ERR_INVALID_ARG),
