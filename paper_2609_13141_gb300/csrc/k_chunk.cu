@@ -50,7 +50,7 @@ constexpr int kItemSlots = 4;     // work items in flight between warp 0 and the
 constexpr int kItemReaders = 7;   // V producer, two MMA issuers, four softmax warps
 constexpr int kStatusBadInput = 1;
 constexpr int kStatusLayout = 3;
-constexpr int kUnitCost = 3;      // what a unit costs beside its pages (its Q tile, its epilogue), in pages
+constexpr int kUnitCost = 4;      // what a unit costs beside its pages (its Q tile, its epilogue: 2 to 3 us), in pages
 constexpr int kSnap = 4;          // pages: ranges do not cut this close to a unit's ends
 constexpr int kMinShare = 4;      // pages of a block's range, at least
 constexpr int kJoinThreads = 512;
