@@ -69,26 +69,24 @@ struct Seq {
         L = __ldg(a.kv_lens + b);
         if (L < n || L > 64LL * a.max_blocks) n = 0;
     }
-    __device__ __forceinline__ int tiles(int R) const { return (n + R - 1) / R; }
+    // R = 2^rl tokens a tile
+    __device__ __forceinline__ int tiles(int rl) const { return (n + (1 << rl) - 1) >> rl; }
     // pages of tile t
-    __device__ __forceinline__ int pages(int t, int R) const { return ((L - n + min(n, (t + 1) * R) - 1) >> 6) + 1; }
-    // cost of tiles 0 .. m - 1, all full: their pages are the sum over t = 1 .. m of floor((p + t R) / 64)
-    // + 1, p = L - n - 1
-    __device__ __forceinline__ long long before(int m, int R) const {
+    __device__ __forceinline__ int pages(int t, int rl) const { return ((L - n + min(n, (t + 1) << rl) - 1) >> 6) + 1; }
+    // Cost of tiles 0 .. m - 1, all full: their pages are the sum over t = 1 .. m of floor((p + t R) / 64) + 1
+    // with p = L - n - 1 = 64 q + r.  For R <= 64 = k R the floor is q + floor((floor(r / R) + t) / k), and sums
+    // of floor(u / k) over u = 0 .. x are k y (y - 1) / 2 + y (x % k + 1), y = floor(x / k).
+    __device__ __forceinline__ long long before(int m, int rl) const {
         const int p = L - n - 1;
-        const long long M = m;
-        if (R >= 64) return M * (p >> 6) + (R >> 6) * (M * (M + 1) / 2) + M * (1 + kUnitCost);
-        const int k = 64 / R;   // tiles of a page's length: t = k s + j gives floor((p + j R) / 64) + s
-        long long sum = M * (1 + kUnitCost);
-        for (int j = 0; j < k; ++j) {
-            const long long cnt = j == 0 ? m / k : (m >= j ? (m - j) / k + 1 : 0);
-            sum += cnt * ((p + j * R) >> 6) + (j == 0 ? cnt * (cnt + 1) : cnt * (cnt - 1)) / 2;
-        }
-        return sum;
+        const long long flat = static_cast<long long>(m) * ((p >> 6) + 1 + kUnitCost);
+        if (rl == 7) return flat + static_cast<long long>(m) * (m + 1);
+        const int kl = 6 - rl, x = ((p & 63) >> rl) + m;
+        const long long y = x >> kl;
+        return flat + ((y * (y - 1) / 2) << kl) + y * ((x & ((1 << kl) - 1)) + 1);
     }
-    __device__ __forceinline__ long long all(int R) const {
-        const int nt = tiles(R);
-        return nt == 0 ? 0 : before(nt - 1, R) + pages(nt - 1, R) + kUnitCost;
+    __device__ __forceinline__ long long all(int rl) const {
+        const int nt = tiles(rl);
+        return nt <= 0 ? 0 : before(nt - 1, rl) + pages(nt - 1, rl) + kUnitCost;
     }
 };
 
@@ -97,29 +95,29 @@ struct Bound {
     int seq, tile, head, page, nb;
 };
 
-// Scratch of the block that finds its range.
+// Where a block's two boundaries are: a sequence, and the cost before them in it.
 struct Shares {
-    long long sum[kThreads / 32];
-    int units[kThreads / 32];
-    Bound at[2];
+    long long sum[kThreads / 32], off[2];
+    int tiles[kThreads / 32], seq[2];
+    bool last[2];   // the end of everything
 };
 
-// The block's range [at[0], at[1]); false if it has none.  All threads call it.  Every
-// block sums up all sequences itself (12 bytes each, from L2): no launch before this
-// one, nothing to wait for.
-__device__ __forceinline__ bool find_range(const ChunkArgs& a, int R, Shares& sh) {
+// Finds the sequences of the block's range; false if it has none.  All threads call it.
+// Every block sums up all sequences itself (12 bytes each, from L2): no launch before
+// this one, nothing to wait for.
+__device__ __forceinline__ bool find_range(const ChunkArgs& a, int rl, Shares& sh) {
     const int t = threadIdx.x, lane = lane_id(), warp = warp_id();
     const int per = (a.B + kThreads - 1) / kThreads;   // neighbouring sequences of a thread
     const int b0 = min(a.B, t * per), b1 = min(a.B, b0 + per);
     long long cost = 0;
-    int units = 0, bad = 0;
+    int tiles = 0, bad = 0;
     for (int b = b0; b < b1; ++b) {
         const int c0 = __ldg(a.cu + b), c1 = __ldg(a.cu + b + 1);
         const Seq x(a, b);
         bad |= c0 < 0 || c1 < c0 || c1 > a.T;
         if (x.n != c1 - c0 && blockIdx.x == 0) atomicExch(a.status, kStatusBadInput);
-        cost += x.all(R);
-        units += x.tiles(R);
+        cost += x.all(rl);
+        tiles += x.tiles(rl);
     }
     long long inc = cost;
 #pragma unroll
@@ -127,34 +125,34 @@ __device__ __forceinline__ bool find_range(const ChunkArgs& a, int R, Shares& sh
         const long long x = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += x;
     }
-    units = __reduce_add_sync(0xffffffffu, units);
+    tiles = __reduce_add_sync(0xffffffffu, tiles);
     if (lane == 31) {
         sh.sum[warp] = inc;
-        sh.units[warp] = units;
+        sh.tiles[warp] = tiles;
     }
     if (__syncthreads_or(bad)) {
         if (blockIdx.x == 0 && t == 0) atomicExch(a.status, kStatusBadInput);
         return false;
     }
-    long long base = 0, total = 0, all_units = 0;
+    long long base = 0, total = 0, units = 0;
 #pragma unroll
     for (int w = 0; w < kThreads / 32; ++w) {
         if (w == warp) base = total;
         total += sh.sum[w];
-        all_units += sh.units[w];
+        units += sh.tiles[w];
     }
     total *= a.Hkv;
-    all_units *= a.Hkv;
+    units *= a.Hkv;
     if (total == 0) return false;
     // as many ranges as blocks, fewer where they would be under kMinShare pages or a unit
-    const long long want = max(all_units, (total - all_units * kUnitCost + kMinShare - 1) / kMinShare);
+    const long long want = max(units, (total - units * kUnitCost + kMinShare - 1) / kMinShare);
     const int ranges = static_cast<int>(min(static_cast<long long>(gridDim.x), want));
     if (static_cast<int>(blockIdx.x) >= ranges) return false;
     // boundary k at k share + min(k, rest): ranges differ by one at most
-    const long long share = total / ranges;
+    const long long share = (total >> 32) == 0 ? static_cast<unsigned>(total) / static_cast<unsigned>(ranges) : total / ranges;
     const int rest = static_cast<int>(total - share * ranges);
     const long long lo = (base + inc - cost) * a.Hkv, hi = (base + inc) * a.Hkv;   // this thread's sequences
-#pragma unroll 1
+#pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int c = blockIdx.x + k;
         const long long p = c * share + min(c, rest);
@@ -163,33 +161,51 @@ __device__ __forceinline__ bool find_range(const ChunkArgs& a, int R, Shares& sh
         if (q < lo || q >= hi) continue;
         long long off = q - lo;
         int b = b0;
-        Seq x(a, b);
-        while (b + 1 < b1) {
-            const long long y = x.all(R) * a.Hkv;
+        for (; b + 1 < b1; ++b) {
+            const long long y = Seq(a, b).all(rl) * a.Hkv;
             if (off < y) break;
             off -= y;
-            x = Seq(a, ++b);
         }
-        int tl = 0, th = x.tiles(R);   // the last tile that starts at or before off
-        while (th - tl > 1) {
-            const int mid = (tl + th) >> 1;
-            if (x.before(mid, R) * a.Hkv <= off) tl = mid;
-            else th = mid;
-        }
-        off -= x.before(tl, R) * a.Hkv;
-        // off < Hkv (pages + kUnitCost) < 2^32
-        Bound y;
-        y.seq = b;
-        y.tile = tl;
-        y.nb = x.pages(tl, R);
-        y.head = static_cast<unsigned>(off) / static_cast<unsigned>(y.nb + kUnitCost);
-        const int page = static_cast<int>(off - static_cast<long long>(y.head) * (y.nb + kUnitCost)) - kUnitCost;
-        y.page = page < kSnap ? 0 : (y.nb - page < kSnap ? y.nb : page);
-        if (p >= total) y.page = y.nb;
-        sh.at[k] = y;
+        sh.off[k] = off;
+        sh.seq[k] = b;
+        sh.last[k] = p >= total;
     }
     __syncthreads();
     return true;
+}
+
+// The boundaries themselves, by one warp: a half-warp searches the tile of one, 16 tiles
+// at a time.
+__device__ __forceinline__ void find_bounds(const ChunkArgs& a, int rl, const Shares& sh, Bound& from, Bound& to) {
+    const int lane = lane_id(), k = lane >> 4, i = lane & 15;
+    long long off = sh.off[k];
+    const Seq x(a, sh.seq[k]);
+    int tl = 0, th = x.tiles(rl), step;   // the last tile that starts at or before off is in [tl, th)
+    do {
+        step = (th - tl + 15) >> 4;
+        const int m = tl + i * step;
+        const unsigned at_or_before = __ballot_sync(0xffffffffu, m < th && x.before(m, rl) * a.Hkv <= off) >> (16 * k) & 0xffffu;
+        tl += (__popc(at_or_before) - 1) * step;
+        th = min(th, tl + step);
+    } while (__any_sync(0xffffffffu, step > 1));
+    off -= x.before(tl, rl) * a.Hkv;   // < Hkv (pages + kUnitCost) < 2^32
+    Bound y;
+    y.seq = sh.seq[k];
+    y.tile = tl;
+    y.nb = x.pages(tl, rl);
+    y.head = static_cast<unsigned>(off) / static_cast<unsigned>(y.nb + kUnitCost);
+    const int page = static_cast<int>(off - static_cast<long long>(y.head) * (y.nb + kUnitCost)) - kUnitCost;
+    y.page = page < kSnap ? 0 : (y.nb - page < kSnap ? y.nb : page);
+    if (sh.last[k]) y.page = y.nb;
+    auto get = [&](Bound& z, int src) {
+        z.seq = __shfl_sync(0xffffffffu, y.seq, src);
+        z.tile = __shfl_sync(0xffffffffu, y.tile, src);
+        z.head = __shfl_sync(0xffffffffu, y.head, src);
+        z.page = __shfl_sync(0xffffffffu, y.page, src);
+        z.nb = __shfl_sync(0xffffffffu, y.nb, src);
+    };
+    get(from, 0);
+    get(to, 16);
 }
 
 // ------------------------------------------------------------------ attention
@@ -321,8 +337,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
     const WaitCtl wc{&ctl.abort_flag, a.status, limit};
     Shares& sh = *reinterpret_cast<Shares*>(smem + C::OFF_CTL + 512);
     grid_dep_wait();   // whatever the stream ran before: lengths, table, cache
-    const int R = kBM / a.G;
-    const bool any = find_range(a, R, sh);
+    const int rl = 31 - __clz(kBM / a.G), R = 1 << rl;   // tokens of a tile (G is 1, 2, 4 or 8)
+    const bool any = find_range(a, rl, sh);
     grid_dep_launch();   // the join's blocks may take the places that open up (they wait for this grid's end)
 
     // Every role walks the same items and counts pages over all of them (g): ring
@@ -332,7 +348,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
         if (warp == 0) {
             // ---------------- items and K pages
             if (lane == 0) tma_prefetch_desc(&mapK);
-            const Bound from = sh.at[0], to = sh.at[1];
+            Bound from = {}, to = {};
+            if (any) find_bounds(a, rl, sh, from, to);
             int seq = from.seq, tile = from.tile, head = from.head;   // the unit to look at next
             bool more = any, first = true;
             int late_lo = 0, late_hi = 0;   // the split of the first unit, left for the end
@@ -345,7 +362,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 x.blk0 = x.blk1 = 0;
                 while (more && x.head < 0) {
                     const Seq q(a, seq);
-                    const int nb = q.pages(tile, R);
+                    const int nb = q.pages(tile, rl);
                     const bool last = seq == to.seq && tile == to.tile && head == to.head;
                     const int lo = first ? from.page : 0, hi = last ? to.page : nb;
                     if (first && lo < hi && (lo > 0 || hi < nb)) {
@@ -359,7 +376,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                     more = !last;
                     if (more && ++head == a.Hkv) {
                         head = 0;
-                        if (++tile >= q.tiles(R)) {
+                        if (++tile >= q.tiles(rl)) {
                             // the next sequence with new tokens; the range's end lies in one
                             tile = 0;
                             for (int b = seq + 1;; b += 32) {
