@@ -90,9 +90,16 @@ struct Seq {
     }
 };
 
-// A boundary between two ranges: page `page` of unit (seq, tile, head) of nb pages.
+// A boundary between two ranges: page `page` of unit (seq, tile, head) of nb pages; `at`
+// is the unit's cost before it, of nb + kUnitCost, where the ranges cut it before kSnap.
 struct Bound {
-    int seq, tile, head, page, nb;
+    int seq, tile, head, page, nb, at;
+};
+
+// How everything is cut: boundary k is at cost k share + min(k, rest).
+struct Cut {
+    long long share;
+    int rest, ranges;
 };
 
 // Where a block's two boundaries are: a sequence, and the cost before them in it.
@@ -100,6 +107,7 @@ struct Shares {
     long long sum[kThreads / 32], off[2];
     int tiles[kThreads / 32], seq[2];
     bool last[2];   // the end of everything
+    Cut cut;
 };
 
 // Finds the sequences of the block's range; false if it has none.  All threads call it.
@@ -148,9 +156,10 @@ __device__ __forceinline__ bool find_range(const ChunkArgs& a, int rl, Shares& s
     const long long want = max(units, (total - units * kUnitCost + kMinShare - 1) / kMinShare);
     const int ranges = static_cast<int>(min(static_cast<long long>(gridDim.x), want));
     if (static_cast<int>(blockIdx.x) >= ranges) return false;
-    // boundary k at k share + min(k, rest): ranges differ by one at most
+    // ranges differ by one at most
     const long long share = (total >> 32) == 0 ? static_cast<unsigned>(total) / static_cast<unsigned>(ranges) : total / ranges;
     const int rest = static_cast<int>(total - share * ranges);
+    if (t == 0) sh.cut = Cut{share, rest, ranges};
     const long long lo = (base + inc - cost) * a.Hkv, hi = (base + inc) * a.Hkv;   // this thread's sequences
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -194,7 +203,8 @@ __device__ __forceinline__ void find_bounds(const ChunkArgs& a, int rl, const Sh
     y.tile = tl;
     y.nb = x.pages(tl, rl);
     y.head = static_cast<unsigned>(off) / static_cast<unsigned>(y.nb + kUnitCost);
-    const int page = static_cast<int>(off - static_cast<long long>(y.head) * (y.nb + kUnitCost)) - kUnitCost;
+    y.at = static_cast<int>(off - static_cast<long long>(y.head) * (y.nb + kUnitCost));
+    const int page = y.at - kUnitCost;
     y.page = page < kSnap ? 0 : (y.nb - page < kSnap ? y.nb : page);
     if (sh.last[k]) y.page = y.nb;
     auto get = [&](Bound& z, int src) {
@@ -203,6 +213,7 @@ __device__ __forceinline__ void find_bounds(const ChunkArgs& a, int rl, const Sh
         z.head = __shfl_sync(0xffffffffu, y.head, src);
         z.page = __shfl_sync(0xffffffffu, y.page, src);
         z.nb = __shfl_sync(0xffffffffu, y.nb, src);
+        z.at = __shfl_sync(0xffffffffu, y.at, src);
     };
     get(from, 0);
     get(to, 16);
@@ -303,8 +314,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
         grid_dep_wait();
         if (threadIdx.x == 0) {
             atomicExch(a.status, kStatusLayout);
-            // no splits, rather than the last call's
-            a.splits[4 * blockIdx.x] = a.splits[4 * blockIdx.x + 2] = make_int4(0, 0, 0, 0);
+            a.joins[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
         }
         return;
     }
@@ -353,7 +363,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
             int seq = from.seq, tile = from.tile, head = from.head;   // the unit to look at next
             bool more = any, first = true;
             int late_lo = 0, late_hi = 0;   // the split of the first unit, left for the end
-            unsigned used = 0;              // partial results written: slots 2 block + 0, + 1
             int g = 0;
             bool ok = true;
             for (int r = 0; ok; ++r) {
@@ -405,11 +414,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
 #pragma unroll
                         for (int h = 0; h < D / 64; ++h) tma_prefetch_3d(&mapQ, h * 64, x.head * a.G, x.tok0);
                     }
-                    if (x.part >= 0 && x.head >= 0) {   // what the join has to know
-                        a.splits[2 * x.part] = make_int4(x.head, x.tok0, x.ntok, 1);
-                        a.splits[2 * x.part + 1] = make_int4(x.blk0, x.blk1, x.nb, 0);
-                        used |= 1u << (x.part & 1);
-                    }
                 }
                 __syncwarp();
                 if (x.head < 0) break;
@@ -429,9 +433,26 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                     __syncwarp();
                 }
             }
+            // off the block's critical path: the unit it begins and does not end, for the join (the boundaries
+            // once more, rather than registers held all the way)
+            if (any) find_bounds(a, rl, sh, from, to);
             if (lane == 0) {
-                for (int k = 0; k < 2; ++k)
-                    if (!((used >> k) & 1u)) a.splits[2 * (2 * blockIdx.x + k)] = make_int4(0, 0, 0, 0);
+                const Cut cut = sh.cut;
+                const bool alone = from.seq == to.seq && from.tile == to.tile && from.head == to.head;
+                int4 y = make_int4(0, 0, 0, 0);
+                if (any && to.page > 0 && to.page < to.nb && !(alone && from.page > 0)) {
+                    // it ends at the first boundary within kSnap of its end, a cost of `left` further on;
+                    // the first `longer` ranges from here have one more than the others
+                    const int left = to.nb + kUnitCost - kSnap + 1 - to.at, here = blockIdx.x + 1;
+                    const int share = static_cast<int>(min(cut.share, 1LL << 30)), longer = max(0, cut.rest - here);
+                    const long long reach = static_cast<long long>(share + 1) * longer;
+                    const int further = left <= reach ? (left + share) / (share + 1)
+                                                      : longer + (left - static_cast<int>(reach) + share - 1) / share;
+                    const Seq q(a, to.seq);
+                    y = make_int4(1 + min(further, cut.ranges - here), 2 * blockIdx.x + (alone ? 0 : 1), to.head, q.c0 + to.tile * R);
+                    a.joins[2 * blockIdx.x + 1] = make_int4(min(R, q.n - to.tile * R), 0, 0, 0);
+                }
+                a.joins[2 * blockIdx.x] = y;
             }
             if (!ok && lane == 0) {   // the last KST loads may be in flight
                 for (int q = g - 1; q >= 0 && q >= g - C::KST; --q)
@@ -770,52 +791,38 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
 
 // ------------------------------------------------------------------ join
 
-// Block c joins the unit whose first split is block c's of the attention: that split
-// and the following blocks' first ones, up to the unit's last page.  Threads are (row,
-// columns, share of the splits): few rows leave many threads for the splits of a row.
-// Latency-bound: what can be loaded without knowing the rest is loaded together, and
-// two blocks fit a multiprocessor, so that all run at once.
+// Block c joins the unit that block c of the attention begins and does not end: that
+// split and the following blocks' first ones, up to the unit's last page.  Threads are
+// (row, columns, share of the splits), each a power of two: few rows leave many threads
+// for the splits of a row.  Latency-bound: a thread's loads are in flight together, and
+// two blocks fit a multiprocessor, so that all run at once.  (A join that finds its
+// splits itself before the wait saves one load's latency, and takes more from the
+// attention blocks still at work: 117 against 113 us for a mixed batch at d = 128.)
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads, 2) chunk_join_kernel(ChunkArgs a) {
     constexpr int QUADS = D / 4;      // of columns
     constexpr int QB = 2, U = 4;      // quads and splits of a thread in flight together
     __shared__ float top[kJoinThreads], len[kJoinThreads];
     __shared__ float4 part[kJoinThreads];
-    __shared__ int ends;
     const int t = threadIdx.x, c = blockIdx.x;
-    if (t == 0) ends = a.blocks;
-    grid_dep_wait();   // the splits
-    const int4 u1 = a.splits[4 * c + 2], u0 = a.splits[4 * c], v0 = a.splits[4 * c + 1];
-    int4 w = make_int4(0, 0, 0, 0), wv = w;
-    if (c + 1 + t < a.blocks) {
-        w = a.splits[4 * (c + 1 + t)];
-        wv = a.splits[4 * (c + 1 + t) + 1];
-    }
-    const bool second = u1.w != 0;
-    if (!second && (u0.w == 0 || v0.x != 0)) return;   // no unit starts here
-    const int4 u = second ? u1 : u0;
-    __syncthreads();
-    // the unit ends in the first following block whose first split reaches its unit's end
-    if (w.w != 0 && wv.y == wv.z) atomicMin(&ends, c + 1 + t);
-    for (int k = c + 1 + t + kJoinThreads; k < a.blocks; k += kJoinThreads) {
-        const int4 y = a.splits[4 * k + 1];
-        if (a.splits[4 * k].w != 0 && y.y == y.z) atomicMin(&ends, k);
-    }
-    __syncthreads();
-    const int ns = ends < a.blocks ? ends - c + 1 : 1, rows = u.z * a.G;
+    const int gl = 31 - __clz(a.G);   // G = 2^gl heads
+    grid_dep_wait();                  // the splits
+    const int4 u = __ldcg(a.joins + 2 * c), v = __ldcg(a.joins + 2 * c + 1);
+    const int ns = u.x, rows = v.x << gl;
+    if (ns == 0) return;
     // split s: the first in its slot, the others in slot 0 of the following blocks
-    const int first = 2 * c + (second ? 1 : 0);
-    auto slot = [&](int s) { return static_cast<size_t>(s == 0 ? first : 2 * (c + s)); };
-    int rp = 4;
-    while (rp < rows) rp *= 2;                          // rows, to a power of two
-    const int groups = min(QUADS, kJoinThreads / rp);   // column groups, of `per` quads each
-    const int per = QUADS / groups, span = rp * groups;
-    const int shares = kJoinThreads / span;             // of the splits; more than one only where per = 1
-    const int row = t % rp, cg = t / rp % groups, mine = t / span;
+    auto slot = [&](int s) { return static_cast<size_t>(s == 0 ? u.y : 2 * (c + s)); };
+    constexpr int QL = D == 128 ? 5 : 4, TL = 9;
+    static_assert(QUADS == 1 << QL && kJoinThreads == 1 << TL, "powers of two");
+    const int rpl = max(2, 32 - __clz(rows - 1));       // rows, to a power of two (a clz of 0 is 32)
+    const int groupl = min(QL, TL - rpl);               // column groups, of `per` quads each
+    const int per = QUADS >> groupl, spanl = rpl + groupl, span = 1 << spanl;
+    const int shares = kJoinThreads >> spanl;           // of the splits; more than one only where per = 1
+    const int row = t & ((1 << rpl) - 1), cg = t >> rpl & ((1 << groupl) - 1), mine = t >> spanl;
     const bool live = row < rows;
     const int at = live ? row : 0;
-    const int tok = at / a.G, h = at - tok * a.G;
-    const size_t orow = (static_cast<size_t>(u.y) + tok) * a.Hq + static_cast<size_t>(u.x) * a.G + h;
+    const int tok = at >> gl, h = at & (a.G - 1);
+    const size_t orow = (static_cast<size_t>(u.w) + tok) * a.Hq + static_cast<size_t>(u.z) * a.G + h;
     const float4* const po = reinterpret_cast<const float4*>(a.part_o) + at;
     for (int q0 = 0; q0 < per; q0 += QB) {
         const int quad = cg * per + q0;

@@ -27,7 +27,7 @@ struct sas_chunk_handle {
     float sm_scale = 0.f;
     int blocks = 0;
     // workspace
-    int4* splits = nullptr;
+    int4* joins = nullptr;
     float* part_o = nullptr;
     float2* part_ml = nullptr;
     unsigned long long* vkey = nullptr;
@@ -157,7 +157,7 @@ sas_status sas_chunk_create(const sas_chunk_config* cfg, sas_chunk_handle** out)
     h->blocks = sas::chunk_blocks();
     h->sm_scale = c.sm_scale > 0.f ? c.sm_scale : 1.0f / std::sqrt(static_cast<float>(c.d));
     const size_t parts = 2 * static_cast<size_t>(h->blocks);
-    cudaError_t e = calloc_dev(&h->splits, 2 * parts);
+    cudaError_t e = calloc_dev(&h->joins, parts);
     if (e == cudaSuccess) e = calloc_dev(&h->part_o, parts * 128 * c.d);
     if (e == cudaSuccess) e = calloc_dev(&h->part_ml, parts * 128);
     if (e == cudaSuccess) e = calloc_dev(&h->vkey, c.max_seqs);
@@ -183,7 +183,7 @@ sas_status sas_chunk_create(const sas_chunk_config* cfg, sas_chunk_handle** out)
 void sas_chunk_destroy(sas_chunk_handle* h) {
     if (h == nullptr) return;
     cudaDeviceSynchronize();
-    cudaFree(h->splits);
+    cudaFree(h->joins);
     cudaFree(h->part_o);
     cudaFree(h->part_ml);
     cudaFree(h->vkey);
@@ -281,7 +281,7 @@ sas_status sas_chunk_attention(sas_chunk_handle* h, int32_t num_seqs, int32_t T,
         a.K_cache = static_cast<const sas::bf16*>(K_cache); a.V_cache = static_cast<const sas::bf16*>(V_cache);
         a.block_table = block_table; a.cu = cu_new; a.kv_lens = kv_lens;
         a.O = static_cast<sas::bf16*>(O); a.LSE = LSE;
-        a.blocks = h->blocks; a.splits = h->splits; a.part_o = h->part_o; a.part_ml = h->part_ml;
+        a.blocks = h->blocks; a.joins = h->joins; a.part_o = h->part_o; a.part_ml = h->part_ml;
         a.status = h->status;
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         const sas::KernelEnv env{s, h->status, h->limit};

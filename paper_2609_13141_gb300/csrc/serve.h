@@ -99,7 +99,7 @@ struct ChunkArgs {
     float* LSE;                 // [T][Hq] or null
     // workspace
     int blocks;                 // chunk_blocks()
-    int4* splits;               // [2 blocks][2] {KV group, first token, tokens, used}, {first page, end page, unit's pages, 0}
+    int4* joins;                // [blocks][2] {splits (0: nothing to join), first one, KV group, first token}, {tokens}
     float* part_o;              // [2 blocks][d / 4][128][4]
     float2* part_ml;            // [2 blocks][128] (max, sum)
     int* status;
