@@ -433,24 +433,27 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                     __syncwarp();
                 }
             }
-            // off the block's critical path: the unit it begins and does not end, for the join (the boundaries
-            // once more, rather than registers held all the way)
+            // off the block's critical path: what it has to join, if its range ends inside a unit (the
+            // boundaries once more, rather than registers held all the way)
             if (any) find_bounds(a, rl, sh, from, to);
             if (lane == 0) {
-                const Cut cut = sh.cut;
-                const bool alone = from.seq == to.seq && from.tile == to.tile && from.head == to.head;
                 int4 y = make_int4(0, 0, 0, 0);
-                if (any && to.page > 0 && to.page < to.nb && !(alone && from.page > 0)) {
-                    // it ends at the first boundary within kSnap of its end, a cost of `left` further on;
-                    // the first `longer` ranges from here have one more than the others
-                    const int left = to.nb + kUnitCost - kSnap + 1 - to.at, here = blockIdx.x + 1;
-                    const int share = static_cast<int>(min(cut.share, 1LL << 30)), longer = max(0, cut.rest - here);
-                    const long long reach = static_cast<long long>(share + 1) * longer;
-                    const int further = left <= reach ? (left + share) / (share + 1)
-                                                      : longer + (left - static_cast<int>(reach) + share - 1) / share;
+                if (any && to.page > 0 && to.page < to.nb) {
+                    const long long share = sh.cut.share;
+                    const int rest = sh.cut.rest, here = blockIdx.x;
+                    auto cost = [&](int k) { return k * share + min(k, rest); };        // before boundary k
+                    auto last = [&](long long x) {                                      // the last boundary at x or before
+                        const long long longer = rest * (share + 1);
+                        return static_cast<int>(x < longer ? x / (share + 1) : rest + (x - longer) / share);
+                    };
+                    // the unit is cut at every boundary from kSnap pages after its start to kSnap before its end
+                    const long long start = cost(here + 1) - to.at;
+                    const int begin = last(start + kUnitCost + kSnap - 1);
+                    const int end = min(sh.cut.ranges, last(start + kUnitCost + to.nb - kSnap) + 1);
                     const Seq q(a, to.seq);
-                    y = make_int4(1 + min(further, cut.ranges - here), 2 * blockIdx.x + (alone ? 0 : 1), to.head, q.c0 + to.tile * R);
-                    a.joins[2 * blockIdx.x + 1] = make_int4(min(R, q.n - to.tile * R), 0, 0, 0);
+                    y = make_int4(end - begin, begin, to.head, q.c0 + to.tile * R);
+                    // the block that begins it has it in its first slot if it has no unit before
+                    a.joins[2 * here + 1] = make_int4(min(R, q.n - to.tile * R), here - begin, cost(begin) < start, 0);
                 }
                 a.joins[2 * blockIdx.x] = y;
             }
@@ -791,34 +794,38 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
 
 // ------------------------------------------------------------------ join
 
-// Block c joins the unit that block c of the attention begins and does not end: that
-// split and the following blocks' first ones, up to the unit's last page.  Threads are
-// (row, columns, share of the splits), each a power of two: few rows leave many threads
-// for the splits of a row.  Latency-bound: a thread's loads are in flight together, and
-// two blocks fit a multiprocessor, so that all run at once.  (A join that finds its
-// splits itself before the wait saves one load's latency, and takes more from the
-// attention blocks still at work: 117 against 113 us for a mixed batch at d = 128.)
+// The splits of a unit are block `begin`'s of the attention and the following blocks'
+// first ones, up to its last page.  All of these blocks but the last join it here, each
+// some of its columns.  Threads are (row, columns, share of the splits), each a power of
+// two: few rows leave many threads for the splits of a row.  Latency-bound: a thread's
+// loads are in flight together, and two blocks fit a multiprocessor, so that all run at
+// once.  (A join that finds its splits itself before the wait saves one load's latency,
+// and takes more from the attention blocks still at work: 117 against 113 us for a mixed
+// batch at d = 128.)
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads, 2) chunk_join_kernel(ChunkArgs a) {
     constexpr int QUADS = D / 4;      // of columns
     constexpr int QB = 2, U = 4;      // quads and splits of a thread in flight together
     __shared__ float top[kJoinThreads], len[kJoinThreads];
     __shared__ float4 part[kJoinThreads];
-    const int t = threadIdx.x, c = blockIdx.x;
+    const int t = threadIdx.x;
     const int gl = 31 - __clz(a.G);   // G = 2^gl heads
     grid_dep_wait();                  // the splits
-    const int4 u = __ldcg(a.joins + 2 * c), v = __ldcg(a.joins + 2 * c + 1);
+    const int4 u = __ldcg(a.joins + 2 * blockIdx.x), v = __ldcg(a.joins + 2 * blockIdx.x + 1);
     const int ns = u.x, rows = v.x << gl;
     if (ns == 0) return;
     // split s: the first in its slot, the others in slot 0 of the following blocks
-    auto slot = [&](int s) { return static_cast<size_t>(s == 0 ? u.y : 2 * (c + s)); };
+    auto slot = [&](int s) { return static_cast<size_t>(2 * (u.y + s) + (s == 0 ? v.z : 0)); };
     constexpr int QL = D == 128 ? 5 : 4, TL = 9;
     static_assert(QUADS == 1 << QL && kJoinThreads == 1 << TL, "powers of two");
     const int rpl = max(2, 32 - __clz(rows - 1));       // rows, to a power of two (a clz of 0 is 32)
-    const int groupl = min(QL, TL - rpl);               // column groups, of `per` quads each
-    const int per = QUADS >> groupl, spanl = rpl + groupl, span = 1 << spanl;
+    // 2^wl blocks share the columns, as long as each has 64 (row, quad) pairs
+    const int wl = min(min(31 - __clz(ns - 1), QL), max(0, rpl + QL - 6)), ql = QL - wl;
+    if (v.y >> wl != 0) return;
+    const int groupl = min(ql, TL - rpl);               // column groups, of `per` quads each
+    const int per = 1 << (ql - groupl), spanl = rpl + groupl, span = 1 << spanl;
     const int shares = kJoinThreads >> spanl;           // of the splits; more than one only where per = 1
-    const int row = t & ((1 << rpl) - 1), cg = t >> rpl & ((1 << groupl) - 1), mine = t >> spanl;
+    const int row = t & ((1 << rpl) - 1), cg = (v.y << groupl) + (t >> rpl & ((1 << groupl) - 1)), mine = t >> spanl;
     const bool live = row < rows;
     const int at = live ? row : 0;
     const int tok = at >> gl, h = at & (a.G - 1);

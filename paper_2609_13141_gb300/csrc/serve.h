@@ -99,7 +99,8 @@ struct ChunkArgs {
     float* LSE;                 // [T][Hq] or null
     // workspace
     int blocks;                 // chunk_blocks()
-    int4* joins;                // [blocks][2] {splits (0: nothing to join), first one, KV group, first token}, {tokens}
+    int4* joins;                // [blocks][2] {splits (0: nothing to join), first one's block, KV group, first token},
+                                // {tokens, which of the joining blocks, first one's slot, 0}
     float* part_o;              // [2 blocks][d / 4][128][4]
     float2* part_ml;            // [2 blocks][128] (max, sum)
     int* status;
