@@ -52,7 +52,12 @@ constexpr int kStatusBadInput = 1;
 constexpr int kStatusLayout = 3;
 constexpr int kUnitCost = 4;      // what a unit costs beside its pages (its Q tile, its epilogue: 2 to 3 us), in pages
 constexpr int kSnap = 4;          // pages: ranges do not cut this close to a unit's ends
-constexpr int kMinShare = 4;      // pages of a block's range, at least
+// A block's range has this many pages at least, twice as many where units have kLongUnit
+// pages on average and would go into many splits: 7 requests of 2 to 12 tokens over 2000
+// to 16000, 2 heads of 128, 31.4 us with 4 and 27.3 with 8; 4 single tokens over 100 to
+// 800, 8 KV groups of 128, 12.5 and 15.1.
+constexpr int kMinShare = 4;
+constexpr int kLongUnit = 64;
 constexpr int kJoinThreads = 512;
 
 __device__ __forceinline__ void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -152,8 +157,10 @@ __device__ __forceinline__ bool find_range(const ChunkArgs& a, int rl, Shares& s
     total *= a.Hkv;
     units *= a.Hkv;
     if (total == 0) return false;
-    // as many ranges as blocks, fewer where they would be under kMinShare pages or a unit
-    const long long want = max(units, (total - units * kUnitCost + kMinShare - 1) / kMinShare);
+    // as many ranges as blocks, fewer where they would be under the least share of pages or a unit
+    const long long pages = total - units * kUnitCost;
+    const int least = pages >= kLongUnit * units ? 2 * kMinShare : kMinShare;
+    const long long want = max(units, (pages + least - 1) / least);
     const int ranges = static_cast<int>(min(static_cast<long long>(gridDim.x), want));
     if (static_cast<int>(blockIdx.x) >= ranges) return false;
     // ranges differ by one at most
