@@ -23,10 +23,11 @@
 // units first: units of one sequence then walk the same pages at about the same time
 // on many blocks, out of L2.
 //
-// Measured: 6.2 TB/s of keys and values for 96 single tokens over 100 to 12000 (126 us),
-// 6.1 TB/s for 6 x 5 tokens over 20000 to 32000 (109 us), 1653 TFLOP/s for 4096 tokens
-// over 32096 (1220 us; 1464 and 1378 us once the card is at its power limit, at 1.64
-// GHz), all d = 128 with 32 and 8 heads.
+// Measured: 6.2 TB/s of keys and values for 96 single tokens over 100 to 12000 (125 us),
+// 6.3 TB/s for 6 x 5 tokens over 20000 to 32000 (106 us), 1653 TFLOP/s for 4096 tokens
+// over 32096 (1220 us; 1450 and 1390 us once the card is at its power limit, at 1.64
+// GHz), all d = 128 with 32 and 8 heads.  d = 64: 920 TFLOP/s for 2048 tokens over 10048
+// (165 us), bound by the softmax warps' chain of waits and arithmetic (Cfg).
 //
 // Keys past a sequence's end in its last page may hold anything: scores there are
 // replaced, not weighted by zero, and values past the tile's last position are
@@ -229,15 +230,17 @@ __device__ __forceinline__ void find_bounds(const ChunkArgs& a, int rl, const Sh
 // ------------------------------------------------------------------ attention
 
 // A step is KPS pages: their scores, softmax and product go through the pipeline together.
-// Each step costs the softmax warps some 400 cycles of waits, tensor-memory loads and
-// stores beside its arithmetic.  At d = 128 the products of the multiprocessor's two
+// Beside its arithmetic a step costs the softmax warps 760 cycles of barriers, votes and
+// tensor-memory loads and stores.  At d = 128 the products of the multiprocessor's two
 // blocks cover that.  They are bound by the operands' way out of shared memory: with 64
 // keys a product step reads 4 KB of Q and 2 KB of K in 48 cycles, for 32 of arithmetic.
 // With the first half of Q in tensor memory (O 128 + S 64 + P 32 + Q 32 columns: no room
 // for more) a page takes 571 cycles of the tensor pipe instead of 618.  At d = 64 the
 // products are half as long and nothing covers the waits: two pages a step, O 64 + S
 // 128 + P 64 columns, with the score rows in registers (184 a softmax thread, 64 for the
-// others, of the 128 the block is launched with).
+// others, of the 128 the block is launched with).  Such a step takes 1650 cycles with one
+// block on the multiprocessor (700 of them exponentials and P, 185 the maximum) and 2370
+// with two, of 1024 that both need the exponential unit.
 template <int D>
 struct Cfg {
     static constexpr int KPS = D == 64 ? 2 : 1;

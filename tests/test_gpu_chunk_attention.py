@@ -94,6 +94,18 @@ def test_splits_and_mixed_batches(G, Hkv, d, lens):
     _run(lens, G * Hkv, Hkv, d, seed=len(lens))
 
 
+@pytest.mark.parametrize("G,Hkv,d,lens", [
+    (8, 1, 128, [(19000, 1)]),                      # one unit of long splits, few rows: all its blocks join it
+    (1, 1, 64, [(6000, 128)]),                      # a full tile, rows blind to the last splits
+    (4, 1, 128, [(4500, 33)]),                      # a full tile and one of four rows
+    (1, 1, 128, [(600, 1)]),                        # one row in two or three splits
+    (2, 2, 64, [(9000, 7), (300, 1)]),
+    (1, 2, 128, [(2500, 70), (2500, 3)]),
+])
+def test_units_of_many_splits(G, Hkv, d, lens):
+    _run(lens, G * Hkv, Hkv, d, seed=2 * len(lens) + G)
+
+
 def test_scale_and_peaked_rows():
     # logits of +-100: the running maximum moves far and often
     _run([(500, 30), (90, 1)], 4, 2, 128, seed=3, scale=0.9, std=4.0)
