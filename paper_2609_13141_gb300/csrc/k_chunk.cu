@@ -61,18 +61,15 @@ constexpr int kMinShare = 4;
 constexpr int kLongUnit = 64;
 constexpr int kJoinThreads = 512;
 
-__device__ __forceinline__ void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void grid_dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // ------------------------------------------------------------------ shares
 
 // Sequence b: its new tokens and its length, no new tokens if the length is wrong.
 struct Seq {
     int c0, n, L;
     __device__ __forceinline__ Seq(const ChunkArgs& a, int b) {
-        c0 = __ldg(a.cu + b);
-        n = __ldg(a.cu + b + 1) - c0;
-        L = __ldg(a.kv_lens + b);
+        c0 = load(a.cu + b);
+        n = load(a.cu + b + 1) - c0;
+        L = load(a.kv_lens + b);
         if (L < n || L > 64LL * a.max_blocks) n = 0;
     }
     // R = 2^rl tokens a tile
@@ -126,7 +123,7 @@ __device__ __forceinline__ bool find_range(const ChunkArgs& a, int rl, Shares& s
     long long cost = 0;
     int tiles = 0, bad = 0;
     for (int b = b0; b < b1; ++b) {
-        const int c0 = __ldg(a.cu + b), c1 = __ldg(a.cu + b + 1);
+        const int c0 = load(a.cu + b), c1 = load(a.cu + b + 1);
         const Seq x(a, b);
         bad |= c0 < 0 || c1 < c0 || c1 > a.T;
         if (x.n != c1 - c0 && blockIdx.x == 0) atomicExch(a.status, kStatusBadInput);
@@ -306,7 +303,7 @@ __device__ __forceinline__ bool read_item(Ctl& ctl, int r, const WaitCtl& wc, It
 // item's sequence (lanes past blk1: unused).
 __device__ __forceinline__ int page_row(const ChunkArgs& a, const Item& x, int m, int lane) {
     if (m + lane >= x.blk1) return 0;
-    int page = __ldg(a.block_table + static_cast<size_t>(x.seq) * a.max_blocks + m + lane);
+    int page = load(a.block_table + static_cast<size_t>(x.seq) * a.max_blocks + m + lane);
     if (page < 0 || page >= a.num_pages) {
         atomicExch(a.status, kStatusBadInput);
         return a.num_pages * a.Hkv;   // past the end: TMA fills with zero
@@ -821,7 +818,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) chunk_join_kernel(ChunkArgs a
     const int t = threadIdx.x;
     const int gl = 31 - __clz(a.G);   // G = 2^gl heads
     grid_dep_wait();                  // the splits
-    const int4 u = __ldcg(a.joins + 2 * blockIdx.x), v = __ldcg(a.joins + 2 * blockIdx.x + 1);
+    const int4 u = load(a.joins + 2 * blockIdx.x), v = load(a.joins + 2 * blockIdx.x + 1);
     const int ns = u.x, rows = v.x << gl;
     if (ns == 0) return;
     // split s: the first in its slot, the others in slot 0 of the following blocks
@@ -937,23 +934,10 @@ cudaError_t launch_d(const ChunkArgs& a, const KernelEnv& env, const char** err)
         return cudaErrorInvalidValue;
     }
     // Two blocks a multiprocessor: their shared memory and tensor memory both fit twice.
-    // Both launches may set up before the kernel ahead of them has ended (they wait for it
-    // themselves, griddepcontrol).
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.stream = env.stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cfg.gridDim = dim3(a.blocks);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = C::SMEM;
-    e = cudaLaunchKernelEx(&cfg, chunk_attn_kernel<D>, mq, mk, mv, a, a.sm_scale * kLog2e, env.limit);
+    e = launch_early(chunk_attn_kernel<D>, dim3(a.blocks), kThreads, C::SMEM, env.stream, mq, mk, mv, a, a.sm_scale * kLog2e,
+                     env.limit);
     if (e != cudaSuccess) { *err = "chunk attention launch"; return e; }
-    cfg.blockDim = dim3(kJoinThreads);
-    cfg.dynamicSmemBytes = 0;
-    e = cudaLaunchKernelEx(&cfg, chunk_join_kernel<D>, a);
+    e = launch_early(chunk_join_kernel<D>, dim3(a.blocks), kJoinThreads, 0, env.stream, a);
     if (e != cudaSuccess) *err = "chunk join launch";
     return e;
 }

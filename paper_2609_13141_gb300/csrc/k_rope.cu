@@ -18,8 +18,8 @@
 // the same heads for all its tokens (their kinds, weights and addresses are then
 // fixed), rows stream through a ring in shared memory (cp.async, no registers held
 // while they are in flight), and the arithmetic runs on packed fp32 pairs.  Measured:
-// 6.2 TB/s forward (131 us for 32768 tokens of 32 + 2 x 8 heads of 128, and as much into
-// cache pages), 5.4 TB/s for the gradient (213 us), where a row is read twice as much
+// 6.4 TB/s forward (128 us for 32768 tokens of 32 + 2 x 8 heads of 128, and as much into
+// cache pages), 5.5 TB/s for the gradient (211 us), where a row is read twice as much
 // as written and the waits for shared memory and reductions show.  One or two more
 // stages of the rings are slower (158 us forward with three): the warps drift apart and
 // DRAM pages are opened more often.
@@ -44,8 +44,8 @@ __device__ __forceinline__ float sum2(uint64_t v) {
 struct Quads {
     uint2 a, b;
     __device__ __forceinline__ void load(const bf16* row, int ia, int ib) {
-        a = __ldg(reinterpret_cast<const uint2*>(row + ia));
-        b = __ldg(reinterpret_cast<const uint2*>(row + ib));
+        a = sas::load(reinterpret_cast<const uint2*>(row + ia));
+        b = sas::load(reinterpret_cast<const uint2*>(row + ib));
     }
     __device__ __forceinline__ void read(const uint8_t* row, int ia, int ib) {   // shared memory
         a = *reinterpret_cast<const uint2*>(row + 2 * ia);
@@ -216,6 +216,7 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
     const Share sh(parts);
     if (g == 0)
         for (int i = 0; i < kFwdStages; ++i) Table<D>::clear(ring + i * UNIT + TAB, l);
+    grid_dep_wait();
     for (int part = sh.part; part < parts; part += sh.part_step) {
         const int h0 = part * R::RPU + g;   // row u of the group is head h0 + u GPW
         bf16* out[kRows];
@@ -235,8 +236,8 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
         unsigned good = 0;   // per fetched token, the latest in bit 0: it has outputs
         auto locate = [&] {
             if (tf >= a.T) return;
-            pos_f = a.pos != nullptr ? __ldg(a.pos + tf) : Where(a, tf).n;
-            if constexpr (PAGED) slot_f = __ldg(a.slots + tf);
+            pos_f = a.pos != nullptr ? load(a.pos + tf) : Where(a, tf).n;
+            if constexpr (PAGED) slot_f = load(a.slots + tf);
         };
         auto fetch = [&](int st) {
             good <<= 1;
@@ -257,11 +258,11 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
         };
         locate();
         for (int i = 0; i < kFwdStages - 1; ++i) fetch(i);
-        if constexpr (PAGED) slot1 = __ldg(a.slots + sh.t0);
+        if constexpr (PAGED) slot1 = load(a.slots + sh.t0);
         int st = 0;
         for (long long t = sh.t0; t < a.T; t += sh.step) {
             slot = slot1;
-            if (PAGED && t + sh.step < a.T) slot1 = __ldg(a.slots + t + sh.step);
+            if (PAGED && t + sh.step < a.T) slot1 = load(a.slots + t + sh.step);
             cp_async_wait<kFwdStages - 2>();
             __syncwarp();   // the lanes' copies of this token have landed; the stage refilled next has been read
             fetch(st == 0 ? kFwdStages - 1 : st - 1);
@@ -336,6 +337,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
         for (int i = 0; i < kBwdStages; ++i) Table<D>::clear(ring + i * UNIT + TAB, l);
     const Place<INTER> pl(a, l);
     const Share sh(parts);
+    grid_dep_wait();
     for (int part = sh.part; part < parts; part += sh.part_step) {
         const int h0 = part * R::RPU + g;
         const bf16* grad[kRows];
@@ -355,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
         int pos_f = 0;
         unsigned good = 0;      // per fetched token, the latest in bit 0: its position is in the tables
         auto locate = [&] {
-            if (tf < a.T) pos_f = a.pos != nullptr ? __ldg(a.pos + tf) : Where(a, tf).n;
+            if (tf < a.T) pos_f = a.pos != nullptr ? load(a.pos + tf) : Where(a, tf).n;
         };
         auto fetch = [&](int st) {
             good <<= 1;
@@ -493,16 +495,16 @@ template <int D, bool INTER, bool PAGED>
 cudaError_t launch_fwd(const RopeArgs& a, const KernelEnv& env) {
     const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(rope_fwd_kernel<D, INTER, PAGED>), rope_fwd_smem<D>(), true);
     if (e != cudaSuccess) return e;
-    rope_fwd_kernel<D, INTER, PAGED><<<blocks_for<D, kFwdRows>(a, kFwdBlocks * device_sm_count(), 1), kThreads, rope_fwd_smem<D>(), env.stream>>>(a);
-    return cudaGetLastError();
+    return launch_early(rope_fwd_kernel<D, INTER, PAGED>, dim3(blocks_for<D, kFwdRows>(a, kFwdBlocks * device_sm_count(), 1)), kThreads,
+                        rope_fwd_smem<D>(), env.stream, a);
 }
 
 template <int D, bool INTER>
 cudaError_t launch_bwd(const RopeArgs& a, const KernelEnv& env) {
     const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(rope_bwd_kernel<D, INTER>), rope_bwd_smem<D>(), true);
     if (e != cudaSuccess) return e;
-    rope_bwd_kernel<D, INTER><<<blocks_for<D, kBwdRows>(a, rope_bwd_max_blocks(), 4), kThreads, rope_bwd_smem<D>(), env.stream>>>(a);
-    return cudaGetLastError();
+    return launch_early(rope_bwd_kernel<D, INTER>, dim3(blocks_for<D, kBwdRows>(a, rope_bwd_max_blocks(), 4)), kThreads,
+                        rope_bwd_smem<D>(), env.stream, a);
 }
 
 template <int D, bool INTER>

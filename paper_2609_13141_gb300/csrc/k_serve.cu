@@ -17,7 +17,7 @@ constexpr int kStatusNoPages = 5;    // == SAS_ERR_OOM
 // Latency-bound: tens of bytes a request.  So it is one launch without
 // communication between blocks: every block scans all requests itself (8 bytes
 // each, from L2 after the first block) into shared memory, then blocks share the
-// tokens, the new pages and the requests.  7 us for 256 requests of one token, 10 us
+// tokens, the new pages and the requests.  7 us for 256 requests of one token, 9 us
 // for 1500 requests and 371104 tokens (4.5 MB out), launch included.
 
 constexpr int kPlanThreads = 512;
@@ -74,7 +74,7 @@ __device__ __forceinline__ int owner(const int* sums, int n, int v) {
 
 // Pages request b holds.
 __device__ __forceinline__ int pages_held(const PlanArgs& a, int b, int s) {
-    return ((a.held_lens != nullptr ? max(s, __ldg(a.held_lens + b)) : s) + 63) / 64;
+    return ((a.held_lens != nullptr ? max(s, load(a.held_lens + b)) : s) + 63) / 64;
 }
 
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
@@ -84,9 +84,10 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
     const int t = threadIdx.x;
     const long long cap = 64LL * a.max_blocks;
     int bad = 0;
+    grid_dep_wait();
     for (int b = t; b < a.B; b += kPlanThreads) {
-        const int s = __ldg(a.seq_lens + b), n = __ldg(a.new_lens + b);
-        const int held = a.held_lens != nullptr ? __ldg(a.held_lens + b) : 0;
+        const int s = load(a.seq_lens + b), n = load(a.new_lens + b);
+        const int held = a.held_lens != nullptr ? load(a.held_lens + b) : 0;
         const bool wrong = s < 0 || n < 0 || static_cast<long long>(s) + n > cap || held < 0 || held > cap;
         bad |= wrong;
         cu[b] = wrong ? 0 : n;
@@ -102,7 +103,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
         p_off += off[b];
     }
     block_scan2(n_off, p_off, n_all, p_all);
-    const int begin = __ldg(a.free_begin);
+    const int begin = load(a.free_begin);
     const bool invalid = bad || n_all > a.T || begin < 0 || begin > a.num_free;
     const bool short_ = !invalid && p_all > a.num_free - begin;
     const bool fits = !invalid && !short_;
@@ -118,7 +119,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
     const int total = fits ? static_cast<int>(n_all) : 0, pages = fits ? p_all : 0;
     const int at = blockIdx.x * kPlanThreads + t, step = gridDim.x * kPlanThreads;
     for (int b = at; b < a.B; b += step) {
-        a.kv_lens[b] = __ldg(a.seq_lens + b) + (fits ? __ldg(a.new_lens + b) : 0);
+        a.kv_lens[b] = load(a.seq_lens + b) + (fits ? load(a.new_lens + b) : 0);
         a.cu_new[b] = cu[b];
     }
     if (at == 0) {
@@ -127,8 +128,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
     }
     for (int p = at; p < pages; p += step) {
         const int b = owner(off, a.B, p);
-        const int blk = pages_held(a, b, __ldg(a.seq_lens + b)) + p - off[b];
-        int page = __ldg(a.free_pages + begin + p);
+        const int blk = pages_held(a, b, load(a.seq_lens + b)) + p - off[b];
+        int page = load(a.free_pages + begin + p);
         if (page < 0 || page >= a.num_pages) {
             atomicExch(a.status, kStatusBadInput);
             page = -1;
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
                 fresh = true;
             }
             if (fresh) {
-                s = __ldg(a.seq_lens + b);
+                s = load(a.seq_lens + b);
                 have = pages_held(a, b, s);
                 last = -1;
                 fresh = false;
@@ -162,7 +163,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
             if (blk != last) {
                 // a page of this call comes from the free list: its table entry may not be written yet
                 page = blk < have ? a.block_table[static_cast<size_t>(b) * a.max_blocks + blk]
-                                  : __ldg(a.free_pages + begin + off[b] + blk - have);
+                                  : load(a.free_pages + begin + off[b] + blk - have);
                 last = blk;
                 if (page < 0 || page >= a.num_pages) {
                     atomicExch(a.status, kStatusBadInput);
@@ -199,8 +200,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
 // w_v ring first at v with probability w_v / sum w, so no sum is needed and the
 // choice does not depend on the order of any addition.
 //
-// HBM-bound: one row of p, q and e a request, read once by several blocks (5.9 TB/s at
-// 128 rows of 151936 columns).  The division is made only where w could beat the thread's best: w >= best e, a
+// HBM-bound: one row of p, q and e a request, read once by several blocks (6.5 TB/s at
+// 128 rows of 151936 columns, 36 us).  The division is made only where w could beat the thread's best: w >= best e, a
 // product smaller by more than both roundings (with the underflow range let
 // through).  Blocks join by a maximum over (quotient bits, ~index): quotients are
 // positive, so their bits order like the values, and ties go to the lower index.
@@ -312,7 +313,8 @@ template <bool VEC>
 __global__ void __launch_bounds__(kVerifyThreads, kVerifyBlocks) verify_kernel(VerifyArgs a) {
     __shared__ int sh_a, sh_last;
     const int b = blockIdx.y, t = threadIdx.x;
-    const int c0 = __ldg(a.cu + b), c1 = __ldg(a.cu + b + 1);
+    grid_dep_wait();
+    const int c0 = load(a.cu + b), c1 = load(a.cu + b + 1);
     if (c0 < 0 || c1 < c0 || c1 > a.Td || c1 - c0 > a.W) {
         if (blockIdx.x == 0) {
             if (t == 0) {
@@ -336,13 +338,13 @@ __global__ void __launch_bounds__(kVerifyThreads, kVerifyBlocks) verify_kernel(V
             const int j = j0 + t;
             bool ok = true;
             if (j < n) {
-                const int x = __ldg(a.tokens + c0 + j);
+                const int x = load(a.tokens + c0 + j);
                 if (x < 0 || x >= a.V) {
                     if (blockIdx.x == 0) atomicExch(a.status, kStatusBadInput);
                     ok = false;
                 } else {
-                    const float q = Qd == nullptr ? 1.f : __ldg(Qd + static_cast<size_t>(j) * a.ldq + x);
-                    ok = __fmul_rn(__ldg(a.u + c0 + j), q) < __ldg(P + static_cast<size_t>(j) * a.ldp + x);
+                    const float q = Qd == nullptr ? 1.f : load(Qd + static_cast<size_t>(j) * a.ldq + x);
+                    ok = __fmul_rn(load(a.u + c0 + j), q) < load(P + static_cast<size_t>(j) * a.ldp + x);
                 }
             }
             const unsigned no = __ballot_sync(0xffffffffu, !ok);
@@ -358,7 +360,7 @@ __global__ void __launch_bounds__(kVerifyThreads, kVerifyBlocks) verify_kernel(V
     const float* p = P + static_cast<size_t>(acc) * a.ldp;
     const float* q = acc < n && Qd != nullptr ? Qd + static_cast<size_t>(acc) * a.ldq : nullptr;
     // without draft probabilities the draft is certain: its token leaves the residual
-    const int drop = acc < n && Qd == nullptr ? __ldg(a.tokens + c0 + acc) : -1;
+    const int drop = acc < n && Qd == nullptr ? load(a.tokens + c0 + acc) : -1;
     Best m;
     scan_row<VEC>(m, p, q, e, drop, v0, v1);
     const unsigned long long mine = block_best(m);
@@ -385,7 +387,7 @@ __global__ void __launch_bounds__(kVerifyThreads, kVerifyBlocks) verify_kernel(V
     }
     int32_t* out = a.out + static_cast<size_t>(b) * (a.W + 1);
     for (int j = t; j <= a.W; j += kVerifyThreads)
-        if (j != acc) out[j] = j < acc ? __ldg(a.tokens + c0 + j) : -1;
+        if (j != acc) out[j] = j < acc ? load(a.tokens + c0 + j) : -1;
     if (t == 0) {
         a.accepted[b] = acc;
         out[acc] = best != 0 ? static_cast<int>(0xffffffffu - static_cast<unsigned>(best)) : -1;
@@ -404,8 +406,7 @@ cudaError_t plan_prepare(int max_seqs) {
 cudaError_t launch_plan(const PlanArgs& a, const KernelEnv& env) {
     const int most = 2 * device_sm_count();
     const int need = (max((a.T + kTokens - 1) / kTokens, a.B) + kPlanThreads - 1) / kPlanThreads;
-    plan_kernel<<<need < most ? need : most, kPlanThreads, plan_smem(a.B), env.stream>>>(a);
-    return cudaGetLastError();
+    return launch_early(plan_kernel, dim3(need < most ? need : most), kPlanThreads, plan_smem(a.B), env.stream, a);
 }
 
 cudaError_t launch_verify(VerifyArgs a, const KernelEnv& env) {
@@ -420,9 +421,7 @@ cudaError_t launch_verify(VerifyArgs a, const KernelEnv& env) {
     auto al = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
     const bool vec = al(a.target) && al(a.draft) && al(a.noise) && a.ldp % 4 == 0 && a.ldq % 4 == 0 && a.lde % 4 == 0 &&
                      a.chunk % 4 == 0;
-    if (vec) verify_kernel<true><<<grid, kVerifyThreads, 0, env.stream>>>(a);
-    else verify_kernel<false><<<grid, kVerifyThreads, 0, env.stream>>>(a);
-    return cudaGetLastError();
+    return launch_early(vec ? verify_kernel<true> : verify_kernel<false>, grid, kVerifyThreads, 0, env.stream, a);
 }
 
 }  // namespace sas

@@ -36,6 +36,34 @@ __device__ __forceinline__ bool mbar_poll_warp(uint64_t* bar, uint32_t parity, c
     return __all_sync(0xffffffffu, ok);
 }
 
+// Waits until the kernel ahead in the stream has ended; lets the next one's blocks come
+// in as places open up (they wait the same way).
+__device__ __forceinline__ void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// A load of what an earlier kernel may have written.  Not through the read-only path: its
+// data must not change while the kernel runs, which begins ahead of the wait, and a load
+// by it may be moved there.
+template <class T>
+__device__ __forceinline__ T load(const T* p) { return *p; }
+
+// Launches a kernel that may set up while the kernel ahead of it is still at work: its
+// every thread calls grid_dep_wait before its first access to global memory.
+template <class... P, class... A>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t stream, A... args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // 16-byte asynchronous copy global -> shared, past L1 (both addresses 16-byte aligned).
 __device__ __forceinline__ void cp_async16(void* smem_dst, const void* gsrc) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(smem_dst)), "l"(gsrc) : "memory");
