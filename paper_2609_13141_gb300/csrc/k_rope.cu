@@ -312,6 +312,12 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
 // its warp's sums at the end; a block adds its warps' sums into one row of `part`,
 // and the last block to finish adds those in their order: equal inputs give equal
 // sums.
+//
+// Values cost no arithmetic.  Where neighbouring rows would give some warps nothing else,
+// which end early, a warp's rows come half from the front of the fused row and half from
+// its back (32768 tokens of 32 + 2 x 8 heads: 207 against 211 us; 58701 of 2 + 2 x 2: 58
+// against 64), elsewhere in one piece (46113 of 4 + 2 x 1: 57.5 against 59.2).  The forward
+// kernel reads its row better in one piece (129 against 133 us at 32768 tokens).
 constexpr int kBwdRows = 2, kBwdStages = 3, kBwdBlocks = 2;
 template <int D>
 constexpr int rope_bwd_unit() { return 2 * kBwdRows * 32 * 16 + Table<D>::BYTES; }
@@ -328,6 +334,8 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
     const int lane = lane_id(), warp = warp_id(), l = lane % R::LPR, g = lane / R::LPR;
     const unsigned group = R::group_mask(g);
     const int H = a.Hq + 2 * a.Hkv, HN = a.Hq + a.Hkv, parts = R::parts(a);
+    const bool spread = (parts - 1) * R::RPU >= HN;
+    const int hp = spread ? R::GPW : R::RPU, hs = spread ? parts * R::GPW : R::GPW;   // heads from part to part, row to row
     uint8_t* const ring = sm + warp * kBwdStages * UNIT;
     const int mine = g * (R::LPR * 16);
     float* const sums = reinterpret_cast<float*>(sm + kWarps * kBwdStages * UNIT);   // [kWarps][2 D]
@@ -339,13 +347,13 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
     const Share sh(parts);
     grid_dep_wait();
     for (int part = sh.part; part < parts; part += sh.part_step) {
-        const int h0 = part * R::RPU + g;
+        const int h0 = part * hp + g;   // row u of the group is head h0 + u hs
         const bf16* grad[kRows];
         Quads w[kRows];
         uint64_t acc[kRows][4];
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
-            const int h = h0 + u * R::GPW;
+            const int h = h0 + u * hs;
             const bool isq = h < a.Hq, isv = h >= HN;
             const int hk = isq ? h : (isv ? h - HN : h - a.Hq);
             grad[u] = (isq ? a.Q : (isv ? a.V : a.K)) + static_cast<long long>(hk) * a.N * D + l * 8;
@@ -368,8 +376,8 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
                 uint8_t* const dst = ring + st * UNIT;
 #pragma unroll
                 for (int u = 0; u < kRows; ++u) {
-                    const int h = h0 + u * R::GPW;
-                    if (h < HN) cp_async16(dst + u * 512 + mine + l * 16, src + u * R::GPW * D);
+                    const int h = h0 + u * hs;
+                    if (h < HN) cp_async16(dst + u * 512 + mine + l * 16, src + u * hs * D);
                     if (h < H) cp_async16(dst + DY + u * 512 + mine + l * 16, grad[u] + (h < a.Hq ? at_q : at_kv));
                 }
                 const bool ok = pos_f >= 0 && pos_f < a.max_pos;
@@ -395,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
             bf16* const dst = a.dqkv + t * a.ld_d + h0 * D;
 #pragma unroll
             for (int u = 0; u < kRows; ++u) {
-                const int h = h0 + u * R::GPW;
+                const int h = h0 + u * hs;
                 const uint8_t* const row = stage + u * 512 + mine;
                 if (h < HN) {
                     Quads q;
@@ -422,9 +430,9 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
 #pragma unroll
                     for (int i = 0; i < 4; ++i) z[i] = mul_f32x2(r, fma_f32x2(m, xf[i], mul_f32x2(z[i], wf[i])));
                     q.pack(z);
-                    q.store(dst + u * R::GPW * D, pl.ia, pl.ib);
+                    q.store(dst + u * hs * D, pl.ia, pl.ib);
                 } else if (h < H) {   // values pass through
-                    *reinterpret_cast<uint4*>(dst + u * R::GPW * D + l * 8) = *reinterpret_cast<const uint4*>(row + DY + l * 16);
+                    *reinterpret_cast<uint4*>(dst + u * hs * D + l * 8) = *reinterpret_cast<const uint4*>(row + DY + l * 16);
                 }
             }
         }
@@ -435,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
             if (g != gg) continue;
 #pragma unroll
             for (int u = 0; u < kRows; ++u) {
-                const int h = h0 + u * R::GPW;
+                const int h = h0 + u * hs;
                 if (h >= HN) continue;
                 float* const col = sum + (h < a.Hq ? 0 : D);
 #pragma unroll
