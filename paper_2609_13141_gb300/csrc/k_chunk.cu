@@ -23,7 +23,7 @@
 // units first: units of one sequence then walk the same pages at about the same time
 // on many blocks, out of L2.
 //
-// Measured: 6.2 TB/s of keys and values for 96 single tokens over 100 to 12000 (125 us),
+// Measured: 6.3 TB/s of keys and values for 96 single tokens over 100 to 12000 (124 us),
 // 6.3 TB/s for 6 x 5 tokens over 20000 to 32000 (106 us), 1653 TFLOP/s for 4096 tokens
 // over 32096 (1220 us; 1450 and 1390 us once the card is at its power limit, at 1.64
 // GHz), all d = 128 with 32 and 8 heads.  d = 64: 920 TFLOP/s for 2048 tokens over 10048
