@@ -258,7 +258,8 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
         };
         locate();
         for (int i = 0; i < kFwdStages - 1; ++i) fetch(i);
-        if constexpr (PAGED) slot1 = load(a.slots + sh.t0);
+        // warps come in whole blocks: the last ones may have no token at all
+        if (PAGED && sh.t0 < a.T) slot1 = load(a.slots + sh.t0);
         int st = 0;
         for (long long t = sh.t0; t < a.T; t += sh.step) {
             slot = slot1;
