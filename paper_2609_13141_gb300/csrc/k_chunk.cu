@@ -821,6 +821,9 @@ __global__ void __launch_bounds__(kJoinThreads, 2) chunk_join_kernel(ChunkArgs a
     const int4 u = load(a.joins + 2 * blockIdx.x), v = load(a.joins + 2 * blockIdx.x + 1);
     const int ns = u.x, rows = v.x << gl;
     if (ns == 0) return;
+    // A split in which the row sees no key does not count, whatever its O holds.  Its sum tells: scores
+    // that are all NaN leave a maximum of -infinity too, but a sum of NaN, which has to come through.
+    auto nothing = [](float m, float l) { return m == -CUDART_INF_F && l == 0.f; };
     // split s: the first in its slot, the others in slot 0 of the following blocks
     auto slot = [&](int s) { return static_cast<size_t>(2 * (u.y + s) + (s == 0 ? v.z : 0)); };
     constexpr int QL = D == 128 ? 5 : 4, TL = 9;
@@ -870,8 +873,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) chunk_join_kernel(ChunkArgs a
             }
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                // a split in which the row sees no key does not count, whatever it holds
-                if (ml[i].x == -CUDART_INF_F) continue;
+                if (nothing(ml[i].x, ml[i].y)) continue;
                 const float g = fast_exp2(ml[i].x - M);
                 L = fmaf(g, ml[i].y, L);
 #pragma unroll
@@ -898,10 +900,11 @@ __global__ void __launch_bounds__(kJoinThreads, 2) chunk_join_kernel(ChunkArgs a
             o[0].x *= f; o[0].y *= f; o[0].z *= f; o[0].w *= f;
             for (int k = 1; k < shares; ++k) {
                 const float mk = top[k * span + t];
-                if (mk == -CUDART_INF_F) continue;
+                const float lk = len[k * span + t];
+                if (nothing(mk, lk)) continue;
                 const float g = fast_exp2(mk - m2);
                 const float4 x = part[k * span + t];
-                L = fmaf(g, len[k * span + t], L);
+                L = fmaf(g, lk, L);
                 o[0].x = fmaf(g, x.x, o[0].x);
                 o[0].y = fmaf(g, x.y, o[0].y);
                 o[0].z = fmaf(g, x.z, o[0].z);
