@@ -685,8 +685,9 @@ sas_status sas_chunk_attention(sas_chunk_handle* h, int32_t num_seqs, int32_t T,
  * p_n.  x_j is accepted while u_j q_j(x_j) < p_j(x_j).  The next token after the a
  * accepted ones is argmax_v w_v / e_v (the lowest v of equal ones) over v with w_v >
  * 0 and e_v > 0, w = max(p_a - q_a, 0) after a rejection, or p_a where that is zero
- * everywhere or all drafts were accepted.  With u uniform on [0, 1) and e exponential
- * (Exp(1)) the tokens are distributed as the target's own.
+ * everywhere or all drafts were accepted (quotients that round to the same fp32 value are
+ * equal).  With u uniform on [0, 1) and e exponential (Exp(1)) the tokens are distributed
+ * as the target's own.
  *   num_drafts  drafts of all requests; max_draft: columns of out_tokens - 1
  *   tokens      int32 [num_drafts]; cu_draft int32 [num_seqs + 1]               (in)
  *   target      fp32 [num_drafts + num_seqs] rows of V, ld_target apart: request
@@ -699,8 +700,8 @@ sas_status sas_chunk_attention(sas_chunk_handle* h, int32_t num_seqs, int32_t T,
  *               token, then -1                                                 (out)
  * tokens, u and draft may be NULL when num_drafts is 0.  Offsets that decrease, leave 0
  * .. num_drafts or give a request more than max_draft drafts: that request gets 0
- * accepted and all -1; a drafted token outside 0 .. V - 1 is rejected; a row without
- * a positive weight gives the token -1; each with status SAS_ERR_INVALID_ARG.
+ * accepted and all -1; a drafted token outside 0 .. V - 1 is rejected; a row without a
+ * column of w_v > 0 and e_v > 0 gives the token -1; each with status SAS_ERR_INVALID_ARG.
  * One launch. */
 sas_status sas_chunk_verify(sas_chunk_handle* h, int32_t num_seqs, int32_t num_drafts, int32_t max_draft, int32_t V,
                             const int32_t* tokens, const int32_t* cu_draft, const float* target, int64_t ld_target,

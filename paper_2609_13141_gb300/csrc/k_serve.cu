@@ -204,17 +204,23 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
 // 128 rows of 151936 columns, 36 us).  The division is made only where w could beat the thread's best: w >= best e, a
 // product smaller by more than both roundings (with the underflow range let
 // through).  Blocks join by a maximum over (quotient bits, ~index): quotients are
-// positive, so their bits order like the values, and ties go to the lower index.
+// not negative, so their bits order like the values, and ties go to the lower index.  Below
+// all of these is the key of a row that has weight only where e cannot be divided by: its
+// residual is not empty, so the target does not stand in for it.
 
 constexpr int kVerifyThreads = 256;
 constexpr int kVerifyBlocks = 5;   // a multiprocessor
 
 __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
+constexpr unsigned long long kWeightOnly = 1;   // < any candidate's key: indices stay below 2^30
+
 struct Best {
-    float v = 0.f;
+    float v = -1.f;   // below a quotient that underflows to zero
     int i = -1;
+    bool weight = false;   // some column has w > 0
     __device__ __forceinline__ void take(float w, float e, int idx) {
+        weight |= w > 0.f;
         const float bar = v * e * 0.999999f;
         if (w > 0.f && e > 0.f && (w >= bar || bar < 1e-30f)) {
             const float s = __fdiv_rn(w, e);
@@ -226,11 +232,13 @@ struct Best {
     }
 };
 
-// The block's best (value bits, ~index), 0 if it has none; in every thread of warp 0.
+// The block's best (value bits, ~index), kWeightOnly if no column with a weight has a positive e, 0 if no column
+// has a weight; in every thread of warp 0.
 __device__ __forceinline__ unsigned long long block_best(const Best& m) {
     __shared__ unsigned long long wk[kVerifyThreads / 32];
     unsigned long long k =
-        m.i < 0 ? 0ull : (static_cast<unsigned long long>(__float_as_uint(m.v)) << 32) | (0xffffffffu - m.i);
+        m.i < 0 ? (m.weight ? kWeightOnly : 0ull)
+                : (static_cast<unsigned long long>(__float_as_uint(m.v)) << 32) | (0xffffffffu - m.i);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         const unsigned long long x = __shfl_xor_sync(0xffffffffu, k, o);
@@ -390,8 +398,8 @@ __global__ void __launch_bounds__(kVerifyThreads, kVerifyBlocks) verify_kernel(V
         if (j != acc) out[j] = j < acc ? load(a.tokens + c0 + j) : -1;
     if (t == 0) {
         a.accepted[b] = acc;
-        out[acc] = best != 0 ? static_cast<int>(0xffffffffu - static_cast<unsigned>(best)) : -1;
-        if (best == 0) atomicExch(a.status, kStatusBadInput);   // no column of the row has a positive weight
+        out[acc] = best > kWeightOnly ? static_cast<int>(0xffffffffu - static_cast<unsigned>(best)) : -1;
+        if (best <= kWeightOnly) atomicExch(a.status, kStatusBadInput);   // no column can be chosen
     }
 }
 
