@@ -88,11 +88,13 @@ struct Place {
 };
 
 // The cosines and sines of a token, 16 bytes a lane each, in a ring stage.  Lanes past
-// the rotated dims keep (1, 0), set once.
+// the rotated dims keep (1, 0), set once; the others are left to the copies, which nothing
+// would order behind an ordinary store.
 template <int D>
 struct Table {
     static constexpr int BYTES = 2 * (D / 8) * 16;
-    __device__ __forceinline__ static void clear(uint8_t* at, int l) {
+    __device__ __forceinline__ static void clear(uint8_t* at, const RopeArgs& a, int l) {
+        if (l < (a.rot >> 3)) return;
         *reinterpret_cast<float4*>(at + l * 16) = make_float4(1.f, 1.f, 1.f, 1.f);
         *reinterpret_cast<float4*>(at + BYTES / 2 + l * 16) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
@@ -215,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
     const Place<INTER> pl(a, l);
     const Share sh(parts);
     if (g == 0)
-        for (int i = 0; i < kFwdStages; ++i) Table<D>::clear(ring + i * UNIT + TAB, l);
+        for (int i = 0; i < kFwdStages; ++i) Table<D>::clear(ring + i * UNIT + TAB, a, l);
     grid_dep_wait();
     for (int part = sh.part; part < parts; part += sh.part_step) {
         const int h0 = part * R::RPU + g;   // row u of the group is head h0 + u GPW
@@ -343,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
     float* const sum = sums + warp * 2 * D;
     for (int i = lane; i < 2 * D; i += 32) sum[i] = 0.f;
     if (g == 0)
-        for (int i = 0; i < kBwdStages; ++i) Table<D>::clear(ring + i * UNIT + TAB, l);
+        for (int i = 0; i < kBwdStages; ++i) Table<D>::clear(ring + i * UNIT + TAB, a, l);
     const Place<INTER> pl(a, l);
     const Share sh(parts);
     grid_dep_wait();
