@@ -73,6 +73,10 @@ struct Quads {
     }
 };
 
+// Whether a lane's dims are turned.  The others pass, as they are: a turn by (1, 0) would take a
+// NaN or an infinity of one dim to another.
+__device__ __forceinline__ bool turned(const RopeArgs& a, int l) { return l < (a.rot >> 3); }
+
 // Where a lane's two quads sit in a row, and its share of the rotation at one
 // position.  A lane always holds whole pairs, so the rotation needs no exchange:
 // half-split pairs put the second quad R / 2 past the first; interleaved pairs, and
@@ -81,33 +85,29 @@ template <bool INTER>
 struct Place {
     int ia, ib;
     __device__ __forceinline__ Place(const RopeArgs& a, int l) {
-        const bool split = !INTER && l < (a.rot >> 3);
+        const bool split = !INTER && turned(a, l);
         ia = split ? 4 * l : 8 * l;
         ib = split ? 4 * l + (a.rot >> 1) : 8 * l + 4;
     }
 };
 
 // The cosines and sines of a token, 16 bytes a lane each, in a ring stage.  Lanes past
-// the rotated dims keep (1, 0), set once; the others are left to the copies, which nothing
-// would order behind an ordinary store.
+// the rotated dims have none.
 template <int D>
 struct Table {
     static constexpr int BYTES = 2 * (D / 8) * 16;
-    __device__ __forceinline__ static void clear(uint8_t* at, const RopeArgs& a, int l) {
-        if (l < (a.rot >> 3)) return;
-        *reinterpret_cast<float4*>(at + l * 16) = make_float4(1.f, 1.f, 1.f, 1.f);
-        *reinterpret_cast<float4*>(at + BYTES / 2 + l * 16) = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
     __device__ __forceinline__ static void fetch(uint8_t* at, const RopeArgs& a, int pos, int l) {
-        if (l >= (a.rot >> 3)) return;
+        if (!turned(a, l)) return;
         const size_t from = static_cast<size_t>(pos) * (a.rot >> 1) + 4 * l;
         cp_async16(at + l * 16, a.cos + from);
         cp_async16(at + BYTES / 2 + l * 16, a.sin + from);
     }
 };
 
-// BACK: the transposed rotation (the sine's sign flips).
-template <bool INTER, bool BACK>
+// BACK: the transposed rotation (the sine's sign flips).  PART: some lanes' dims pass.  Whole
+// rotations have kernels without that choice: at 32768 tokens of 32 + 2 x 8 heads of 128 it
+// costs them 2 us (129 against 127 forward, 212 against 209 back).
+template <bool INTER, bool BACK, bool PART>
 struct Turn {
     uint64_t c[INTER ? 4 : 2], s[INTER ? 4 : 2], t[INTER ? 1 : 2];
     __device__ __forceinline__ Turn(const uint8_t* cos, const uint8_t* sin) {
@@ -130,20 +130,22 @@ struct Turn {
             t[1] = BACK ? n1 : p1;
         }
     }
-    __device__ __forceinline__ void apply(uint64_t (&z)[4]) const {
+    __device__ __forceinline__ void apply(uint64_t (&z)[4], bool turns) const {
         if constexpr (INTER) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float lo, hi;
                 f32x2_split(z[i], lo, hi);
-                z[i] = fma_f32x2(f32x2(hi, lo), s[i], mul_f32x2(z[i], c[i]));
+                const uint64_t y = fma_f32x2(f32x2(hi, lo), s[i], mul_f32x2(z[i], c[i]));
+                z[i] = !PART || turns ? y : z[i];
             }
         } else {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const uint64_t x = z[i], y = z[i + 2];
-                z[i] = fma_f32x2(y, s[i], mul_f32x2(x, c[i]));
-                z[i + 2] = fma_f32x2(x, t[i], mul_f32x2(y, c[i]));
+                const uint64_t u = fma_f32x2(y, s[i], mul_f32x2(x, c[i])), v = fma_f32x2(x, t[i], mul_f32x2(y, c[i]));
+                z[i] = !PART || turns ? u : x;
+                z[i + 2] = !PART || turns ? v : y;
             }
         }
     }
@@ -203,7 +205,7 @@ constexpr int rope_fwd_unit() { return kFwdRows * 32 * 16 + Table<D>::BYTES; }  
 template <int D>
 constexpr int rope_fwd_smem() { return kWarps * kFwdStages * rope_fwd_unit<D>(); }
 
-template <int D, bool INTER, bool PAGED>
+template <int D, bool INTER, bool PAGED, bool PART>
 __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs a) {
     constexpr int kRows = kFwdRows;
     using R = Rows<D, kRows>;
@@ -215,9 +217,8 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
     uint8_t* const ring = sm + warp_id() * kFwdStages * UNIT;
     const int mine = g * (R::LPR * 16);   // the group's row within 512 bytes
     const Place<INTER> pl(a, l);
+    const bool turns = turned(a, l);
     const Share sh(parts);
-    if (g == 0)
-        for (int i = 0; i < kFwdStages; ++i) Table<D>::clear(ring + i * UNIT + TAB, a, l);
     grid_dep_wait();
     for (int part = sh.part; part < parts; part += sh.part_step) {
         const int h0 = part * R::RPU + g;   // row u of the group is head h0 + u GPW
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
             const uint8_t* const stage = ring + st * UNIT;
             st = st + 1 == kFwdStages ? 0 : st + 1;
             if (!((good >> (kFwdStages - 1)) & 1u)) continue;
-            const Turn<INTER, false> turn(stage + TAB + l * 16, stage + TAB + Table<D>::BYTES / 2 + l * 16);
+            const Turn<INTER, false, PART> turn(stage + TAB + l * 16, stage + TAB + Table<D>::BYTES / 2 + l * 16);
             long long at_q, at_kv;   // the token's offset in Q, and in K and V
             if constexpr (PAGED) {
                 at_q = t * a.Hq * D;
@@ -298,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
                     const uint64_t r = dup2(rsqrtf(R::sum(sum2(ss), group) * (1.f / D) + a.eps));
 #pragma unroll
                     for (int i = 0; i < 4; ++i) z[i] = mul_f32x2(mul_f32x2(z[i], r), wf[i]);
-                    turn.apply(z);
+                    turn.apply(z, turns);
                     q.pack(z);
                     q.store(out[u] + (h < a.Hq ? at_q : at_kv), pl.ia, pl.ib);
                 } else if (h < H) {   // values pass through
@@ -327,7 +328,7 @@ constexpr int rope_bwd_unit() { return 2 * kBwdRows * 32 * 16 + Table<D>::BYTES;
 template <int D>
 constexpr int rope_bwd_smem() { return kWarps * (kBwdStages * rope_bwd_unit<D>() + 2 * D * 4); }
 
-template <int D, bool INTER>
+template <int D, bool INTER, bool PART>
 __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs a) {
     constexpr int kRows = kBwdRows;
     using R = Rows<D, kRows>;
@@ -344,9 +345,8 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
     float* const sums = reinterpret_cast<float*>(sm + kWarps * kBwdStages * UNIT);   // [kWarps][2 D]
     float* const sum = sums + warp * 2 * D;
     for (int i = lane; i < 2 * D; i += 32) sum[i] = 0.f;
-    if (g == 0)
-        for (int i = 0; i < kBwdStages; ++i) Table<D>::clear(ring + i * UNIT + TAB, a, l);
     const Place<INTER> pl(a, l);
+    const bool turns = turned(a, l);
     const Share sh(parts);
     grid_dep_wait();
     for (int part = sh.part; part < parts; part += sh.part_step) {
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
             const uint8_t* const stage = ring + st * UNIT;
             st = st + 1 == kBwdStages ? 0 : st + 1;
             if (!((good >> (kBwdStages - 1)) & 1u)) continue;
-            const Turn<INTER, true> turn(stage + TAB + l * 16, stage + TAB + Table<D>::BYTES / 2 + l * 16);
+            const Turn<INTER, true, PART> turn(stage + TAB + l * 16, stage + TAB + Table<D>::BYTES / 2 + l * 16);
             bf16* const dst = a.dqkv + t * a.ld_d + h0 * D;
 #pragma unroll
             for (int u = 0; u < kRows; ++u) {
@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
 #pragma unroll
                     for (int i = 1; i < 4; ++i) ss = fma_f32x2(xf[i], xf[i], ss);
                     const uint64_t r = dup2(rsqrtf(R::sum(sum2(ss), group) * (1.f / D) + a.eps));
-                    turn.apply(z);
+                    turn.apply(z, turns);
                     uint64_t dot = 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -502,25 +502,43 @@ int blocks_for(const RopeArgs& a, int most, int tokens) {
     return static_cast<int>(need < most ? need : most);
 }
 
-template <int D, bool INTER, bool PAGED>
+template <int D, bool INTER, bool PAGED, bool PART>
 cudaError_t launch_fwd(const RopeArgs& a, const KernelEnv& env) {
-    const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(rope_fwd_kernel<D, INTER, PAGED>), rope_fwd_smem<D>(), true);
+    const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(rope_fwd_kernel<D, INTER, PAGED, PART>), rope_fwd_smem<D>(), true);
     if (e != cudaSuccess) return e;
-    return launch_early(rope_fwd_kernel<D, INTER, PAGED>, dim3(blocks_for<D, kFwdRows>(a, kFwdBlocks * device_sm_count(), 1)), kThreads,
+    return launch_early(rope_fwd_kernel<D, INTER, PAGED, PART>, dim3(blocks_for<D, kFwdRows>(a, kFwdBlocks * device_sm_count(), 1)), kThreads,
                         rope_fwd_smem<D>(), env.stream, a);
 }
 
-template <int D, bool INTER>
+template <int D, bool INTER, bool PART>
 cudaError_t launch_bwd(const RopeArgs& a, const KernelEnv& env) {
-    const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(rope_bwd_kernel<D, INTER>), rope_bwd_smem<D>(), true);
+    const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(rope_bwd_kernel<D, INTER, PART>), rope_bwd_smem<D>(), true);
     if (e != cudaSuccess) return e;
-    return launch_early(rope_bwd_kernel<D, INTER>, dim3(blocks_for<D, kBwdRows>(a, rope_bwd_max_blocks(), 4)), kThreads,
+    return launch_early(rope_bwd_kernel<D, INTER, PART>, dim3(blocks_for<D, kBwdRows>(a, rope_bwd_max_blocks(), 4)), kThreads,
                         rope_bwd_smem<D>(), env.stream, a);
 }
 
 template <int D, bool INTER>
 cudaError_t launch_any_fwd(const RopeArgs& a, const KernelEnv& env) {
-    return a.slots != nullptr ? launch_fwd<D, INTER, true>(a, env) : launch_fwd<D, INTER, false>(a, env);
+    if (a.rot < D) return a.slots != nullptr ? launch_fwd<D, INTER, true, true>(a, env) : launch_fwd<D, INTER, false, true>(a, env);
+    return a.slots != nullptr ? launch_fwd<D, INTER, true, false>(a, env) : launch_fwd<D, INTER, false, false>(a, env);
+}
+
+template <int D, bool INTER>
+cudaError_t launch_any_bwd(const RopeArgs& a, const KernelEnv& env) {
+    return a.rot < D ? launch_bwd<D, INTER, true>(a, env) : launch_bwd<D, INTER, false>(a, env);
+}
+
+template <int D>
+cudaError_t prepare_fwd() {
+    const void* kernels[] = {reinterpret_cast<const void*>(rope_fwd_kernel<D, true, true, true>),
+                             reinterpret_cast<const void*>(rope_fwd_kernel<D, true, true, false>),
+                             reinterpret_cast<const void*>(rope_fwd_kernel<D, false, true, true>),
+                             reinterpret_cast<const void*>(rope_fwd_kernel<D, false, true, false>)};
+    cudaError_t e = cudaSuccess;
+    for (const void* k : kernels)
+        if (e == cudaSuccess) e = ensure_smem_attr(k, rope_fwd_smem<D>(), true);
+    return e;
 }
 
 }  // namespace
@@ -541,15 +559,7 @@ bool rope_supported(const RopeArgs& a) { return a.T <= 0x7fffffffLL; }
 int rope_bwd_max_blocks() { return kBwdBlocks * device_sm_count(); }   // all resident
 
 cudaError_t rope_paged_prepare(int d) {
-    auto set = [](const void* f, int smem) { return ensure_smem_attr(f, smem, true); };
-    cudaError_t e = cudaSuccess;
-    if (d == 128) {
-        e = set(reinterpret_cast<const void*>(rope_fwd_kernel<128, true, true>), rope_fwd_smem<128>());
-        if (e == cudaSuccess) e = set(reinterpret_cast<const void*>(rope_fwd_kernel<128, false, true>), rope_fwd_smem<128>());
-    } else {
-        e = set(reinterpret_cast<const void*>(rope_fwd_kernel<64, true, true>), rope_fwd_smem<64>());
-        if (e == cudaSuccess) e = set(reinterpret_cast<const void*>(rope_fwd_kernel<64, false, true>), rope_fwd_smem<64>());
-    }
+    cudaError_t e = d == 128 ? prepare_fwd<128>() : prepare_fwd<64>();
     return e;
 }
 
@@ -560,8 +570,8 @@ cudaError_t launch_rope_fwd(const RopeArgs& a, int d, const KernelEnv& env) {
 }
 
 cudaError_t launch_rope_bwd(const RopeArgs& a, int d, const KernelEnv& env) {
-    if (d == 128) return a.interleaved ? launch_bwd<128, true>(a, env) : launch_bwd<128, false>(a, env);
-    if (d == 64) return a.interleaved ? launch_bwd<64, true>(a, env) : launch_bwd<64, false>(a, env);
+    if (d == 128) return a.interleaved ? launch_any_bwd<128, true>(a, env) : launch_any_bwd<128, false>(a, env);
+    if (d == 64) return a.interleaved ? launch_any_bwd<64, true>(a, env) : launch_any_bwd<64, false>(a, env);
     return cudaErrorInvalidValue;
 }
 
