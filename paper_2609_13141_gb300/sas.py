@@ -238,6 +238,19 @@ def _refuse(t, dtype, name, dev, shape):
         raise ValueError(f"{name} must be on device {dev}")
 
 
+class _Handle(ctypes.c_void_p):
+    """A handle with the sizes it was made with, which the tensors of its calls are compared with: the library takes
+    addresses and goes by its own sizes."""
+    sizes = None
+
+
+def _sizes(h):
+    sizes = getattr(h, "sizes", None)
+    if sizes is None:
+        raise SasError(SAS_ERR_INVALID_ARG, "the handle must be one that sas_create or sas_chunk_create returned, not closed")
+    return sizes
+
+
 def _rope_config(cos, eps, interleaved):
     try:
         max_pos, half = cos.shape
@@ -304,8 +317,9 @@ def sas_create(B, H, N, d, topk, mode=SAS_MODE_TRAIN_SOFT, selector=SAS_SEL_SCOR
                max_seqlen=0, scope=SAS_SCOPE_SPARSE):
     cfg = SasConfig(B, H, N, d, block, topk, sm_scale, mode, selector, d_sel, gate_act, gate_pos, Hkv, max_seqs,
                     max_seqlen, scope)
-    h = ctypes.c_void_p()
+    h = _Handle()
     _check(lib().sas_create(ctypes.byref(cfg), ctypes.byref(h)), None, "sas_create")
+    h.sizes = B, H, Hkv or H, N, d
     return h
 
 
@@ -373,13 +387,13 @@ def sas_attention_bwd(h, Q, K, V, O, LSE, dO, dQ, dK, dV, scores=None, sel_idx=N
 
 def sas_qk_norm_rope_fwd(h, qkv, wq, wk, cos, sin, Q, K, V, positions=None, eps=1e-6, interleaved=False, stream=None):
     """qkv [B, N, H + 2 Hkv, d] (tokens evenly spaced, any distance) to Q [B, H, N, d], K and V [B, Hkv, N, d]."""
-    B, H, N, d = Q.shape
-    Hkv, dev, bf, f32 = K.shape[1], Q.get_device(), torch.bfloat16, torch.float32
+    B, H, Hkv, N, d = _sizes(h)
+    dev, bf, f32 = Q.get_device(), torch.bfloat16, torch.float32
     cfg = _rope_config(cos, eps, interleaved)
     st = lib().sas_qk_norm_rope_fwd(
         h, cfg, _rows(qkv, bf, "qkv", dev, (B, N, H + 2 * Hkv, d)), _token_stride(qkv, "qkv", 2),
         _arg(wq, bf, "wq", dev, (d,)), _arg(wk, bf, "wk", dev, (d,)), _arg(cos, f32, "cos", dev), _arg(sin, f32, "sin", dev, cos.shape),
-        None if positions is None else _arg(positions, torch.int32, "positions", dev, (B, N)), _arg(Q, bf, "Q", dev),
+        None if positions is None else _arg(positions, torch.int32, "positions", dev, (B, N)), _arg(Q, bf, "Q", dev, (B, H, N, d)),
         _arg(K, bf, "K", dev, (B, Hkv, N, d)), _arg(V, bf, "V", dev, (B, Hkv, N, d)), _raw_stream(stream, dev))
     if st != SAS_OK:
         _check(st, h, "sas_qk_norm_rope_fwd")
@@ -388,14 +402,14 @@ def sas_qk_norm_rope_fwd(h, qkv, wq, wk, cos, sin, Q, K, V, positions=None, eps=
 def sas_qk_norm_rope_bwd(h, qkv, wq, wk, cos, sin, dQ, dK, dV, dqkv, dwq, dwk, positions=None, eps=1e-6,
                          interleaved=False, stream=None):
     """Gradients of sas_qk_norm_rope_fwd: dqkv like qkv, dwq and dwk fp32 [d]."""
-    B, H, N, d = dQ.shape
-    Hkv, dev, bf, f32 = dK.shape[1], dQ.get_device(), torch.bfloat16, torch.float32
+    B, H, Hkv, N, d = _sizes(h)
+    dev, bf, f32 = dQ.get_device(), torch.bfloat16, torch.float32
     rows = (B, N, H + 2 * Hkv, d)
     cfg = _rope_config(cos, eps, interleaved)
     st = lib().sas_qk_norm_rope_bwd(
         h, cfg, _rows(qkv, bf, "qkv", dev, rows), _token_stride(qkv, "qkv", 2), _arg(wq, bf, "wq", dev, (d,)),
         _arg(wk, bf, "wk", dev, (d,)), _arg(cos, f32, "cos", dev), _arg(sin, f32, "sin", dev, cos.shape),
-        None if positions is None else _arg(positions, torch.int32, "positions", dev, (B, N)), _arg(dQ, bf, "dQ", dev),
+        None if positions is None else _arg(positions, torch.int32, "positions", dev, (B, N)), _arg(dQ, bf, "dQ", dev, (B, H, N, d)),
         _arg(dK, bf, "dK", dev, (B, Hkv, N, d)), _arg(dV, bf, "dV", dev, (B, Hkv, N, d)), _rows(dqkv, bf, "dqkv", dev, rows),
         _token_stride(dqkv, "dqkv", 2), _arg(dwq, f32, "dwq", dev, (d,)), _arg(dwk, f32, "dwk", dev, (d,)),
         _raw_stream(stream, dev))
@@ -578,21 +592,12 @@ class SasLayer:
                 Q = torch.empty(self.B, self.H, self.N, self.d, device=qkv.device, dtype=torch.bfloat16)
                 K = torch.empty(self.B, self.Hkv, self.N, self.d, device=qkv.device, dtype=torch.bfloat16)
                 out = (Q, K, torch.empty_like(K))
-        else:
-            self._heads("Q", out[0], self.H)
-            self._heads("K", out[1], self.Hkv)
         sas_qk_norm_rope_fwd(self.h, qkv, wq, wk, cos, sin, *out, positions, eps, interleaved, stream)
         return out
-
-    def _heads(self, name, t, heads):
-        if t.shape != (self.B, heads, self.N, self.d):
-            raise ValueError(f"{name} must have shape {(self.B, heads, self.N, self.d)}, got {tuple(t.shape)}")
 
     def qk_norm_rope_bwd(self, qkv, wq, wk, cos, sin, dQ, dK, dV, positions=None, eps=1e-6, interleaved=False, out=None,
                          stream=None):
         """Returns (dqkv [B, N, H + 2 Hkv, d] bf16, dwq, dwk fp32 [d]); out reuses the caller's."""
-        self._heads("dQ", dQ, self.H)
-        self._heads("dK", dK, self.Hkv)
         if out is None:
             with _on(stream):
                 dqkv = torch.empty(qkv.shape, device=qkv.device, dtype=torch.bfloat16)
@@ -749,8 +754,9 @@ def _ccheck(status, handle, what):
 
 def sas_chunk_create(max_seqs, Hq, Hkv, d, max_blocks, num_pages, max_tokens, sm_scale=0.0, block=64):
     cfg = SasChunkConfig(max_seqs, Hq, Hkv, d, block, max_blocks, num_pages, max_tokens, sm_scale)
-    h = ctypes.c_void_p()
+    h = _Handle()
     _ccheck(lib().sas_chunk_create(ctypes.byref(cfg), ctypes.byref(h)), None, "sas_chunk_create")
+    h.sizes = Hq, d, max_blocks, (num_pages, Hkv, block, d)
     return h
 
 
@@ -768,11 +774,15 @@ def sas_chunk_destroy(h):
     lib().sas_chunk_destroy(h)
 
 
+def _table(h, block_table, B):
+    if block_table.shape != (B, _sizes(h)[2]):
+        raise ValueError(f"block_table must have {B} rows and {_sizes(h)[2]} columns, got {tuple(block_table.shape)}")
+
+
 def sas_chunk_plan(h, seq_lens, new_lens, free_pages, free_begin, block_table, kv_lens, cu_new, positions, slots,
                    free_end, held_lens=None, stream=None):
     i32, B, T, dev = torch.int32, seq_lens.shape[0], positions.shape[0], seq_lens.get_device()
-    if block_table.dim() != 2 or block_table.shape[0] != B:
-        raise ValueError(f"block_table must have {B} rows")
+    _table(h, block_table, B)
     st = lib().sas_chunk_plan(
         h, B, T, _arg(seq_lens, i32, "seq_lens", dev, (B,)), _arg(new_lens, i32, "new_lens", dev, (B,)),
         None if held_lens is None else _arg(held_lens, i32, "held_lens", dev, (B,)),
@@ -787,25 +797,26 @@ def sas_chunk_plan(h, seq_lens, new_lens, free_pages, free_begin, block_table, k
 def sas_chunk_append(h, qkv, wq, wk, cos, sin, positions, slots, Q, K_cache, V_cache, eps=1e-6, interleaved=False,
                      stream=None):
     """qkv [T, Hq + 2 Hkv, d] (tokens evenly spaced, any distance)."""
-    T, Hq, d = Q.shape
-    Hkv, dev, bf, f32 = K_cache.shape[1], Q.get_device(), torch.bfloat16, torch.float32
+    Hq, d, _, cache = _sizes(h)
+    T, Hkv, dev, bf, f32 = Q.shape[0], cache[1], Q.get_device(), torch.bfloat16, torch.float32
     cfg = _rope_config(cos, eps, interleaved)
     st = lib().sas_chunk_append(
         h, cfg, T, _rows(qkv, bf, "qkv", dev, (T, Hq + 2 * Hkv, d)), _token_stride(qkv, "qkv", 1),
         _arg(wq, bf, "wq", dev, (d,)), _arg(wk, bf, "wk", dev, (d,)), _arg(cos, f32, "cos", dev), _arg(sin, f32, "sin", dev, cos.shape),
         _arg(positions, torch.int32, "positions", dev, (T,)), _arg(slots, torch.int64, "slots", dev, (T,)),
-        _arg(Q, bf, "Q", dev), _arg(K_cache, bf, "K_cache", dev), _arg(V_cache, bf, "V_cache", dev, K_cache.shape), _raw_stream(stream, dev))
+        _arg(Q, bf, "Q", dev, (T, Hq, d)), _arg(K_cache, bf, "K_cache", dev, cache), _arg(V_cache, bf, "V_cache", dev, cache),
+        _raw_stream(stream, dev))
     if st != SAS_OK:
         _ccheck(st, h, "sas_chunk_append")
 
 
 def sas_chunk_attention(h, Q, K_cache, V_cache, block_table, cu_new, kv_lens, O, LSE=None, stream=None):
-    i32, bf, B, dev = torch.int32, torch.bfloat16, kv_lens.shape[0], Q.get_device()
-    if block_table.dim() != 2 or block_table.shape[0] != B:
-        raise ValueError(f"block_table must have {B} rows")
+    i32, bf, B, T, dev = torch.int32, torch.bfloat16, kv_lens.shape[0], Q.shape[0], Q.get_device()
+    _table(h, block_table, B)
+    Hq, d, _, cache = _sizes(h)
     st = lib().sas_chunk_attention(
-        h, B, Q.shape[0], _arg(Q, bf, "Q", dev), _arg(K_cache, bf, "K_cache", dev),
-        _arg(V_cache, bf, "V_cache", dev, K_cache.shape), _arg(block_table, i32, "block_table", dev),
+        h, B, T, _arg(Q, bf, "Q", dev, (T, Hq, d)), _arg(K_cache, bf, "K_cache", dev, cache),
+        _arg(V_cache, bf, "V_cache", dev, cache), _arg(block_table, i32, "block_table", dev),
         _arg(cu_new, i32, "cu_new", dev, (B + 1,)), _arg(kv_lens, i32, "kv_lens", dev, (B,)), _arg(O, bf, "O", dev, Q.shape),
         None if LSE is None else _arg(LSE, torch.float32, "LSE", dev, Q.shape[:2]), _raw_stream(stream, dev))
     if st != SAS_OK:
@@ -886,19 +897,10 @@ class SasChunk:
                          torch.empty(T, device=device, dtype=i32), torch.empty(T, device=device, dtype=torch.int64),
                          torch.empty(1, device=device, dtype=i32))
 
-    def _table(self, block_table):
-        if block_table.dim() != 2 or block_table.shape[1] != self.max_blocks:
-            raise ValueError(f"block_table must have {self.max_blocks} columns")
-
-    def _caches(self, K_cache):
-        if K_cache.shape != self.cache_shape:
-            raise ValueError(f"K_cache must have shape {self.cache_shape}, got {tuple(K_cache.shape)}")
-
     def plan(self, seq_lens, new_lens, free_pages, free_begin, block_table, T, held_lens=None, out=None, stream=None):
         """Pages and slots of the new tokens: a ChunkPlan; block_table gets the new pages.  T: capacity for new
         tokens (positions and slots are -1 past their number).  held_lens: tokens whose pages each request holds
         (seq_lens if not given)."""
-        self._table(block_table)
         if out is None:
             with _on(stream):
                 out = self.plan_buffers(seq_lens.shape[0], T, seq_lens.device)
@@ -911,22 +913,15 @@ class SasChunk:
                stream=None):
         """Norm + rotation of the new tokens' queries and keys; keys and values into the cache.  Returns Q
         [T, Hq, d] (rows of slot -1 are not written)."""
-        self._caches(K_cache)
         if out is None:
             with _on(stream):
                 out = torch.empty(qkv.shape[0], self.Hq, self.d, device=qkv.device, dtype=torch.bfloat16)
-        elif out.dim() != 3 or out.shape[1] != self.Hq or out.shape[2] != self.d:
-            raise ValueError(f"out must have shape [T, {self.Hq}, {self.d}]")
         sas_chunk_append(self.h, qkv, wq, wk, cos, sin, positions, slots, out, K_cache, V_cache, eps, interleaved, stream)
         return out
 
     def attention(self, Q, K_cache, V_cache, block_table, cu_new, kv_lens, out=None, stream=None):
         """Dense causal attention of the new tokens.  Returns (O [T, Hq, d], LSE [T, Hq]); out = (O, LSE) reuses
         caller buffers (LSE may be None)."""
-        self._table(block_table)
-        self._caches(K_cache)
-        if Q.dim() != 3 or Q.shape[1] != self.Hq or Q.shape[2] != self.d:
-            raise ValueError(f"Q must have shape [T, {self.Hq}, {self.d}]")
         if out is None:
             with _on(stream):
                 out = (torch.empty_like(Q), torch.empty(Q.shape[:2], device=Q.device, dtype=torch.float32))
