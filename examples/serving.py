@@ -65,17 +65,24 @@ class Server:
 
     def enter(self, qkv, new_lens):
         """The new tokens of every request (rows of qkv in request order, `new_lens` each; spare rows at the end) into
-        the cache.  Returns the plan and the queries."""
+        the cache.  Returns the plan and the queries.
+
+        A plan that does not fit (no pages left, a request past its table) is refused whole, and the status word of
+        the handle says so: the lengths and pages stay, and self.entered, the tokens that the last plan let in, is zero.
+        Rows of no token are zero."""
         p = self.step.plan(self.lens, new_lens, self.free, self.taken, self.table, qkv.shape[0], held_lens=self.held)
-        Q = self.step.append(qkv, self.wq, self.wk, self.cos, self.sin, p.positions, p.slots, self.K, self.V)
-        self.lens, self.taken = p.kv_lens, p.free_end
+        Q = torch.zeros(qkv.shape[0], *self.shape[::2], device=self.dev, dtype=BF)
+        self.step.append(qkv, self.wq, self.wk, self.cos, self.sin, p.positions, p.slots, self.K, self.V, out=Q)
+        self.lens, self.taken, self.entered = p.kv_lens, p.free_end, p.cu_new[-1]
         self.held = torch.maximum(self.held, self.lens)
         return p, Q
 
     def forward(self, qkv, new_lens):
         """enter(), and the dense attention of the new tokens."""
         p, Q = self.enter(qkv, new_lens)
-        return self.step.attention(Q, self.K, self.V, self.table, p.cu_new, p.kv_lens)[0]
+        O = torch.zeros_like(Q)
+        self.step.attention(Q, self.K, self.V, self.table, p.cu_new, p.kv_lens, out=(O, None))
+        return O
 
     def summarize(self):
         """The selector's summaries of the full blocks, which steps of several tokens leave to this call."""
@@ -83,7 +90,8 @@ class Server:
 
     def prefill(self, prompts):
         """Prompts (a [tokens, heads, d] projection each) in steps of at most `chunk` tokens over all requests.
-        Returns each prompt's attention output."""
+        Returns each prompt's attention output.  Raises RuntimeError when a step is refused (the host waits for each
+        step's plan); the steps before it stand, and self.lens counts their tokens."""
         done, out = [0] * len(prompts), [[] for _ in prompts]
         while any(d < p.shape[0] for d, p in zip(done, prompts)):
             room, take = self.chunk, []
@@ -92,6 +100,9 @@ class Server:
                 room -= take[-1]
             qkv = torch.cat([p[d:d + n] for p, d, n in zip(prompts, done, take)])
             O = self.forward(qkv, torch.tensor(take, device=self.dev, dtype=I32))
+            if int(self.entered) != sum(take):
+                self.summarize()
+                raise RuntimeError("no pages, or no room in a request's table, for a chunk of the prompts")
             at = 0
             for b, n in enumerate(take):
                 out[b].append(O[at:at + n])
@@ -101,14 +112,15 @@ class Server:
         return [torch.cat(o) for o in out]
 
     def decode(self, qkv):
-        """One token per request with SAS selection.  qkv [requests, heads, d]."""
+        """One token per request with SAS selection.  qkv [requests, heads, d].  A refused step gives zeros."""
         p, Q = self.enter(qkv, torch.ones_like(self.lens))
         O, _, kept = self.dec.step(Q, self.K, self.V, self.table, p.kv_lens, Wq=self.sel_q, Wk=self.sel_k, Ksum=self.Ksum)
-        return O, kept
+        return torch.where(self.entered > 0, O, 0), kept
 
     def drafted(self, qkv, drafts, draft_probs, target_probs_of):
         """A step over `drafts` [requests, n] and the token before them: target_probs_of(O) gives the n + 1 target
-        rows of every request.  Keeps the accepted tokens; returns (accepted, tokens)."""
+        rows of every request.  Keeps the accepted tokens; returns (accepted, tokens): 0 and -1 throughout from a
+        refused step, which keeps nothing.  The drafts are attended densely, also where decode() would select."""
         B, n = drafts.shape
         lens = self.lens
         O = self.forward(qkv, torch.full_like(lens, n + 1))
@@ -117,9 +129,11 @@ class Server:
         u = torch.rand(B * n, generator=self.g, device=self.dev)
         noise = torch.empty(B, target.shape[1], device=self.dev).exponential_(1, generator=self.g)
         accepted, tokens = self.step.verify(drafts.reshape(-1), cu, target, draft_probs, u, noise, n)
+        granted = self.entered > 0
+        accepted, tokens = torch.where(granted, accepted, 0), torch.where(granted, tokens, -1)
         # the cache keeps the token before the drafts and the accepted ones; pages opened for the rest stay
         # with the request, and their slots are written again by the next step
-        self.lens = lens + 1 + accepted
+        self.lens = lens + (1 + accepted) * granted
         self.summarize()
         return accepted, tokens
 
