@@ -162,9 +162,7 @@ struct Rows {
         for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(group, v, o);
         return v;
     }
-    __device__ __forceinline__ static unsigned group_mask(int g) {
-        return (LPR == 32 ? 0xffffffffu : (1u << LPR) - 1u) << (g * LPR);
-    }
+    __device__ __forceinline__ static unsigned group_mask(int g) { return ((1u << LPR) - 1u) << (g * LPR); }
 };
 
 // How the warps share the work: a part (RPU neighbouring heads of the fused row) per
