@@ -310,7 +310,7 @@ sas_status sas_attention_fwd_varlen(sas_handle* h, const int32_t* cu_seqlens, in
  *   xh = x / sqrt(mean(x^2) + eps),  z = w xh,  y = R_p z,
  * R_p rotating pair i of the first `rot` dims, y_a = z_a c - z_b s, y_b = z_b c
  * + z_a s with c = cos[p][i], s = sin[p][i]; pair i is (i, i + rot / 2), or (2i,
- * 2i + 1) when interleaved; dims past rot pass.  Value rows pass unchanged.
+ * 2i + 1) when interleaved; dims past rot pass, each alone.  Value rows pass unchanged.
  * fp32 arithmetic, one rounding to bf16. */
 typedef struct {
     int32_t rot;          /* rotated dims of a head: a multiple of 16, 16 .. d            */
@@ -672,7 +672,10 @@ sas_status sas_chunk_append(sas_chunk_handle* h, const sas_rope_config* rope, in
  *   cu_new       int32 [num_seqs + 1]; kv_lens int32 [num_seqs]               (in)
  *   O            bf16 [T, Hq, d]; LSE fp32 [T, Hq] natural log, or NULL       (out)
  * Rows past cu_new[num_seqs] are not written; requests without new tokens cost
- * nothing.  What a page holds past a request's end does not matter.  Offsets that
+ * nothing.  What a page holds past a request's end does not matter.  A NaN score makes
+ * the row's O and LSE NaN.  A new token's value that is not finite also reaches rows
+ * before it, as NaN in its columns: those of the same 128 / (Hq / Hkv) neighbouring
+ * tokens of the chunk, in whose product its weight is 0 (keys do not).  Offsets that
  * decrease or leave 0 .. T: nothing is computed; n > kv_lens[b] or kv_lens[b] > 64
  * max_blocks: that request is skipped; a page index outside the cache reads as zero
  * keys and values; each with status SAS_ERR_INVALID_ARG.  Two launches. */

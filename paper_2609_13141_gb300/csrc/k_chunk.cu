@@ -31,7 +31,8 @@
 //
 // Keys past a sequence's end in its last page may hold anything: scores there are
 // replaced, not weighted by zero, and values past the tile's last position are
-// zeroed in shared memory before the product.  A table entry out of range is never
+// zeroed in shared memory before the product.  (A value of the tile's own later tokens that
+// is not finite does reach the rows that do not see it, as 0 times it.)  A table entry out of range is never
 // used as an address: it becomes the row past the cache, which TMA reads as zero.
 #include <math_constants.h>
 

@@ -18,8 +18,8 @@
 // the same heads for all its tokens (their kinds, weights and addresses are then
 // fixed), rows stream through a ring in shared memory (cp.async, no registers held
 // while they are in flight), and the arithmetic runs on packed fp32 pairs.  Measured:
-// 6.4 TB/s forward (128 us for 32768 tokens of 32 + 2 x 8 heads of 128, and as much into
-// cache pages), 5.5 TB/s for the gradient (211 us), where a row is read twice as much
+// 6.4 TB/s forward (127 us for 32768 tokens of 32 + 2 x 8 heads of 128, and as much into
+// cache pages), 5.5 TB/s for the gradient (206 to 211 us), where a row is read twice as much
 // as written and the waits for shared memory and reductions show.  One or two more
 // stages of the rings are slower (158 us forward with three): the warps drift apart and
 // DRAM pages are opened more often.
@@ -317,9 +317,9 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
 //
 // Values cost no arithmetic.  Where neighbouring rows would give some warps nothing else,
 // which end early, a warp's rows come half from the front of the fused row and half from
-// its back (32768 tokens of 32 + 2 x 8 heads: 207 against 211 us; 58701 of 2 + 2 x 2: 58
-// against 64), elsewhere in one piece (46113 of 4 + 2 x 1: 57.5 against 59.2).  The forward
-// kernel reads its row better in one piece (129 against 133 us at 32768 tokens).
+// its back (32768 tokens of 32 + 2 x 8 heads: 209 against 216 us; 58701 of 2 + 2 x 2: 52
+// against 58), elsewhere in one piece (46113 of 4 + 2 x 1: 51.5 against 53.1).  The forward
+// kernel reads its row better in one piece (by 3% at 32768 tokens).
 constexpr int kBwdRows = 2, kBwdStages = 3, kBwdBlocks = 2;
 template <int D>
 constexpr int rope_bwd_unit() { return 2 * kBwdRows * 32 * 16 + Table<D>::BYTES; }
