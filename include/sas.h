@@ -417,6 +417,35 @@ const char* sas_last_error(const sas_handle* h);
  * device first. */
 sas_status sas_get_device_status(sas_handle* h, int32_t* out_status);
 
+/* Log probabilities of given tokens, for a loss or a policy gradient, with the rows'
+ * entropy; V columns, of any handle (rows are not the layer's tokens).
+ *   T        rows, 1 .. 2^26
+ *   logits   SAS_DTYPE_BF16 or SAS_DTYPE_FP32 [T] rows of V, ld elements apart (ld >=
+ *            V; any alignment of the type)                                     (in)
+ *   tokens   int32 [T]; -1: the row does not count                            (in)
+ *   logprob  fp32 [T]  logits[t, tokens[t]] - lse                             (out)
+ *   entropy  fp32 [T]  -sum_v p log p                                         (out)
+ *   lse      fp32 [T]  log sum_v exp logits                                   (out)
+ * Rows of token -1 are not read and give zeros; so do rows of another token outside 0 ..
+ * V - 1, with status SAS_ERR_INVALID_ARG.  Columns of -infinity have probability 0; a
+ * row of nothing else has lse -infinity, the others NaN.  A NaN or +infinity makes the
+ * row's three results NaN.  Everything is fp32 from the logits on.  One launch. */
+#define SAS_DTYPE_BF16 0
+#define SAS_DTYPE_FP32 1
+sas_status sas_token_logprobs(sas_handle* h, int32_t T, int32_t V, const void* logits, int32_t dtype, int64_t ld,
+                              const int32_t* tokens, float* logprob, float* entropy, float* lse, void* stream);
+
+/* Its gradient: dlogits = dlogprob (onehot(token) - p) - dentropy p (log p + entropy),
+ * rounded once to the logits' type.
+ *   lse, entropy        fp32 [T] of the forward                               (in)
+ *   dlogprob, dentropy  fp32 [T]; dentropy may be NULL (0)                    (in)
+ *   dlogits  [T] rows of V, ld_d apart: the logits' own memory (ld_d = ld) or memory
+ *            apart from it                                                    (out)
+ * Rows that do not count get zeros.  One launch. */
+sas_status sas_token_logprobs_bwd(sas_handle* h, int32_t T, int32_t V, const void* logits, int32_t dtype, int64_t ld,
+                                  const int32_t* tokens, const float* lse, const float* entropy, const float* dlogprob,
+                                  const float* dentropy, void* dlogits, int64_t ld_d, void* stream);
+
 /* Per-kernel timing with CUDA events recorded on the launch stream around
  * every kernel.  sas_set_timing(h, 1) starts recording (and clears earlier
  * records); sas_get_timings synchronises, then writes, for each kernel kind,
@@ -424,8 +453,9 @@ sas_status sas_get_device_status(sas_handle* h, int32_t* out_status);
  * 0 block summaries, 1 (unused: the selector's query projection runs inside
  * the selection kernel), 2 selection, 3 attention, 4 MLP up-projection +
  * GELU, 5 MLP down-projection, 6 attention backward (all its kernels), 7 norm +
- * rotation and its gradient.  n_kinds <= 8. */
-#define SAS_NUM_KERNEL_KINDS 8
+ * rotation and its gradient, 8 token log probabilities and their gradient.
+ * n_kinds <= 9. */
+#define SAS_NUM_KERNEL_KINDS 9
 sas_status sas_set_timing(sas_handle* h, int32_t enable);
 sas_status sas_get_timings(sas_handle* h, int64_t* launches, double* total_ms, int32_t n_kinds);
 
@@ -711,11 +741,24 @@ sas_status sas_chunk_verify(sas_chunk_handle* h, int32_t num_seqs, int32_t num_d
                             const float* draft, int64_t ld_draft, const float* u, const float* noise, int64_t ld_noise,
                             int32_t* accepted, int32_t* out_tokens, void* stream);
 
+/* sas_token_logprobs of a step's rows (drafted, sampled or given tokens; the model's logits
+ * are also what sas_chunk_verify's distributions come from), with the likeliest columns.
+ *   T            rows, 1 .. max_tokens
+ *   topk         0 .. 32 and at most V
+ *   top_index    int32 [T, topk] columns of the largest logits, the largest first, the
+ *                lowest column of equal ones; NULL when topk is 0                (out)
+ *   top_logprob  fp32 [T, topk]                                               (out)
+ * NaN is no alternative: a row with fewer than topk other columns has index -1 and NaN for
+ * the rest.  Rows that do not count: -1 and 0.  One launch. */
+sas_status sas_chunk_logprobs(sas_chunk_handle* h, int32_t T, int32_t V, const void* logits, int32_t dtype, int64_t ld,
+                              const int32_t* tokens, int32_t topk, float* logprob, float* entropy, float* lse,
+                              int32_t* top_index, float* top_logprob, void* stream);
+
 /* As their sas_decode_ counterparts.  Kinds: 0 plan, 1 append, 2 attention (both its
- * kernels), 3 verification.  n_kinds <= 4. */
+ * kernels), 3 verification, 4 log probabilities.  n_kinds <= 5. */
 const char* sas_chunk_last_error(const sas_chunk_handle* h);
 sas_status sas_chunk_get_device_status(sas_chunk_handle* h, int32_t* out_status);
-#define SAS_CHUNK_NUM_KERNEL_KINDS 4
+#define SAS_CHUNK_NUM_KERNEL_KINDS 5
 sas_status sas_chunk_set_timing(sas_chunk_handle* h, int32_t enable);
 sas_status sas_chunk_get_timings(sas_chunk_handle* h, int64_t* launches, double* total_ms, int32_t n_kinds);
 int64_t sas_chunk_launch_count(const sas_chunk_handle* h);

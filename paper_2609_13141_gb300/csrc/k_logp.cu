@@ -1,0 +1,502 @@
+// Log probabilities of given tokens with the row's entropy, log-sum-exp and likeliest
+// columns, in one pass over the logits, and their gradient.
+//
+// Row z, token x:  lse = m + log l,  l = sum_v exp(z_v - m),  logprob = z_x - lse,
+//   entropy = -sum_v p_v log p_v = log l - sum_v exp(z_v - m) (z_v - m) / l,  p = exp(z - lse);
+// gradient of a g_lp logprob + g_h entropy:
+//   dz_v = g_lp ([v = x] - p_v) - g_h p_v (log p_v + entropy).
+// A thread keeps (m, l, s = sum exp(z - m) (z - m)) in fp32 over the columns it walks and
+// moves l and s to a new maximum when it finds one; threads, then blocks, join in a fixed order.
+//
+// Bound: HBM, a read of the logits (and a write of as much for the gradient); the
+// exponential unit and the arithmetic take about half of that time.  So: 16-byte loads, four a
+// thread in flight, a row a block, or a warp where rows are short, and where there are fewer
+// rows than places for blocks a row in several parts, whose last block to end joins them.
+//
+// The likeliest columns come along in the same pass: a column is a candidate while its key
+// (order of the value, then of the index) is above the k-th best known.  That bar starts at
+// the k-th largest of the threads' first maxima, so that few columns pass it, and rises
+// whenever the candidates, kept in shared memory, are cut down to the best k.
+#include <cmath>
+
+#include <math_constants.h>
+
+#include "serve.h"
+#include "serve_ptx.cuh"
+
+namespace sas {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBlocks = 4;            // a multiprocessor, as many as their registers allow
+constexpr int kMaxParts = 32;         // of a row
+constexpr int kMinPart = 2048;        // columns
+constexpr int kSmallRow = 4096;       // columns of rows that a warp takes
+constexpr int kStatusBadInput = 1;    // == SAS_ERR_INVALID_ARG
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.69314718055994531f;
+// Below this exponent 2^y is 0 in fp32; y itself is kept finite, as 0 times it is added.
+constexpr float kLowest = -1000.f;
+constexpr float kNone = -HUGE_VALF;   // maximum of no column
+
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
+// 16 bytes of logits as fp32.
+template <class E>
+struct Vec;
+template <>
+struct Vec<bf16> {
+    static constexpr int N = 8, UNROLL = 4;
+    __device__ __forceinline__ static void unpack(const uint4& u, float* f) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    __device__ __forceinline__ static uint4 pack(const float* f) {
+        return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+    }
+    __device__ __forceinline__ static float one(const bf16* p) { return __bfloat162float(load(p)); }
+    __device__ __forceinline__ static void put(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
+};
+template <>
+struct Vec<float> {
+    static constexpr int N = 4, UNROLL = 4;
+    __device__ __forceinline__ static void unpack(const uint4& u, float* f) {
+        f[0] = __uint_as_float(u.x);
+        f[1] = __uint_as_float(u.y);
+        f[2] = __uint_as_float(u.z);
+        f[3] = __uint_as_float(u.w);
+    }
+    __device__ __forceinline__ static uint4 pack(const float* f) {
+        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+    __device__ __forceinline__ static float one(const float* p) { return load(p); }
+    __device__ __forceinline__ static void put(float* p, float v) { *p = v; }
+};
+
+// Columns [v0, v1) of a row as 16-byte vectors: vector j holds columns first + j N .., the
+// first and the last one maybe in part.
+template <class E>
+struct Span {
+    const E* row;
+    int v0, v1, first, count;
+    __device__ __forceinline__ Span(const E* row_, int v0_, int v1_) : row(row_), v0(v0_), v1(v1_) {
+        const int off = static_cast<int>((reinterpret_cast<uintptr_t>(row + v0) & 15u) / sizeof(E));
+        first = v0 - off;
+        count = (v1 - first + Vec<E>::N - 1) / Vec<E>::N;
+    }
+    __device__ __forceinline__ int column(int j) const { return first + j * Vec<E>::N; }
+    __device__ __forceinline__ bool whole(int j) const { return column(j) >= v0 && column(j) + Vec<E>::N <= v1; }
+};
+
+// Sums over columns relative to the maximum m, in the log2 domain: y = (z - m) log2(e).
+struct Sums {
+    float m, l, s;   // s = sum 2^y y
+    __device__ __forceinline__ Sums() : m(kNone), l(0.f), s(0.f) {}
+    __device__ __forceinline__ Sums(float m_, float l_, float s_) : m(m_), l(l_), s(s_) {}
+    // To another maximum.  No column so far (or none but NaN): nothing to move.
+    __device__ __forceinline__ void move(float to) {
+        if (m == -CUDART_INF_F) {
+            m = to;
+            return;
+        }
+        const float d = (m - to) * kLog2e;
+        if (d == 0.f || to == -CUDART_INF_F) return;
+        const float f = exp2f(d);
+        s = f * fmaf(max_nan(d, kLowest), l, s);
+        l *= f;
+        m = to;
+    }
+    __device__ __forceinline__ void join(Sums o) {
+        const float to = fmaxf(m, o.m);
+        move(to);
+        o.move(to);
+        l += o.l;
+        s += o.s;
+    }
+};
+
+__device__ __forceinline__ Sums shfl_xor(const Sums& x, int o) {
+    return Sums(__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.l, o), __shfl_xor_sync(0xffffffffu, x.s, o));
+}
+
+// The same in every lane: which of two joined sums is the left one must not matter, so both
+// lanes of a pair add them in lane order.
+__device__ __forceinline__ Sums warp_join(Sums x) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const Sums y = shfl_xor(x, o);
+        Sums a = (lane_id() & o) ? y : x;
+        a.join((lane_id() & o) ? x : y);
+        x = a;
+    }
+    return x;
+}
+
+// Keys order columns by value, equal ones by index; 0 is below every column.  Zeros of both
+// signs are equal.
+__device__ __forceinline__ unsigned long long key_of(float z, int v) {
+    const uint32_t b = __float_as_uint(z + 0.f);
+    const uint32_t order = (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+    return (static_cast<unsigned long long>(order) << 32) | (0xffffffffu - static_cast<uint32_t>(v));
+}
+__device__ __forceinline__ float key_value(unsigned long long k) {
+    const uint32_t o = static_cast<uint32_t>(k >> 32);
+    return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
+}
+__device__ __forceinline__ int key_index(unsigned long long k) { return static_cast<int>(0xffffffffu - static_cast<uint32_t>(k)); }
+
+constexpr int kMaxTop = 32;
+constexpr int kCand = 512;     // candidates kept: kMaxParts * kMaxTop at the join are taken in pieces
+constexpr int kCut = 128;      // cut down when there are this many at the end of a round
+
+// A team (a block, or one of its warps) and the candidates of its row.
+template <int TEAM>
+struct Team {
+    __device__ __forceinline__ static int rank() { return TEAM == 32 ? lane_id() : threadIdx.x; }
+    __device__ __forceinline__ static void sync() {
+        if constexpr (TEAM == 32) __syncwarp();
+        else __syncthreads();
+    }
+};
+struct Cand {
+    unsigned long long key[kCand];
+    unsigned long long top[kMaxTop];
+    float first[kThreads];   // the threads' maxima of their first columns
+    int n;                   // asked for; at most kCand are kept
+    float bar_value;
+};
+
+// The best k of the n candidates, best first, become the candidates.  All threads of the team.
+template <int TEAM>
+__device__ __forceinline__ int cut(Cand& c, int n, int k) {
+    for (int i = Team<TEAM>::rank(); i < k; i += TEAM) c.top[i] = 0;   // keys of no column, all equal, fill one place at most
+    Team<TEAM>::sync();
+    for (int i = Team<TEAM>::rank(); i < n; i += TEAM) {
+        const unsigned long long mine = c.key[i];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += c.key[j] > mine;
+        if (above < k) c.top[above] = mine;
+    }
+    Team<TEAM>::sync();
+    n = min(n, k);
+    for (int i = Team<TEAM>::rank(); i < n; i += TEAM) c.key[i] = c.top[i];
+    if (Team<TEAM>::rank() == 0) c.n = n;
+    Team<TEAM>::sync();
+    return n;
+}
+
+// What a row gives, by one thread.
+__device__ __forceinline__ void put_row(const LogpArgs& a, int row, const Sums& x, float zx) {
+    const float ll = logf(x.l);
+    // a row without a finite column: its sum is 0 and everything but lse is undefined
+    a.lse[row] = x.l == 0.f ? -CUDART_INF_F : x.m + ll;
+    a.logprob[row] = x.l == 0.f ? CUDART_NAN_F : (zx - x.m) - ll;
+    a.entropy[row] = x.l == 0.f ? CUDART_NAN_F : ll - kLn2 * (x.s / x.l);
+}
+
+template <class E, int TEAM, bool TOP>
+__global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
+    using V = Vec<E>;
+    constexpr int N = V::N, U = V::UNROLL, ROUND = TEAM * U, TEAMS = kThreads / TEAM;
+    static_assert(N * U <= 32, "a thread's columns of a round have a bit each");
+    __shared__ Cand cands[TOP ? TEAMS : 1];
+    __shared__ float3 joined[kThreads / 32];
+    __shared__ int sh_last;
+    const int rank = Team<TEAM>::rank(), part = TEAM == kThreads ? blockIdx.x % a.parts : 0;
+    const int row = TEAM == kThreads ? blockIdx.x / a.parts : blockIdx.x * TEAMS + static_cast<int>(warp_id());
+    Cand& c = cands[TOP && TEAM == 32 ? warp_id() : 0];
+    grid_dep_wait();
+    if (TEAM == 32 && row >= a.rows) return;
+    const int x = load(a.tokens + row);
+    if (x < 0 || x >= a.V) {   // a row that does not count: its logits are not read
+        if (part == 0) {
+            if (rank == 0) {
+                if (x != -1) atomicExch(a.status, kStatusBadInput);
+                a.logprob[row] = 0.f;
+                a.entropy[row] = 0.f;
+                a.lse[row] = 0.f;
+            }
+            if (TOP) {
+                for (int i = rank; i < a.k; i += TEAM) {
+                    a.top_index[static_cast<size_t>(row) * a.k + i] = -1;
+                    a.top_logprob[static_cast<size_t>(row) * a.k + i] = 0.f;
+                }
+            }
+        }
+        return;
+    }
+    const E* const z = static_cast<const E*>(a.logits) + static_cast<size_t>(row) * a.ld;
+    const int v0 = part * a.chunk;
+    const Span<E> sp(z, v0, min(a.V, v0 + a.chunk));
+    Sums t;
+    unsigned long long bar = 0;
+    float bar_value = -CUDART_INF_F;   // below it no column is a candidate
+    int held = 0;
+    if (TOP && rank == 0) c.n = 0;
+    for (int j0 = 0; j0 < sp.count; j0 += ROUND) {
+        uint4 raw[U];
+        bool in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * TEAM + rank;
+            in[u] = j < sp.count;
+            if (in[u] && sp.whole(j)) raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + sp.column(j)));
+        }
+        float f[U * N];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * TEAM + rank, v = sp.column(j);
+            if (in[u] && sp.whole(j)) {
+                V::unpack(raw[u], f + u * N);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) f[u * N + e] = in[u] && v + e >= sp.v0 && v + e < sp.v1 ? V::one(z + v + e) : -CUDART_INF_F;
+            }
+        }
+        float top = -CUDART_INF_F;   // passes over NaN
+#pragma unroll
+        for (int i = 0; i < U * N; ++i) top = fmaxf(top, f[i]);
+        if (top > t.m) t.move(top);
+        const float m = t.m == -CUDART_INF_F ? 0.f : t.m;
+        float l[2] = {0.f, 0.f}, s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < U * N; ++i) {
+            const float y = max_nan((f[i] - m) * kLog2e, kLowest);
+            const float e = fast_exp2(y);
+            l[i & 1] += e;
+            s[i & 1] = fmaf(e, y, s[i & 1]);
+        }
+        t.l += l[0] + l[1];
+        t.s += s[0] + s[1];
+        if constexpr (TOP) {
+            if (j0 == 0) {
+                c.first[rank] = top;
+                Team<TEAM>::sync();
+                int above = 0;
+                for (int i = 0; i < TEAM; ++i) above += c.first[i] > top || (c.first[i] == top && i < rank);
+                if (above == a.k - 1) c.bar_value = top;
+                Team<TEAM>::sync();
+                bar_value = c.bar_value;   // a.k <= TEAM: some thread has that place (NaN: fmaxf has left none)
+            }
+            unsigned todo = 0;   // columns to offer
+            if (top >= bar_value) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int v = sp.column(j0 + u * TEAM + rank);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const int i = u * N + e;
+                        if (in[u] && f[i] >= bar_value && v + e >= sp.v0 && v + e < sp.v1 && key_of(f[i], v + e) > bar)
+                            todo |= 1u << i;
+                    }
+                }
+            }
+            for (;;) {
+                while (todo != 0) {
+                    const int i = __ffs(todo) - 1;
+                    const int v = sp.column(j0 + i / N * TEAM + rank) + i % N;
+                    const unsigned long long key = key_of(V::one(z + v), v);
+                    if (key > bar) {
+                        const int at = atomicAdd(&c.n, 1);
+                        if (at >= kCand) break;   // full: offered again once they are cut down
+                        c.key[at] = key;
+                    }
+                    todo &= todo - 1;
+                }
+                Team<TEAM>::sync();
+                const int asked = c.n;
+                held = min(asked, kCand);
+                Team<TEAM>::sync();
+                if (held < kCut) break;
+                held = cut<TEAM>(c, held, a.k);
+                if (held == a.k) {
+                    bar = c.key[a.k - 1];
+                    bar_value = fmaxf(bar_value, key_value(bar));
+                }
+                if (asked <= kCand) break;
+            }
+        }
+    }
+    t = warp_join(t);
+    if constexpr (TEAM == kThreads) {
+        if (lane_id() == 0) joined[warp_id()] = make_float3(t.m, t.l, t.s);
+        __syncthreads();
+        t = Sums();
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) t.join(Sums(joined[w].x, joined[w].y, joined[w].z));
+    }
+    if constexpr (TOP) {
+        Team<TEAM>::sync();
+        if (sp.count > 0) held = cut<TEAM>(c, held, a.k);
+    }
+    if (TEAM == kThreads && a.parts > 1) {
+        // the part's results; the row's last block joins them in their order
+        const size_t at = static_cast<size_t>(row) * a.parts + part;
+        if (rank == 0) a.part[at] = make_float4(t.m, t.l, t.s, 0.f);
+        if constexpr (TOP)
+            for (int i = rank; i < a.k; i += TEAM) a.part_top[at * kMaxTop + i] = i < held ? c.key[i] : 0ull;
+        __threadfence();
+        __syncthreads();
+        if (rank == 0) sh_last = atomicAdd(a.count + row, 1) == a.parts - 1;
+        __syncthreads();
+        if (!sh_last) return;
+        __threadfence();
+        if (rank == 0) a.count[row] = 0;
+        const size_t row0 = static_cast<size_t>(row) * a.parts;
+        t = Sums();
+        for (int p = 0; p < a.parts; ++p) {
+            const float4 q = __ldcg(a.part + row0 + p);
+            t.join(Sums(q.x, q.y, q.z));
+        }
+        if constexpr (TOP) {
+            held = 0;
+            const int step = (kCand - kMaxTop) / kMaxTop;   // parts whose candidates fit beside the best so far
+            for (int p0 = 0; p0 < a.parts; p0 += step) {
+                const int np = min(step, a.parts - p0);
+                for (int i = rank; i < np * a.k; i += TEAM)
+                    c.key[held + i] = __ldcg(a.part_top + (row0 + p0 + i / a.k) * kMaxTop + i % a.k);
+                __syncthreads();
+                held = cut<TEAM>(c, held + np * a.k, a.k);
+            }
+        }
+    }
+    if (rank == 0) put_row(a, row, t, V::one(z + x));
+    if constexpr (TOP) {
+        for (int i = rank; i < a.k; i += TEAM) {
+            const unsigned long long key = i < held ? c.key[i] : 0ull;
+            const size_t at = static_cast<size_t>(row) * a.k + i;
+            a.top_index[at] = key == 0 ? -1 : key_index(key);
+            a.top_logprob[at] = key == 0 || t.l == 0.f ? CUDART_NAN_F : (key_value(key) - t.m) - logf(t.l);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ gradient
+
+template <class E, int TEAM>
+__global__ void __launch_bounds__(kThreads) logp_bwd_kernel(LogpBwdArgs a) {
+    using V = Vec<E>;
+    constexpr int N = V::N, U = V::UNROLL, TEAMS = kThreads / TEAM;
+    const int rank = Team<TEAM>::rank(), part = TEAM == kThreads ? blockIdx.x % a.parts : 0;
+    const int row = TEAM == kThreads ? blockIdx.x / a.parts : blockIdx.x * TEAMS + static_cast<int>(warp_id());
+    grid_dep_wait();
+    if (TEAM == 32 && row >= a.rows) return;
+    const int x = load(a.tokens + row);
+    const bool counts = x >= 0 && x < a.V;
+    if (!counts && x != -1 && part == 0 && rank == 0) atomicExch(a.status, kStatusBadInput);
+    const E* const z = static_cast<const E*>(a.logits) + static_cast<size_t>(row) * a.ld;
+    E* const dz = static_cast<E*>(a.dlogits) + static_cast<size_t>(row) * a.ld_d;
+    float lse = 0.f, h = 0.f, gl = 0.f, gh = 0.f;
+    if (counts) {
+        lse = load(a.lse + row);
+        h = load(a.entropy + row);
+        gl = load(a.dlogprob + row);
+        if (a.dentropy != nullptr) gh = load(a.dentropy + row);
+    }
+    // with y = log p:  dz = -p (gl + gh (y + h)), and gl more at the token
+    const float base = fmaf(gh, h, gl);
+    auto grad = [&](float zv, int v) {
+        const float y = max_nan(zv - lse, kLowest);
+        return fmaf(-exp2f(y * kLog2e), fmaf(gh, y, base), v == x ? gl : 0.f);
+    };
+    const int v0 = part * a.chunk;
+    const Span<E> sp(z, v0, min(a.V, v0 + a.chunk));
+    // output vectors of the same columns
+    const bool same = ((reinterpret_cast<uintptr_t>(dz) ^ reinterpret_cast<uintptr_t>(z)) & 15u) == 0;
+    for (int j0 = rank; j0 < sp.count; j0 += U * TEAM) {
+        uint4 raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * TEAM;
+            if (counts && j < sp.count && sp.whole(j)) raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + sp.column(j)));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * TEAM, v = sp.column(j);
+            if (j >= sp.count) continue;
+            float f[N];
+            if (sp.whole(j)) {
+                if (counts) {
+                    V::unpack(raw[u], f);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) f[e] = grad(f[e], v + e);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) f[e] = 0.f;
+                }
+                if (same) {
+                    __stcs(reinterpret_cast<uint4*>(dz + v), V::pack(f));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) V::put(dz + v + e, f[e]);
+                }
+            } else {
+                for (int e = 0; e < N; ++e)
+                    if (v + e >= sp.v0 && v + e < sp.v1) V::put(dz + v + e, counts ? grad(V::one(z + v + e), v + e) : 0.f);
+            }
+        }
+    }
+}
+
+// Parts of a row, so that all places for blocks are taken, and a part's columns.
+void split_rows(int rows, int V, int places, int& parts, int& chunk) {
+    const int most = (V + kMinPart - 1) / kMinPart;
+    parts = places / rows;
+    if (parts > kMaxParts) parts = kMaxParts;
+    if (parts > most) parts = most;
+    if (parts < 1) parts = 1;
+    chunk = ((V + parts - 1) / parts + 63) / 64 * 64;   // whole vectors, if the row begins with one
+    parts = (V + chunk - 1) / chunk;
+}
+
+template <class E>
+cudaError_t launch_fwd(LogpArgs a, const KernelEnv& env) {
+    const bool small = a.V <= kSmallRow;
+    a.parts = 1;
+    a.chunk = a.V;
+    if (!small) split_rows(a.rows, a.V, logp_max_splits(), a.parts, a.chunk);
+    const dim3 grid(small ? (a.rows + kThreads / 32 - 1) / (kThreads / 32) : a.rows * a.parts);
+    if (a.k > 0) return launch_early(small ? logp_kernel<E, 32, true> : logp_kernel<E, kThreads, true>, grid, kThreads, 0, env.stream, a);
+    return launch_early(small ? logp_kernel<E, 32, false> : logp_kernel<E, kThreads, false>, grid, kThreads, 0, env.stream, a);
+}
+
+template <class E>
+cudaError_t launch_bwd(LogpBwdArgs a, const KernelEnv& env) {
+    const bool small = a.V <= kSmallRow;
+    a.parts = 1;
+    a.chunk = a.V;
+    if (!small) split_rows(a.rows, a.V, 8 * device_sm_count(), a.parts, a.chunk);
+    const dim3 grid(small ? (a.rows + kThreads / 32 - 1) / (kThreads / 32) : a.rows * a.parts);
+    return launch_early(small ? logp_bwd_kernel<E, 32> : logp_bwd_kernel<E, kThreads>, grid, kThreads, 0, env.stream, a);
+}
+
+}  // namespace
+
+const char* logp_check(int V, int dtype, const void* logits, long long ld) {
+    if (V < 1 || V > (1 << 30)) return "V must be 1 .. 2^30";
+    if (dtype != 0 && dtype != 1) return "dtype must be SAS_DTYPE_BF16 or SAS_DTYPE_FP32";
+    if (ld < V) return "a row stride is below V";
+    if ((reinterpret_cast<uintptr_t>(logits) & (dtype == 0 ? 1u : 3u)) != 0) return "misaligned pointer";
+    return nullptr;
+}
+
+int logp_max_splits() { return kBlocks * device_sm_count(); }
+int logp_max_top() { return kMaxTop; }
+
+cudaError_t launch_logp(const LogpArgs& a, const KernelEnv& env) {
+    return a.is_bf16 ? launch_fwd<bf16>(a, env) : launch_fwd<float>(a, env);
+}
+
+cudaError_t launch_logp_bwd(const LogpBwdArgs& a, const KernelEnv& env) {
+    return a.is_bf16 ? launch_bwd<bf16>(a, env) : launch_bwd<float>(a, env);
+}
+
+}  // namespace sas

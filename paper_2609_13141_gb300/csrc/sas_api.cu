@@ -173,6 +173,9 @@ struct sas_handle {
     // gradient of the norm + rotation: weight sums of each block, arrival counter
     float* rope_part = nullptr;
     int* rope_count = nullptr;
+    // token log probabilities: sums of rows in several parts, arrival counters
+    float4* logp_part = nullptr;
+    int* logp_count = nullptr;
     // timing
     bool timing = false;
     std::vector<TimeRec> recs;
@@ -364,6 +367,10 @@ sas_status sas_create(const sas_config* cfg, sas_handle** out) {
     if (e == cudaSuccess) e = alloc(&h->rope_part, static_cast<size_t>(sas::rope_bwd_max_blocks()) * 2 * c.d * 4);
     if (e == cudaSuccess) e = alloc(&h->rope_count, 16);
     if (e == cudaSuccess) e = cudaMemset(h->rope_count, 0, 16);
+    const size_t splits = sas::logp_max_splits();
+    if (e == cudaSuccess) e = alloc(&h->logp_part, splits * sizeof(float4));
+    if (e == cudaSuccess) e = alloc(&h->logp_count, splits * sizeof(int));
+    if (e == cudaSuccess) e = cudaMemset(h->logp_count, 0, splits * sizeof(int));
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) {
         sas_status s = e == cudaErrorMemoryAllocation ? SAS_ERR_OOM : SAS_ERR_CUDA;
@@ -389,6 +396,8 @@ void sas_destroy(sas_handle* h) {
     cudaFree(h->sched);
     cudaFree(h->rope_part);
     cudaFree(h->rope_count);
+    cudaFree(h->logp_part);
+    cudaFree(h->logp_count);
     cudaFree(h->full_lse);
     cudaFree(h->full_table);
     cudaFree(h->seg_union_idx);
@@ -928,6 +937,62 @@ sas_status sas_qk_norm_rope_bwd(sas_handle* h, const sas_rope_config* rope, cons
     const sas::KernelEnv env{s, h->status, h->limit};
     const cudaError_t e = timed_launch(h, 7, s, [&] { return sas::launch_rope_bwd(a, h->cfg.d, env); });
     return e == cudaSuccess ? SAS_OK : cuda_fail(h, e, "gradient of norm + rotation");
+} catch (...) {
+    return SAS_ERR_OOM;   // only the host's own bookkeeping throws
+}
+
+namespace {
+
+// Checks and arguments common to the token log probabilities and their gradient.
+sas_status logp_args(sas_handle* h, int32_t T, int32_t V, const void* logits, int32_t dtype, int64_t ld, const int32_t* tokens) {
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return fail(h, SAS_ERR_CUDA, "cudaGetDevice");
+    if (dev != h->device) return fail(h, SAS_ERR_INVALID_ARG, "the current device is not the handle's");
+    if (T < 1 || T > (1 << 26)) return fail(h, SAS_ERR_INVALID_ARG, "T must be 1 .. 2^26");
+    if (!logits || !tokens) return fail(h, SAS_ERR_INVALID_ARG, "a required argument is NULL");
+    if (const char* why = sas::logp_check(V, dtype, logits, ld)) return fail(h, SAS_ERR_INVALID_ARG, why);
+    if (!aligned4(tokens)) return fail(h, SAS_ERR_INVALID_ARG, "misaligned pointer");
+    return SAS_OK;
+}
+
+}  // namespace
+
+sas_status sas_token_logprobs(sas_handle* h, int32_t T, int32_t V, const void* logits, int32_t dtype, int64_t ld,
+                              const int32_t* tokens, float* logprob, float* entropy, float* lse, void* stream) try {
+    if (h == nullptr) return SAS_ERR_INVALID_ARG;
+    if (sas_status st = logp_args(h, T, V, logits, dtype, ld, tokens); st != SAS_OK) return st;
+    if (!logprob || !entropy || !lse) return fail(h, SAS_ERR_INVALID_ARG, "a required argument is NULL");
+    if (!aligned4(logprob) || !aligned4(entropy) || !aligned4(lse)) return fail(h, SAS_ERR_INVALID_ARG, "misaligned pointer");
+    sas::LogpArgs a{};
+    a.rows = T; a.V = V; a.is_bf16 = dtype == SAS_DTYPE_BF16; a.logits = logits; a.ld = ld; a.tokens = tokens;
+    a.logprob = logprob; a.entropy = entropy; a.lse = lse;
+    a.part = h->logp_part; a.count = h->logp_count; a.status = h->status;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const sas::KernelEnv env{s, h->status, h->limit};
+    const cudaError_t e = timed_launch(h, 8, s, [&] { return sas::launch_logp(a, env); });
+    return e == cudaSuccess ? SAS_OK : cuda_fail(h, e, "token log probabilities");
+} catch (...) {
+    return SAS_ERR_OOM;   // only the host's own bookkeeping throws
+}
+
+sas_status sas_token_logprobs_bwd(sas_handle* h, int32_t T, int32_t V, const void* logits, int32_t dtype, int64_t ld,
+                                  const int32_t* tokens, const float* lse, const float* entropy, const float* dlogprob,
+                                  const float* dentropy, void* dlogits, int64_t ld_d, void* stream) try {
+    if (h == nullptr) return SAS_ERR_INVALID_ARG;
+    if (sas_status st = logp_args(h, T, V, logits, dtype, ld, tokens); st != SAS_OK) return st;
+    if (!lse || !entropy || !dlogprob || !dlogits) return fail(h, SAS_ERR_INVALID_ARG, "a required argument is NULL");
+    if (!aligned4(lse) || !aligned4(entropy) || !aligned4(dlogprob) || !aligned4(dentropy))
+        return fail(h, SAS_ERR_INVALID_ARG, "misaligned pointer");
+    if (const char* why = sas::logp_check(V, dtype, dlogits, ld_d)) return fail(h, SAS_ERR_INVALID_ARG, why);
+    if (dlogits == logits && ld_d != ld) return fail(h, SAS_ERR_INVALID_ARG, "dlogits in the logits' memory must have their row stride");
+    sas::LogpBwdArgs a{};
+    a.rows = T; a.V = V; a.is_bf16 = dtype == SAS_DTYPE_BF16; a.logits = logits; a.ld = ld; a.tokens = tokens;
+    a.lse = lse; a.entropy = entropy; a.dlogprob = dlogprob; a.dentropy = dentropy; a.dlogits = dlogits; a.ld_d = ld_d;
+    a.status = h->status;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const sas::KernelEnv env{s, h->status, h->limit};
+    const cudaError_t e = timed_launch(h, 8, s, [&] { return sas::launch_logp_bwd(a, env); });
+    return e == cudaSuccess ? SAS_OK : cuda_fail(h, e, "gradient of token log probabilities");
 } catch (...) {
     return SAS_ERR_OOM;   // only the host's own bookkeeping throws
 }

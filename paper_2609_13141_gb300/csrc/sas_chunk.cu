@@ -32,6 +32,9 @@ struct sas_chunk_handle {
     float2* part_ml = nullptr;
     unsigned long long* vkey = nullptr;
     int* vcount = nullptr;
+    float4* logp_part = nullptr;
+    unsigned long long* logp_top = nullptr;
+    int* logp_count = nullptr;
     int* status = nullptr;
     // timing
     bool timing = false;
@@ -162,6 +165,11 @@ sas_status sas_chunk_create(const sas_chunk_config* cfg, sas_chunk_handle** out)
     if (e == cudaSuccess) e = calloc_dev(&h->part_ml, parts * 128);
     if (e == cudaSuccess) e = calloc_dev(&h->vkey, c.max_seqs);
     if (e == cudaSuccess) e = calloc_dev(&h->vcount, c.max_seqs);
+    const size_t splits = sas::logp_max_splits();
+    if (e == cudaSuccess) e = calloc_dev(&h->logp_part, splits);
+    if (e == cudaSuccess) e = calloc_dev(&h->logp_top, splits * sas::logp_max_top());
+    if (e == cudaSuccess) e = calloc_dev(&h->logp_count, splits);
+    if (e == cudaSuccess) e = cudaMemset(h->logp_count, 0, splits * 4);
     if (e == cudaSuccess) e = calloc_dev(&h->status, 4);
     if (e == cudaSuccess) e = cudaMemset(h->vkey, 0, static_cast<size_t>(c.max_seqs) * 8);
     if (e == cudaSuccess) e = cudaMemset(h->vcount, 0, static_cast<size_t>(c.max_seqs) * 4);
@@ -188,6 +196,9 @@ void sas_chunk_destroy(sas_chunk_handle* h) {
     cudaFree(h->part_ml);
     cudaFree(h->vkey);
     cudaFree(h->vcount);
+    cudaFree(h->logp_part);
+    cudaFree(h->logp_top);
+    cudaFree(h->logp_count);
     cudaFree(h->status);
     for (cudaEvent_t ev : h->events) cudaEventDestroy(ev);
     delete h;
@@ -319,6 +330,31 @@ sas_status sas_chunk_verify(sas_chunk_handle* h, int32_t num_seqs, int32_t num_d
         const sas::KernelEnv env{s, h->status, h->limit};
         const cudaError_t e = ctimed(h, 3, 1, s, [&] { return sas::launch_verify(a, env); });
         return e == cudaSuccess ? SAS_OK : ccuda_fail(h, e, "draft verification");
+    });
+}
+
+sas_status sas_chunk_logprobs(sas_chunk_handle* h, int32_t T, int32_t V, const void* logits, int32_t dtype, int64_t ld,
+                              const int32_t* tokens, int32_t topk, float* logprob, float* entropy, float* lse,
+                              int32_t* top_index, float* top_logprob, void* stream) {
+    if (h == nullptr) return SAS_ERR_INVALID_ARG;
+    return guarded(h, [&]() -> sas_status {
+        if (sas_status st = on_device(h); st != SAS_OK) return st;
+        if (T < 1 || T > h->cfg.max_tokens) return cfail(h, SAS_ERR_INVALID_ARG, "T must be 1 .. max_tokens");
+        if (!logits || !tokens || !logprob || !entropy || !lse || (topk > 0 && (!top_index || !top_logprob)))
+            return cfail(h, SAS_ERR_INVALID_ARG, "a required argument is NULL");
+        if (const char* why = sas::logp_check(V, dtype, logits, ld)) return cfail(h, SAS_ERR_INVALID_ARG, why);
+        if (topk < 0 || topk > sas::logp_max_top() || topk > V) return cfail(h, SAS_ERR_INVALID_ARG, "topk must be 0 .. 32 and at most V");
+        if (!al4(tokens) || !al4(logprob) || !al4(entropy) || !al4(lse) || !al4(top_index) || !al4(top_logprob))
+            return cfail(h, SAS_ERR_INVALID_ARG, "misaligned pointer");
+        sas::LogpArgs a{};
+        a.rows = T; a.V = V; a.is_bf16 = dtype == SAS_DTYPE_BF16; a.logits = logits; a.ld = ld; a.tokens = tokens;
+        a.logprob = logprob; a.entropy = entropy; a.lse = lse;
+        a.k = topk; a.top_index = top_index; a.top_logprob = top_logprob;
+        a.part = h->logp_part; a.part_top = h->logp_top; a.count = h->logp_count; a.status = h->status;
+        cudaStream_t s = static_cast<cudaStream_t>(stream);
+        const sas::KernelEnv env{s, h->status, h->limit};
+        const cudaError_t e = ctimed(h, 4, 1, s, [&] { return sas::launch_logp(a, env); });
+        return e == cudaSuccess ? SAS_OK : ccuda_fail(h, e, "log probabilities");
     });
 }
 

@@ -109,4 +109,44 @@ int chunk_blocks();             // blocks of the attention; each writes at most 
 cudaError_t chunk_attn_prepare(int d);   // shared-memory limit (before any capture)
 cudaError_t launch_chunk_attn(const ChunkArgs& a, const KernelEnv& env, const char** err);
 
+// ---- log probabilities of given tokens, entropy and likeliest columns; their gradient.
+struct LogpArgs {
+    int rows, V, is_bf16;
+    const void* logits;         // [rows] rows of V, ld apart, bf16 or fp32
+    long long ld;
+    const int32_t* tokens;      // [rows], -1: the row does not count
+    float* logprob;             // [rows]
+    float* entropy;
+    float* lse;
+    int k;                      // likeliest columns, 0 .. logp_max_top()
+    int32_t* top_index;         // [rows][k]
+    float* top_logprob;
+    // workspace of rows in several parts; rows x parts <= logp_max_splits()
+    float4* part;               // [splits] (max, sum, weighted sum)
+    unsigned long long* part_top;   // [splits][logp_max_top()]
+    int* count;                 // [splits] zero between launches
+    int parts, chunk;           // set by the launch
+    int* status;
+};
+struct LogpBwdArgs {
+    int rows, V, is_bf16;
+    const void* logits;
+    long long ld;
+    const int32_t* tokens;
+    const float* lse;           // [rows]
+    const float* entropy;
+    const float* dlogprob;
+    const float* dentropy;      // or null
+    void* dlogits;              // the logits' type, rows ld_d apart
+    long long ld_d;
+    int parts, chunk;           // set by the launch
+    int* status;
+};
+// What is wrong with logits of V columns, rows ld elements of type `dtype` apart, or null.
+const char* logp_check(int V, int dtype, const void* logits, long long ld);
+int logp_max_splits();
+int logp_max_top();
+cudaError_t launch_logp(const LogpArgs& a, const KernelEnv& env);
+cudaError_t launch_logp_bwd(const LogpBwdArgs& a, const KernelEnv& env);
+
 }  // namespace sas

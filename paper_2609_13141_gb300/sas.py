@@ -37,9 +37,11 @@ SAS_GATE_INNER = 0
 SAS_GATE_OUTER = 1
 SAS_SCOPE_SPARSE = 0
 SAS_SCOPE_FULL = 1
-SAS_NUM_KERNEL_KINDS = 8
+SAS_DTYPE_BF16 = 0
+SAS_DTYPE_FP32 = 1
+SAS_NUM_KERNEL_KINDS = 9
 KERNEL_KINDS = ["block_summaries", "query_projection", "selection", "attention", "mlp_up_gelu", "mlp_down",
-                "attention_bwd", "qk_norm_rope"]
+                "attention_bwd", "qk_norm_rope", "token_logprobs"]
 
 HEADER = os.path.join(_build.ROOT, "include", "sas.h")
 
@@ -72,8 +74,8 @@ class SasChunkConfig(ctypes.Structure):
 
 SAS_DECODE_NUM_KERNEL_KINDS = 4
 DECODE_KERNEL_KINDS = ["prep", "select", "attention", "summarize"]
-SAS_CHUNK_NUM_KERNEL_KINDS = 4
-CHUNK_KERNEL_KINDS = ["plan", "append", "attention", "verify"]
+SAS_CHUNK_NUM_KERNEL_KINDS = 5
+CHUNK_KERNEL_KINDS = ["plan", "append", "attention", "verify", "logprobs"]
 
 
 class SasError(RuntimeError):
@@ -167,6 +169,12 @@ def lib():
     L.sas_chunk_attention.restype = i32
     L.sas_chunk_verify.argtypes = [vp] + [i32] * 4 + [vp, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp]
     L.sas_chunk_verify.restype = i32
+    L.sas_token_logprobs.argtypes = [vp, i32, i32, vp, i32, i64] + [vp] * 5
+    L.sas_token_logprobs.restype = i32
+    L.sas_token_logprobs_bwd.argtypes = [vp, i32, i32, vp, i32, i64] + [vp] * 6 + [i64, vp]
+    L.sas_token_logprobs_bwd.restype = i32
+    L.sas_chunk_logprobs.argtypes = [vp, i32, i32, vp, i32, i64, vp, i32] + [vp] * 6
+    L.sas_chunk_logprobs.restype = i32
     L.sas_chunk_last_error.argtypes = [vp]
     L.sas_chunk_last_error.restype = ctypes.c_char_p
     L.sas_chunk_get_device_status.argtypes = [vp, ctypes.POINTER(i32)]
@@ -187,7 +195,7 @@ def header_functions():
     """Names of the functions include/sas.h declares."""
     text = open(HEADER).read()
     text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
-    return sorted(set(re.findall(r"\b(sas_[a-z_]+)\s*\(", text)))
+    return sorted(set(re.findall(r"\b(sas_[a-z0-9_]+)\s*\(", text)))
 
 
 def _ptr(t, dtype, name, required=True):
@@ -453,6 +461,55 @@ def sas_mlp_noalloc_get_device_status():
     return v.value
 
 
+# Results of sas_token_logprobs and sas_chunk_logprobs; the last two are None without alternatives.
+TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprob entropy lse top_index top_logprob")
+
+
+def _logprob_buffers(T, topk, device):
+    f32 = lambda *shape: torch.empty(*shape, device=device, dtype=torch.float32)  # noqa: E731
+    top = (torch.empty(T, topk, device=device, dtype=torch.int32), f32(T, topk)) if topk else (None, None)
+    return TokenLogprobs(f32(T), f32(T), f32(T), *top)
+
+
+def _logits(t, name, dev, shape=None, dtype=None):
+    """Address, type and row stride of a bf16 or fp32 [rows, V] tensor with contiguous columns."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a [rows, V] tensor")
+    kind = dtype or t.dtype
+    if kind not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{name} must be torch.bfloat16 or torch.float32, got {kind}")
+    at = _rows(t, kind, name, dev, shape or t.shape)
+    (T, V), st = t.shape, t.stride()
+    if V > 1 and st[1] != 1:
+        raise ValueError(f"{name} must have contiguous columns")
+    return at, SAS_DTYPE_BF16 if kind is torch.bfloat16 else SAS_DTYPE_FP32, st[0] if T > 1 else max(st[0], V)
+
+
+def sas_token_logprobs(h, logits, tokens, logprob, entropy, lse, stream=None):
+    dev, f32 = logits.get_device(), torch.float32
+    at, dtype, ld = _logits(logits, "logits", dev)
+    T, V = logits.shape
+    st = lib().sas_token_logprobs(
+        h, T, V, at, dtype, ld, _arg(tokens, torch.int32, "tokens", dev, (T,)), _arg(logprob, f32, "logprob", dev, (T,)),
+        _arg(entropy, f32, "entropy", dev, (T,)), _arg(lse, f32, "lse", dev, (T,)), _raw_stream(stream, dev))
+    if st != SAS_OK:
+        _check(st, h, "sas_token_logprobs")
+
+
+def sas_token_logprobs_bwd(h, logits, tokens, lse, entropy, dlogprob, dentropy, dlogits, stream=None):
+    """dentropy None: zero."""
+    dev, f32 = logits.get_device(), torch.float32
+    at, dtype, ld = _logits(logits, "logits", dev)
+    T, V = logits.shape
+    at_d, _, ld_d = _logits(dlogits, "dlogits", dev, logits.shape, logits.dtype)
+    st = lib().sas_token_logprobs_bwd(
+        h, T, V, at, dtype, ld, _arg(tokens, torch.int32, "tokens", dev, (T,)), _arg(lse, f32, "lse", dev, (T,)),
+        _arg(entropy, f32, "entropy", dev, (T,)), _arg(dlogprob, f32, "dlogprob", dev, (T,)),
+        None if dentropy is None else _arg(dentropy, f32, "dentropy", dev, (T,)), at_d, ld_d, _raw_stream(stream, dev))
+    if st != SAS_OK:
+        _check(st, h, "sas_token_logprobs_bwd")
+
+
 def sas_get_device_status(h):
     v = ctypes.c_int32(0)
     _check(lib().sas_get_device_status(h, ctypes.byref(v)), h, "sas_get_device_status")
@@ -604,6 +661,23 @@ class SasLayer:
                 dwq = torch.empty(self.d, device=qkv.device, dtype=torch.float32)
                 out = (dqkv, dwq, torch.empty_like(dwq))
         sas_qk_norm_rope_bwd(self.h, qkv, wq, wk, cos, sin, dQ, dK, dV, *out, positions, eps, interleaved, stream)
+        return out
+
+    def token_logprobs(self, logits, tokens, out=None, stream=None):
+        """Log probability of tokens[t] (int32, -1: the row does not count) under row t of logits [T, V] (bf16 or fp32),
+        with the row's entropy and log-sum-exp: a TokenLogprobs; out reuses the caller's."""
+        if out is None:
+            with _on(stream):
+                out = _logprob_buffers(logits.shape[0], 0, logits.device)
+        sas_token_logprobs(self.h, logits, tokens, out.logprob, out.entropy, out.lse, stream)
+        return out
+
+    def token_logprobs_bwd(self, logits, tokens, lse, entropy, dlogprob, dentropy=None, out=None, stream=None):
+        """Returns dlogits [T, V] in the logits' type; out reuses the caller's (the logits themselves, for one)."""
+        if out is None:
+            with _on(stream):
+                out = torch.empty(logits.shape, device=logits.device, dtype=logits.dtype)
+        sas_token_logprobs_bwd(self.h, logits, tokens, lse, entropy, dlogprob, dentropy, out, stream)
         return out
 
     def mlp(self, X, W1, W2, b1=None, b2=None, stream=None):
@@ -848,6 +922,24 @@ def sas_chunk_verify(h, tokens, cu_draft, target, draft, u, noise, accepted, out
         _ccheck(st, h, "sas_chunk_verify")
 
 
+def sas_chunk_logprobs(h, logits, tokens, logprob, entropy, lse, top_index=None, top_logprob=None, stream=None):
+    """top_index, top_logprob [T, topk]: the likeliest columns, or None."""
+    dev, i32, f32 = logits.get_device(), torch.int32, torch.float32
+    at, dtype, ld = _logits(logits, "logits", dev)
+    (T, V), topk = logits.shape, 0
+    if top_index is not None:
+        if top_index.dim() != 2:
+            raise ValueError("top_index must be a [T, topk] tensor")
+        topk = top_index.shape[1]
+    st = lib().sas_chunk_logprobs(
+        h, T, V, at, dtype, ld, _arg(tokens, i32, "tokens", dev, (T,)), topk, _arg(logprob, f32, "logprob", dev, (T,)),
+        _arg(entropy, f32, "entropy", dev, (T,)), _arg(lse, f32, "lse", dev, (T,)),
+        _arg(top_index, i32, "top_index", dev, (T, topk)) if topk else None,
+        _arg(top_logprob, f32, "top_logprob", dev, (T, topk)) if topk else None, _raw_stream(stream, dev))
+    if st != SAS_OK:
+        _ccheck(st, h, "sas_chunk_logprobs")
+
+
 def sas_chunk_get_device_status(h):
     v = ctypes.c_int32(0)
     _ccheck(lib().sas_chunk_get_device_status(h, ctypes.byref(v)), h, "sas_chunk_get_device_status")
@@ -926,6 +1018,21 @@ class SasChunk:
             with _on(stream):
                 out = (torch.empty_like(Q), torch.empty(Q.shape[:2], device=Q.device, dtype=torch.float32))
         sas_chunk_attention(self.h, Q, K_cache, V_cache, block_table, cu_new, kv_lens, out[0], out[1], stream)
+        return out
+
+    def logprob_buffers(self, T, topk, device):
+        return _logprob_buffers(T, topk, device)
+
+    def logprobs(self, logits, tokens, topk=0, out=None, stream=None):
+        """Log probability of tokens[t] (int32, -1: the row does not count) under row t of logits [T, V] (bf16 or fp32),
+        with the row's entropy, log-sum-exp and topk likeliest columns: a TokenLogprobs; out (logprob_buffers) reuses
+        the caller's."""
+        if out is None:
+            with _on(stream):
+                out = _logprob_buffers(logits.shape[0], topk, logits.device)
+        elif (0 if out.top_index is None else out.top_index.shape[-1]) != topk:
+            raise ValueError(f"out.top_index must have {topk} columns")
+        sas_chunk_logprobs(self.h, logits, tokens, *out, stream)
         return out
 
     def verify(self, tokens, cu_draft, target, draft, u, noise, max_draft, out=None, stream=None):
