@@ -693,6 +693,25 @@ sas_status sas_chunk_append(sas_chunk_handle* h, const sas_rope_config* rope, in
                             const int32_t* positions, const int64_t* slots, void* Q, void* K_cache, void* V_cache,
                             void* stream);
 
+/* The 8-bit cache: e4m3 numbers (torch.float8_e4m3fn) under one scale for each page and KV
+ * head, fp32 and a power of two: a key is K_cache * K_scale.
+ *   K_cache, V_cache  e4m3 [num_pages, Hkv, 64, d]
+ *   K_scale, V_scale  fp32 [num_pages, Hkv]
+ * sas_chunk_append8: as sas_chunk_append, into such a cache.  The scale of a page and head
+ * is the least power of two (2^-64 .. 2^120) under which its new rows' largest number does
+ * not exceed 448, from their fp32 values; where the page's row 0 is not among the new
+ * rows, it is at least the one the page has, and where that makes it grow, the rows that
+ * stay are rounded again under it.  So K_scale and V_scale need no values before a page's
+ * row 0 is written.  Rounding is to nearest; what is not finite has no say in the scale
+ * and is stored as NaN.
+ * The new tokens of a page must stand next to each other in the batch (as sas_chunk_plan
+ * lists them, any order within the page).  Tokens are skipped as in sas_chunk_append.  Two
+ * launches. */
+sas_status sas_chunk_append8(sas_chunk_handle* h, const sas_rope_config* rope, int32_t T, const void* qkv, int64_t ld,
+                             const void* wq, const void* wk, const float* cos, const float* sin,
+                             const int32_t* positions, const int64_t* slots, void* Q, void* K_cache, void* V_cache,
+                             float* K_scale, float* V_scale, void* stream);
+
 /* Dense causal attention of the new tokens over the paged cache, which holds them
  * already: token i of request b (i = 0 .. n - 1, n = cu_new[b + 1] - cu_new[b]) has
  * position kv_lens[b] - n + i and attends to every token of its request up to itself.
@@ -712,6 +731,14 @@ sas_status sas_chunk_append(sas_chunk_handle* h, const sas_rope_config* rope, in
 sas_status sas_chunk_attention(sas_chunk_handle* h, int32_t num_seqs, int32_t T, const void* Q, const void* K_cache,
                                const void* V_cache, const int32_t* block_table, const int32_t* cu_new,
                                const int32_t* kv_lens, void* O, float* LSE, void* stream);
+
+/* sas_chunk_attention over an 8-bit cache (see sas_chunk_append8), the same otherwise: sums
+ * and softmax in fp32, the weights rounded to fp16.  A value's NaN reaches earlier rows of
+ * its tile as there.  Scales must be positive and finite.  Two launches. */
+sas_status sas_chunk_attention8(sas_chunk_handle* h, int32_t num_seqs, int32_t T, const void* Q, const void* K_cache,
+                                const void* V_cache, const float* K_scale, const float* V_scale,
+                                const int32_t* block_table, const int32_t* cu_new, const int32_t* kv_lens, void* O,
+                                float* LSE, void* stream);
 
 /* Verification of drafted tokens.  Request b drafted x_0 .. x_{n-1} (n = cu_draft[b +
  * 1] - cu_draft[b]), x_j drawn from q_j; the target model's distributions are p_0 ..

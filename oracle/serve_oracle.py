@@ -138,3 +138,46 @@ def verify(tokens, cu, target, draft, u, noise, max_draft):
         row.append(int(score.argmax()) if ok.any() else -1)   # argmax: the lowest of equal ones
         out.append(row + [-1] * (max_draft + 1 - len(row)))
     return np.array(accepted), np.array(out)
+
+
+def page_scale(amax):
+    """Least power of two s, 2^-64 <= s <= 2^120, with amax <= 448 s."""
+    k = -64
+    while amax > 448.0 * 2.0 ** k and k < 120:
+        k += 1
+    return 2.0 ** k
+
+
+def round_e4m3(x):
+    """To the nearest e4m3 number (4 significant bits, least step 2^-9, largest 448), ties to even; what is not finite
+    becomes NaN."""
+    x = np.asarray(x, dtype=np.float64)
+    finite = np.isfinite(x)
+    a = np.abs(np.where(finite, x, 0.0))
+    _, e = np.frexp(np.where(a > 0, a, 1.0))
+    step = np.ldexp(1.0, np.maximum(e - 4, -9))
+    r = np.minimum(np.round(a / step) * step, 448.0)
+    return np.where(finite, np.copysign(r, np.where(finite, x, 0.0)), np.nan)
+
+
+def append8(qkv, wq, wk, cos, sin, positions, slots, Hq, eps, interleaved, K_cache, V_cache, K_scale, V_scale):
+    """Caches [P, Hkv, 64, d] of e4m3 numbers, scales [P, Hkv].  Returns Q, the new caches before rounding (in units of the
+    new scales), and the new scales.  Tokens of slot -1 are left out."""
+    live = [t for t, s in enumerate(slots) if s >= 0]
+    Q, K, V = qk_norm_rope(qkv, wq, wk, cos, sin, np.maximum(positions, 0), Hq, eps, interleaved)
+    out = []
+    for new, cache, scale in ((K, K_cache, K_scale), (V, V_cache, V_scale)):
+        cache, scale = np.array(cache, dtype=np.float64), np.array(scale, dtype=np.float64)
+        for page in sorted({slots[t] // PAGE for t in live}):
+            ts = [t for t in live if slots[t] // PAGE == page]
+            for g in range(scale.shape[1]):
+                y = np.array([new[t, g] for t in ts])
+                s = page_scale(float(np.abs(y[np.isfinite(y)]).max(initial=0.0)))
+                if all(slots[t] % PAGE != 0 for t in ts):
+                    s = max(s, scale[page, g])
+                    cache[page, g] *= scale[page, g] / s
+                for t in ts:
+                    cache[page, g, slots[t] % PAGE] = new[t, g] / s
+                scale[page, g] = s
+        out += [cache, scale]
+    return Q, out[0], out[2], out[1], out[3]

@@ -23,6 +23,10 @@
 // as written and the waits for shared memory and reductions show.  One or two more
 // stages of the rings are slower (158 us forward with three): the warps drift apart and
 // DRAM pages are opened more often.
+#include <type_traits>
+
+#include <cuda_fp16.h>
+
 #include "serve.h"
 #include "serve_ptx.cuh"
 
@@ -527,6 +531,250 @@ cudaError_t launch_any_bwd(const RopeArgs& a, const KernelEnv& env) {
     return a.rot < D ? launch_bwd<D, INTER, true>(a, env) : launch_bwd<D, INTER, false>(a, env);
 }
 
+// ------------------------------------------------------------------ into pages of 8 bits
+//
+// A page of a KV head holds e4m3 numbers under one scale, a power of two s with max |x| <=
+// 448 s.  A page whose row 0 is new starts a scale; otherwise the scale only grows, and where
+// it does the rows that stay are rounded again under the larger one.  So the maximum of a
+// page's new rows has to be known before any of them is written: the tokens of a page stand
+// next to each other, and a run of them of one page and head is one piece of work, whose rows
+// wait in registers.  A run of up to 8 tokens is a warp's, a longer one a block's, 8 tokens a
+// warp; a block looks for the runs that begin in 8 neighbouring tokens (one of them at most is
+// longer than 8).
+constexpr int kRunRows = 8;                       // of a warp
+static_assert(kWarps == kRunRows, "a block's window is a token a warp, its longest run a page");
+
+// Least power of two s with amax <= 448 s, 448 = 1.75 * 2^8, within 2^-64 .. 2^120.
+__device__ __forceinline__ float page_scale(float amax) {
+    const uint32_t b = __float_as_uint(amax);
+    int k = static_cast<int>(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u);
+    k = max(-64, min(120, k));
+    return __uint_as_float(static_cast<uint32_t>(k + 127) << 23);
+}
+// Two numbers as e4m3, to nearest.  What is not finite becomes NaN (there is no infinity).
+__device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi) {
+    lo = fabsf(lo) <= 3.4e38f ? lo : __uint_as_float(0x7fc00000u);
+    hi = fabsf(hi) <= 3.4e38f ? hi : __uint_as_float(0x7fc00000u);
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_quad(uint64_t a, uint64_t b, float inv) {
+    float x0, x1, x2, x3;
+    f32x2_split(a, x0, x1);
+    f32x2_split(b, x2, x3);
+    return pack_e4m3x2(x0 * inv, x1 * inv) | (pack_e4m3x2(x2 * inv, x3 * inv) << 16);
+}
+// Four numbers under a larger scale.
+__device__ __forceinline__ uint32_t shrink_quad(uint32_t w, float ratio) {
+    uint32_t out = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t f;
+        asm("{\n\t.reg .b16 x;\n\tcvt.u16.u32 x, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\t}" : "=r"(f) : "r"((w >> (16 * h)) & 0xffffu));
+        const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&f));
+        out |= pack_e4m3x2(v.x * ratio, v.y * ratio) << (16 * h);
+    }
+    return out;
+}
+
+// A run as its warps know it.
+struct Run {
+    long long t0, page;
+    int n;
+    unsigned lo, hi;   // its rows of the page
+
+    // The run that begins at token t; none if t has no slot or stands behind one of its page.
+    __device__ __forceinline__ bool find(const RopeArgs& a, long long t) {
+        const int lane = lane_id();
+        auto page_of = [&](long long i) {   // of token i, -1 if it has none
+            const long long s = i >= 0 && i < a.T ? load(a.slots + i) : -1;
+            return s >= 0 && s < a.n_slots ? s >> 6 : -1LL;
+        };
+        t0 = t;
+        const long long before = page_of(t - 1), p0 = page_of(t + lane), p1 = page_of(t + 32 + lane);
+        page = __shfl_sync(0xffffffffu, p0, 0);
+        if (page < 0 || before == page) return false;
+        const unsigned m0 = __ballot_sync(0xffffffffu, p0 == page), m1 = __ballot_sync(0xffffffffu, p1 == page);
+        n = ~m0 != 0 ? __ffs(~m0) - 1 : 32 + (~m1 != 0 ? __ffs(~m1) - 1 : 32);
+        auto row_of = [&](int i) {   // of the run's token i; 64 where it has no place in the tables
+            if (i >= n) return 64;
+            const int p = t + i < a.T ? load(a.pos + t + i) : -1;
+            if (p < 0 || p >= a.max_pos) {
+                atomicExch(a.status, kStatusBadInput);
+                return 64;
+            }
+            return static_cast<int>((t + i < a.T ? load(a.slots + t + i) : 0) & 63);
+        };
+        const int r0 = row_of(lane), r1 = row_of(lane + 32);
+        lo = __reduce_or_sync(0xffffffffu, (r0 < 32 ? 1u << r0 : 0u) | (r1 < 32 ? 1u << r1 : 0u));
+        hi = __reduce_or_sync(0xffffffffu, (r0 >= 32 && r0 < 64 ? 1u << (r0 - 32) : 0u) | (r1 >= 32 && r1 < 64 ? 1u << (r1 - 32) : 0u));
+        return (lo | hi) != 0;
+    }
+};
+
+template <int D, bool INTER>
+__global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8 c) {
+    using R = Rows<D, 1>;
+    constexpr int P = kRunRows / R::GPW;   // passes: a group's rows
+    __shared__ Run longest;
+    __shared__ float tops[2][kWarps];
+    const int lane = lane_id(), warp = warp_id(), l = lane % R::LPR, g = lane / R::LPR;
+    const unsigned window = blockIdx.x / static_cast<unsigned>(a.Hkv);
+    const int head = static_cast<int>(blockIdx.x - window * a.Hkv);
+    const Place<INTER> pl(a, l);
+    const bool turns = turned(a, l);
+    if (threadIdx.x == 0) longest.n = 0;
+    grid_dep_wait();
+    Quads w;
+    w.load(a.wk, pl.ia, pl.ib);
+    // The warp's tokens i0 .. i0 + 7 of a run; JOINT: with the block's other warps.
+    auto work = [&](const Run& run, int i0, auto joint) {
+        constexpr bool JOINT = decltype(joint)::value;
+        const size_t at_scale = static_cast<size_t>(run.page) * a.Hkv + head;
+        const float old_k = load(c.k_scale + at_scale), old_v = load(c.v_scale + at_scale);
+        Quads kq[P];
+        uint4 v[P];
+        int pos[P], row[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int i = i0 + p * R::GPW + g;
+            const long long t = run.t0 + i;
+            row[p] = -1;
+            kq[p].a = kq[p].b = make_uint2(0, 0);
+            v[p] = make_uint4(0, 0, 0, 0);
+            pos[p] = 0;
+            if (i < run.n) {
+                pos[p] = t < a.T ? load(a.pos + t) : -1;
+                row[p] = static_cast<int>((t < a.T ? load(a.slots + t) : 0) & 63);
+                const bf16* const src = a.qkv + t * a.ld + static_cast<long long>(a.Hq + head) * D;
+                kq[p].load(src, pl.ia, pl.ib);
+                v[p] = load(reinterpret_cast<const uint4*>(src + static_cast<long long>(a.Hkv) * D + l * 8));
+            }
+        }
+        uint64_t y[P][4];
+        float top_k = 0.f, top_v = 0.f;
+        auto grow = [](float top, uint64_t x) {   // what is not finite has no say
+            float lo, hi;
+            f32x2_split(x, lo, hi);
+            lo = fabsf(lo);
+            hi = fabsf(hi);
+            return max3f(top, lo <= 3.4e38f ? lo : 0.f, hi <= 3.4e38f ? hi : 0.f);
+        };
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if (pos[p] < 0 || pos[p] >= a.max_pos) row[p] = -1;   // left out
+            uint64_t wf[4];
+            kq[p].unpack(y[p]);
+            w.unpack(wf);
+            uint64_t ss = mul_f32x2(y[p][0], y[p][0]);
+#pragma unroll
+            for (int i = 1; i < 4; ++i) ss = fma_f32x2(y[p][i], y[p][i], ss);
+            const uint64_t r = dup2(rsqrtf(R::sum(sum2(ss), 0xffffffffu) * (1.f / D) + a.eps));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[p][i] = mul_f32x2(mul_f32x2(y[p][i], r), wf[i]);
+            if (row[p] >= 0) {
+                if (turns) {
+                    const size_t from = static_cast<size_t>(pos[p]) * (a.rot >> 1) + 4 * l;
+                    const Turn<INTER, false, false> turn(reinterpret_cast<const uint8_t*>(a.cos + from),
+                                                         reinterpret_cast<const uint8_t*>(a.sin + from));
+                    turn.apply(y[p], true);
+                }
+                Quads q;
+                uint64_t vf[4];
+                q.a = make_uint2(v[p].x, v[p].y);
+                q.b = make_uint2(v[p].z, v[p].w);
+                q.unpack(vf);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    top_k = grow(top_k, y[p][i]);
+                    top_v = grow(top_v, vf[i]);
+                }
+            }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            top_k = fmaxf(top_k, __shfl_xor_sync(0xffffffffu, top_k, o));
+            top_v = fmaxf(top_v, __shfl_xor_sync(0xffffffffu, top_v, o));
+        }
+        if constexpr (JOINT) {
+            if (lane == 0) {
+                tops[0][warp] = top_k;
+                tops[1][warp] = top_v;
+            }
+            __syncthreads();   // and the old scales have been read
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) {
+                top_k = fmaxf(top_k, tops[0][i]);
+                top_v = fmaxf(top_v, tops[1][i]);
+            }
+        }
+        __syncwarp();
+        const bool fresh = (run.lo & 1u) != 0;
+        const float sk = fresh ? page_scale(top_k) : fmaxf(old_k, page_scale(top_k));
+        const float sv = fresh ? page_scale(top_v) : fmaxf(old_v, page_scale(top_v));
+        if (lane == 0 && (!JOINT || warp == 0)) {
+            c.k_scale[at_scale] = sk;
+            c.v_scale[at_scale] = sv;
+        }
+        const size_t base = at_scale * (64 * D);
+        const float ik = 1.f / sk, iv = 1.f / sv;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if (row[p] < 0) continue;
+            uint8_t* const k8 = c.K + base + row[p] * D;
+            *reinterpret_cast<uint32_t*>(k8 + pl.ia) = pack_quad(y[p][0], y[p][1], ik);
+            *reinterpret_cast<uint32_t*>(k8 + pl.ib) = pack_quad(y[p][2], y[p][3], ik);
+            Quads q;
+            uint64_t vf[4];
+            q.a = make_uint2(v[p].x, v[p].y);
+            q.b = make_uint2(v[p].z, v[p].w);
+            q.unpack(vf);
+            *reinterpret_cast<uint2*>(c.V + base + row[p] * D + l * 8) =
+                make_uint2(pack_quad(vf[0], vf[1], iv), pack_quad(vf[2], vf[3], iv));
+        }
+        // rows that stay, under a scale that grew
+        auto shrink = [&](uint8_t* page8, float ratio) {
+            constexpr int CH = D / 16;   // 16-byte chunks of a row
+            for (int i = JOINT ? static_cast<int>(threadIdx.x) : lane; i < 64 * CH; i += JOINT ? kThreads : 32) {
+                const int r = i / CH;
+                if (((r < 32 ? run.lo >> r : run.hi >> (r - 32)) & 1u) != 0) continue;
+                uint4* const p = reinterpret_cast<uint4*>(page8) + i;
+                const uint4 x = load(p);
+                *p = make_uint4(shrink_quad(x.x, ratio), shrink_quad(x.y, ratio), shrink_quad(x.z, ratio), shrink_quad(x.w, ratio));
+            }
+        };
+        if (!fresh && sk > old_k) shrink(c.K + base, old_k / sk);
+        if (!fresh && sv > old_v) shrink(c.V + base, old_v / sv);
+    };
+    const long long t = static_cast<long long>(window) * kRunRows + warp;
+    Run run;
+    __syncthreads();
+    if (t < a.T && run.find(a, t)) {
+        if (run.n > kRunRows) {
+            if (lane == 0) longest = run;
+        } else {
+            work(run, 0, std::false_type());
+        }
+    }
+    // slots that name no row of the cache (-1: padding)
+    if (head == 0 && lane == 0) {
+        const long long s = t < a.T ? load(a.slots + t) : -1;
+        if (s < -1 || s >= a.n_slots) atomicExch(a.status, kStatusBadInput);
+    }
+    __syncthreads();
+    if (longest.n > 0) {
+        const Run all = longest;
+        work(all, warp * kRunRows, std::true_type());
+    }
+}
+
+template <int D>
+cudaError_t launch_append8(const RopeArgs& a, const Cache8& c, const KernelEnv& env) {
+    const dim3 grid(static_cast<unsigned>((a.T + kRunRows - 1) / kRunRows * a.Hkv));
+    return launch_early(a.interleaved ? append8_kernel<D, true> : append8_kernel<D, false>, grid, kThreads, 0, env.stream, a, c);
+}
+
 template <int D>
 cudaError_t prepare_fwd() {
     const void* kernels[] = {reinterpret_cast<const void*>(rope_fwd_kernel<D, true, true, true>),
@@ -554,6 +802,8 @@ const char* rope_check(int rot, int interleaved, int max_pos, float eps, long lo
 // Tokens are counted in 32 bits where a batch row is found by division.
 bool rope_supported(const RopeArgs& a) { return a.T <= 0x7fffffffLL; }
 
+bool append8_supported(const RopeArgs& a) { return (a.T + kRunRows - 1) / kRunRows * a.Hkv <= 0x7fffffffLL; }
+
 int rope_bwd_max_blocks() { return kBwdBlocks * device_sm_count(); }   // all resident
 
 cudaError_t rope_paged_prepare(int d) {
@@ -565,6 +815,14 @@ cudaError_t launch_rope_fwd(const RopeArgs& a, int d, const KernelEnv& env) {
     if (d == 128) return a.interleaved ? launch_any_fwd<128, true>(a, env) : launch_any_fwd<128, false>(a, env);
     if (d == 64) return a.interleaved ? launch_any_fwd<64, true>(a, env) : launch_any_fwd<64, false>(a, env);
     return cudaErrorInvalidValue;
+}
+
+cudaError_t launch_append8(const RopeArgs& a, const Cache8& c, int d, const KernelEnv& env) {
+    RopeArgs q = a;   // the queries alone: rows of the fused projection's first heads
+    q.Hkv = 0;
+    const cudaError_t e = launch_rope_fwd(q, d, env);
+    if (e != cudaSuccess) return e;
+    return d == 128 ? launch_append8<128>(a, c, env) : launch_append8<64>(a, c, env);
 }
 
 cudaError_t launch_rope_bwd(const RopeArgs& a, int d, const KernelEnv& env) {

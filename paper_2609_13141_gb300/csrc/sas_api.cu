@@ -53,6 +53,19 @@ int make_tmap_bf16_box(CUtensorMap* map, const void* base, uint64_t inner, uint6
     return static_cast<int>(r);
 }
 
+int make_tmap_u8_3d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t outer) {
+    std::call_once(g_encode_once, resolve_encode);
+    if (g_encode == nullptr) return -1;
+    cuuint64_t dims[3] = {inner, rows, outer};
+    cuuint64_t strides[2] = {inner, inner * rows};
+    cuuint32_t box[3] = {static_cast<cuuint32_t>(inner), static_cast<cuuint32_t>(rows), 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, inner == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return static_cast<int>(r);
+}
+
 // --------------------------------------------- per-device launch attributes
 
 namespace {

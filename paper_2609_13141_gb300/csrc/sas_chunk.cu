@@ -178,6 +178,7 @@ sas_status sas_chunk_create(const sas_chunk_config* cfg, sas_chunk_handle** out)
     if (e == cudaSuccess) e = sas::plan_prepare(c.max_seqs);
     if (e == cudaSuccess) e = sas::rope_paged_prepare(c.d);
     if (e == cudaSuccess) e = sas::chunk_attn_prepare(c.d);
+    if (e == cudaSuccess) e = sas::chunk8_prepare(c.d);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) {
         const sas_status s = e == cudaErrorMemoryAllocation ? SAS_ERR_OOM : SAS_ERR_CUDA;
@@ -270,6 +271,41 @@ sas_status sas_chunk_append(sas_chunk_handle* h, const sas_rope_config* rope, in
     });
 }
 
+sas_status sas_chunk_append8(sas_chunk_handle* h, const sas_rope_config* rope, int32_t T, const void* qkv, int64_t ld,
+                             const void* wq, const void* wk, const float* cos, const float* sin,
+                             const int32_t* positions, const int64_t* slots, void* Q, void* K_cache, void* V_cache,
+                             float* K_scale, float* V_scale, void* stream) {
+    if (h == nullptr) return SAS_ERR_INVALID_ARG;
+    return guarded(h, [&]() -> sas_status {
+        if (sas_status st = on_device(h); st != SAS_OK) return st;
+        const sas_chunk_config& c = h->cfg;
+        if (T < 1 || T > c.max_tokens) return cfail(h, SAS_ERR_INVALID_ARG, "T must be 1 .. max_tokens");
+        if (!rope || !qkv || !wq || !wk || !cos || !sin || !positions || !slots || !Q || !K_cache || !V_cache || !K_scale ||
+            !V_scale)
+            return cfail(h, SAS_ERR_INVALID_ARG, "a required argument is NULL");
+        if (!al16(qkv) || !al16(wq) || !al16(wk) || !al16(cos) || !al16(sin) || !al4(positions) || !al8(slots) || !al16(Q) ||
+            !al16(K_cache) || !al16(V_cache) || !al4(K_scale) || !al4(V_scale))
+            return cfail(h, SAS_ERR_INVALID_ARG, "misaligned pointer");
+        if (const char* why = sas::rope_check(rope->rot, rope->interleaved, rope->max_pos, rope->eps,
+                                              c.Hq + 2LL * c.Hkv, c.d, ld))
+            return cfail(h, SAS_ERR_INVALID_ARG, why);
+        sas::RopeArgs a{};
+        a.qkv = static_cast<const sas::bf16*>(qkv); a.ld = ld;
+        a.wq = static_cast<const sas::bf16*>(wq); a.wk = static_cast<const sas::bf16*>(wk);
+        a.cos = cos; a.sin = sin; a.pos = positions;
+        a.max_pos = rope->max_pos; a.rot = rope->rot; a.interleaved = rope->interleaved; a.eps = rope->eps;
+        a.Hq = c.Hq; a.Hkv = c.Hkv; a.T = T; a.N = T;
+        a.Q = static_cast<sas::bf16*>(Q);
+        const sas::Cache8 cache{static_cast<uint8_t*>(K_cache), static_cast<uint8_t*>(V_cache), K_scale, V_scale};
+        a.slots = slots; a.n_slots = 64LL * c.num_pages; a.status = h->status;
+        if (!sas::rope_supported(a) || !sas::append8_supported(a)) return cfail(h, SAS_ERR_UNSUPPORTED, "too many tokens");
+        cudaStream_t s = static_cast<cudaStream_t>(stream);
+        const sas::KernelEnv env{s, h->status, h->limit};
+        const cudaError_t e = ctimed(h, 1, 2, s, [&] { return sas::launch_append8(a, cache, c.d, env); });
+        return e == cudaSuccess ? SAS_OK : ccuda_fail(h, e, "norm + rotation + 8-bit append");
+    });
+}
+
 sas_status sas_chunk_attention(sas_chunk_handle* h, int32_t num_seqs, int32_t T, const void* Q, const void* K_cache,
                                const void* V_cache, const int32_t* block_table, const int32_t* cu_new,
                                const int32_t* kv_lens, void* O, float* LSE, void* stream) {
@@ -298,6 +334,40 @@ sas_status sas_chunk_attention(sas_chunk_handle* h, int32_t num_seqs, int32_t T,
         const sas::KernelEnv env{s, h->status, h->limit};
         const char* err = "chunk attention";
         const cudaError_t e = ctimed(h, 2, 2, s, [&] { return sas::launch_chunk_attn(a, env, &err); });
+        return e == cudaSuccess ? SAS_OK : ccuda_fail(h, e, err);
+    });
+}
+
+sas_status sas_chunk_attention8(sas_chunk_handle* h, int32_t num_seqs, int32_t T, const void* Q, const void* K_cache,
+                                const void* V_cache, const float* K_scale, const float* V_scale,
+                                const int32_t* block_table, const int32_t* cu_new, const int32_t* kv_lens, void* O,
+                                float* LSE, void* stream) {
+    if (h == nullptr) return SAS_ERR_INVALID_ARG;
+    return guarded(h, [&]() -> sas_status {
+        if (sas_status st = on_device(h); st != SAS_OK) return st;
+        const sas_chunk_config& c = h->cfg;
+        if (num_seqs < 1 || num_seqs > c.max_seqs)
+            return cfail(h, SAS_ERR_INVALID_ARG, "num_seqs must be 1 .. max_seqs");
+        if (T < 1 || T > c.max_tokens) return cfail(h, SAS_ERR_INVALID_ARG, "T must be 1 .. max_tokens");
+        if (!Q || !K_cache || !V_cache || !K_scale || !V_scale || !block_table || !cu_new || !kv_lens || !O)
+            return cfail(h, SAS_ERR_INVALID_ARG, "a required argument is NULL");
+        if (!al16(Q) || !al16(K_cache) || !al16(V_cache) || !al4(block_table) || !al4(cu_new) || !al4(kv_lens) || !al16(O) ||
+            !al4(LSE) || !al4(K_scale) || !al4(V_scale))
+            return cfail(h, SAS_ERR_INVALID_ARG, "misaligned pointer");
+        sas::ChunkArgs a{};
+        a.B = num_seqs; a.T = T; a.Hq = c.Hq; a.Hkv = c.Hkv; a.G = h->G; a.d = c.d; a.max_blocks = c.max_blocks;
+        a.num_pages = c.num_pages; a.sm_scale = h->sm_scale;
+        a.Q = static_cast<const sas::bf16*>(Q);
+        a.K8 = static_cast<const uint8_t*>(K_cache); a.V8 = static_cast<const uint8_t*>(V_cache);
+        a.k_scale = K_scale; a.v_scale = V_scale;
+        a.block_table = block_table; a.cu = cu_new; a.kv_lens = kv_lens;
+        a.O = static_cast<sas::bf16*>(O); a.LSE = LSE;
+        a.blocks = h->blocks; a.joins = h->joins; a.part_o = h->part_o; a.part_ml = h->part_ml;
+        a.status = h->status;
+        cudaStream_t s = static_cast<cudaStream_t>(stream);
+        const sas::KernelEnv env{s, h->status, h->limit};
+        const char* err = "8-bit attention";
+        const cudaError_t e = ctimed(h, 2, 2, s, [&] { return sas::launch_chunk8(a, env, &err); });
         return e == cudaSuccess ? SAS_OK : ccuda_fail(h, e, err);
     });
 }

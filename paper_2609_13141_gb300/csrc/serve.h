@@ -9,6 +9,10 @@ namespace sas {
 int make_tmap_bf16_box(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t outer,
                        uint32_t box_inner, uint32_t box_rows, uint32_t box_outer);
 
+// 3-D map of bytes [outer][rows][inner] with an (inner x rows x 1) box, swizzled over its rows of 64
+// or 128 bytes.
+int make_tmap_u8_3d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t outer);
+
 // ---- per-head RMS norm of queries and keys + rotation (forward, into cache pages, gradient).
 struct RopeArgs {
     const bf16* qkv;            // [T] rows of (Hq + 2 Hkv) d elements, ld elements apart
@@ -38,12 +42,22 @@ struct RopeArgs {
     int* counter;               // zero between launches
     int* status;
 };
+// Cache of e4m3 numbers, a scale for each page and KV head.
+struct Cache8 {
+    uint8_t* K;                 // [num_pages][Hkv][64][d]
+    uint8_t* V;
+    float* k_scale;             // [num_pages][Hkv]
+    float* v_scale;
+};
 // What is wrong with a rotation of rows of `heads` heads, ld elements apart, or null.
 const char* rope_check(int rot, int interleaved, int max_pos, float eps, long long heads, int d, long long ld);
 bool rope_supported(const RopeArgs& a);   // the kernels can count this many tokens
 int rope_bwd_max_blocks();
 cudaError_t rope_paged_prepare(int d);    // shared-memory limit of the form into cache pages (before any capture)
 cudaError_t launch_rope_fwd(const RopeArgs& a, int d, const KernelEnv& env);
+bool append8_supported(const RopeArgs& a);   // one block a head and 8 tokens
+// Queries to a.Q, keys and values into an 8-bit cache (a.K and a.V are not used): two launches.
+cudaError_t launch_append8(const RopeArgs& a, const Cache8& c, int d, const KernelEnv& env);
 cudaError_t launch_rope_bwd(const RopeArgs& a, int d, const KernelEnv& env);
 
 // ---- page plan of a serving step.
@@ -92,6 +106,10 @@ struct ChunkArgs {
     const bf16* Q;              // [T][Hq][d]
     const bf16* K_cache;        // [num_pages][Hkv][64][d]
     const bf16* V_cache;
+    const uint8_t* K8;          // the 8-bit form: [num_pages][Hkv][64][d] and [num_pages][Hkv]
+    const uint8_t* V8;
+    const float* k_scale;
+    const float* v_scale;
     const int32_t* block_table; // [B][max_blocks]
     const int32_t* cu;          // [B + 1] first new token of each sequence
     const int32_t* kv_lens;     // [B] tokens of each sequence, the new ones included
@@ -108,6 +126,8 @@ struct ChunkArgs {
 int chunk_blocks();             // blocks of the attention; each writes at most two splits
 cudaError_t chunk_attn_prepare(int d);   // shared-memory limit (before any capture)
 cudaError_t launch_chunk_attn(const ChunkArgs& a, const KernelEnv& env, const char** err);
+cudaError_t chunk8_prepare(int d);
+cudaError_t launch_chunk8(ChunkArgs a, const KernelEnv& env, const char** err);   // over an 8-bit cache
 
 // ---- log probabilities of given tokens, entropy and likeliest columns; their gradient.
 struct LogpArgs {

@@ -167,6 +167,10 @@ def lib():
     L.sas_chunk_append.restype = i32
     L.sas_chunk_attention.argtypes = [vp, i32, i32] + [vp] * 9
     L.sas_chunk_attention.restype = i32
+    L.sas_chunk_append8.argtypes = [vp, rope, i32, vp, i64] + [vp] * 12
+    L.sas_chunk_append8.restype = i32
+    L.sas_chunk_attention8.argtypes = [vp, i32, i32] + [vp] * 11
+    L.sas_chunk_attention8.restype = i32
     L.sas_chunk_verify.argtypes = [vp] + [i32] * 4 + [vp, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp]
     L.sas_chunk_verify.restype = i32
     L.sas_token_logprobs.argtypes = [vp, i32, i32, vp, i32, i64] + [vp] * 5
@@ -897,6 +901,37 @@ def sas_chunk_attention(h, Q, K_cache, V_cache, block_table, cu_new, kv_lens, O,
         _ccheck(st, h, "sas_chunk_attention")
 
 
+def sas_chunk_append8(h, qkv, wq, wk, cos, sin, positions, slots, Q, K_cache, V_cache, K_scale, V_scale, eps=1e-6,
+                      interleaved=False, stream=None):
+    """As sas_chunk_append, into a cache of e4m3 numbers with a scale for each page and KV head."""
+    Hq, d, _, cache = _sizes(h)
+    T, Hkv, dev, bf, f32, e4 = Q.shape[0], cache[1], Q.get_device(), torch.bfloat16, torch.float32, torch.float8_e4m3fn
+    cfg = _rope_config(cos, eps, interleaved)
+    st = lib().sas_chunk_append8(
+        h, cfg, T, _rows(qkv, bf, "qkv", dev, (T, Hq + 2 * Hkv, d)), _token_stride(qkv, "qkv", 1),
+        _arg(wq, bf, "wq", dev, (d,)), _arg(wk, bf, "wk", dev, (d,)), _arg(cos, f32, "cos", dev), _arg(sin, f32, "sin", dev, cos.shape),
+        _arg(positions, torch.int32, "positions", dev, (T,)), _arg(slots, torch.int64, "slots", dev, (T,)),
+        _arg(Q, bf, "Q", dev, (T, Hq, d)), _arg(K_cache, e4, "K_cache", dev, cache), _arg(V_cache, e4, "V_cache", dev, cache),
+        _arg(K_scale, f32, "K_scale", dev, cache[:2]), _arg(V_scale, f32, "V_scale", dev, cache[:2]), _raw_stream(stream, dev))
+    if st != SAS_OK:
+        _ccheck(st, h, "sas_chunk_append8")
+
+
+def sas_chunk_attention8(h, Q, K_cache, V_cache, K_scale, V_scale, block_table, cu_new, kv_lens, O, LSE=None, stream=None):
+    i32, bf, f32, e4 = torch.int32, torch.bfloat16, torch.float32, torch.float8_e4m3fn
+    B, T, dev = kv_lens.shape[0], Q.shape[0], Q.get_device()
+    _table(h, block_table, B)
+    Hq, d, _, cache = _sizes(h)
+    st = lib().sas_chunk_attention8(
+        h, B, T, _arg(Q, bf, "Q", dev, (T, Hq, d)), _arg(K_cache, e4, "K_cache", dev, cache),
+        _arg(V_cache, e4, "V_cache", dev, cache), _arg(K_scale, f32, "K_scale", dev, cache[:2]),
+        _arg(V_scale, f32, "V_scale", dev, cache[:2]), _arg(block_table, i32, "block_table", dev),
+        _arg(cu_new, i32, "cu_new", dev, (B + 1,)), _arg(kv_lens, i32, "kv_lens", dev, (B,)), _arg(O, bf, "O", dev, Q.shape),
+        None if LSE is None else _arg(LSE, f32, "LSE", dev, Q.shape[:2]), _raw_stream(stream, dev))
+    if st != SAS_OK:
+        _ccheck(st, h, "sas_chunk_attention8")
+
+
 def _prob_rows(t, name, rows, dev, V):
     """Address and row stride of an fp32 [rows, V] tensor with contiguous columns."""
     at = _rows(t, torch.float32, name, dev, (rows, V))
@@ -1018,6 +1053,25 @@ class SasChunk:
             with _on(stream):
                 out = (torch.empty_like(Q), torch.empty(Q.shape[:2], device=Q.device, dtype=torch.float32))
         sas_chunk_attention(self.h, Q, K_cache, V_cache, block_table, cu_new, kv_lens, out[0], out[1], stream)
+        return out
+
+    def append8(self, qkv, wq, wk, cos, sin, positions, slots, K_cache, V_cache, K_scale, V_scale, eps=1e-6, interleaved=False,
+                out=None, stream=None):
+        """append into an 8-bit cache: K_cache, V_cache torch.float8_e4m3fn, K_scale, V_scale fp32 [num_pages, Hkv], which
+        need no values before their page's first row is written.  The new tokens of a page stand next to each other."""
+        if out is None:
+            with _on(stream):
+                out = torch.empty(qkv.shape[0], self.Hq, self.d, device=qkv.device, dtype=torch.bfloat16)
+        sas_chunk_append8(self.h, qkv, wq, wk, cos, sin, positions, slots, out, K_cache, V_cache, K_scale, V_scale, eps,
+                          interleaved, stream)
+        return out
+
+    def attention8(self, Q, K_cache, V_cache, K_scale, V_scale, block_table, cu_new, kv_lens, out=None, stream=None):
+        """attention over an 8-bit cache (append8).  Returns (O [T, Hq, d], LSE [T, Hq]); out as in attention."""
+        if out is None:
+            with _on(stream):
+                out = (torch.empty_like(Q), torch.empty(Q.shape[:2], device=Q.device, dtype=torch.float32))
+        sas_chunk_attention8(self.h, Q, K_cache, V_cache, K_scale, V_scale, block_table, cu_new, kv_lens, out[0], out[1], stream)
         return out
 
     def logprob_buffers(self, T, topk, device):
