@@ -594,9 +594,15 @@ cudaError_t prepare() {
 
 }  // namespace
 
-cudaError_t chunk8_prepare(int d) { return d == 128 ? prepare<128>() : prepare<64>(); }
+cudaError_t chunk8_prepare(int d) {
+    const cudaError_t e = d == 128 ? prepare<128>() : prepare<64>();
+    return e == cudaSuccess ? chunk8_tile_prepare(d) : e;
+}
 
 cudaError_t launch_chunk8(ChunkArgs a, const KernelEnv& env, const char** err) {
+    // Requests of more than 32 rows on average: tiles of 128 rows, whose products cost the same however many of
+    // the rows there are.
+    if (static_cast<long long>(a.T) * a.G > 32LL * a.B) return launch_chunk8_tile(a, env, err);
     a.blocks = device_sm_count();   // one a multiprocessor
     if (a.d == 128) return launch_rows<128>(a, env, err);
     if (a.d == 64) return launch_rows<64>(a, env, err);

@@ -127,6 +127,8 @@ int chunk_blocks();             // blocks of the attention; each writes at most 
 cudaError_t chunk_attn_prepare(int d);   // shared-memory limit (before any capture)
 cudaError_t launch_chunk_attn(const ChunkArgs& a, const KernelEnv& env, const char** err);
 cudaError_t chunk8_prepare(int d);
+cudaError_t chunk8_tile_prepare(int d);
+cudaError_t launch_chunk8_tile(const ChunkArgs& a, const KernelEnv& env, const char** err);
 cudaError_t launch_chunk8(ChunkArgs a, const KernelEnv& env, const char** err);   // over an 8-bit cache
 
 // ---- log probabilities of given tokens, entropy and likeliest columns; their gradient.
