@@ -49,12 +49,13 @@ struct Seq {
     // pages of tile t
     __device__ __forceinline__ int pages(int t, int rl) const { return ((L - n + min(n, (t + 1) << rl) - 1) >> 6) + 1; }
     // Cost of tiles 0 .. m - 1, all full: their pages are the sum over t = 1 .. m of floor((p + t R) / 64) + 1
-    // with p = L - n - 1 = 64 q + r.  For R <= 64 = k R the floor is q + floor((floor(r / R) + t) / k), and sums
+    // with p = L - n - 1 = 64 q + r.  For R >= 64 the floor is q + t R / 64.  For R = 64 / k it
+    // is q + floor((floor(r / R) + t) / k), and sums
     // of floor(u / k) over u = 0 .. x are k y (y - 1) / 2 + y (x % k + 1), y = floor(x / k).
     __device__ __forceinline__ long long before(int m, int rl) const {
         const int p = L - n - 1;
         const long long flat = static_cast<long long>(m) * ((p >> 6) + 1 + kUnitCost);
-        if (rl == 7) return flat + static_cast<long long>(m) * (m + 1);
+        if (rl >= 6) return flat + (static_cast<long long>(m) * (m + 1) / 2 << (rl - 6));
         const int kl = 6 - rl, x = ((p & 63) >> rl) + m;
         const long long y = x >> kl;
         return flat + ((y * (y - 1) / 2) << kl) + y * ((x & ((1 << kl) - 1)) + 1);
@@ -314,7 +315,8 @@ struct Walk {
 // once.  (A join that finds its splits itself before the wait saves one load's latency,
 // and takes more from the attention blocks still at work: 117 against 113 us for a mixed
 // batch at d = 128.)
-template <int D>
+// TILES: a tile's rows come 128 to a slot of the splits.
+template <int D, int TILES = 1>
 __global__ void __launch_bounds__(kJoinThreads, 2) chunk_join_kernel(ChunkArgs a) {
     constexpr int QUADS = D / 4;      // of columns
     constexpr int QB = 2, U = 4;      // quads and splits of a thread in flight together
@@ -330,7 +332,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) chunk_join_kernel(ChunkArgs a
     // that are all NaN leave a maximum of -infinity too, but a sum of NaN, which has to come through.
     auto nothing = [](float m, float l) { return m == -CUDART_INF_F && l == 0.f; };
     // split s: the first in its slot, the others in slot 0 of the following blocks
-    auto slot = [&](int s) { return static_cast<size_t>(2 * (u.y + s) + (s == 0 ? v.z : 0)); };
+    auto slot = [&](int s) { return static_cast<size_t>(2 * (u.y + s) + (s == 0 ? v.z : 0)) * TILES; };
     constexpr int QL = D == 128 ? 5 : 4, TL = 9;
     static_assert(QUADS == 1 << QL && kJoinThreads == 1 << TL, "powers of two");
     const int rpl = max(2, 32 - __clz(rows - 1));       // rows, to a power of two (a clz of 0 is 32)
@@ -345,7 +347,8 @@ __global__ void __launch_bounds__(kJoinThreads, 2) chunk_join_kernel(ChunkArgs a
     const int at = live ? row : 0;
     const int tok = at >> gl, h = at & (a.G - 1);
     const size_t orow = (static_cast<size_t>(u.w) + tok) * a.Hq + static_cast<size_t>(u.z) * a.G + h;
-    const float4* const po = reinterpret_cast<const float4*>(a.part_o) + at;
+    const int sub = TILES > 1 ? at >> 7 : 0, in = TILES > 1 ? at & 127 : at;
+    const float4* const po = reinterpret_cast<const float4*>(a.part_o) + in;
     for (int q0 = 0; q0 < per; q0 += QB) {
         const int quad = cg * per + q0;
         float M = -CUDART_INF_F, L = 0.f;
@@ -360,10 +363,10 @@ __global__ void __launch_bounds__(kJoinThreads, 2) chunk_join_kernel(ChunkArgs a
                 const int s = s0 + i * shares;
                 ml[i] = make_float2(-CUDART_INF_F, 0.f);
                 if (s < ns) {
-                    ml[i] = __ldcg(a.part_ml + slot(s) * kBM + at);
+                    ml[i] = __ldcg(a.part_ml + (slot(s) + sub) * kBM + in);
 #pragma unroll
                     for (int k = 0; k < QB; ++k)
-                        if (k < per) x[i][k] = __ldcg(po + (slot(s) * QUADS + quad + k) * kBM);
+                        if (k < per) x[i][k] = __ldcg(po + ((slot(s) + sub) * QUADS + quad + k) * kBM);
                 }
             }
             float m2 = M;

@@ -6,13 +6,18 @@
 // weights to 8 bits would show.  So the pages' numbers become f16, exactly, in shared memory:
 //   * warp 0 takes work items, publishes them and loads 8-bit pages by bulk copies (one ring,
 //     K and V pages in turn);
-//   * warps 2 and 3 convert, half of a page's rows each, into rings of f16 tiles in the tensor
-//     core's layout, value rows of no key as zero;
+//   * two or four warps convert, a share of a page's rows each, into rings of f16 tiles in the
+//     tensor core's layout, value rows of no key as zero;
 //   * warp 1 issues S = Q K^T and O += P V (P read from tensor memory);
-//   * warps 4-7, a thread per row: Q as f16 under a power of two of the row's own (k_chunk8.cu),
-//     mask, online softmax in the log2 domain, P as f16 pairs into tensor memory, O rescaled
-//     only when the maximum grows by 2^8, or where a page's value scale leaves 2^-6 .. 2^6 times
-//     the one that O stands under.
+//   * four warps a tile, a thread per row: Q as f16 under a power of two of the row's own
+//     (k_chunk8.cu), mask, online softmax in the log2 domain, P as f16 pairs into tensor memory,
+//     O rescaled only when the maximum grows by 2^8, or where a page's value scale leaves 2^-6 ..
+//     2^6 times the one that O stands under.
+//
+// TILES: 128-row tiles of a block, which share its converted pages.  The conversion costs shared
+// memory 64 d bytes in and 128 d out a page and matrix, as much time as the products' operands
+// take, so long requests have two tiles a block and one block a multiprocessor; requests of fewer
+// rows one tile a block and two blocks, each with its own pages.
 #include <cuda_fp16.h>
 
 #include "chunk_work.cuh"
@@ -20,34 +25,37 @@
 namespace sas {
 namespace {
 
-constexpr int kThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescaleThreshold = 8.0f;   // log2 units
-constexpr float kScaleRange = 64.f;
+constexpr float kScaleRange = 6.f;              // log2 units
 constexpr int kItemSlots = 4;     // work items in flight between warp 0 and the other roles
-constexpr int kItemReaders = 7;   // the MMA issuer, two that convert, four softmax warps
 constexpr int kStatusLayout = 3;
-static_assert(kThreads == kRangeThreads, "find_range");
+constexpr long long kTwoTiles = 192;   // rows of a request on average
 
 // As in k_chunk.cu: a step is KPS pages, whose scores, softmax and product go through the
 // pipeline together; half of Q in tensor memory at d = 128.
-template <int D>
+template <int D, int TILES>
 struct Cfg {
     static constexpr int KPS = D == 64 ? 2 : 1;
     static constexpr bool QT = D == 128;
-    static constexpr int Q_BYTES = kBM * 128;        // 64 dims of the rows in shared memory
-    static constexpr int QST = D == 64 ? 2 : 1;      // Q tiles (of the item at work, and the next one's)
+    static constexpr int THREADS = 256 * TILES;
+    static constexpr int CONV0 = 2 * TILES, CONV = 2 * TILES;   // the warps that convert
+    static constexpr int SOFT0 = 4 * TILES;                     // the softmax warps, four a tile
+    static constexpr int READERS = TILES + CONV + 4 * TILES;   // of an item
+    static constexpr int Q_BYTES = kBM * 128;        // 64 dims of a tile's rows in shared memory
     static constexpr int KV_BYTES = kBN * D * 2;
     static constexpr int PAGE = kBN * D;
-    static constexpr int KST = D == 64 ? 4 : 2;      // f16 pages of a ring
-    static constexpr int SST = D == 64 ? 4 : 4;      // 8-bit pages
-    static constexpr int OFF_K = QST * Q_BYTES;
+    static constexpr int KST = D == 64 ? (TILES == 2 ? 6 : 4) : (TILES == 2 ? 3 : 2);     // f16 pages of a ring
+    static constexpr int SST = D == 64 ? (TILES == 2 ? 16 : 8) : (TILES == 2 ? 10 : 4);   // 8-bit pages
+    static constexpr int SCALES = TILES == 2 ? 32 : 16;   // pages' scales: the loads are SST / 2 + KST + 2 KPS pages ahead of the softmax at most
+    static_assert(SST / 2 + KST + 2 * KPS <= SCALES, "scales");
+    static constexpr int OFF_K = TILES * Q_BYTES;
     static constexpr int OFF_V = OFF_K + KST * KV_BYTES;
     static constexpr int OFF_S = OFF_V + KST * KV_BYTES;
     static constexpr int OFF_CTL = OFF_S + SST * PAGE;
-    static constexpr int SMEM = OFF_CTL + 1024;      // barriers and items, then Shares
-    static_assert(2 * (SMEM + 1024) <= 233472, "two blocks a multiprocessor");
-    static constexpr int TMEM_COLS = 256;
+    static constexpr int SMEM = OFF_CTL + 1024 * TILES;      // barriers and items, then Shares
+    static_assert(2 / TILES * (SMEM + 1024) <= 233472, "blocks a multiprocessor");
+    static constexpr int TMEM_COLS = 256;               // of a tile
     static constexpr int TMEM_O = 0;
     static constexpr int TMEM_S = D;
     static constexpr int TMEM_P = TMEM_S + KPS * kBN;   // keys packed in pairs
@@ -57,31 +65,33 @@ struct Cfg {
     static constexpr uint32_t IDESC_O = idesc_f16(kBM, D, 0, 1);
 };
 
-// Moves registers between the block's two warpgroups (the sum stays within what it was
-// launched with: 128 threads x (64 + 184) <= 256 x 128).
-template <int D>
+// Moves registers between the block's warpgroups (the sum stays within what it was launched
+// with: 128 threads x (64 + 184) <= 256 x 128, 128 x (64 + 64 + 2 x 192) = 512 x 128).
+template <int D, int TILES>
 __device__ __forceinline__ void give_registers() {
-    if constexpr (Cfg<D>::KPS == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if constexpr (TILES == 2 || D == 64) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
 }
-template <int D>
+template <int D, int TILES>
 __device__ __forceinline__ void take_registers() {
-    if constexpr (Cfg<D>::KPS == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    if constexpr (TILES == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    else if constexpr (D == 64) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
 }
 
+template <class C, int TILES>
 struct Ctl {
-    uint64_t s_full[4], s_empty[4], k_full[4], k_empty[4], v_full[4], v_empty[4];
-    uint64_t sc_full, sc_free, p_full, pv_done, q_ready, drain_bar;
+    uint64_t s_full[C::SST], s_empty[C::SST], k_full[C::KST], k_empty[C::KST], v_full[C::KST], v_empty[C::KST];
+    uint64_t sc_full[TILES], sc_free[TILES], p_full[TILES], pv_done[TILES], q_ready[TILES], drain_bar;
     uint64_t item_full[kItemSlots], item_empty[kItemSlots];
-    float ks[16], vs[16];      // scales of page g at g % 16 (the loads are 8 pages ahead of the softmax at most)
+    float4 scale[C::SCALES];   // of page g at g % SCALES: the keys', the values' log2, inverse and itself
     Item item[kItemSlots];
     uint32_t tmem_base;
     int abort_flag;
-    int again;                 // the step's product comes in two parts
+    int again[TILES];          // the step's product comes in two parts
 };
-static_assert(sizeof(Ctl) <= 720 && sizeof(Shares) <= 304, "control block");
-constexpr int kSharesAt = 720;
+constexpr int kSharesAt = 832;
 
-__device__ __forceinline__ bool read_item(Ctl& ctl, int r, const WaitCtl& wc, Item& x) {
+template <class K>
+__device__ __forceinline__ bool read_item(K& ctl, int r, const WaitCtl& wc, Item& x) {
     const int slot = r % kItemSlots;
     if (!mbar_poll_warp(&ctl.item_full[slot], (r / kItemSlots) & 1, wc)) return false;
     x = ctl.item[slot];
@@ -101,39 +111,52 @@ __device__ __forceinline__ void to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
         : "r"(w));
 }
 
-// Half of a page's rows (32 half ..) from bytes to a 128-byte-swizzled f16 tile [D / 64][64][64];
-// rows from `live` on become zero.  Reads are 16 bytes a lane in order; a lane writes two
-// neighbouring 16-byte pieces, at D = 128 in an order that keeps eight lanes' pieces in
-// different banks.
-template <int D>
-__device__ __forceinline__ void convert(uint8_t* dst, const uint8_t* src, int half, int lane, int live) {
-    constexpr int CH = D / 16, N = 32 * CH / 32;   // 16-byte chunks of a row, of a lane
+// The share-th of NC shares of a page's rows from bytes to a 128-byte-swizzled f16 tile [D /
+// 64][64][64]; rows from `live` on become zero.  Eight lanes read 64 bytes of a row and 64 of the
+// next one, at D = 128 the other half of it, which puts both their 16-byte reads and the two
+// 16-byte pieces that each writes into different banks, at offsets that are a lane's own all the
+// way.
+template <int D, int NC>
+__device__ __forceinline__ void convert(uint8_t* dst, const uint8_t* src, int share, int lane, int live) {
+    constexpr int ROWS = kBN / NC, PASS = D / 64, N = ROWS / 8 * PASS, B = N < 4 ? N : 4;
+    const int sub = lane >> 2 & 1, c = lane & 3, row = share * ROWS + (lane >> 2);
+    const int piece = ((2 * c) ^ (row & 7)) << 4;
+    src += row * D + c * 16;
+    dst += row * 128;
 #pragma unroll
-    for (int i0 = 0; i0 < N; i0 += 4) {
-        uint4 w[4];
+    for (int i0 = 0; i0 < N; i0 += B) {
+        uint4 w[B];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint4*>(src + half * (32 * D) + ((i0 + i) * 32 + lane) * 16);
+        for (int i = 0; i < B; ++i) {   // 8 rows further every PASS pieces
+            const int at = (i0 + i) / PASS * 8, half = PASS == 2 ? sub ^ (i & 1) : 0;
+            w[i] = *reinterpret_cast<const uint4*>(src + at * D + half * 64);
+        }
+        if (live < kBN) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = (i0 + i) * 32 + lane, row = half * 32 + at / CH, c = at % CH;
+            for (int i = 0; i < B; ++i)
+                if (row + (i0 + i) / PASS * 8 >= live) w[i] = make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            const int at = (i0 + i) / PASS * 8, half = PASS == 2 ? sub ^ (i & 1) : 0;
             uint4 a, b;
             to_f16(w[i].x, a.x, a.y);
             to_f16(w[i].y, a.z, a.w);
             to_f16(w[i].z, b.x, b.y);
             to_f16(w[i].w, b.z, b.w);
-            if (row >= live) a = b = make_uint4(0, 0, 0, 0);
-            const int h = c >> 2, p = (2 * c) & 7, x = row & 7;
-            uint8_t* const to = dst + h * (kBN * 128) + row * 128;
-            const bool swap = h != 0;
-            *reinterpret_cast<uint4*>(to + (((p + swap) ^ x) << 4)) = swap ? b : a;
-            *reinterpret_cast<uint4*>(to + (((p + !swap) ^ x) << 4)) = swap ? a : b;
+            uint8_t* const to = dst + at * 128 + half * (kBN * 128);
+            *reinterpret_cast<uint4*>(to + piece) = a;
+            *reinterpret_cast<uint4*>(to + (piece ^ 16)) = b;
         }
     }
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, float scale_log2, long long limit) {
-    using C = Cfg<D>;
+template <int D, int TILES>
+__global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(ChunkArgs a, float scale_log2, long long limit) {
+    using C = Cfg<D, TILES>;
+    using K = Ctl<C, TILES>;
+    constexpr int shares_at = TILES == 1 ? kSharesAt : 1600;
+    static_assert(sizeof(K) <= shares_at && shares_at + sizeof(Shares) <= 1024 * TILES, "control block");
     extern __shared__ __align__(1024) uint8_t smem[];
     if ((smem_u32(smem) & 1023u) != 0) {
         grid_dep_wait();
@@ -143,45 +166,48 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
         }
         return;
     }
-    Ctl& ctl = *reinterpret_cast<Ctl*>(smem + C::OFF_CTL);
+    K& ctl = *reinterpret_cast<K*>(smem + C::OFF_CTL);
     const uint32_t warp = warp_id(), lane = lane_id();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < C::SST; ++s) { mbar_init(&ctl.s_full[s], 1); mbar_init(&ctl.s_empty[s], 2); }
-        for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.k_full[s], 2); mbar_init(&ctl.k_empty[s], 1); }
-        for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.v_full[s], 2); mbar_init(&ctl.v_empty[s], 1); }
-        mbar_init(&ctl.sc_full, 1);
-        mbar_init(&ctl.sc_free, 4);
-        mbar_init(&ctl.pv_done, 1);
-        mbar_init(&ctl.p_full, 4);
-        mbar_init(&ctl.q_ready, 4);
-        mbar_init(&ctl.drain_bar, 1);
+        for (int s = 0; s < C::SST; ++s) { mbar_init(&ctl.s_full[s], 1); mbar_init(&ctl.s_empty[s], C::CONV); }
+        for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.k_full[s], C::CONV); mbar_init(&ctl.k_empty[s], TILES); }
+        for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.v_full[s], C::CONV); mbar_init(&ctl.v_empty[s], TILES); }
+        for (int t = 0; t < TILES; ++t) {
+            mbar_init(&ctl.sc_full[t], 1);
+            mbar_init(&ctl.sc_free[t], 4);
+            mbar_init(&ctl.pv_done[t], 1);
+            mbar_init(&ctl.p_full[t], 4);
+            mbar_init(&ctl.q_ready[t], 4);
+            ctl.again[t] = 0;
+        }
+        mbar_init(&ctl.drain_bar, TILES);
         for (int s = 0; s < kItemSlots; ++s) {
             mbar_init(&ctl.item_full[s], 1);
-            mbar_init(&ctl.item_empty[s], kItemReaders);
+            mbar_init(&ctl.item_empty[s], C::READERS);
         }
         ctl.abort_flag = 0;
-        ctl.again = 0;
         fence_barrier_init();
     }
     if (warp == 1) {
-        tmem_alloc(&ctl.tmem_base, C::TMEM_COLS);
+        tmem_alloc(&ctl.tmem_base, TILES * C::TMEM_COLS);
         tmem_relinquish();
     }
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = ctl.tmem_base;
     const WaitCtl wc{&ctl.abort_flag, a.status, limit};
-    Shares& sh = *reinterpret_cast<Shares*>(smem + C::OFF_CTL + kSharesAt);
+    Shares& sh = *reinterpret_cast<Shares*>(smem + C::OFF_CTL + shares_at);
     grid_dep_wait();   // whatever the stream ran before: lengths, table, cache
-    const int rl = 31 - __clz(kBM / a.G);   // 2^rl tokens of a tile (G is 1, 2, 4 or 8)
+    const int R = kBM / a.G;                           // tokens of a tile (G is 1, 2, 4 or 8)
+    const int rl = 31 - __clz(TILES * R);   // 2^rl tokens of an item
     const bool any = find_range(a, rl, sh);
     grid_dep_launch();   // the join's blocks may take the places that open up (they wait for this grid's end)
 
     // Every role walks the same items and counts pages over all of them (g): ring slots, score
     // buffers and barrier phases follow g across item boundaries.  K page g is the 8-bit ring's
     // 2 g, V page g its 2 g + 1.
-    if (warp < 4) {
-        give_registers<D>();
+    if (warp < C::SOFT0) {
+        give_registers<D, TILES>();
         if (warp == 0) {
             // ---------------- items and 8-bit pages
             Walk walk(a, rl, sh, any);
@@ -220,8 +246,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                         }
                         if (lane == 0) {
                             if (v == 0) {
-                                ctl.ks[(n >> 1) % 16] = ksj;
-                                ctl.vs[(n >> 1) % 16] = vsj;
+                                ctl.scale[(n >> 1) % C::SCALES] = make_float4(ksj, log2f(vsj), 1.f / vsj, vsj);
                             }
                             if (bad) {
                                 mbar_arrive(&ctl.s_full[s]);
@@ -239,9 +264,9 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                 for (int q = n - 1; q >= 0 && q >= n - C::SST; --q)
                     mbar_wait_drain(&ctl.s_full[q % C::SST], (q / C::SST) & 1, limit, a.status);
             }
-        } else if (warp >= 2) {
+        } else if (warp >= C::CONV0) {
             // ---------------- 8-bit pages to f16 tiles
-            const int half = warp - 2;
+            const int share = warp - C::CONV0;
             int g = 0;
             bool ok = true;
             for (int r = 0; ok; ++r) {
@@ -260,8 +285,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                         }
                         // P is 0 past the end, and 0 times a stale NaN is NaN: such value rows become zero.  Keys
                         // there may be anything.
-                        convert<D>(smem + (v == 0 ? C::OFF_K : C::OFF_V) + s * C::KV_BYTES, smem + C::OFF_S + ss * C::PAGE, half, lane,
-                                   v == 0 ? kBN : end - m * kBN);
+                        convert<D, C::CONV>(smem + (v == 0 ? C::OFF_K : C::OFF_V) + s * C::KV_BYTES, smem + C::OFF_S + ss * C::PAGE, share,
+                                            lane, v == 0 ? kBN : end - m * kBN);
                         fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
@@ -272,81 +297,93 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                     }
                 }
             }
-        } else {
-            // ---------------- products: S of a step ahead of the P V of the one before
-            const uint64_t dq0 = smem_desc_sw128(smem_u32(smem), 16, 1024);
+        } else if (warp <= TILES) {
+            // ---------------- products of a tile: S of a step, then P V of the one before.  A warp a tile: it waits
+            // while its products are at work, and its own waits and commits cost as much again.
+            const int t = warp - 1;
+            const uint32_t tile = tmem_base + t * C::TMEM_COLS;
+            const uint64_t dq = smem_desc_sw128(smem_u32(smem + t * C::Q_BYTES), 16, 1024);
             const uint64_t dk0 = smem_desc_sw128(smem_u32(smem + C::OFF_K), 16, 1024);
             const uint64_t dv0 = smem_desc_sw128(smem_u32(smem + C::OFF_V), kBN * 128, 1024);
-            int g = 0, gp = 0, tc = 0;   // steps, pages, items
-            int vp = 0, np = 0;          // pages of finished products, arrivals of P
-            int left = 0;                // pages of the step whose product is due
-            bool start = false, ok = true;
-            auto product = [&]() {       // P V of the step before; its first page starts a new accumulator
-                if (left == 0) return true;
-                bool fresh = start;
+            bool ok = true;
+            int ns = 0, np = 0;   // scores, arrivals of P
+            auto product = [&](int vp, int pages, bool fresh) {   // fresh: a new accumulator
+                for (int i = 0; i < pages; ++i)
+                    if (!mbar_wait_warp(&ctl.v_full[(vp + i) % C::KST], ((vp + i) / C::KST) & 1, wc)) return false;
                 for (bool more = true; more;) {
-                    for (int i = 0; i < left; ++i)
-                        if (!mbar_wait_warp(&ctl.v_full[(vp + i) % C::KST], ((vp + i) / C::KST) & 1, wc)) return false;
-                    if (!mbar_wait_warp(&ctl.p_full, np & 1, wc)) return false;
+                    if (!mbar_wait_warp(&ctl.p_full[t], np & 1, wc)) return false;
                     ++np;
-                    more = C::KPS > 1 && *static_cast<volatile int*>(&ctl.again) != 0;
+                    more = C::KPS > 1 && *static_cast<volatile int*>(&ctl.again[t]) != 0;
                     tc_fence_after();
-                    for (int i = 0; i < left; ++i) {
-                        const int vs = (vp + i) % C::KST;
-                        const uint64_t dv = dv0 + static_cast<uint64_t>((vs * C::KV_BYTES) >> 4);
-                        if (elect_one()) {
+                    if (elect_one()) {
+#pragma unroll
+                        for (int i = 0; i < C::KPS; ++i) {
+                            if (i >= pages) break;
+                            const int vs = (vp + i) % C::KST;
+                            const uint64_t dv = dv0 + static_cast<uint64_t>((vs * C::KV_BYTES) >> 4);
 #pragma unroll
                             for (int k = 0; k < kBN / 16; ++k)
-                                umma_bf16_ta(tmem_base + C::TMEM_O, tmem_base + C::TMEM_P + i * 32 + k * 8, dv + ((k * 2048) >> 4),
-                                             C::IDESC_O, (!fresh || i > 0 || k > 0) ? 1u : 0u);
+                                umma_bf16_ta(tile + C::TMEM_O, tile + C::TMEM_P + i * 32 + k * 8, dv + ((k * 2048) >> 4), C::IDESC_O,
+                                             (!fresh || i > 0 || k > 0) ? 1u : 0u);
                             if (!more) umma_commit(&ctl.v_empty[vs]);
                         }
-                        __syncwarp();
+                        umma_commit(&ctl.pv_done[t]);
                     }
-                    if (elect_one()) umma_commit(&ctl.pv_done);
                     __syncwarp();
                     fresh = false;
                 }
-                vp += left;
-                left = 0;
                 return true;
             };
-            for (int r = 0; ok; ++r, ++tc) {
+            auto score = [&](int gp, int pages) {
+                for (int i = 0; i < pages; ++i)
+                    if (!mbar_wait_warp(&ctl.k_full[(gp + i) % C::KST], ((gp + i) / C::KST) & 1, wc)) return false;
+                if (ns >= 1 && !mbar_wait_warp(&ctl.sc_free[t], (ns - 1) & 1, wc)) return false;
+                ++ns;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int i = 0; i < C::KPS; ++i) {
+                        if (i >= pages) break;
+                        const int s = (gp + i) % C::KST;
+                        const uint64_t dk = dk0 + static_cast<uint64_t>((s * C::KV_BYTES) >> 4);
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint32_t off_q = (k & 3) * 32;
+                            const uint32_t off_k = (k >> 2) * (kBN * 128) + (k & 3) * 32;
+                            if (C::QT && k < 4)
+                                umma_bf16_ta(tile + C::TMEM_S, tile + C::TMEM_Q + k * 8, dk + (off_k >> 4), C::IDESC_S, k > 0);
+                            else
+                                umma_bf16(tile + C::TMEM_S + i * kBN, dq + (off_q >> 4), dk + (off_k >> 4), C::IDESC_S, k > 0);
+                        }
+                        umma_commit(&ctl.k_empty[s]);
+                    }
+                    umma_commit(&ctl.sc_full[t]);
+                }
+                __syncwarp();
+                return true;
+            };
+            int gp = 0, nq = 0;   // pages; items of the tile
+            for (int r = 0; ok; ++r) {
                 Item x;
                 if (!read_item(ctl, r, wc, x)) { ok = false; break; }
-                if (!product()) { ok = false; break; }
                 if (x.head < 0) break;
-                const int qs = tc % C::QST;
-                const uint64_t dq = dq0 + static_cast<uint64_t>((qs * C::Q_BYTES) >> 4);
-                if (!mbar_wait_warp(&ctl.q_ready, tc & 1, wc)) { ok = false; break; }
-                for (int m = x.blk0; ok && m < x.blk1; m += C::KPS, ++g) {
-                    if (g >= 1 && !mbar_wait_warp(&ctl.sc_free, (g - 1) & 1, wc)) { ok = false; break; }
-                    int pages = 0;
-                    for (int i = 0; i < C::KPS && m + i < x.blk1; ++i, ++gp, ++pages) {
-                        const int s = gp % C::KST;
-                        if (!mbar_wait_warp(&ctl.k_full[s], (gp / C::KST) & 1, wc)) { ok = false; break; }
-                        tc_fence_after();
-                        const uint64_t dk = dk0 + static_cast<uint64_t>((s * C::KV_BYTES) >> 4);
-                        if (elect_one()) {
-#pragma unroll
-                            for (int k = 0; k < D / 16; ++k) {
-                                const uint32_t off_q = (k & 3) * 32;
-                                const uint32_t off_k = (k >> 2) * (kBN * 128) + (k & 3) * 32;
-                                if (C::QT && k < 4)
-                                    umma_bf16_ta(tmem_base + C::TMEM_S, tmem_base + C::TMEM_Q + k * 8, dk + (off_k >> 4), C::IDESC_S, k > 0);
-                                else
-                                    umma_bf16(tmem_base + C::TMEM_S + i * kBN, dq + (off_q >> 4), dk + (off_k >> 4), C::IDESC_S, k > 0);
-                            }
-                            umma_commit(&ctl.k_empty[s]);
+                if (t * R >= x.ntok) {   // nothing to do but to let the pages go, once they are there: an arrival of this phase
+                    for (int m = x.blk0; ok && m < x.blk1; ++m, ++gp) {
+                        const int s = gp % C::KST, phase = (gp / C::KST) & 1;
+                        ok = mbar_wait_warp(&ctl.k_full[s], phase, wc) && mbar_wait_warp(&ctl.v_full[s], phase, wc);
+                        if (ok && lane == 0) {
+                            mbar_arrive(&ctl.k_empty[s]);
+                            mbar_arrive(&ctl.v_empty[s]);
                         }
-                        __syncwarp();
                     }
-                    if (!ok) break;
-                    if (elect_one()) umma_commit(&ctl.sc_full);
-                    __syncwarp();
-                    if (!product()) { ok = false; break; }
-                    left = pages;
-                    start = m == x.blk0;
+                    continue;
+                }
+                ok = mbar_wait_warp(&ctl.q_ready[t], nq++ & 1, wc) && score(gp, min(C::KPS, x.blk1 - x.blk0));
+                for (int m = x.blk0; ok && m < x.blk1; m += C::KPS) {
+                    const int pages = min(C::KPS, x.blk1 - m);
+                    if (m + C::KPS < x.blk1) ok = score(gp + pages, min(C::KPS, x.blk1 - m - C::KPS));
+                    ok = ok && product(gp, pages, m == x.blk0);
+                    gp += pages;
                 }
             }
             if (elect_one()) {
@@ -357,20 +394,23 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
         }
     } else {
         // ---------------- softmax, one thread per row
-        take_registers<D>();
+        take_registers<D, TILES>();
         constexpr int NK = C::KPS * kBN;   // keys of a step
-        const int q = warp - 4;
-        const int row = q * 32 + lane;
-        const int tok = row / a.G, hq = row - tok * a.G;
-        const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
+        const int tile = (warp - C::SOFT0) >> 2, q = warp & 3;
+        const int row = q * 32 + lane;                          // of the tile
+        const int tok = tile * R + row / a.G, hq = row % a.G;   // of the item
+        const uint32_t lane_addr = tmem_base + tile * C::TMEM_COLS + (static_cast<uint32_t>(q * 32) << 16);
+        // whether anything of this warp is ever read, of this tile
+        auto warp_has_rows = [&](const Item& x) { return tile * R * a.G + q * 32 < x.ntok * a.G; };
+        auto tile_has_rows = [&](const Item& x) { return tile * R < x.ntok; };
         float row_scale = 0.f, next_scale = 0.f;
         // the r-th item, and its rows as f16: the first 64 dims of 128 into tensor memory, the others into
         // shared memory (the products of the item before, which read the ones there, are done: this warp has
         // seen their scores)
         auto take_item = [&](int r, Item& x) {
             if (!read_item(ctl, r, wc, x)) return false;
-            if (x.head < 0) return true;
-            if (q * 32 < x.ntok * a.G) {
+            if (x.head < 0 || !tile_has_rows(x)) return true;
+            if (warp_has_rows(x)) {
                 // twice 64 dims at a time, rather than 128 held: the second time they come out of L2
                 const size_t at = (static_cast<size_t>(x.tok0) + tok) * a.Hq + static_cast<size_t>(x.head) * a.G + hq;
                 const uint4* const src = reinterpret_cast<const uint4*>(a.Q + at * D);
@@ -401,7 +441,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                 next_scale = scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23);
                 auto half2 = [&](uint32_t w) { return pack_f16x2(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up); };
                 // the second half is at hand
-                uint8_t* const dst = smem + (r % C::QST) * C::Q_BYTES + row * 128;
+                uint8_t* const dst = smem + tile * C::Q_BYTES + row * 128;
 #pragma unroll
                 for (int c = 0; c < 8; ++c)   // 16-byte chunks, swizzled within the 128-byte row
                     *reinterpret_cast<uint4*>(dst + ((c ^ (row & 7)) << 4)) =
@@ -423,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl.q_ready);
+            if (lane == 0) mbar_arrive(&ctl.q_ready[tile]);
             return true;
         };
         int g = 0, gp = 0, np = 0;   // steps, pages, arrivals of P
@@ -432,48 +472,61 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
         for (int r = 1; ok && x.head >= 0; x = nx, ++r) {
             row_scale = next_scale;
             const bool valid = tok < x.ntok;
-            const bool warp_rows = q * 32 < x.ntok * a.G;   // else nothing of this warp is ever read
+            const bool warp_rows = warp_has_rows(x);
+            if (!tile_has_rows(x)) {
+                gp += x.blk1 - x.blk0;
+                if (!take_item(r, nx)) { ok = false; break; }
+                continue;
+            }
             const int pos = x.pos0 + tok;
             float m_use = -CUDART_INF_F, l = 0.f;
-            float v_ref = 0.f;   // what one of O stands for
+            float v_ref = 0.f, v_log = 0.f;   // what one of O stands for
             for (int m = x.blk0; ok && m < x.blk1; m += C::KPS, ++g) {
                 const int pages = min(C::KPS, x.blk1 - m);
                 // last key column of the step that this row sees (< 0: none; none of a page that is not
                 // there).  Rows of no token are never read: they go unmasked.
                 const int lim = valid ? min(min(NK - 1, pos - m * kBN), (x.blk1 - m) * kBN - 1) : NK - 1;
-                if (!mbar_wait_warp(&ctl.sc_full, g & 1, wc)) { ok = false; break; }
-                float ks[C::KPS], vs[C::KPS];
+                if (!mbar_wait_warp(&ctl.sc_full[tile], g & 1, wc)) { ok = false; break; }
+                float4 sc[C::KPS];
 #pragma unroll
-                for (int i = 0; i < C::KPS; ++i) {
-                    ks[i] = i < pages ? ctl.ks[(gp + i) % 16] : 1.f;
-                    vs[i] = i < pages ? ctl.vs[(gp + i) % 16] : vs[0];
-                }
+                for (int i = 0; i < C::KPS; ++i) sc[i] = ctl.scale[(gp + (i < pages ? i : 0)) % C::SCALES];
                 gp += pages;
-                if (v_ref == 0.f) v_ref = vs[0];
-                auto near = [](float v, float ref) { return v <= kScaleRange * ref && v * kScaleRange >= ref; };
+                if (m == x.blk0) {
+                    v_log = sc[0].y;
+                    v_ref = sc[0].w;
+                }
+                auto near = [](float v, float ref) { return fabsf(v - ref) <= kScaleRange; };   // logarithms
+                bool move = !near(sc[0].y, v_log);
+                if constexpr (C::KPS == 2) move |= !near(sc[1].y, v_log);
                 // a step whose pages cannot stand under one scale has its product in two parts
-                const bool parts = C::KPS == 2 && !(near(vs[0], v_ref) && near(vs[C::KPS - 1], v_ref)) && !near(vs[C::KPS - 1], vs[0]);
+                const bool parts = C::KPS == 2 && move && !near(sc[C::KPS - 1].y, sc[0].y);
                 // P is free once the product before has read it
                 auto p_free = [&] {
-                    if (np >= 1 && !mbar_wait_warp(&ctl.pv_done, (np - 1) & 1, wc)) return false;
+                    if (np >= 1 && !mbar_wait_warp(&ctl.pv_done[tile], (np - 1) & 1, wc)) return false;
                     tc_fence_after();
                     return true;
                 };
                 auto p_ready = [&] {
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&ctl.p_full);
+                    if (lane == 0) mbar_arrive(&ctl.p_full[tile]);
                     ++np;
                 };
-                auto move_to = [&](float v) {   // the factor that O takes
-                    const float by = v_ref / v;
-                    v_ref = v;
+                auto move_to = [&](const float4& v) {   // the factor that O takes
+                    const float by = v_ref * v.z;
+                    v_ref = v.w;
+                    v_log = v.y;
                     return by;
                 };
                 if (!warp_rows) {
-                    if (lane == 0) mbar_arrive(&ctl.sc_free);
-                    if (!near(vs[0], v_ref) || (!parts && !near(vs[C::KPS - 1], v_ref))) v_ref = vs[0];
-                    if (parts && !near(vs[C::KPS - 1], v_ref)) v_ref = vs[C::KPS - 1];
+                    if (lane == 0) mbar_arrive(&ctl.sc_free[tile]);
+                    if (parts) {
+#pragma unroll
+                        for (int i = 0; i < C::KPS; ++i)
+                            if (!near(sc[i].y, v_log)) move_to(sc[i]);
+                    } else if (move) {
+                        move_to(sc[0]);
+                    }
                     for (int i = 0; ok && i <= static_cast<int>(parts); ++i) {
                         ok = p_free();
                         if (ok) p_ready();
@@ -492,9 +545,9 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&ctl.sc_free);
+                if (lane == 0) mbar_arrive(&ctl.sc_free[tile]);
                 float cr[C::KPS];
-                if (__any_sync(0xffffffffu, lim < NK - 1)) {
+                if (m * kBN + NK - 1 > x.pos0 + tile * R || pages < C::KPS) {   // some row does not see all of it
 #pragma unroll
                     for (int k = 0; k < NK; ++k) xs[k] = k <= lim ? xs[k] : -CUDART_INF_F;
                 }
@@ -507,7 +560,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
 #pragma unroll
                         for (int j = 0; j < 4; ++j) mx[j] = max3f(mx[j], xs[k + 2 * j], xs[k + 2 * j + 1]);
                     }
-                    cr[i] = row_scale * ks[i];
+                    cr[i] = row_scale * sc[i].x;
                     mb = fmaxf(mb, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * cr[i]);
                 }
                 bool need = valid && mb > m_use + kRescaleThreshold;
@@ -519,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                 // O to another maximum, or under another value scale: once the product before is done
                 auto rescale = [&](bool change, float by) {
                     if (!__any_sync(0xffffffffu, change)) return true;
-                    if (!mbar_wait_warp(&ctl.pv_done, (np - 1) & 1, wc)) return false;
+                    if (!mbar_wait_warp(&ctl.pv_done[tile], (np - 1) & 1, wc)) return false;
                     tc_fence_after();
 #pragma unroll 1
                     for (int cc = 0; cc < D / 32; ++cc) {
@@ -535,10 +588,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                 };
                 // P = 2^(z - m) of page i, times its value scale over O's; the row's sum
                 auto weights = [&](int i, uint32_t (&pk)[32]) {
-                    const float ratio = vs[i] / v_ref;
-                    float lr;
-                    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lr) : "f"(ratio));
-                    const uint64_t scale2 = f32x2(cr[i], cr[i]), off2 = f32x2(off + lr, off + lr);
+                    const float by = off + (sc[i].y - v_log);
+                    const uint64_t scale2 = f32x2(cr[i], cr[i]), off2 = f32x2(by, by);
                     uint64_t acc[4] = {0, 0, 0, 0};
 #pragma unroll
                     for (int k = 0; k < kBN; k += 2) {
@@ -550,16 +601,16 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                     }
                     float s0, s1;
                     f32x2_split(add_f32x2(add_f32x2(acc[0], acc[1]), add_f32x2(acc[2], acc[3])), s0, s1);
-                    l = fmaf(s0 + s1, 1.f / ratio, l);
+                    l = fmaf(s0 + s1, sc[i].z * v_ref, l);
                 };
                 if (parts) {
                     // rare: a page at a time, the other one's weights zero
 #pragma unroll
                     for (int i = 0; i < C::KPS; ++i) {
-                        const bool move = !near(vs[i], v_ref);
-                        if (move) factor *= move_to(vs[i]);
+                        const bool moves = !near(sc[i].y, v_log);
+                        if (moves) factor *= move_to(sc[i]);
                         uint32_t pk[32];
-                        if ((m > x.blk0 || i > 0) && !rescale(need || move, factor)) { ok = false; break; }
+                        if ((m > x.blk0 || i > 0) && !rescale(need || moves, factor)) { ok = false; break; }
                         weights(i, pk);
                         if (!p_free()) { ok = false; break; }
                         tmem_st32(lane_addr + C::TMEM_P + i * 32, pk);
@@ -567,7 +618,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                         for (int k = 0; k < 32; ++k) pk[k] = 0;
                         tmem_st32(lane_addr + C::TMEM_P + (1 - i) * 32, pk);
                         tmem_wait_st();
-                        if (threadIdx.x == 128) ctl.again = i == 0;   // warp 4 has rows whenever there are any
+                        if (q == 0 && lane == 0) ctl.again[tile] = i == 0;   // a tile's first warp has rows whenever it has any
                         p_ready();
                         factor = 1.f;
                         need = false;
@@ -575,10 +626,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                     if (!ok) break;
                     continue;
                 }
-                bool move = false;
-#pragma unroll
-                for (int i = 0; i < C::KPS; ++i) move |= !near(vs[i], v_ref);
-                if (move) factor *= move_to(vs[0]);
+                if (move) factor *= move_to(sc[0]);
                 if (m > x.blk0 && !rescale(need || move, factor)) { ok = false; break; }
                 uint32_t pk[C::KPS][32];
 #pragma unroll
@@ -593,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
             if (!ok || !take_item(r, nx)) { ok = false; break; }
             // The next item's first PV overwrites O only after this warp's next arrival on
             // p_full, which follows the reads below.
-            if (!mbar_wait_warp(&ctl.pv_done, (np - 1) & 1, wc)) { ok = false; break; }
+            if (!mbar_wait_warp(&ctl.pv_done[tile], (np - 1) & 1, wc)) { ok = false; break; }
             tc_fence_after();
             const size_t orow = (static_cast<size_t>(x.tok0) + tok) * a.Hq + static_cast<size_t>(x.head) * a.G + hq;
             if (x.part < 0) {
@@ -625,7 +673,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
             // ---- a split: (max, sum) and the unnormalised O of every row in fp32, laid out
             // [quad of columns][row], so that a warp's 32 rows write 512 bytes at a time
             if (warp_rows) {
-                float4* po = reinterpret_cast<float4*>(a.part_o) + static_cast<size_t>(x.part) * (D / 4) * kBM + row;
+                float4* po = reinterpret_cast<float4*>(a.part_o) + (static_cast<size_t>(x.part) * TILES + tile) * (D / 4) * kBM + row;
 #pragma unroll 1
                 for (int cc = 0; cc < D / 32; ++cc) {
                     uint32_t o[32];
@@ -638,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
                             po[(cc * 8 + e) * kBM] = make_float4(at(4 * e), at(4 * e + 1), at(4 * e + 2), at(4 * e + 3));
                     }
                 }
-                if (valid) a.part_ml[static_cast<size_t>(x.part) * kBM + row] = make_float2(m_use, l);
+                if (valid) a.part_ml[(static_cast<size_t>(x.part) * TILES + tile) * kBM + row] = make_float2(m_use, l);
             }
             tc_fence_before();
         }
@@ -646,32 +694,41 @@ __global__ void __launch_bounds__(kThreads, 2) chunk8_tile_kernel(ChunkArgs a, f
     __syncthreads();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem_base, C::TMEM_COLS);
+        tmem_dealloc(tmem_base, TILES * C::TMEM_COLS);
     }
 }
 
-template <int D>
-cudaError_t launch_d(const ChunkArgs& a, const KernelEnv& env, const char** err) {
-    using C = Cfg<D>;
-    cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<D>), C::SMEM);
+template <int D, int TILES>
+cudaError_t launch_d(ChunkArgs a, const KernelEnv& env, const char** err) {
+    using C = Cfg<D, TILES>;
+    cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<D, TILES>), C::SMEM);
     if (e != cudaSuccess) { *err = "cudaFuncSetAttribute(8-bit tile attention)"; return e; }
-    // Two blocks a multiprocessor: their shared memory and tensor memory both fit twice.
-    e = launch_early(chunk8_tile_kernel<D>, dim3(a.blocks), kThreads, C::SMEM, env.stream, a, a.sm_scale * kLog2e, env.limit);
+    a.blocks = 2 / TILES * device_sm_count();   // their shared memory and tensor memory fit at once
+    e = launch_early(chunk8_tile_kernel<D, TILES>, dim3(a.blocks), C::THREADS, C::SMEM, env.stream, a, a.sm_scale * kLog2e, env.limit);
     if (e != cudaSuccess) { *err = "8-bit tile attention launch"; return e; }
-    e = launch_early(chunk_join_kernel<D>, dim3(a.blocks), kJoinThreads, 0, env.stream, a);
+    e = launch_early(chunk_join_kernel<D, TILES>, dim3(a.blocks), kJoinThreads, 0, env.stream, a);
     if (e != cudaSuccess) *err = "8-bit attention join launch";
     return e;
 }
 
-}  // namespace
-
-cudaError_t chunk8_tile_prepare(int d) {
-    return d == 128 ? ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<128>), Cfg<128>::SMEM)
-                    : ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<64>), Cfg<64>::SMEM);
+template <int D>
+cudaError_t prepare() {
+    const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<D, 1>), Cfg<D, 1>::SMEM);
+    return e == cudaSuccess ? ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<D, 2>), Cfg<D, 2>::SMEM) : e;
 }
 
+template <int D>
+cudaError_t launch_tiles(const ChunkArgs& a, const KernelEnv& env, const char** err) {
+    // two tiles a block where most items fill them
+    return static_cast<long long>(a.T) * a.G > kTwoTiles * a.B ? launch_d<D, 2>(a, env, err) : launch_d<D, 1>(a, env, err);
+}
+
+}  // namespace
+
+cudaError_t chunk8_tile_prepare(int d) { return d == 128 ? prepare<128>() : prepare<64>(); }
+
 cudaError_t launch_chunk8_tile(const ChunkArgs& a, const KernelEnv& env, const char** err) {
-    return a.d == 128 ? launch_d<128>(a, env, err) : launch_d<64>(a, env, err);
+    return a.d == 128 ? launch_tiles<128>(a, env, err) : launch_tiles<64>(a, env, err);
 }
 
 }  // namespace sas
