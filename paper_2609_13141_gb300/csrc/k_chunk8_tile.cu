@@ -4,20 +4,21 @@
 //
 // The tensor core takes 8-bit numbers only beside 8-bit numbers, and rounding queries and
 // weights to 8 bits would show.  So the pages' numbers become f16, exactly, in shared memory:
-//   * warp 0 takes work items, publishes them and loads 8-bit pages by bulk copies (one ring,
-//     K and V pages in turn);
-//   * two or four warps convert, a share of a page's rows each, into rings of f16 tiles in the
-//     tensor core's layout, value rows of no key as zero;
-//   * warp 1 issues S = Q K^T and O += P V (P read from tensor memory);
+//   * warp 0 takes work items, publishes them and loads their Q by TMA;
+//   * two or four warps load pages, a share of a page's rows each and one or two pages ahead in
+//     registers, and convert them into rings of f16 tiles in the tensor core's layout, value rows of no key
+//     as zero;
+//   * a warp a tile issues S = Q K^T and O += P V (P read from tensor memory);
 //   * four warps a tile, a thread per row: Q as f16 under a power of two of the row's own
 //     (k_chunk8.cu), mask, online softmax in the log2 domain, P as f16 pairs into tensor memory,
 //     O rescaled only when the maximum grows by 2^8, or where a page's value scale leaves 2^-6 ..
 //     2^6 times the one that O stands under.
 //
 // TILES: 128-row tiles of a block, which share its converted pages.  The conversion costs shared
-// memory 64 d bytes in and 128 d out a page and matrix, as much time as the products' operands
-// take, so long requests have two tiles a block and one block a multiprocessor; requests of fewer
-// rows one tile a block and two blocks, each with its own pages.
+// memory 128 d bytes a page and matrix, beside the products' operands (which take it for two
+// thirds of the time that the tensor core needs), so at d = 128 long requests have two tiles a
+// block and one block a multiprocessor; requests of fewer rows, and those of d = 64, one tile a
+// block and two blocks, each with its own pages.
 #include <cuda_fp16.h>
 
 #include "chunk_work.cuh"
@@ -42,18 +43,18 @@ struct Cfg {
     static constexpr int CONV0 = 2 * TILES, CONV = 2 * TILES;   // the warps that convert
     static constexpr int SOFT0 = 4 * TILES;                     // the softmax warps, four a tile
     static constexpr int READERS = TILES + CONV + 4 * TILES;   // of an item
-    static constexpr int Q_BYTES = kBM * 128;        // 64 dims of a tile's rows in shared memory
+    static constexpr int Q_BYTES = kBM * D * 2;      // of a tile
+    static constexpr int QST = D == 64 ? 2 : 1;      // Q of the item at work, and the next one's
     static constexpr int KV_BYTES = kBN * D * 2;
     static constexpr int PAGE = kBN * D;
-    static constexpr int KST = D == 64 ? (TILES == 2 ? 6 : 4) : (TILES == 2 ? 3 : 2);     // f16 pages of a ring
-    static constexpr int SST = D == 64 ? (TILES == 2 ? 16 : 8) : (TILES == 2 ? 10 : 4);   // 8-bit pages
-    static constexpr int SCALES = TILES == 2 ? 32 : 16;   // pages' scales: the loads are SST / 2 + KST + 2 KPS pages ahead of the softmax at most
-    static_assert(SST / 2 + KST + 2 * KPS <= SCALES, "scales");
-    static constexpr int OFF_K = TILES * Q_BYTES;
+    static constexpr int KST = D == 64 ? 4 : (TILES == 2 ? 4 : 2);   // f16 pages of a ring
+    static constexpr int AHEAD = TILES == 2 ? 2 : 1;   // pages in registers on their way to conversion
+    static constexpr int SCALES = 16;                // pages' scales: the loads are AHEAD + KST + 2 KPS pages ahead of the softmax at most
+    static_assert(AHEAD + KST + 2 * KPS <= SCALES, "scales");
+    static constexpr int OFF_K = QST * TILES * Q_BYTES;
     static constexpr int OFF_V = OFF_K + KST * KV_BYTES;
-    static constexpr int OFF_S = OFF_V + KST * KV_BYTES;
-    static constexpr int OFF_CTL = OFF_S + SST * PAGE;
-    static constexpr int SMEM = OFF_CTL + 1024 * TILES;      // barriers and items, then Shares
+    static constexpr int OFF_CTL = OFF_V + KST * KV_BYTES;
+    static constexpr int SMEM = OFF_CTL + 1024;      // barriers and items, then Shares
     static_assert(2 / TILES * (SMEM + 1024) <= 233472, "blocks a multiprocessor");
     static constexpr int TMEM_COLS = 256;               // of a tile
     static constexpr int TMEM_O = 0;
@@ -66,20 +67,30 @@ struct Cfg {
 };
 
 // Moves registers between the block's warpgroups (the sum stays within what it was launched
-// with: 128 threads x (64 + 184) <= 256 x 128, 128 x (64 + 64 + 2 x 192) = 512 x 128).
+// with: 128 threads x (80 + 176) <= 256 x 128, and 128 x (56 + 120 + 2 x 168) = 512 x 128).
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int D, int TILES>
 __device__ __forceinline__ void give_registers() {
-    if constexpr (TILES == 2 || D == 64) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if constexpr (TILES == 1) {
+        if constexpr (D == 64) fewer_registers<80>();
+    } else if (warp_id() < 4) {
+        fewer_registers<56>();
+    } else {
+        fewer_registers<120>();
+    }
 }
 template <int D, int TILES>
 __device__ __forceinline__ void take_registers() {
-    if constexpr (TILES == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
-    else if constexpr (D == 64) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    if constexpr (D == 64) more_registers<176>();
+    else if constexpr (TILES == 2) more_registers<168>();
 }
 
 template <class C, int TILES>
 struct Ctl {
-    uint64_t s_full[C::SST], s_empty[C::SST], k_full[C::KST], k_empty[C::KST], v_full[C::KST], v_empty[C::KST];
+    uint64_t q_full[C::QST], q_empty[C::QST], k_full[C::KST], k_empty[C::KST], v_full[C::KST], v_empty[C::KST];
     uint64_t sc_full[TILES], sc_free[TILES], p_full[TILES], pv_done[TILES], q_ready[TILES], drain_bar;
     uint64_t item_full[kItemSlots], item_empty[kItemSlots];
     float4 scale[C::SCALES];   // of page g at g % SCALES: the keys', the values' log2, inverse and itself
@@ -88,7 +99,7 @@ struct Ctl {
     int abort_flag;
     int again[TILES];          // the step's product comes in two parts
 };
-constexpr int kSharesAt = 832;
+constexpr int kSharesAt = 872;
 
 template <class K>
 __device__ __forceinline__ bool read_item(K& ctl, int r, const WaitCtl& wc, Item& x) {
@@ -111,52 +122,56 @@ __device__ __forceinline__ void to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
         : "r"(w));
 }
 
-// The share-th of NC shares of a page's rows from bytes to a 128-byte-swizzled f16 tile [D /
-// 64][64][64]; rows from `live` on become zero.  Eight lanes read 64 bytes of a row and 64 of the
-// next one, at D = 128 the other half of it, which puts both their 16-byte reads and the two
-// 16-byte pieces that each writes into different banks, at offsets that are a lane's own all the
-// way.
+// The share-th of NC shares of a page's rows: from memory, and as a 128-byte-swizzled f16 tile [D /
+// 64][64][64], rows from `live` on as zero.  Eight lanes take 64 bytes of a row and 64 of the next
+// one, at D = 128 the other half of it, which puts the two 16-byte pieces that each of them writes
+// into different banks, at offsets that are a lane's own all the way.
 template <int D, int NC>
-__device__ __forceinline__ void convert(uint8_t* dst, const uint8_t* src, int share, int lane, int live) {
-    constexpr int ROWS = kBN / NC, PASS = D / 64, N = ROWS / 8 * PASS, B = N < 4 ? N : 4;
-    const int sub = lane >> 2 & 1, c = lane & 3, row = share * ROWS + (lane >> 2);
-    const int piece = ((2 * c) ^ (row & 7)) << 4;
-    src += row * D + c * 16;
-    dst += row * 128;
+struct Piece {
+    static constexpr int ROWS = kBN / NC, PASS = D / 64, N = ROWS / 8 * PASS;
+    uint4 w[N];
+    __device__ __forceinline__ static int row(int share, int lane) { return share * ROWS + (lane >> 2); }
+    __device__ __forceinline__ static int half(int lane, int i) { return PASS == 2 ? (lane >> 2 & 1) ^ (i & 1) : 0; }
+    __device__ __forceinline__ void fetch(const uint8_t* page, bool there, int share, int lane) {   // nothing there: zeros
+        page += row(share, lane) * D + (lane & 3) * 16;
 #pragma unroll
-    for (int i0 = 0; i0 < N; i0 += B) {
-        uint4 w[B];
-#pragma unroll
-        for (int i = 0; i < B; ++i) {   // 8 rows further every PASS pieces
-            const int at = (i0 + i) / PASS * 8, half = PASS == 2 ? sub ^ (i & 1) : 0;
-            w[i] = *reinterpret_cast<const uint4*>(src + at * D + half * 64);
+        for (int i = 0; i < N; ++i) {   // 8 rows further every PASS pieces
+            w[i] = make_uint4(0, 0, 0, 0);
+            if (there) w[i] = __ldcg(reinterpret_cast<const uint4*>(page + i / PASS * 8 * D + half(lane, i) * 64));
         }
+    }
+    __device__ __forceinline__ void convert(uint8_t* dst, int share, int lane, int live) {
+        const int r = row(share, lane), at = ((2 * (lane & 3)) ^ (r & 7)) << 4;
+        dst += r * 128;
         if (live < kBN) {
 #pragma unroll
-            for (int i = 0; i < B; ++i)
-                if (row + (i0 + i) / PASS * 8 >= live) w[i] = make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < N; ++i)
+                if (r + i / PASS * 8 >= live) w[i] = make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < B; ++i) {
-            const int at = (i0 + i) / PASS * 8, half = PASS == 2 ? sub ^ (i & 1) : 0;
+        for (int i = 0; i < N; ++i) {
             uint4 a, b;
             to_f16(w[i].x, a.x, a.y);
             to_f16(w[i].y, a.z, a.w);
             to_f16(w[i].z, b.x, b.y);
             to_f16(w[i].w, b.z, b.w);
-            uint8_t* const to = dst + at * 128 + half * (kBN * 128);
-            *reinterpret_cast<uint4*>(to + piece) = a;
-            *reinterpret_cast<uint4*>(to + (piece ^ 16)) = b;
+            uint8_t* const to = dst + i / PASS * 8 * 128 + half(lane, i) * (kBN * 128);
+            *reinterpret_cast<uint4*>(to + at) = a;
+            *reinterpret_cast<uint4*>(to + (at ^ 16)) = b;
         }
     }
+};
+constexpr int kAhead = 6;   // pages that are on their way into L2
+
+__device__ __forceinline__ void prefetch_page(const void* p, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
 }
 
 template <int D, int TILES>
-__global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(ChunkArgs a, float scale_log2, long long limit) {
+__global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(const __grid_constant__ CUtensorMap mapQ, ChunkArgs a, float scale_log2, long long limit) {
     using C = Cfg<D, TILES>;
     using K = Ctl<C, TILES>;
-    constexpr int shares_at = TILES == 1 ? kSharesAt : 1600;
-    static_assert(sizeof(K) <= shares_at && shares_at + sizeof(Shares) <= 1024 * TILES, "control block");
+    static_assert(sizeof(K) <= kSharesAt && kSharesAt + sizeof(Shares) <= 1024, "control block");
     extern __shared__ __align__(1024) uint8_t smem[];
     if ((smem_u32(smem) & 1023u) != 0) {
         grid_dep_wait();
@@ -169,7 +184,7 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
     K& ctl = *reinterpret_cast<K*>(smem + C::OFF_CTL);
     const uint32_t warp = warp_id(), lane = lane_id();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < C::SST; ++s) { mbar_init(&ctl.s_full[s], 1); mbar_init(&ctl.s_empty[s], C::CONV); }
+        for (int s = 0; s < C::QST; ++s) { mbar_init(&ctl.q_full[s], 1); mbar_init(&ctl.q_empty[s], TILES); }
         for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.k_full[s], C::CONV); mbar_init(&ctl.k_empty[s], TILES); }
         for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.v_full[s], C::CONV); mbar_init(&ctl.v_empty[s], TILES); }
         for (int t = 0; t < TILES; ++t) {
@@ -196,7 +211,7 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
     tc_fence_after();
     const uint32_t tmem_base = ctl.tmem_base;
     const WaitCtl wc{&ctl.abort_flag, a.status, limit};
-    Shares& sh = *reinterpret_cast<Shares*>(smem + C::OFF_CTL + shares_at);
+    Shares& sh = *reinterpret_cast<Shares*>(smem + C::OFF_CTL + kSharesAt);
     grid_dep_wait();   // whatever the stream ran before: lengths, table, cache
     const int R = kBM / a.G;                           // tokens of a tile (G is 1, 2, 4 or 8)
     const int rl = 31 - __clz(TILES * R);   // 2^rl tokens of an item
@@ -204,14 +219,14 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
     grid_dep_launch();   // the join's blocks may take the places that open up (they wait for this grid's end)
 
     // Every role walks the same items and counts pages over all of them (g): ring slots, score
-    // buffers and barrier phases follow g across item boundaries.  K page g is the 8-bit ring's
-    // 2 g, V page g its 2 g + 1.
+    // buffers and barrier phases follow g across item boundaries.
     if (warp < C::SOFT0) {
         give_registers<D, TILES>();
         if (warp == 0) {
-            // ---------------- items and 8-bit pages
+            // ---------------- items and their Q
+            if (lane == 0) tma_prefetch_desc(&mapQ);
             Walk walk(a, rl, sh, any);
-            int n = 0;   // pages loaded
+            int n = 0;   // items with Q on its way
             bool ok = true;
             for (int r = 0; ok; ++r) {
                 const Item x = walk.next(a, rl);
@@ -223,49 +238,26 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
                 }
                 __syncwarp();
                 if (x.head < 0) break;
-                int rows = 0;
-                float ks = 1.f, vs = 1.f;
-                for (int m = x.blk0; ok && m < x.blk1; ++m) {
-                    const int j = (m - x.blk0) & 31;
-                    if (j == 0) {
-                        rows = page_row(a, x, m, lane);
-                        const bool real = m + static_cast<int>(lane) < x.blk1 && rows < a.num_pages * a.Hkv;
-                        ks = real ? load(a.k_scale + rows) : 1.f;
-                        vs = real ? load(a.v_scale + rows) : 1.f;
-                    }
-                    const int row = __shfl_sync(0xffffffffu, rows, j);
-                    const float ksj = __shfl_sync(0xffffffffu, ks, j), vsj = __shfl_sync(0xffffffffu, vs, j);
-                    const bool bad = row >= a.num_pages * a.Hkv;   // reads as zero
-                    for (int v = 0; v < 2; ++v, ++n) {
-                        const int s = n % C::SST;
-                        if (!mbar_wait_warp(&ctl.s_empty[s], ((n / C::SST) & 1) ^ 1u, wc)) { ok = false; break; }
-                        uint8_t* const dst = smem + C::OFF_S + s * C::PAGE;
-                        if (bad) {
-                            for (int i = lane; i < C::PAGE / 16; i += 32) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0, 0, 0, 0);
-                            __syncwarp();
-                        }
-                        if (lane == 0) {
-                            if (v == 0) {
-                                ctl.scale[(n >> 1) % C::SCALES] = make_float4(ksj, log2f(vsj), 1.f / vsj, vsj);
-                            }
-                            if (bad) {
-                                mbar_arrive(&ctl.s_full[s]);
-                            } else {
-                                mbar_arrive_expect_tx(&ctl.s_full[s], C::PAGE);
-                                bulk_load(dst, (v == 0 ? a.K8 : a.V8) + static_cast<size_t>(row) * C::PAGE, C::PAGE, &ctl.s_full[s]);
-                            }
-                        }
-                        __syncwarp();
-                    }
+                const int qs = r % C::QST, tiles = TILES == 2 && x.ntok > R ? 2 : 1;
+                if (!mbar_wait_warp(&ctl.q_empty[qs], ((r / C::QST) & 1) ^ 1u, wc)) { ok = false; break; }
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(&ctl.q_full[qs], tiles * C::Q_BYTES);
+                    for (int t = 0; t < tiles; ++t)
+#pragma unroll
+                        for (int h = 0; h < D / 64; ++h)
+                            tma_load_3d(smem + (qs * TILES + t) * C::Q_BYTES + h * (kBM * 128), &mapQ, &ctl.q_full[qs], h * 64,
+                                        x.head * a.G, x.tok0 + t * R);
                 }
+                ++n;
+                __syncwarp();
             }
             walk.record(a, rl, sh);
-            if (!ok && lane == 0) {   // the last SST loads may be in flight
-                for (int q = n - 1; q >= 0 && q >= n - C::SST; --q)
-                    mbar_wait_drain(&ctl.s_full[q % C::SST], (q / C::SST) & 1, limit, a.status);
+            if (!ok && lane == 0) {   // the last loads may be in flight
+                for (int q = n - 1; q >= 0 && q >= n - C::QST; --q)
+                    mbar_wait_drain(&ctl.q_full[q % C::QST], (q / C::QST) & 1, limit, a.status);
             }
         } else if (warp >= C::CONV0) {
-            // ---------------- 8-bit pages to f16 tiles
+            // ---------------- pages to f16 tiles
             const int share = warp - C::CONV0;
             int g = 0;
             bool ok = true;
@@ -273,40 +265,80 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
                 Item x;
                 if (!read_item(ctl, r, wc, x)) { ok = false; break; }
                 if (x.head < 0) break;
-                const int end = x.pos0 + x.ntok;   // keys from here on belong to no row of the tile
-                for (int m = x.blk0; ok && m < x.blk1; ++m, ++g) {
-#pragma unroll
-                    for (int v = 0; v < 2; ++v) {
-                        const int n = 2 * g + v, ss = n % C::SST, s = g % C::KST;
-                        if (!mbar_wait_warp(v == 0 ? &ctl.k_empty[s] : &ctl.v_empty[s], ((g / C::KST) & 1) ^ 1u, wc) ||
-                            !mbar_wait_warp(&ctl.s_full[ss], (n / C::SST) & 1, wc)) {
-                            ok = false;
-                            break;
+                const int end = x.pos0 + x.ntok;   // keys from here on belong to no row of the item
+                const int none = a.num_pages * a.Hkv;
+                int rows = 0;              // of 32 pages, a lane each
+                float4 sc = make_float4(1.f, 0.f, 1.f, 1.f);
+                Piece<D, C::CONV> k[C::AHEAD], v[C::AHEAD];
+                int row = none;
+                // Page i of the item: where it is, its scales, the pages behind it into L2.
+                auto locate = [&](int i) {
+                    const int m = x.blk0 + i, j = i & 31;
+                    if (j == 0) {
+                        rows = page_row(a, x, m, lane);
+                        sc = make_float4(1.f, 0.f, 1.f, 1.f);
+                        if (m + static_cast<int>(lane) < x.blk1 && rows < none) {
+                            if (share == 0) {
+                                const float vs = load(a.v_scale + rows);
+                                sc = make_float4(load(a.k_scale + rows), log2f(vs), 1.f / vs, vs);
+                            }
+                            if (lane < kAhead && share < 2) prefetch_page((share == 0 ? a.K8 : a.V8) + static_cast<size_t>(rows) * C::PAGE, C::PAGE);
                         }
-                        // P is 0 past the end, and 0 times a stale NaN is NaN: such value rows become zero.  Keys
-                        // there may be anything.
-                        convert<D, C::CONV>(smem + (v == 0 ? C::OFF_K : C::OFF_V) + s * C::KV_BYTES, smem + C::OFF_S + ss * C::PAGE, share,
-                                            lane, v == 0 ? kBN : end - m * kBN);
+                    }
+                    row = __shfl_sync(0xffffffffu, rows, j);
+                    if (share < 2) {
+                        const int far = __shfl_sync(0xffffffffu, rows, (j + kAhead) & 31);
+                        if (lane == 0 && j + kAhead < 32 && m + kAhead < x.blk1 && far < none)
+                            prefetch_page((share == 0 ? a.K8 : a.V8) + static_cast<size_t>(far) * C::PAGE, C::PAGE);
+                    }
+                    if (share == 0 && static_cast<int>(lane) == j) ctl.scale[(g + i) % C::SCALES] = sc;
+                };
+                const int np = x.blk1 - x.blk0;
+#pragma unroll
+                for (int d = 0; d < C::AHEAD; ++d) {
+                    if (d >= np) break;
+                    locate(d);
+                    k[d].fetch(a.K8 + static_cast<size_t>(row) * C::PAGE, row < none, share, lane);
+                    v[d].fetch(a.V8 + static_cast<size_t>(row) * C::PAGE, row < none, share, lane);
+                }
+                for (int i0 = 0; ok && i0 < np; i0 += C::AHEAD) {
+#pragma unroll
+                    for (int d = 0; d < C::AHEAD; ++d) {
+                        const int i = i0 + d, s = (g + i) % C::KST;
+                        if (i >= np) break;
+                        const uint32_t phase = (((g + i) / C::KST) & 1) ^ 1u;
+                        const bool more = i + C::AHEAD < np;
+                        if (more) locate(i + C::AHEAD);
+                        if (!mbar_wait_warp(&ctl.k_empty[s], phase, wc)) { ok = false; break; }
+                        k[d].convert(smem + C::OFF_K + s * C::KV_BYTES, share, lane, kBN);   // late keys may be anything
                         fence_proxy_async_smem();
                         __syncwarp();
-                        if (lane == 0) {
-                            mbar_arrive(v == 0 ? &ctl.k_full[s] : &ctl.v_full[s]);
-                            mbar_arrive(&ctl.s_empty[ss]);
-                        }
+                        if (lane == 0) mbar_arrive(&ctl.k_full[s]);
                         __syncwarp();
+                        if (more) k[d].fetch(a.K8 + static_cast<size_t>(row) * C::PAGE, row < none, share, lane);
+                        if (!mbar_wait_warp(&ctl.v_empty[s], phase, wc)) { ok = false; break; }
+                        // P is 0 past the end, and 0 times a stale NaN is NaN: such value rows become zero
+                        v[d].convert(smem + C::OFF_V + s * C::KV_BYTES, share, lane, end - (x.blk0 + i) * kBN);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&ctl.v_full[s]);
+                        __syncwarp();
+                        if (more) v[d].fetch(a.V8 + static_cast<size_t>(row) * C::PAGE, row < none, share, lane);
                     }
                 }
+                g += np;
             }
         } else if (warp <= TILES) {
             // ---------------- products of a tile: S of a step, then P V of the one before.  A warp a tile: it waits
             // while its products are at work, and its own waits and commits cost as much again.
             const int t = warp - 1;
             const uint32_t tile = tmem_base + t * C::TMEM_COLS;
-            const uint64_t dq = smem_desc_sw128(smem_u32(smem + t * C::Q_BYTES), 16, 1024);
+            const uint64_t dq0 = smem_desc_sw128(smem_u32(smem + t * C::Q_BYTES), 16, 1024);
             const uint64_t dk0 = smem_desc_sw128(smem_u32(smem + C::OFF_K), 16, 1024);
             const uint64_t dv0 = smem_desc_sw128(smem_u32(smem + C::OFF_V), kBN * 128, 1024);
             bool ok = true;
             int ns = 0, np = 0;   // scores, arrivals of P
+            uint64_t* q_free = nullptr;
             auto product = [&](int vp, int pages, bool fresh) {   // fresh: a new accumulator
                 for (int i = 0; i < pages; ++i)
                     if (!mbar_wait_warp(&ctl.v_full[(vp + i) % C::KST], ((vp + i) / C::KST) & 1, wc)) return false;
@@ -334,7 +366,8 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
                 }
                 return true;
             };
-            auto score = [&](int gp, int pages) {
+            // (the dims in tensor memory come first)
+            auto score = [&](uint64_t dq, int gp, int pages, bool last) {   // last: Q is free after it
                 for (int i = 0; i < pages; ++i)
                     if (!mbar_wait_warp(&ctl.k_full[(gp + i) % C::KST], ((gp + i) / C::KST) & 1, wc)) return false;
                 if (ns >= 1 && !mbar_wait_warp(&ctl.sc_free[t], (ns - 1) & 1, wc)) return false;
@@ -348,7 +381,7 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
                         const uint64_t dk = dk0 + static_cast<uint64_t>((s * C::KV_BYTES) >> 4);
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k) {
-                            const uint32_t off_q = (k & 3) * 32;
+                            const uint32_t off_q = (k >> 2) * (kBM * 128) + (k & 3) * 32;
                             const uint32_t off_k = (k >> 2) * (kBN * 128) + (k & 3) * 32;
                             if (C::QT && k < 4)
                                 umma_bf16_ta(tile + C::TMEM_S, tile + C::TMEM_Q + k * 8, dk + (off_k >> 4), C::IDESC_S, k > 0);
@@ -358,6 +391,7 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
                         umma_commit(&ctl.k_empty[s]);
                     }
                     umma_commit(&ctl.sc_full[t]);
+                    if (last) umma_commit(q_free);
                 }
                 __syncwarp();
                 return true;
@@ -367,7 +401,12 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
                 Item x;
                 if (!read_item(ctl, r, wc, x)) { ok = false; break; }
                 if (x.head < 0) break;
-                if (t * R >= x.ntok) {   // nothing to do but to let the pages go, once they are there: an arrival of this phase
+                const int qs = r % C::QST;
+                const uint64_t dq = dq0 + static_cast<uint64_t>((qs * TILES * C::Q_BYTES) >> 4);
+                q_free = &ctl.q_empty[qs];
+                if (t * R >= x.ntok) {   // nothing to do but to let all go, once it is there: arrivals of these phases
+                    ok = mbar_wait_warp(&ctl.q_full[qs], (r / C::QST) & 1, wc);
+                    if (ok && lane == 0) mbar_arrive(q_free);
                     for (int m = x.blk0; ok && m < x.blk1; ++m, ++gp) {
                         const int s = gp % C::KST, phase = (gp / C::KST) & 1;
                         ok = mbar_wait_warp(&ctl.k_full[s], phase, wc) && mbar_wait_warp(&ctl.v_full[s], phase, wc);
@@ -378,10 +417,10 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
                     }
                     continue;
                 }
-                ok = mbar_wait_warp(&ctl.q_ready[t], nq++ & 1, wc) && score(gp, min(C::KPS, x.blk1 - x.blk0));
+                ok = mbar_wait_warp(&ctl.q_ready[t], nq++ & 1, wc) && score(dq, gp, min(C::KPS, x.blk1 - x.blk0), x.blk1 - x.blk0 <= C::KPS);
                 for (int m = x.blk0; ok && m < x.blk1; m += C::KPS) {
                     const int pages = min(C::KPS, x.blk1 - m);
-                    if (m + C::KPS < x.blk1) ok = score(gp + pages, min(C::KPS, x.blk1 - m - C::KPS));
+                    if (m + C::KPS < x.blk1) ok = score(dq, gp + pages, min(C::KPS, x.blk1 - m - C::KPS), m + 2 * C::KPS >= x.blk1);
                     ok = ok && product(gp, pages, m == x.blk0);
                     gp += pages;
                 }
@@ -404,23 +443,21 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
         auto warp_has_rows = [&](const Item& x) { return tile * R * a.G + q * 32 < x.ntok * a.G; };
         auto tile_has_rows = [&](const Item& x) { return tile * R < x.ntok; };
         float row_scale = 0.f, next_scale = 0.f;
-        // the r-th item, and its rows as f16: the first 64 dims of 128 into tensor memory, the others into
-        // shared memory (the products of the item before, which read the ones there, are done: this warp has
-        // seen their scores)
+        // the r-th item, and its rows as f16, in place; the first 64 dims of 128 into tensor memory (the products
+        // of the item before, which read the ones there, are done: this warp has seen their scores)
         auto take_item = [&](int r, Item& x) {
             if (!read_item(ctl, r, wc, x)) return false;
             if (x.head < 0 || !tile_has_rows(x)) return true;
+            const int qs = r % C::QST;
+            if (!mbar_wait_warp(&ctl.q_full[qs], (r / C::QST) & 1, wc)) return false;
             if (warp_has_rows(x)) {
-                // twice 64 dims at a time, rather than 128 held: the second time they come out of L2
-                const size_t at = (static_cast<size_t>(x.tok0) + tok) * a.Hq + static_cast<size_t>(x.head) * a.G + hq;
-                const uint4* const src = reinterpret_cast<const uint4*>(a.Q + at * D);
+                // 64 dims at a time, 16-byte chunks swizzled within the 128-byte row
+                uint8_t* const mine = smem + (qs * TILES + tile) * C::Q_BYTES + row * 128;
+                auto chunk = [&](int h, int c) { return reinterpret_cast<uint4*>(mine + h * (kBM * 128) + ((c ^ (row & 7)) << 4)); };
                 uint4 raw[8];
                 auto fetch = [&](int h) {
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        raw[c] = make_uint4(0, 0, 0, 0);
-                        if (tok < x.ntok) raw[c] = load(src + h * 8 + c);
-                    }
+                    for (int c = 0; c < 8; ++c) raw[c] = *chunk(h, c);
                 };
                 float top = 0.f;
                 auto big = [&](uint32_t w) { top = max3f(top, fabsf(__uint_as_float(w << 16)), fabsf(__uint_as_float(w & 0xffff0000u))); };
@@ -441,11 +478,9 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(Chu
                 next_scale = scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23);
                 auto half2 = [&](uint32_t w) { return pack_f16x2(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up); };
                 // the second half is at hand
-                uint8_t* const dst = smem + tile * C::Q_BYTES + row * 128;
 #pragma unroll
-                for (int c = 0; c < 8; ++c)   // 16-byte chunks, swizzled within the 128-byte row
-                    *reinterpret_cast<uint4*>(dst + ((c ^ (row & 7)) << 4)) =
-                        make_uint4(half2(raw[c].x), half2(raw[c].y), half2(raw[c].z), half2(raw[c].w));
+                for (int c = 0; c < 8; ++c)
+                    *chunk(D / 64 - 1, c) = make_uint4(half2(raw[c].x), half2(raw[c].y), half2(raw[c].z), half2(raw[c].w));
                 if constexpr (C::QT) {
                     fetch(0);
                     uint32_t w[32];
@@ -704,31 +739,30 @@ cudaError_t launch_d(ChunkArgs a, const KernelEnv& env, const char** err) {
     cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<D, TILES>), C::SMEM);
     if (e != cudaSuccess) { *err = "cudaFuncSetAttribute(8-bit tile attention)"; return e; }
     a.blocks = 2 / TILES * device_sm_count();   // their shared memory and tensor memory fit at once
-    e = launch_early(chunk8_tile_kernel<D, TILES>, dim3(a.blocks), C::THREADS, C::SMEM, env.stream, a, a.sm_scale * kLog2e, env.limit);
+    CUtensorMap mq;
+    if (make_tmap_bf16_box(&mq, a.Q, D, a.Hq, a.T, 64, a.G, kBM / a.G) != 0) {
+        *err = "tensor map";
+        return cudaErrorInvalidValue;
+    }
+    e = launch_early(chunk8_tile_kernel<D, TILES>, dim3(a.blocks), C::THREADS, C::SMEM, env.stream, mq, a, a.sm_scale * kLog2e, env.limit);
     if (e != cudaSuccess) { *err = "8-bit tile attention launch"; return e; }
     e = launch_early(chunk_join_kernel<D, TILES>, dim3(a.blocks), kJoinThreads, 0, env.stream, a);
     if (e != cudaSuccess) *err = "8-bit attention join launch";
     return e;
 }
 
-template <int D>
-cudaError_t prepare() {
-    const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<D, 1>), Cfg<D, 1>::SMEM);
-    return e == cudaSuccess ? ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<D, 2>), Cfg<D, 2>::SMEM) : e;
-}
-
-template <int D>
-cudaError_t launch_tiles(const ChunkArgs& a, const KernelEnv& env, const char** err) {
-    // two tiles a block where most items fill them
-    return static_cast<long long>(a.T) * a.G > kTwoTiles * a.B ? launch_d<D, 2>(a, env, err) : launch_d<D, 1>(a, env, err);
-}
-
 }  // namespace
 
-cudaError_t chunk8_tile_prepare(int d) { return d == 128 ? prepare<128>() : prepare<64>(); }
+cudaError_t chunk8_tile_prepare(int d) {
+    if (d == 64) return ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<64, 1>), Cfg<64, 1>::SMEM);
+    const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<128, 1>), Cfg<128, 1>::SMEM);
+    return e == cudaSuccess ? ensure_smem_attr(reinterpret_cast<const void*>(chunk8_tile_kernel<128, 2>), Cfg<128, 2>::SMEM) : e;
+}
 
 cudaError_t launch_chunk8_tile(const ChunkArgs& a, const KernelEnv& env, const char** err) {
-    return a.d == 128 ? launch_tiles<128>(a, env, err) : launch_tiles<64>(a, env, err);
+    if (a.d == 64) return launch_d<64, 1>(a, env, err);
+    // two tiles a block where most items fill them
+    return static_cast<long long>(a.T) * a.G > kTwoTiles * a.B ? launch_d<128, 2>(a, env, err) : launch_d<128, 1>(a, env, err);
 }
 
 }  // namespace sas
