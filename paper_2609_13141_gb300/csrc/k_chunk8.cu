@@ -4,13 +4,15 @@
 //   O_i = sum_j softmax_j(scale s_K(j) q_i.k_j) s_V(j) v_j,  LSE_i = log sum_j exp(scale s_K(j) q_i.k_j),
 // j over the tokens of the request up to i, s_K(j) and s_V(j) the scales of j's page.
 //
-// Work is cut as chunk_work.cuh says.  A tile has few rows here (8, 16 or 32: R tokens times
-// the G heads of a KV group), and each of the block's four pairs of warps takes whole pages of
-// the item, each warp half of the keys, with a running maximum, sum and output of its own, which
-// the block joins at the item's end.  Another warp loads the pages by TMA into rings of shared
-// memory.  A ring has a multiple of four places, so that a place is always the same pair's: a
-// pair that waited for a place of another's could find it two loads behind, which a barrier's
-// parity does not tell from loaded (loads end out of order by microseconds when HBM is busy).
+// Work is cut as chunk_work.cuh says.  A tile has few rows here (8 or 16: R tokens times the G
+// heads of a KV group), and each of four teams of warps takes whole pages of the item, each warp
+// a share of the keys, with a running maximum, sum and output of its own, which the block joins
+// at the item's end.  A warp alone converts a number in 2.5 times the cycles that the unit needs,
+// so there are as many as their registers allow: teams of four at 8 rows, of two at 16.  Another
+// warp loads the pages by TMA into rings of shared memory.  A ring has a multiple of four places,
+// so that a place is always the same team's: one that waited for a place of another's could find
+// it two loads behind, which a barrier's parity does not tell from loaded (loads end out of order
+// by microseconds when HBM is busy).
 //
 // Bound: HBM, 2 d bytes a token and KV head.  What stands between a byte in shared memory and
 // the tensor core is its conversion, exact, to f16 (two numbers an instruction, 64 a cycle of
@@ -40,39 +42,45 @@
 namespace sas {
 namespace {
 
-constexpr int kWarps = 8, kPairs = kWarps / 2;  // that compute; one more loads
-constexpr int kThreads = (kWarps + 4) * 32;    // a warpgroup beside them, of which one warp is at work: registers move by warpgroups
+constexpr int kTeams = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescaleThreshold = 8.0f;       // log2 units
 constexpr float kScaleRange = 64.f;
 constexpr int kItemSlots = 4;
 constexpr int kStatusLayout = 3;
-static_assert(kThreads >= kRangeThreads, "find_range");
 
 // NT: 8-row steps of a tile.
 template <int D, int NT>
 struct Cfg {
+    static constexpr int TEAM = 2;                          // warps of a team
+    static constexpr int WARPS = kTeams * TEAM;            // that compute
+    static constexpr int THREADS = (WARPS + 4) * 32;       // a warpgroup beside them, of which one warp is at work: registers move by warpgroups
+    static_assert(THREADS >= kRangeThreads, "find_range");
     static constexpr int ROWS = 8 * NT;
     static constexpr int PAGE = kBN * D;
     static constexpr int ST = D == 128 ? 12 : 24;          // pages of the rings
-    static_assert(ST % kPairs == 0, "a place of the rings is one pair's");
+    static_assert(ST % kTeams == 0, "a place of the rings is one team's");
     static constexpr int OFF_V = ST * PAGE;
-    static constexpr int OFF_SUM = 2 * ST * PAGE;          // the warps' outputs of 4 rows, joined
+    static constexpr int OFF_SUM = 2 * ST * PAGE;          // the warps' outputs of RR rows, joined
+    static constexpr int RR = 8 / TEAM;
     static constexpr int SUM_LD = D + 4;
-    static constexpr int SUM_BYTES = kWarps * 4 * SUM_LD * 4;
+    static constexpr int SUM_BYTES = WARPS * RR * SUM_LD * 4;
     static constexpr int OFF_Q = OFF_SUM + SUM_BYTES;
     static constexpr int Q_LD = 2 * D + 8;                 // bytes: the lanes' 8-byte reads fall into different banks
     static constexpr int OFF_ML = OFF_Q + ROWS * Q_LD;     // [warp][row] (max, sum)
-    static constexpr int OFF_CTL = OFF_ML + kWarps * ROWS * 8;
+    static constexpr int OFF_CTL = OFF_ML + WARPS * ROWS * 8;
     static constexpr int SMEM = OFF_CTL + 2048;
     static_assert(SMEM <= 232448 && OFF_SUM % 16 == 0 && OFF_Q % 16 == 0 && OFF_CTL % 16 == 0, "shared memory");
+    // Registers of the loading and of the computing warpgroups; the sum stays within what the block is launched
+    // with: 128 x 64 + 512 x 104 = 640 x 96, 128 x 88 + 256 x 208 = 384 x 168.
+    static constexpr int FEWER = 88, MORE = 208;
 };
 
 struct Ctl {
     uint64_t k_full[24], k_empty[24], v_full[24], v_empty[24];
     uint64_t item_full[kItemSlots], item_empty[kItemSlots];
     float ks[24], vs[24];       // the pages' scales
-    float row_scale[32];        // of the item's rows: log2(e) scale over the row's power of two
+    float row_scale[16];        // of the item's rows: log2(e) scale over the row's power of two
     Item item[kItemSlots];
     int abort_flag;
 };
@@ -104,17 +112,17 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
 }
-// Waits for the computing warps; true if any of them says so.
+// Waits for the computing threads; true if any of them says so.
+template <int THREADS>
 __device__ __forceinline__ bool compute_sync_or(bool x) {
     uint32_t r;
     asm volatile(
         "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
         : "=r"(r)
-        : "r"(static_cast<uint32_t>(x)), "n"(kWarps * 32)
+        : "r"(static_cast<uint32_t>(x)), "n"(THREADS)
         : "memory");
     return r != 0;
 }
-__device__ __forceinline__ void compute_sync() { named_bar_sync(1, kWarps * 32); }
 
 // The key, of eight, in place i of an operand.  Even and odd places differ in the bit that moves
 // a 64-byte half (D = 128) or a row's half of 128 bytes (D = 64) in a read of two keys by four lanes
@@ -127,11 +135,13 @@ __device__ __forceinline__ int place(int i) {
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
 chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, ChunkArgs a, float scale_log2,
               int rl, long long limit) {
     using C = Cfg<D, NT>;
     constexpr int MT = D / 16;             // 16-dim steps of O^T
+    constexpr int kWarps = C::WARPS;
+    auto compute_sync = [] { named_bar_sync(1, kWarps * 32); };
     extern __shared__ __align__(1024) uint8_t smem[];
     if ((smem_u32(smem) & 1023u) != 0) {
         grid_dep_wait();
@@ -147,9 +157,9 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::ST; ++s) {
             mbar_init(&ctl.k_full[s], 1);
-            mbar_init(&ctl.k_empty[s], 2);
+            mbar_init(&ctl.k_empty[s], C::TEAM);
             mbar_init(&ctl.v_full[s], 1);
-            mbar_init(&ctl.v_empty[s], 2);
+            mbar_init(&ctl.v_empty[s], C::TEAM);
         }
         for (int s = 0; s < kItemSlots; ++s) {
             mbar_init(&ctl.item_full[s], 1);
@@ -165,11 +175,9 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     grid_dep_launch();   // the join's blocks may take the places that open up (they wait for this grid's end)
 
     // Every warp walks the same items and counts pages over all of them (g): ring slots and
-    // barrier phases follow g across item boundaries, and page g is pair g % kPairs's.
+    // barrier phases follow g across item boundaries, and page g is team g % kTeams's.
     if (warp >= kWarps) {
-        // the sum stays within what the block was launched with: 128 x 56 + 256 x 224 = 128 x 88 + 256 x 208 = 384 x 168
-        if constexpr (NT == 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::FEWER));
         if (warp != kWarps) return;
         if (lane == 0) {
             tma_prefetch_desc(&mapK);
@@ -230,8 +238,7 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     }
 
     // ---------------- the computing warps
-    if constexpr (NT == 4) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::MORE));
     const int gq = lane >> 2, t = lane & 3;   // the lane's group of four and its place there
     const int gl = 31 - __clz(a.G);
     const int key_a = place<D>(gq);                                  // S^T: the lane's key, of eight
@@ -254,7 +261,7 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             }
         }
         // the warps leave together: none waits at a barrier that another does not reach
-        if (compute_sync_or(!ok) || x.head < 0) break;
+        if (compute_sync_or<kWarps * 32>(!ok) || x.head < 0) break;
         const int nrow = x.ntok << gl, nt = (nrow + 7) >> 3;
 
         // ---- Q as f16 in shared memory, a row by D / 8 lanes
@@ -300,7 +307,7 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         }
         float v_ref = 0.f;   // what one of o stands for; 0: nothing yet
         const int np = x.blk1 - x.blk0;
-        for (int i = (static_cast<int>(warp >> 1) - g0) & (kPairs - 1); ok && i < np; i += kPairs) {
+        for (int i = (static_cast<int>(warp / C::TEAM) - g0) & (kTeams - 1); ok && i < np; i += kTeams) {
             const int g = g0 + i, s = g % C::ST, m = x.blk0 + i;
             const uint32_t phase = (g / C::ST) & 1;
             const uint8_t* const K = smem + s * C::PAGE;
@@ -309,8 +316,8 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             const float ks = ctl.ks[s], vs = ctl.vs[s];
             const int first = m * kBN;
             const bool late = first + kBN - 1 > x.pos0;   // some row does not see all of the page
-            constexpr int KT = 2;   // 16-key steps of a warp's half
-            const int half = warp & 1;
+            constexpr int KT = 4 / C::TEAM;   // 16-key steps of a warp's share
+            const int share = warp % C::TEAM;
             if (v_ref == 0.f) v_ref = vs;
             if (!(vs <= kScaleRange * v_ref && vs * kScaleRange >= v_ref)) {
                 const float f = v_ref / vs;
@@ -336,7 +343,7 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 for (int k = 0; k < KT; ++k) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int key = (half * KT + k) * 16 + h * 8 + key_a;
+                        const int key = (share * KT + k) * 16 + h * 8 + key_a;
                         const int chunk = D == 128 ? (4 * j + t) ^ (key_a & 7) : t ^ ((key_a >> 1) & 3);
                         w[k][h] = *reinterpret_cast<const uint4*>(K + key * D + chunk * 16);
                     }
@@ -375,7 +382,7 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                         const int lim = x.pos0 + (row >> gl) - first;   // its last key of the page
 #pragma unroll
                         for (int k = 0; k < KT; ++k) {
-                            const int key = (half * KT + k) * 16 + key_a;
+                            const int key = (share * KT + k) * 16 + key_a;
                             if (key > lim) c[k][n][e] = -CUDART_INF_F;
                             if (key + 8 > lim) c[k][n][2 + e] = -CUDART_INF_F;
                         }
@@ -434,7 +441,7 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             const int end = x.pos0 + x.ntok - first;   // keys from here on belong to no row: their P is 0, but 0 times NaN is not
 #pragma unroll
             for (int k = 0; k < KT; ++k) {
-                const int key = (half * KT + k) * 16;
+                const int key = (share * KT + k) * 16;
                 constexpr int W = D / 32;   // words of a lane's dims
                 uint32_t v[4][W];
 #pragma unroll
@@ -496,7 +503,7 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         }
         compute_sync();
         constexpr int QUADS = D / 4;
-        const int jr = threadIdx.x / QUADS, jq = threadIdx.x % QUADS;   // the row, of four, and the columns this thread joins
+        const int jr = threadIdx.x / QUADS, jq = threadIdx.x % QUADS;   // the row, of RR, and the columns this thread joins
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float f[2];
@@ -511,11 +518,11 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 f[e] = (top == -CUDART_INF_F ? 1.f : m_use[n][e] == -CUDART_INF_F ? l[n][e] : fast_exp2(m_use[n][e] - top)) * v_ref;
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (n * 8 + h * 4 >= nrow) continue;
+            for (int h = 0; h < 8 / C::RR; ++h) {
+                if (n * 8 + h * C::RR >= nrow) continue;
                 if (n + h > 0) compute_sync();   // the rows before have been read
-                if (t >> 1 == h) {
-                    float* const dst = sums + (warp * 4 + 2 * (t & 1)) * C::SUM_LD + gq * (D / 8);
+                if (t / (C::RR / 2) == h) {
+                    float* const dst = sums + (warp * C::RR + 2 * (t % (C::RR / 2))) * C::SUM_LD + gq * (D / 8);
 #pragma unroll
                     for (int y = 0; y < MT; y += 2) {
                         *reinterpret_cast<float4*>(dst + 2 * y) =
@@ -525,8 +532,8 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                     }
                 }
                 compute_sync();
-                const int row = n * 8 + h * 4 + jr;
-                if (jr >= 4 || row >= nrow || !ok) continue;
+                const int row = n * 8 + h * C::RR + jr;
+                if (jr >= C::RR || row >= nrow || !ok) continue;
                 float top = -CUDART_INF_F, sum = 0.f;
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[w * C::ROWS + row].x);
@@ -536,7 +543,7 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                     const float2 z = ml[w * C::ROWS + row];
                     if (z.x == -CUDART_INF_F && z.y == 0.f) continue;   // no key: whatever its output holds
                     sum += z.x == -CUDART_INF_F ? z.y : z.y * fast_exp2(z.x - top);
-                    const float4 q = *reinterpret_cast<const float4*>(sums + (w * 4 + jr) * C::SUM_LD + jq * 4);
+                    const float4 q = *reinterpret_cast<const float4*>(sums + (w * C::RR + jr) * C::SUM_LD + jq * 4);
                     y.x += q.x;
                     y.y += q.y;
                     y.z += q.z;
@@ -568,7 +575,7 @@ cudaError_t launch_d(const ChunkArgs& a, const KernelEnv& env, const char** err)
         return cudaErrorInvalidValue;
     }
     const int rl = 31 - __builtin_clz(C::ROWS / a.G);
-    e = launch_early(chunk8_kernel<D, NT>, dim3(a.blocks), kThreads, C::SMEM, env.stream, mk, mv, a, a.sm_scale * kLog2e, rl, env.limit);
+    e = launch_early(chunk8_kernel<D, NT>, dim3(a.blocks), C::THREADS, C::SMEM, env.stream, mk, mv, a, a.sm_scale * kLog2e, rl, env.limit);
     if (e != cudaSuccess) { *err = "8-bit attention launch"; return e; }
     e = launch_early(chunk_join_kernel<D>, dim3(a.blocks), kJoinThreads, 0, env.stream, a);
     if (e != cudaSuccess) *err = "8-bit attention join launch";
@@ -580,15 +587,13 @@ cudaError_t launch_rows(const ChunkArgs& a, const KernelEnv& env, const char** e
     // tiles as high as the requests' rows are on average
     const long long rows = static_cast<long long>(a.T) * a.G;
     if (rows <= 8LL * a.B) return launch_d<D, 1>(a, env, err);
-    if (rows <= 16LL * a.B) return launch_d<D, 2>(a, env, err);
-    return launch_d<D, 4>(a, env, err);
+    return launch_d<D, 2>(a, env, err);
 }
 
 template <int D>
 cudaError_t prepare() {
     cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(chunk8_kernel<D, 1>), Cfg<D, 1>::SMEM);
     if (e == cudaSuccess) e = ensure_smem_attr(reinterpret_cast<const void*>(chunk8_kernel<D, 2>), Cfg<D, 2>::SMEM);
-    if (e == cudaSuccess) e = ensure_smem_attr(reinterpret_cast<const void*>(chunk8_kernel<D, 4>), Cfg<D, 4>::SMEM);
     return e;
 }
 
@@ -600,9 +605,10 @@ cudaError_t chunk8_prepare(int d) {
 }
 
 cudaError_t launch_chunk8(ChunkArgs a, const KernelEnv& env, const char** err) {
-    // Requests of more than 32 rows on average: tiles of 128 rows, whose products cost the same however many of
-    // the rows there are.
-    if (static_cast<long long>(a.T) * a.G > 32LL * a.B) return launch_chunk8_tile(a, env, err);
+    // Requests of more than 16 rows on average: tiles of 128 rows, whose products cost the same however many of
+    // the rows there are (12 requests over 8000 to 20000, 8 heads of 128: 96 us at 20 rows, 98 at 16; here 76 at 16,
+    // and 172 at 20 with tiles of 32 rows, whose outputs take all registers).
+    if (static_cast<long long>(a.T) * a.G > 16LL * a.B) return launch_chunk8_tile(a, env, err);
     a.blocks = device_sm_count();   // one a multiprocessor
     if (a.d == 128) return launch_rows<128>(a, env, err);
     if (a.d == 64) return launch_rows<64>(a, env, err);
