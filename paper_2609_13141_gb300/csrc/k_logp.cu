@@ -29,7 +29,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBlocks = 4;            // a multiprocessor, as many as their registers allow
-constexpr int kMaxParts = 32;         // of a row
+constexpr int kMaxParts = 32;         // of a row: a lane each at the join
+constexpr int kWaves = 4;             // of blocks, so that their ends do not leave places empty for long
 constexpr int kMinPart = 2048;        // columns
 constexpr int kSmallRow = 4096;       // columns of rows that a warp takes
 constexpr int kStatusBadInput = 1;    // == SAS_ERR_INVALID_ARG
@@ -62,6 +63,19 @@ struct Vec<bf16> {
     __device__ __forceinline__ static uint4 pack(const float* f) {
         return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
     }
+    // The largest number, NaN passed over (-infinity if there is no other).
+    __device__ __forceinline__ static uint32_t max2(uint32_t a, uint32_t b) {
+        uint32_t d;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+        return d;
+    }
+    template <int U>
+    __device__ __forceinline__ static float top(const uint4 (&u)[U]) {
+        uint32_t m = 0xff80ff80u;
+#pragma unroll
+        for (int i = 0; i < U; ++i) m = max2(max2(m, u[i].x), max2(max2(u[i].y, u[i].z), u[i].w));
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    }
     __device__ __forceinline__ static float one(const bf16* p) { return __bfloat162float(load(p)); }
     __device__ __forceinline__ static void put(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
 };
@@ -76,6 +90,16 @@ struct Vec<float> {
     }
     __device__ __forceinline__ static uint4 pack(const float* f) {
         return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+    template <int U>
+    __device__ __forceinline__ static float top(const uint4 (&u)[U]) {
+        float m = -CUDART_INF_F;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            m = max3f(m, __uint_as_float(u[i].x), __uint_as_float(u[i].y));
+            m = max3f(m, __uint_as_float(u[i].z), __uint_as_float(u[i].w));
+        }
+        return m;
     }
     __device__ __forceinline__ static float one(const float* p) { return load(p); }
     __device__ __forceinline__ static void put(float* p, float v) { *p = v; }
@@ -96,9 +120,10 @@ struct Span {
     __device__ __forceinline__ bool whole(int j) const { return column(j) >= v0 && column(j) + Vec<E>::N <= v1; }
 };
 
-// Sums over columns relative to the maximum m, in the log2 domain: y = (z - m) log2(e).
+// Sums over columns relative to the maximum m, in the log2 domain: y = (z - m) log2(e).  (One FMA, z
+// log2(e) - m log2(e), would not be 0 at the maximum.)
 struct Sums {
-    float m, l, s;   // s = sum 2^y y
+    float m, l, s;   // sums of 2^y and of 2^y y
     __device__ __forceinline__ Sums() : m(kNone), l(0.f), s(0.f) {}
     __device__ __forceinline__ Sums(float m_, float l_, float s_) : m(m_), l(l_), s(s_) {}
     // To another maximum.  No column so far (or none but NaN): nothing to move.
@@ -155,7 +180,7 @@ __device__ __forceinline__ int key_index(unsigned long long k) { return static_c
 
 constexpr int kMaxTop = 32;
 constexpr int kCand = 512;     // candidates kept: kMaxParts * kMaxTop at the join are taken in pieces
-constexpr int kCut = 128;      // cut down when there are this many at the end of a round
+constexpr int kCut = 128;      // cut down at the end of a round that brings this many
 
 // A team (a block, or one of its warps) and the candidates of its row.
 template <int TEAM>
@@ -165,13 +190,21 @@ struct Team {
         if constexpr (TEAM == 32) __syncwarp();
         else __syncthreads();
     }
+    __device__ __forceinline__ static bool sync_or(bool x) {
+        if constexpr (TEAM == 32) {
+            const bool any = __any_sync(0xffffffffu, x);
+            __syncwarp();
+            return any;
+        } else {
+            return __syncthreads_or(x) != 0;
+        }
+    }
 };
 struct Cand {
     unsigned long long key[kCand];
     unsigned long long top[kMaxTop];
-    float first[kThreads];   // the threads' maxima of their first columns
+    float first[32];         // maxima of 32 groups of threads over their first columns
     int n;                   // asked for; at most kCand are kept
-    float bar_value;
 };
 
 // The best k of the n candidates, best first, become the candidates.  All threads of the team.
@@ -243,85 +276,114 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
     if (TOP && rank == 0) c.n = 0;
     for (int j0 = 0; j0 < sp.count; j0 += ROUND) {
         uint4 raw[U];
-        bool in[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = j0 + u * TEAM + rank;
-            in[u] = j < sp.count;
-            if (in[u] && sp.whole(j)) raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + sp.column(j)));
-        }
-        float f[U * N];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = j0 + u * TEAM + rank, v = sp.column(j);
-            if (in[u] && sp.whole(j)) {
-                V::unpack(raw[u], f + u * N);
-            } else {
+            if (j < sp.count && sp.whole(j)) {
+                raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + v));
+            } else {   // columns of the row alone, -infinity for the others
+                float f[N];
 #pragma unroll
-                for (int e = 0; e < N; ++e) f[u * N + e] = in[u] && v + e >= sp.v0 && v + e < sp.v1 ? V::one(z + v + e) : -CUDART_INF_F;
+                for (int e = 0; e < N; ++e) f[e] = j < sp.count && v + e >= sp.v0 && v + e < sp.v1 ? V::one(z + v + e) : -CUDART_INF_F;
+                raw[u] = V::pack(f);
             }
         }
-        float top = -CUDART_INF_F;   // passes over NaN
-#pragma unroll
-        for (int i = 0; i < U * N; ++i) top = fmaxf(top, f[i]);
+        const float top = V::top(raw);
         if (top > t.m) t.move(top);
         const float m = t.m == -CUDART_INF_F ? 0.f : t.m;
-        float l[2] = {0.f, 0.f}, s[2] = {0.f, 0.f};
+        float l, s;
+        {
+            const uint64_t scale2 = f32x2(kLog2e, kLog2e), off2 = f32x2(-m, -m);
+            uint64_t l2[2] = {0, 0}, s2[2] = {0, 0};
 #pragma unroll
-        for (int i = 0; i < U * N; ++i) {
-            const float y = max_nan((f[i] - m) * kLog2e, kLowest);
-            const float e = fast_exp2(y);
-            l[i & 1] += e;
-            s[i & 1] = fmaf(e, y, s[i & 1]);
+            for (int u = 0; u < U; ++u) {
+                float f[N];
+                V::unpack(raw[u], f);
+#pragma unroll
+                for (int e = 0; e < N; e += 2) {
+                    const uint64_t y = mul_f32x2(add_f32x2(f32x2(f[e], f[e + 1]), off2), scale2);
+                    float y0, y1;
+                    f32x2_split(y, y0, y1);
+                    const uint64_t p = f32x2(fast_exp2(y0), fast_exp2(y1));
+                    l2[e >> 1 & 1] = add_f32x2(l2[e >> 1 & 1], p);
+                    s2[e >> 1 & 1] = fma_f32x2(p, y, s2[e >> 1 & 1]);
+                }
+            }
+            float a0, a1;
+            f32x2_split(add_f32x2(l2[0], l2[1]), a0, a1);
+            l = a0 + a1;
+            f32x2_split(add_f32x2(s2[0], s2[1]), a0, a1);
+            s = a0 + a1;
         }
-        t.l += l[0] + l[1];
-        t.s += s[0] + s[1];
+        if (s != s) {   // columns of -infinity (0 times y) or none at all, unless it is NaN's
+            l = s = 0.f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float f[N];
+                V::unpack(raw[u], f);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float y = max_nan((f[e] - m) * kLog2e, kLowest);
+                    const float p = fast_exp2(y);
+                    l += p;
+                    s = fmaf(p, y, s);
+                }
+            }
+        }
+        t.l += l;
+        t.s += s;
         if constexpr (TOP) {
             if (j0 == 0) {
-                c.first[rank] = top;
-                Team<TEAM>::sync();
+                // the k-th largest of 32 disjoint groups' maxima: k columns are no smaller
+                float v = top;
+                if constexpr (TEAM == kThreads) {
+#pragma unroll
+                    for (int o = 1; o < 8; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+                    if (lane_id() % 8 == 0) c.first[rank / 8] = v;
+                    __syncthreads();
+                    v = c.first[lane_id()];
+                }
                 int above = 0;
-                for (int i = 0; i < TEAM; ++i) above += c.first[i] > top || (c.first[i] == top && i < rank);
-                if (above == a.k - 1) c.bar_value = top;
-                Team<TEAM>::sync();
-                bar_value = c.bar_value;   // a.k <= TEAM: some thread has that place (NaN: fmaxf has left none)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const float o = __shfl_sync(0xffffffffu, v, i);
+                    above += o > v || (o == v && i < static_cast<int>(lane_id()));
+                }
+                bar_value = __shfl_sync(0xffffffffu, v, __ffs(__ballot_sync(0xffffffffu, above == a.k - 1)) - 1);
+                if constexpr (TEAM == 32) __syncwarp();   // c.n
             }
             unsigned todo = 0;   // columns to offer
             if (top >= bar_value) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const int v = sp.column(j0 + u * TEAM + rank);
+                    const int j = j0 + u * TEAM + rank, v = sp.column(j);
+                    float f[N];
+                    V::unpack(raw[u], f);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const int i = u * N + e;
-                        if (in[u] && f[i] >= bar_value && v + e >= sp.v0 && v + e < sp.v1 && key_of(f[i], v + e) > bar)
-                            todo |= 1u << i;
-                    }
+                    for (int e = 0; e < N; ++e)
+                        if (f[e] >= bar_value && j < sp.count && v + e >= sp.v0 && v + e < sp.v1) todo |= 1u << (u * N + e);
                 }
             }
             for (;;) {
+                bool many = false;
                 while (todo != 0) {
                     const int i = __ffs(todo) - 1;
                     const int v = sp.column(j0 + i / N * TEAM + rank) + i % N;
                     const unsigned long long key = key_of(V::one(z + v), v);
                     if (key > bar) {
                         const int at = atomicAdd(&c.n, 1);
+                        many |= at >= kCut - 1;
                         if (at >= kCand) break;   // full: offered again once they are cut down
                         c.key[at] = key;
                     }
                     todo &= todo - 1;
                 }
-                Team<TEAM>::sync();
-                const int asked = c.n;
-                held = min(asked, kCand);
-                Team<TEAM>::sync();
-                if (held < kCut) break;
-                held = cut<TEAM>(c, held, a.k);
+                if (!Team<TEAM>::sync_or(many)) break;
+                held = cut<TEAM>(c, min(c.n, kCand), a.k);
                 if (held == a.k) {
                     bar = c.key[a.k - 1];
                     bar_value = fmaxf(bar_value, key_value(bar));
                 }
-                if (asked <= kCand) break;
             }
         }
     }
@@ -335,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
     }
     if constexpr (TOP) {
         Team<TEAM>::sync();
-        if (sp.count > 0) held = cut<TEAM>(c, held, a.k);
+        held = cut<TEAM>(c, min(c.n, kCand), a.k);
     }
     if (TEAM == kThreads && a.parts > 1) {
         // the part's results; the row's last block joins them in their order
@@ -352,10 +414,11 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
         if (rank == 0) a.count[row] = 0;
         const size_t row0 = static_cast<size_t>(row) * a.parts;
         t = Sums();
-        for (int p = 0; p < a.parts; ++p) {
-            const float4 q = __ldcg(a.part + row0 + p);
-            t.join(Sums(q.x, q.y, q.z));
+        if (static_cast<int>(lane_id()) < a.parts) {
+            const float4 q = __ldcg(a.part + row0 + lane_id());
+            t = Sums(q.x, q.y, q.z);
         }
+        t = warp_join(t);
         if constexpr (TOP) {
             held = 0;
             const int step = (kCand - kMaxTop) / kMaxTop;   // parts whose candidates fit beside the best so far
@@ -473,7 +536,7 @@ cudaError_t launch_bwd(LogpBwdArgs a, const KernelEnv& env) {
     const bool small = a.V <= kSmallRow;
     a.parts = 1;
     a.chunk = a.V;
-    if (!small) split_rows(a.rows, a.V, 8 * device_sm_count(), a.parts, a.chunk);
+    if (!small) split_rows(a.rows, a.V, 4 * 8 * device_sm_count(), a.parts, a.chunk);
     const dim3 grid(small ? (a.rows + kThreads / 32 - 1) / (kThreads / 32) : a.rows * a.parts);
     return launch_early(small ? logp_bwd_kernel<E, 32> : logp_bwd_kernel<E, kThreads>, grid, kThreads, 0, env.stream, a);
 }
@@ -488,7 +551,7 @@ const char* logp_check(int V, int dtype, const void* logits, long long ld) {
     return nullptr;
 }
 
-int logp_max_splits() { return kBlocks * device_sm_count(); }
+int logp_max_splits() { return kWaves * kBlocks * device_sm_count(); }
 int logp_max_top() { return kMaxTop; }
 
 cudaError_t launch_logp(const LogpArgs& a, const KernelEnv& env) {
