@@ -14,9 +14,13 @@
 // rows than places for blocks a row in several parts, whose last block to end joins them.
 //
 // The likeliest columns come along in the same pass: a column is a candidate while its key
-// (order of the value, then of the index) is above the k-th best known.  That bar starts at
-// the k-th largest of the threads' first maxima, so that few columns pass it, and rises
-// whenever the candidates, kept in shared memory, are cut down to the best k.
+// (order of the value, then of the index) is above a bar that k columns reach.  The bar is the
+// k-th largest of the threads' maxima so far, taken after rounds 1, 2, 4, ..., so that about k
+// columns pass it from one of these to the next.  Each warp keeps its candidates in shared memory
+// (a block's warps need not wait for one another: a maximum that has moved on since it was read
+// only makes the bar too low), its lanes look together at the columns of a lane whose maximum
+// passes, and cuts them down to the best k where they are many.  A bar from the first columns
+// alone, and each lane at its own columns: 122 us for 640 rows of 151936 and 20 columns.
 #include <cmath>
 
 #include <math_constants.h>
@@ -30,8 +34,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBlocks = 4;            // a multiprocessor, as many as their registers allow
 constexpr int kMaxParts = 32;         // of a row: a lane each at the join
-constexpr int kWaves = 4;             // of blocks, so that their ends do not leave places empty for long
-constexpr int kMinPart = 2048;        // columns
+constexpr int kWaves = 2;             // of blocks, where rows come in parts (640 rows of 32000: 13 us, with four waves 26)
+constexpr int kMinPart = 4096;        // columns
 constexpr int kSmallRow = 4096;       // columns of rows that a warp takes
 constexpr int kStatusBadInput = 1;    // == SAS_ERR_INVALID_ARG
 constexpr float kLog2e = 1.4426950408889634f;
@@ -117,6 +121,7 @@ struct Span {
         count = (v1 - first + Vec<E>::N - 1) / Vec<E>::N;
     }
     __device__ __forceinline__ int column(int j) const { return first + j * Vec<E>::N; }
+    __device__ __forceinline__ int head() const { return count > 0 && !whole(0); }   // its first vector is partial
     __device__ __forceinline__ bool whole(int j) const { return column(j) >= v0 && column(j) + Vec<E>::N <= v1; }
 };
 
@@ -154,9 +159,10 @@ __device__ __forceinline__ Sums shfl_xor(const Sums& x, int o) {
 
 // The same in every lane: which of two joined sums is the left one must not matter, so both
 // lanes of a pair add them in lane order.
-__device__ __forceinline__ Sums warp_join(Sums x) {
+template <int LANES = 32>
+__device__ __forceinline__ Sums warp_join(Sums x) {   // of the first LANES
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
+    for (int o = 1; o < LANES; o <<= 1) {
         const Sums y = shfl_xor(x, o);
         Sums a = (lane_id() & o) ? y : x;
         a.join((lane_id() & o) ? x : y);
@@ -165,24 +171,30 @@ __device__ __forceinline__ Sums warp_join(Sums x) {
     return x;
 }
 
-// Keys order columns by value, equal ones by index; 0 is below every column.  Zeros of both
-// signs are equal.
-__device__ __forceinline__ unsigned long long key_of(float z, int v) {
+// The order of a value, as a whole number; zeros of both signs are equal.
+__device__ __forceinline__ uint32_t order_of(float z) {
     const uint32_t b = __float_as_uint(z + 0.f);
-    const uint32_t order = (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-    return (static_cast<unsigned long long>(order) << 32) | (0xffffffffu - static_cast<uint32_t>(v));
+    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
+// Keys order columns by value, equal ones by index; 0 is below every column.
+__device__ __forceinline__ unsigned long long key_of(float z, int v) {
+    return (static_cast<unsigned long long>(order_of(z)) << 32) | (0xffffffffu - static_cast<uint32_t>(v));
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o); }
 __device__ __forceinline__ float key_value(unsigned long long k) {
-    const uint32_t o = static_cast<uint32_t>(k >> 32);
-    return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
+    return value_of(static_cast<uint32_t>(k >> 32));
 }
 __device__ __forceinline__ int key_index(unsigned long long k) { return static_cast<int>(0xffffffffu - static_cast<uint32_t>(k)); }
 
 constexpr int kMaxTop = 32;
-constexpr int kCand = 512;     // candidates kept: kMaxParts * kMaxTop at the join are taken in pieces
-constexpr int kCut = 128;      // cut down at the end of a round that brings this many
+constexpr int kCand = 128;     // candidates of a warp
+constexpr int kCut = 64;       // cut down at the end of a round that leaves this many
+constexpr int kJoin = 512;     // candidates that the block joins at a time
+constexpr int kGroups = kThreads / 4;
+static_assert(kMaxTop <= kGroups, "the k-th of the groups' maxima");
+static_assert(kThreads / 32 * kMaxTop + kMaxTop <= kJoin, "the warps' best at a time");
 
-// A team (a block, or one of its warps) and the candidates of its row.
+// A team: a block, or one of its warps.
 template <int TEAM>
 struct Team {
     __device__ __forceinline__ static int rank() { return TEAM == 32 ? lane_id() : threadIdx.x; }
@@ -190,38 +202,27 @@ struct Team {
         if constexpr (TEAM == 32) __syncwarp();
         else __syncthreads();
     }
-    __device__ __forceinline__ static bool sync_or(bool x) {
-        if constexpr (TEAM == 32) {
-            const bool any = __any_sync(0xffffffffu, x);
-            __syncwarp();
-            return any;
-        } else {
-            return __syncthreads_or(x) != 0;
-        }
-    }
 };
-struct Cand {
+struct Cand {   // of a warp
     unsigned long long key[kCand];
     unsigned long long top[kMaxTop];
-    float first[32];         // maxima of 32 groups of threads over their first columns
-    int n;                   // asked for; at most kCand are kept
 };
 
-// The best k of the n candidates, best first, become the candidates.  All threads of the team.
+// The best k of n keys, best first, into their place (keys of 0, of no column, fill one place at most: the
+// others are 0 as well).  Returns how many there are.
 template <int TEAM>
-__device__ __forceinline__ int cut(Cand& c, int n, int k) {
-    for (int i = Team<TEAM>::rank(); i < k; i += TEAM) c.top[i] = 0;   // keys of no column, all equal, fill one place at most
+__device__ __forceinline__ int cut(unsigned long long* key, unsigned long long* top, int n, int k) {
+    for (int i = Team<TEAM>::rank(); i < k; i += TEAM) top[i] = 0;
     Team<TEAM>::sync();
     for (int i = Team<TEAM>::rank(); i < n; i += TEAM) {
-        const unsigned long long mine = c.key[i];
+        const unsigned long long mine = key[i];
         int above = 0;
-        for (int j = 0; j < n; ++j) above += c.key[j] > mine;
-        if (above < k) c.top[above] = mine;
+        for (int j = 0; j < n; ++j) above += key[j] > mine;
+        if (above < k) top[above] = mine;
     }
     Team<TEAM>::sync();
     n = min(n, k);
-    for (int i = Team<TEAM>::rank(); i < n; i += TEAM) c.key[i] = c.top[i];
-    if (Team<TEAM>::rank() == 0) c.n = n;
+    for (int i = Team<TEAM>::rank(); i < n; i += TEAM) key[i] = top[i];
     Team<TEAM>::sync();
     return n;
 }
@@ -239,13 +240,18 @@ template <class E, int TEAM, bool TOP>
 __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
     using V = Vec<E>;
     constexpr int N = V::N, U = V::UNROLL, ROUND = TEAM * U, TEAMS = kThreads / TEAM;
-    static_assert(N * U <= 32, "a thread's columns of a round have a bit each");
-    __shared__ Cand cands[TOP ? TEAMS : 1];
+    static_assert(N * U <= 32, "a thread's columns of a round, a lane each");
+    static_assert(kMaxTop + 32 <= kCut && kCut + 32 <= kCand, "room for a lane's columns after a cut");
+    __shared__ Cand cands[TOP ? kThreads / 32 : 1];
+    __shared__ unsigned long long all[TOP && TEAM == kThreads ? kJoin : 1], all_top[kMaxTop];
+    __shared__ uint4 seen[TOP ? U * kThreads : 1];
+    __shared__ float tops[TOP && TEAM == kThreads ? kGroups : 1];   // maxima so far, of four threads each
+    __shared__ int sh_held[kThreads / 32];
     __shared__ float3 joined[kThreads / 32];
     __shared__ int sh_last;
     const int rank = Team<TEAM>::rank(), part = TEAM == kThreads ? blockIdx.x % a.parts : 0;
     const int row = TEAM == kThreads ? blockIdx.x / a.parts : blockIdx.x * TEAMS + static_cast<int>(warp_id());
-    Cand& c = cands[TOP && TEAM == 32 ? warp_id() : 0];
+    Cand& c = cands[TOP ? warp_id() : 0];
     grid_dep_wait();
     if (TEAM == 32 && row >= a.rows) return;
     const int x = load(a.tokens + row);
@@ -267,25 +273,41 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
         return;
     }
     const E* const z = static_cast<const E*>(a.logits) + static_cast<size_t>(row) * a.ld;
+    const float zx = rank == 0 ? V::one(z + x) : 0.f;   // of use at the end
     const int v0 = part * a.chunk;
     const Span<E> sp(z, v0, min(a.V, v0 + a.chunk));
     Sums t;
     unsigned long long bar = 0;
     float bar_value = -CUDART_INF_F;   // below it no column is a candidate
-    int held = 0;
-    if (TOP && rank == 0) c.n = 0;
-    for (int j0 = 0; j0 < sp.count; j0 += ROUND) {
+    int held = 0;                      // the warp's candidates
+    // Whole vectors in whole rounds, then the others, of which the row's first may be one.
+    const int head = sp.head(), rounds = (sp.count - head - (sp.count > head && !sp.whole(sp.count - 1))) / ROUND;
+    const int late = rounds * ROUND + head, others = sp.count - late + head;   // where they begin, how many
+    const int all_rounds = rounds + (others + ROUND - 1) / ROUND;
+    const E* from = z + sp.column(head + rank);
+    for (int round = 0; round < all_rounds; ++round) {
+        // this thread's u-th vector
+        auto vector = [&](int u, int rank) {
+            const int q = (round < rounds ? round : round - rounds) * ROUND + u * TEAM + rank;
+            return round < rounds ? head + q : q < head ? 0 : late + q - head;
+        };
         uint4 raw[U];
+        if (round < rounds) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = j0 + u * TEAM + rank, v = sp.column(j);
-            if (j < sp.count && sp.whole(j)) {
-                raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + v));
-            } else {   // columns of the row alone, -infinity for the others
-                float f[N];
+            for (int u = 0; u < U; ++u) raw[u] = __ldcs(reinterpret_cast<const uint4*>(from + u * (TEAM * N)));
+            from += ROUND * N;
+        } else {
 #pragma unroll
-                for (int e = 0; e < N; ++e) f[e] = j < sp.count && v + e >= sp.v0 && v + e < sp.v1 ? V::one(z + v + e) : -CUDART_INF_F;
-                raw[u] = V::pack(f);
+            for (int u = 0; u < U; ++u) {
+                const int j = vector(u, rank), v = sp.column(j);
+                if (j < sp.count && sp.whole(j)) {
+                    raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + v));
+                } else {   // columns of the row alone, -infinity for the others
+                    float f[N];
+#pragma unroll
+                    for (int e = 0; e < N; ++e) f[e] = j < sp.count && v + e >= sp.v0 && v + e < sp.v1 ? V::one(z + v + e) : -CUDART_INF_F;
+                    raw[u] = V::pack(f);
+                }
             }
         }
         const float top = V::top(raw);
@@ -333,57 +355,64 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
         t.l += l;
         t.s += s;
         if constexpr (TOP) {
-            if (j0 == 0) {
-                // the k-th largest of 32 disjoint groups' maxima: k columns are no smaller
-                float v = top;
+            if ((round & (round - 1)) == 0) {
+                // The k-th largest of the maxima (k columns are no smaller), down to the upper 16 bits of its order:
+                // the largest such number that k of them reach.
+                constexpr int M = TEAM == 32 ? 1 : kGroups / 32;
+                uint32_t o[M];
                 if constexpr (TEAM == kThreads) {
+                    float v = fmaxf(t.m, __shfl_xor_sync(0xffffffffu, t.m, 1));
+                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+                    if (rank % 4 == 0) tops[rank / 4] = v;
+                    if (round == 0) __syncthreads();
+                    else __syncwarp();
 #pragma unroll
-                    for (int o = 1; o < 8; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-                    if (lane_id() % 8 == 0) c.first[rank / 8] = v;
-                    __syncthreads();
-                    v = c.first[lane_id()];
+                    for (int i = 0; i < M; ++i) o[i] = order_of(*static_cast<volatile float*>(&tops[i * 32 + lane_id()]));
+                } else {
+                    o[0] = order_of(t.m);
                 }
-                int above = 0;
+                uint32_t at = 0;
+#pragma unroll 1
+                for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+                    int n = 0;
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const float o = __shfl_sync(0xffffffffu, v, i);
-                    above += o > v || (o == v && i < static_cast<int>(lane_id()));
+                    for (int i = 0; i < M; ++i) n += o[i] >= (at | bit);
+                    if (__reduce_add_sync(0xffffffffu, n) >= a.k) at |= bit;
                 }
-                bar_value = __shfl_sync(0xffffffffu, v, __ffs(__ballot_sync(0xffffffffu, above == a.k - 1)) - 1);
-                if constexpr (TEAM == 32) __syncwarp();   // c.n
+                if (at > order_of(-CUDART_INF_F)) bar_value = fmaxf(bar_value, value_of(at));
             }
-            unsigned todo = 0;   // columns to offer
-            if (top >= bar_value) {
+            unsigned pass = __ballot_sync(0xffffffffu, top >= bar_value);   // lanes with a candidate, maybe
+            if (pass != 0) {
+                if (top >= bar_value) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int j = j0 + u * TEAM + rank, v = sp.column(j);
-                    float f[N];
-                    V::unpack(raw[u], f);
-#pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (f[e] >= bar_value && j < sp.count && v + e >= sp.v0 && v + e < sp.v1) todo |= 1u << (u * N + e);
+                    for (int u = 0; u < U; ++u) seen[u * kThreads + threadIdx.x] = raw[u];
                 }
-            }
-            for (;;) {
-                bool many = false;
-                while (todo != 0) {
-                    const int i = __ffs(todo) - 1;
-                    const int v = sp.column(j0 + i / N * TEAM + rank) + i % N;
-                    const unsigned long long key = key_of(V::one(z + v), v);
-                    if (key > bar) {
-                        const int at = atomicAdd(&c.n, 1);
-                        many |= at >= kCut - 1;
-                        if (at >= kCand) break;   // full: offered again once they are cut down
-                        c.key[at] = key;
+                __syncwarp();
+                for (; pass != 0; pass &= pass - 1) {
+                    // a lane's N U columns, one of them each
+                    const int at = __ffs(pass) - 1, i = lane_id(), u = i / N;
+                    const int j = vector(u, rank - i + at), v = sp.column(j) + i % N;
+                    const bool there = u < U && j < sp.count && v >= sp.v0 && v < sp.v1;
+                    const float f = there ? V::one(reinterpret_cast<const E*>(seen + u * kThreads + threadIdx.x - i + at) + i % N) : 0.f;
+                    const unsigned long long key = key_of(f, v);
+                    auto candidate = [&] { return there && f >= bar_value && key > bar; };
+                    auto raise = [&] {
+                        __syncwarp();
+                        held = cut<32>(c.key, c.top, held, a.k);
+                        if (held < a.k) return;
+                        bar = c.key[a.k - 1];
+                        bar_value = fmaxf(bar_value, key_value(bar));
+                    };
+                    unsigned who = __ballot_sync(0xffffffffu, candidate());
+                    if (held + __popc(who) > kCand) {
+                        raise();
+                        who = __ballot_sync(0xffffffffu, candidate());
                     }
-                    todo &= todo - 1;
+                    if (who >> i & 1u) c.key[held + __popc(who & ((1u << i) - 1))] = key;
+                    held += __popc(who);
+                    if (held >= kCut) raise();
                 }
-                if (!Team<TEAM>::sync_or(many)) break;
-                held = cut<TEAM>(c, min(c.n, kCand), a.k);
-                if (held == a.k) {
-                    bar = c.key[a.k - 1];
-                    bar_value = fmaxf(bar_value, key_value(bar));
-                }
+                __syncwarp();   // before other columns are put there
             }
         }
     }
@@ -392,22 +421,38 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
         if (lane_id() == 0) joined[warp_id()] = make_float3(t.m, t.l, t.s);
         __syncthreads();
         t = Sums();
-#pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) t.join(Sums(joined[w].x, joined[w].y, joined[w].z));
+        if (lane_id() < kThreads / 32) t = Sums(joined[lane_id()].x, joined[lane_id()].y, joined[lane_id()].z);
+        t = warp_join<kThreads / 32>(t);
     }
+    unsigned long long* best = c.key;   // the best k, and how many of them are columns
     if constexpr (TOP) {
-        Team<TEAM>::sync();
-        held = cut<TEAM>(c, min(c.n, kCand), a.k);
+        __syncwarp();
+        held = cut<32>(c.key, c.top, held, a.k);
+        if constexpr (TEAM == kThreads) {
+            best = all;
+            if (lane_id() == 0) sh_held[warp_id()] = held;
+            __syncthreads();
+            int before = 0, sum = 0;
+#pragma unroll
+            for (int w = 0; w < kThreads / 32; ++w) {
+                if (w == static_cast<int>(warp_id())) before = sum;
+                sum += sh_held[w];
+            }
+            for (int i = lane_id(); i < held; i += 32) all[before + i] = c.key[i];
+            __syncthreads();
+            held = cut<TEAM>(all, all_top, sum, a.k);
+        }
     }
     if (TEAM == kThreads && a.parts > 1) {
         // the part's results; the row's last block joins them in their order
         const size_t at = static_cast<size_t>(row) * a.parts + part;
-        if (rank == 0) a.part[at] = make_float4(t.m, t.l, t.s, 0.f);
-        if constexpr (TOP)
-            for (int i = rank; i < a.k; i += TEAM) a.part_top[at * kMaxTop + i] = i < held ? c.key[i] : 0ull;
-        __threadfence();
-        __syncthreads();
-        if (rank == 0) sh_last = atomicAdd(a.count + row, 1) == a.parts - 1;
+        if (rank < 32) {
+            if (rank == 0) a.part[at] = make_float4(t.m, t.l, t.s, 0.f);
+            if (TOP && rank < a.k) a.part_top[at * kMaxTop + rank] = rank < held ? best[rank] : 0ull;
+            __threadfence();
+            __syncwarp();
+            if (rank == 0) sh_last = atomicAdd(a.count + row, 1) == a.parts - 1;
+        }
         __syncthreads();
         if (!sh_last) return;
         __threadfence();
@@ -421,20 +466,20 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
         t = warp_join(t);
         if constexpr (TOP) {
             held = 0;
-            const int step = (kCand - kMaxTop) / kMaxTop;   // parts whose candidates fit beside the best so far
+            const int step = (kJoin - kMaxTop) / kMaxTop;   // parts whose candidates fit beside the best so far
             for (int p0 = 0; p0 < a.parts; p0 += step) {
                 const int np = min(step, a.parts - p0);
                 for (int i = rank; i < np * a.k; i += TEAM)
-                    c.key[held + i] = __ldcg(a.part_top + (row0 + p0 + i / a.k) * kMaxTop + i % a.k);
+                    all[held + i] = __ldcg(a.part_top + (row0 + p0 + i / a.k) * kMaxTop + i % a.k);
                 __syncthreads();
-                held = cut<TEAM>(c, held + np * a.k, a.k);
+                held = cut<TEAM>(all, all_top, held + np * a.k, a.k);
             }
         }
     }
-    if (rank == 0) put_row(a, row, t, V::one(z + x));
+    if (rank == 0) put_row(a, row, t, zx);
     if constexpr (TOP) {
         for (int i = rank; i < a.k; i += TEAM) {
-            const unsigned long long key = i < held ? c.key[i] : 0ull;
+            const unsigned long long key = i < held ? best[i] : 0ull;
             const size_t at = static_cast<size_t>(row) * a.k + i;
             a.top_index[at] = key == 0 ? -1 : key_index(key);
             a.top_logprob[at] = key == 0 || t.l == 0.f ? CUDART_NAN_F : (key_value(key) - t.m) - logf(t.l);
