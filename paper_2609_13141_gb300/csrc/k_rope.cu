@@ -538,11 +538,11 @@ cudaError_t launch_any_bwd(const RopeArgs& a, const KernelEnv& env) {
 // it does the rows that stay are rounded again under the larger one.  So the maximum of a
 // page's new rows has to be known before any of them is written: the tokens of a page stand
 // next to each other, and a run of them of one page and head is one piece of work, whose rows
-// wait in registers.  A run of up to 8 tokens is a warp's, a longer one a block's, 8 tokens a
-// warp; a block looks for the runs that begin in 8 neighbouring tokens (one of them at most is
-// longer than 8).
+// wait in registers.  A block has the runs of a head that begin in a window of neighbouring
+// tokens: the ones of up to 8 tokens a warp each, the longer ones all together, 8 tokens a warp.
 constexpr int kRunRows = 8;                       // of a warp
-static_assert(kWarps == kRunRows, "a block's window is a token a warp, its longest run a page");
+constexpr int kMaxWindow = 64;                    // tokens; runs have 64 at most
+static_assert(kWarps * kRunRows >= 64, "a block's longest run is a page");
 
 // Least power of two s with amax <= 448 s, 448 = 1.75 * 2^8, within 2^-64 .. 2^120.
 __device__ __forceinline__ float page_scale(float amax) {
@@ -578,76 +578,60 @@ __device__ __forceinline__ uint32_t shrink_quad(uint32_t w, float ratio) {
     return out;
 }
 
-// A run as its warps know it.
+// A run as its warps know it: tokens first .. first + n - 1 of the window.
 struct Run {
-    long long t0, page;
-    int n;
+    int first, n, page;
     unsigned lo, hi;   // its rows of the page
-
-    // The run that begins at token t; none if t has no slot or stands behind one of its page.
-    __device__ __forceinline__ bool find(const RopeArgs& a, long long t) {
-        const int lane = lane_id();
-        auto page_of = [&](long long i) {   // of token i, -1 if it has none
-            const long long s = i >= 0 && i < a.T ? load(a.slots + i) : -1;
-            return s >= 0 && s < a.n_slots ? s >> 6 : -1LL;
-        };
-        t0 = t;
-        const long long before = page_of(t - 1), p0 = page_of(t + lane), p1 = page_of(t + 32 + lane);
-        page = __shfl_sync(0xffffffffu, p0, 0);
-        if (page < 0 || before == page) return false;
-        const unsigned m0 = __ballot_sync(0xffffffffu, p0 == page), m1 = __ballot_sync(0xffffffffu, p1 == page);
-        n = ~m0 != 0 ? __ffs(~m0) - 1 : 32 + (~m1 != 0 ? __ffs(~m1) - 1 : 32);
-        auto row_of = [&](int i) {   // of the run's token i; 64 where it has no place in the tables
-            if (i >= n) return 64;
-            const int p = t + i < a.T ? load(a.pos + t + i) : -1;
-            if (p < 0 || p >= a.max_pos) {
-                atomicExch(a.status, kStatusBadInput);
-                return 64;
-            }
-            return static_cast<int>((t + i < a.T ? load(a.slots + t + i) : 0) & 63);
-        };
-        const int r0 = row_of(lane), r1 = row_of(lane + 32);
-        lo = __reduce_or_sync(0xffffffffu, (r0 < 32 ? 1u << r0 : 0u) | (r1 < 32 ? 1u << r1 : 0u));
-        hi = __reduce_or_sync(0xffffffffu, (r0 >= 32 && r0 < 64 ? 1u << (r0 - 32) : 0u) | (r1 >= 32 && r1 < 64 ? 1u << (r1 - 32) : 0u));
-        return (lo | hi) != 0;
-    }
 };
 
 template <int D, bool INTER>
-__global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8 c) {
+__global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8 c, int window) {
     using R = Rows<D, 1>;
     constexpr int P = kRunRows / R::GPW;   // passes: a group's rows
-    __shared__ Run longest;
-    __shared__ float tops[2][kWarps];
+    __shared__ int pages[kMaxWindow + 65], rows[kMaxWindow + 64], spots[kMaxWindow + 64];   // pages: of the token before, too
+    __shared__ float tops[2][2][kWarps];
     const int lane = lane_id(), warp = warp_id(), l = lane % R::LPR, g = lane / R::LPR;
-    const unsigned window = blockIdx.x / static_cast<unsigned>(a.Hkv);
-    const int head = static_cast<int>(blockIdx.x - window * a.Hkv);
+    const unsigned at_window = blockIdx.x / static_cast<unsigned>(a.Hkv);
+    const int head = static_cast<int>(blockIdx.x - at_window * a.Hkv);
+    const long long t0 = static_cast<long long>(at_window) * window;
     const Place<INTER> pl(a, l);
     const bool turns = turned(a, l);
-    if (threadIdx.x == 0) longest.n = 0;
     grid_dep_wait();
     Quads w;
     w.load(a.wk, pl.ia, pl.ib);
+    // the window's tokens, and as many after it as its last run may have: page (-1: none), row of the page (64: no
+    // place in the tables) and position
+    for (int i = threadIdx.x; i < window + 65; i += kThreads) {
+        const long long t = t0 + i - 1;
+        const long long slot = t >= 0 && t < a.T ? load(a.slots + t) : -1;
+        const bool there = slot >= 0 && slot < a.n_slots;
+        pages[i] = there ? static_cast<int>(slot >> 6) : -1;
+        if (i == 0) continue;
+        const int p = t < a.T ? load(a.pos + t) : 0;
+        const bool placed = p >= 0 && p < a.max_pos;
+        rows[i - 1] = placed ? static_cast<int>(slot & 63) : 64;
+        spots[i - 1] = p;
+        // slots that name no row of the cache (-1: padding), positions outside the tables
+        if (head == 0 && i <= window && ((!there && slot != -1) || (there && !placed))) atomicExch(a.status, kStatusBadInput);
+    }
+    __syncthreads();
     // The warp's tokens i0 .. i0 + 7 of a run; JOINT: with the block's other warps.
+    int turn_of = 0;
     auto work = [&](const Run& run, int i0, auto joint) {
         constexpr bool JOINT = decltype(joint)::value;
         const size_t at_scale = static_cast<size_t>(run.page) * a.Hkv + head;
         const float old_k = load(c.k_scale + at_scale), old_v = load(c.v_scale + at_scale);
         Quads kq[P];
         uint4 v[P];
-        int pos[P], row[P];
+        int row[P];
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int i = i0 + p * R::GPW + g;
-            const long long t = run.t0 + i;
-            row[p] = -1;
+            row[p] = i < run.n ? rows[run.first + i] : 64;
             kq[p].a = kq[p].b = make_uint2(0, 0);
             v[p] = make_uint4(0, 0, 0, 0);
-            pos[p] = 0;
-            if (i < run.n) {
-                pos[p] = t < a.T ? load(a.pos + t) : -1;
-                row[p] = static_cast<int>((t < a.T ? load(a.slots + t) : 0) & 63);
-                const bf16* const src = a.qkv + t * a.ld + static_cast<long long>(a.Hq + head) * D;
+            if (row[p] < 64) {
+                const bf16* const src = a.qkv + (t0 + run.first + i) * a.ld + static_cast<long long>(a.Hq + head) * D;
                 kq[p].load(src, pl.ia, pl.ib);
                 v[p] = load(reinterpret_cast<const uint4*>(src + static_cast<long long>(a.Hkv) * D + l * 8));
             }
@@ -663,7 +647,6 @@ __global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8
         };
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            if (pos[p] < 0 || pos[p] >= a.max_pos) row[p] = -1;   // left out
             uint64_t wf[4];
             kq[p].unpack(y[p]);
             w.unpack(wf);
@@ -673,9 +656,9 @@ __global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8
             const uint64_t r = dup2(rsqrtf(R::sum(sum2(ss), 0xffffffffu) * (1.f / D) + a.eps));
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[p][i] = mul_f32x2(mul_f32x2(y[p][i], r), wf[i]);
-            if (row[p] >= 0) {
+            if (row[p] < 64) {
                 if (turns) {
-                    const size_t from = static_cast<size_t>(pos[p]) * (a.rot >> 1) + 4 * l;
+                    const size_t from = static_cast<size_t>(spots[run.first + i0 + p * R::GPW + g]) * (a.rot >> 1) + 4 * l;
                     const Turn<INTER, false, false> turn(reinterpret_cast<const uint8_t*>(a.cos + from),
                                                          reinterpret_cast<const uint8_t*>(a.sin + from));
                     turn.apply(y[p], true);
@@ -699,15 +682,16 @@ __global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8
         }
         if constexpr (JOINT) {
             if (lane == 0) {
-                tops[0][warp] = top_k;
-                tops[1][warp] = top_v;
+                tops[turn_of][0][warp] = top_k;
+                tops[turn_of][1][warp] = top_v;
             }
             __syncthreads();   // and the old scales have been read
 #pragma unroll
             for (int i = 0; i < kWarps; ++i) {
-                top_k = fmaxf(top_k, tops[0][i]);
-                top_v = fmaxf(top_v, tops[1][i]);
+                top_k = fmaxf(top_k, tops[turn_of][0][i]);
+                top_v = fmaxf(top_v, tops[turn_of][1][i]);
             }
+            turn_of ^= 1;      // the next run's maxima do not wait for these to be read
         }
         __syncwarp();
         const bool fresh = (run.lo & 1u) != 0;
@@ -721,7 +705,7 @@ __global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8
         const float ik = 1.f / sk, iv = 1.f / sv;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            if (row[p] < 0) continue;
+            if (row[p] == 64) continue;
             uint8_t* const k8 = c.K + base + row[p] * D;
             *reinterpret_cast<uint32_t*>(k8 + pl.ia) = pack_quad(y[p][0], y[p][1], ik);
             *reinterpret_cast<uint32_t*>(k8 + pl.ib) = pack_quad(y[p][2], y[p][3], ik);
@@ -747,32 +731,48 @@ __global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8
         if (!fresh && sk > old_k) shrink(c.K + base, old_k / sk);
         if (!fresh && sv > old_v) shrink(c.V + base, old_v / sv);
     };
-    const long long t = static_cast<long long>(window) * kRunRows + warp;
-    Run run;
-    __syncthreads();
-    if (t < a.T && run.find(a, t)) {
-        if (run.n > kRunRows) {
-            if (lane == 0) longest = run;
-        } else {
-            work(run, 0, std::false_type());
+    // The runs that begin in the window, in every warp.
+    unsigned begins[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = h * 32 + lane;
+        begins[h] = __ballot_sync(0xffffffffu, i < window && pages[i + 1] >= 0 && pages[i] != pages[i + 1]);
+    }
+    auto find = [&](int first) {
+        Run run;
+        run.first = first;
+        run.page = pages[first + 1];
+        const unsigned m0 = __ballot_sync(0xffffffffu, pages[first + 1 + lane] == run.page);
+        const unsigned m1 = __ballot_sync(0xffffffffu, pages[first + 33 + lane] == run.page);
+        run.n = ~m0 != 0 ? __ffs(~m0) - 1 : 32 + (~m1 != 0 ? __ffs(~m1) - 1 : 32);
+        const int r0 = lane < run.n ? rows[first + lane] : 64, r1 = lane + 32 < run.n ? rows[first + 32 + lane] : 64;
+        run.lo = __reduce_or_sync(0xffffffffu, (r0 < 32 ? 1u << r0 : 0u) | (r1 < 32 ? 1u << r1 : 0u));
+        run.hi = __reduce_or_sync(0xffffffffu, (r0 >= 32 && r0 < 64 ? 1u << (r0 - 32) : 0u) | (r1 >= 32 && r1 < 64 ? 1u << (r1 - 32) : 0u));
+        return run;
+    };
+    int k = 0;
+    for (int h = 0; h < 2; ++h) {
+        for (unsigned m = begins[h]; m != 0; m &= m - 1, ++k) {
+            const Run run = find(h * 32 + __ffs(m) - 1);
+            if ((run.lo | run.hi) == 0) continue;   // no token of it has a place
+            if (run.n > kRunRows) work(run, warp * kRunRows, std::true_type());
+            else if (k % kWarps == warp) work(run, 0, std::false_type());
         }
     }
-    // slots that name no row of the cache (-1: padding)
-    if (head == 0 && lane == 0) {
-        const long long s = t < a.T ? load(a.slots + t) : -1;
-        if (s < -1 || s >= a.n_slots) atomicExch(a.status, kStatusBadInput);
-    }
-    __syncthreads();
-    if (longest.n > 0) {
-        const Run all = longest;
-        work(all, warp * kRunRows, std::true_type());
-    }
+}
+
+// Tokens of a window: as few as give every warp a token, more where there are blocks enough
+// (eight a multiprocessor: an empty window costs a block 2 us).
+int append8_window(const RopeArgs& a) {
+    const long long w = a.T * a.Hkv / (8LL * device_sm_count());
+    return w < kWarps ? kWarps : (w > kMaxWindow ? kMaxWindow : static_cast<int>(w));
 }
 
 template <int D>
 cudaError_t launch_append8(const RopeArgs& a, const Cache8& c, const KernelEnv& env) {
-    const dim3 grid(static_cast<unsigned>((a.T + kRunRows - 1) / kRunRows * a.Hkv));
-    return launch_early(a.interleaved ? append8_kernel<D, true> : append8_kernel<D, false>, grid, kThreads, 0, env.stream, a, c);
+    const int window = append8_window(a);
+    const dim3 grid(static_cast<unsigned>((a.T + window - 1) / window * a.Hkv));
+    return launch_early(a.interleaved ? append8_kernel<D, true> : append8_kernel<D, false>, grid, kThreads, 0, env.stream, a, c, window);
 }
 
 template <int D>
@@ -802,7 +802,7 @@ const char* rope_check(int rot, int interleaved, int max_pos, float eps, long lo
 // Tokens are counted in 32 bits where a batch row is found by division.
 bool rope_supported(const RopeArgs& a) { return a.T <= 0x7fffffffLL; }
 
-bool append8_supported(const RopeArgs& a) { return (a.T + kRunRows - 1) / kRunRows * a.Hkv <= 0x7fffffffLL; }
+bool append8_supported(const RopeArgs& a) { return (a.T + kWarps - 1) / kWarps * a.Hkv <= 0x7fffffffLL; }
 
 int rope_bwd_max_blocks() { return kBwdBlocks * device_sm_count(); }   // all resident
 
