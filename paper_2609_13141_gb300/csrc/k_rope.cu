@@ -551,19 +551,27 @@ __device__ __forceinline__ float page_scale(float amax) {
     k = max(-64, min(120, k));
     return __uint_as_float(static_cast<uint32_t>(k + 127) << 23);
 }
-// Two numbers as e4m3, to nearest.  What is not finite becomes NaN (there is no infinity).
+// Two numbers as e4m3, to nearest; NaN stays, infinities become the largest number.
 __device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi) {
-    lo = fabsf(lo) <= 3.4e38f ? lo : __uint_as_float(0x7fc00000u);
-    hi = fabsf(hi) <= 3.4e38f ? hi : __uint_as_float(0x7fc00000u);
     uint16_t r;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ uint32_t pack_quad(uint64_t a, uint64_t b, float inv) {
+__device__ __forceinline__ float finite_or(float x, float other) { return fabsf(x) < __uint_as_float(0x7f800000u) ? x : other; }
+// Four numbers times inv; NaN (there is no infinity) for what is not finite, where any may be.
+__device__ __forceinline__ uint32_t pack_quad(uint64_t a, uint64_t b, float inv, bool odd) {
+    const uint64_t i2 = dup2(inv);
     float x0, x1, x2, x3;
-    f32x2_split(a, x0, x1);
-    f32x2_split(b, x2, x3);
-    return pack_e4m3x2(x0 * inv, x1 * inv) | (pack_e4m3x2(x2 * inv, x3 * inv) << 16);
+    f32x2_split(mul_f32x2(a, i2), x0, x1);
+    f32x2_split(mul_f32x2(b, i2), x2, x3);
+    if (odd) {
+        const float nan = __uint_as_float(0x7fc00000u);
+        x0 = finite_or(x0, nan);
+        x1 = finite_or(x1, nan);
+        x2 = finite_or(x2, nan);
+        x3 = finite_or(x3, nan);
+    }
+    return pack_e4m3x2(x0, x1) | (pack_e4m3x2(x2, x3) << 16);
 }
 // Four numbers under a larger scale.
 __device__ __forceinline__ uint32_t shrink_quad(uint32_t w, float ratio) {
@@ -637,14 +645,6 @@ __global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8
             }
         }
         uint64_t y[P][4];
-        float top_k = 0.f, top_v = 0.f;
-        auto grow = [](float top, uint64_t x) {   // what is not finite has no say
-            float lo, hi;
-            f32x2_split(x, lo, hi);
-            lo = fabsf(lo);
-            hi = fabsf(hi);
-            return max3f(top, lo <= 3.4e38f ? lo : 0.f, hi <= 3.4e38f ? hi : 0.f);
-        };
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             uint64_t wf[4];
@@ -663,36 +663,61 @@ __global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8
                                                          reinterpret_cast<const uint8_t*>(a.sin + from));
                     turn.apply(y[p], true);
                 }
-                Quads q;
-                uint64_t vf[4];
-                q.a = make_uint2(v[p].x, v[p].y);
-                q.b = make_uint2(v[p].z, v[p].w);
-                q.unpack(vf);
+            }
+        }
+        auto value = [&](int p, uint64_t (&f)[4]) {
+            Quads q;
+            q.a = make_uint2(v[p].x, v[p].y);
+            q.b = make_uint2(v[p].z, v[p].w);
+            q.unpack(f);
+        };
+        // The run's largest numbers: infinities among them, and where there are, without what is not finite (which
+        // has no say in the scale).  Maxima pass over NaN.
+        float top_k, top_v;
+        auto largest = [&](bool finite) {
+            top_k = top_v = 0.f;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                if (row[p] == 64) continue;
+                uint64_t f[4];
+                value(p, f);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    top_k = grow(top_k, y[p][i]);
-                    top_v = grow(top_v, vf[i]);
+                    float a0, a1, b0, b1;
+                    f32x2_split(y[p][i], a0, a1);
+                    f32x2_split(f[i], b0, b1);
+                    if (finite) {
+                        a0 = finite_or(a0, 0.f);
+                        a1 = finite_or(a1, 0.f);
+                        b0 = finite_or(b0, 0.f);
+                        b1 = finite_or(b1, 0.f);
+                    }
+                    top_k = max3f(top_k, fabsf(a0), fabsf(a1));
+                    top_v = max3f(top_v, fabsf(b0), fabsf(b1));
                 }
             }
-        }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            top_k = fmaxf(top_k, __shfl_xor_sync(0xffffffffu, top_k, o));
-            top_v = fmaxf(top_v, __shfl_xor_sync(0xffffffffu, top_v, o));
-        }
-        if constexpr (JOINT) {
-            if (lane == 0) {
-                tops[turn_of][0][warp] = top_k;
-                tops[turn_of][1][warp] = top_v;
+            for (int o = 16; o > 0; o >>= 1) {
+                top_k = fmaxf(top_k, __shfl_xor_sync(0xffffffffu, top_k, o));
+                top_v = fmaxf(top_v, __shfl_xor_sync(0xffffffffu, top_v, o));
             }
-            __syncthreads();   // and the old scales have been read
+            if constexpr (JOINT) {
+                if (lane == 0) {
+                    tops[turn_of][0][warp] = top_k;
+                    tops[turn_of][1][warp] = top_v;
+                }
+                __syncthreads();   // and the old scales have been read
 #pragma unroll
-            for (int i = 0; i < kWarps; ++i) {
-                top_k = fmaxf(top_k, tops[turn_of][0][i]);
-                top_v = fmaxf(top_v, tops[turn_of][1][i]);
+                for (int i = 0; i < kWarps; ++i) {
+                    top_k = fmaxf(top_k, tops[turn_of][0][i]);
+                    top_v = fmaxf(top_v, tops[turn_of][1][i]);
+                }
+                turn_of ^= 1;      // the next maxima do not wait for these to be read
             }
-            turn_of ^= 1;      // the next run's maxima do not wait for these to be read
-        }
+        };
+        largest(false);
+        const bool odd = fmaxf(top_k, top_v) == __uint_as_float(0x7f800000u);
+        if (odd) largest(true);
         __syncwarp();
         const bool fresh = (run.lo & 1u) != 0;
         const float sk = fresh ? page_scale(top_k) : fmaxf(old_k, page_scale(top_k));
@@ -707,15 +732,12 @@ __global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8
         for (int p = 0; p < P; ++p) {
             if (row[p] == 64) continue;
             uint8_t* const k8 = c.K + base + row[p] * D;
-            *reinterpret_cast<uint32_t*>(k8 + pl.ia) = pack_quad(y[p][0], y[p][1], ik);
-            *reinterpret_cast<uint32_t*>(k8 + pl.ib) = pack_quad(y[p][2], y[p][3], ik);
-            Quads q;
+            *reinterpret_cast<uint32_t*>(k8 + pl.ia) = pack_quad(y[p][0], y[p][1], ik, odd);
+            *reinterpret_cast<uint32_t*>(k8 + pl.ib) = pack_quad(y[p][2], y[p][3], ik, odd);
             uint64_t vf[4];
-            q.a = make_uint2(v[p].x, v[p].y);
-            q.b = make_uint2(v[p].z, v[p].w);
-            q.unpack(vf);
+            value(p, vf);
             *reinterpret_cast<uint2*>(c.V + base + row[p] * D + l * 8) =
-                make_uint2(pack_quad(vf[0], vf[1], iv), pack_quad(vf[2], vf[3], iv));
+                make_uint2(pack_quad(vf[0], vf[1], iv, odd), pack_quad(vf[2], vf[3], iv, odd));
         }
         // rows that stay, under a scale that grew
         auto shrink = [&](uint8_t* page8, float ratio) {
