@@ -5,7 +5,7 @@
 // The tensor core takes 8-bit numbers only beside 8-bit numbers, and rounding queries and
 // weights to 8 bits would show.  So the pages' numbers become f16, exactly, in shared memory:
 //   * warp 0 takes work items, publishes them and loads their Q by TMA;
-//   * two or four warps load pages, a share of a page's rows each and one or two pages ahead in
+//   * four warps load pages, a quarter of a page's rows each and one or two pages ahead in
 //     registers, and convert them into rings of f16 tiles in the tensor core's layout, value rows of no key
 //     as zero;
 //   * a warp a tile issues S = Q K^T and O += P V (P read from tensor memory);
@@ -33,15 +33,16 @@ constexpr int kItemSlots = 4;     // work items in flight between warp 0 and the
 constexpr int kStatusLayout = 3;
 constexpr long long kTwoTiles = 192;   // rows of a request on average
 
-// As in k_chunk.cu: a step is KPS pages, whose scores, softmax and product go through the
-// pipeline together; half of Q in tensor memory at d = 128.
+// As in k_chunk.cu, half of Q is in tensor memory at d = 128.  A step is one page: the second
+// page of a step, which helps bf16 pages at d = 64, would need the registers that two more
+// converting warps take here (2 of them set the pace: 2200 cycles a page, 154 us for a ragged
+// batch of 2626 tokens and 24 heads of 64).
 template <int D, int TILES>
 struct Cfg {
-    static constexpr int KPS = D == 64 ? 2 : 1;
     static constexpr bool QT = D == 128;
-    static constexpr int THREADS = 256 * TILES;
-    static constexpr int CONV0 = 2 * TILES, CONV = 2 * TILES;   // the warps that convert
-    static constexpr int SOFT0 = 4 * TILES;                     // the softmax warps, four a tile
+    static constexpr int THREADS = 256 + 128 * TILES;
+    static constexpr int CONV0 = 4, CONV = 4;                   // the warps that convert
+    static constexpr int SOFT0 = 8;                             // the softmax warps, four a tile
     static constexpr int READERS = TILES + CONV + 4 * TILES;   // of an item
     static constexpr int Q_BYTES = kBM * D * 2;      // of a tile
     static constexpr int QST = D == 64 ? 2 : 1;      // Q of the item at work, and the next one's
@@ -49,8 +50,8 @@ struct Cfg {
     static constexpr int PAGE = kBN * D;
     static constexpr int KST = D == 64 ? 4 : (TILES == 2 ? 4 : 2);   // f16 pages of a ring
     static constexpr int AHEAD = TILES == 2 ? 2 : 1;   // pages in registers on their way to conversion
-    static constexpr int SCALES = 16;                // pages' scales: the loads are AHEAD + KST + 2 KPS pages ahead of the softmax at most
-    static_assert(AHEAD + KST + 2 * KPS <= SCALES, "scales");
+    static constexpr int SCALES = 16;                // pages' scales: the loads are AHEAD + KST + 2 pages ahead of the softmax at most
+    static_assert(AHEAD + KST + 2 <= SCALES, "scales");
     static constexpr int OFF_K = QST * TILES * Q_BYTES;
     static constexpr int OFF_V = OFF_K + KST * KV_BYTES;
     static constexpr int OFF_CTL = OFF_V + KST * KV_BYTES;
@@ -59,33 +60,28 @@ struct Cfg {
     static constexpr int TMEM_COLS = 256;               // of a tile
     static constexpr int TMEM_O = 0;
     static constexpr int TMEM_S = D;
-    static constexpr int TMEM_P = TMEM_S + KPS * kBN;   // keys packed in pairs
-    static constexpr int TMEM_Q = TMEM_P + 32 * KPS;    // the row's first 64 dims packed in pairs
+    static constexpr int TMEM_P = TMEM_S + kBN;         // keys packed in pairs
+    static constexpr int TMEM_Q = TMEM_P + 32;          // the row's first 64 dims packed in pairs
     static_assert(TMEM_Q + (QT ? 32 : 0) <= TMEM_COLS, "tensor memory");
     static constexpr uint32_t IDESC_S = idesc_f16(kBM, kBN, 0, 0);
     static constexpr uint32_t IDESC_O = idesc_f16(kBM, D, 0, 1);
 };
 
 // Moves registers between the block's warpgroups (the sum stays within what it was launched
-// with: 128 threads x (80 + 176) <= 256 x 128, and 128 x (56 + 120 + 2 x 168) = 512 x 128).
+// with: 128 x (40 + 72 + 128) = 128 x (56 + 56 + 128) = 384 x 80, 128 x (56 + 120 + 2 x 168) = 512 x 128).
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int D, int TILES>
 __device__ __forceinline__ void give_registers() {
-    if constexpr (TILES == 1) {
-        if constexpr (D == 64) fewer_registers<80>();
-    } else if (warp_id() < 4) {
-        fewer_registers<56>();
-    } else {
-        fewer_registers<120>();
-    }
+    constexpr bool two_pages = D == 128 && TILES == 1;   // of a lane's registers, 32 are on their way
+    if (warp_id() < 4) fewer_registers<two_pages ? 40 : 56>();
+    else fewer_registers<TILES == 2 ? 120 : two_pages ? 72 : 56>();
 }
-template <int D, int TILES>
+template <int TILES>
 __device__ __forceinline__ void take_registers() {
-    if constexpr (D == 64) more_registers<176>();
-    else if constexpr (TILES == 2) more_registers<168>();
+    more_registers<TILES == 1 ? 128 : 168>();
 }
 
 template <class C, int TILES>
@@ -97,7 +93,6 @@ struct Ctl {
     Item item[kItemSlots];
     uint32_t tmem_base;
     int abort_flag;
-    int again[TILES];          // the step's product comes in two parts
 };
 constexpr int kSharesAt = 872;
 
@@ -168,7 +163,7 @@ __device__ __forceinline__ void prefetch_page(const void* p, uint32_t bytes) {
 }
 
 template <int D, int TILES>
-__global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(const __grid_constant__ CUtensorMap mapQ, ChunkArgs a, float scale_log2, long long limit) {
+__global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile_kernel(const __grid_constant__ CUtensorMap mapQ, ChunkArgs a, float scale_log2, long long limit) {
     using C = Cfg<D, TILES>;
     using K = Ctl<C, TILES>;
     static_assert(sizeof(K) <= kSharesAt && kSharesAt + sizeof(Shares) <= 1024, "control block");
@@ -193,7 +188,6 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(con
             mbar_init(&ctl.pv_done[t], 1);
             mbar_init(&ctl.p_full[t], 4);
             mbar_init(&ctl.q_ready[t], 4);
-            ctl.again[t] = 0;
         }
         mbar_init(&ctl.drain_bar, TILES);
         for (int s = 0; s < kItemSlots; ++s) {
@@ -338,77 +332,60 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(con
             const uint64_t dv0 = smem_desc_sw128(smem_u32(smem + C::OFF_V), kBN * 128, 1024);
             bool ok = true;
             int ns = 0, np = 0;   // scores, arrivals of P
-            uint64_t* q_free = nullptr;
-            auto product = [&](int vp, int pages, bool fresh) {   // fresh: a new accumulator
-                for (int i = 0; i < pages; ++i)
-                    if (!mbar_wait_warp(&ctl.v_full[(vp + i) % C::KST], ((vp + i) / C::KST) & 1, wc)) return false;
-                for (bool more = true; more;) {
-                    if (!mbar_wait_warp(&ctl.p_full[t], np & 1, wc)) return false;
-                    ++np;
-                    more = C::KPS > 1 && *static_cast<volatile int*>(&ctl.again[t]) != 0;
-                    tc_fence_after();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int i = 0; i < C::KPS; ++i) {
-                            if (i >= pages) break;
-                            const int vs = (vp + i) % C::KST;
-                            const uint64_t dv = dv0 + static_cast<uint64_t>((vs * C::KV_BYTES) >> 4);
-#pragma unroll
-                            for (int k = 0; k < kBN / 16; ++k)
-                                umma_bf16_ta(tile + C::TMEM_O, tile + C::TMEM_P + i * 32 + k * 8, dv + ((k * 2048) >> 4), C::IDESC_O,
-                                             (!fresh || i > 0 || k > 0) ? 1u : 0u);
-                            if (!more) umma_commit(&ctl.v_empty[vs]);
-                        }
-                        umma_commit(&ctl.pv_done[t]);
-                    }
-                    __syncwarp();
-                    fresh = false;
-                }
-                return true;
-            };
-            // (the dims in tensor memory come first)
-            auto score = [&](uint64_t dq, int gp, int pages, bool last) {   // last: Q is free after it
-                for (int i = 0; i < pages; ++i)
-                    if (!mbar_wait_warp(&ctl.k_full[(gp + i) % C::KST], ((gp + i) / C::KST) & 1, wc)) return false;
-                if (ns >= 1 && !mbar_wait_warp(&ctl.sc_free[t], (ns - 1) & 1, wc)) return false;
-                ++ns;
+            auto product = [&](int g, bool fresh) {   // fresh: a new accumulator
+                const int vs = g % C::KST;
+                if (!mbar_wait_warp(&ctl.v_full[vs], (g / C::KST) & 1, wc) || !mbar_wait_warp(&ctl.p_full[t], np & 1, wc)) return false;
+                ++np;
                 tc_fence_after();
                 if (elect_one()) {
+                    const uint64_t dv = dv0 + static_cast<uint64_t>((vs * C::KV_BYTES) >> 4);
 #pragma unroll
-                    for (int i = 0; i < C::KPS; ++i) {
-                        if (i >= pages) break;
-                        const int s = (gp + i) % C::KST;
-                        const uint64_t dk = dk0 + static_cast<uint64_t>((s * C::KV_BYTES) >> 4);
-#pragma unroll
-                        for (int k = 0; k < D / 16; ++k) {
-                            const uint32_t off_q = (k >> 2) * (kBM * 128) + (k & 3) * 32;
-                            const uint32_t off_k = (k >> 2) * (kBN * 128) + (k & 3) * 32;
-                            if (C::QT && k < 4)
-                                umma_bf16_ta(tile + C::TMEM_S, tile + C::TMEM_Q + k * 8, dk + (off_k >> 4), C::IDESC_S, k > 0);
-                            else
-                                umma_bf16(tile + C::TMEM_S + i * kBN, dq + (off_q >> 4), dk + (off_k >> 4), C::IDESC_S, k > 0);
-                        }
-                        umma_commit(&ctl.k_empty[s]);
-                    }
-                    umma_commit(&ctl.sc_full[t]);
-                    if (last) umma_commit(q_free);
+                    for (int k = 0; k < kBN / 16; ++k)
+                        umma_bf16_ta(tile + C::TMEM_O, tile + C::TMEM_P + k * 8, dv + ((k * 2048) >> 4), C::IDESC_O, (!fresh || k > 0) ? 1u : 0u);
+                    umma_commit(&ctl.v_empty[vs]);
+                    umma_commit(&ctl.pv_done[t]);
                 }
                 __syncwarp();
                 return true;
             };
-            int gp = 0, nq = 0;   // pages; items of the tile
+            // (the dims in tensor memory come first)
+            auto score = [&](uint64_t dq, int g, uint64_t* q_free) {   // q_free: Q's place is free after it
+                const int s = g % C::KST;
+                if (!mbar_wait_warp(&ctl.k_full[s], (g / C::KST) & 1, wc)) return false;
+                if (ns >= 1 && !mbar_wait_warp(&ctl.sc_free[t], (ns - 1) & 1, wc)) return false;
+                ++ns;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t dk = dk0 + static_cast<uint64_t>((s * C::KV_BYTES) >> 4);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off_q = (k >> 2) * (kBM * 128) + (k & 3) * 32;
+                        const uint32_t off_k = (k >> 2) * (kBN * 128) + (k & 3) * 32;
+                        if (C::QT && k < 4)
+                            umma_bf16_ta(tile + C::TMEM_S, tile + C::TMEM_Q + k * 8, dk + (off_k >> 4), C::IDESC_S, k > 0);
+                        else
+                            umma_bf16(tile + C::TMEM_S, dq + (off_q >> 4), dk + (off_k >> 4), C::IDESC_S, k > 0);
+                    }
+                    umma_commit(&ctl.k_empty[s]);
+                    umma_commit(&ctl.sc_full[t]);
+                    if (q_free != nullptr) umma_commit(q_free);
+                }
+                __syncwarp();
+                return true;
+            };
+            int g = 0, nq = 0;   // pages; items of the tile
             for (int r = 0; ok; ++r) {
                 Item x;
                 if (!read_item(ctl, r, wc, x)) { ok = false; break; }
                 if (x.head < 0) break;
                 const int qs = r % C::QST;
                 const uint64_t dq = dq0 + static_cast<uint64_t>((qs * TILES * C::Q_BYTES) >> 4);
-                q_free = &ctl.q_empty[qs];
+                uint64_t* const q_free = &ctl.q_empty[qs];
                 if (t * R >= x.ntok) {   // nothing to do but to let all go, once it is there: arrivals of these phases
                     ok = mbar_wait_warp(&ctl.q_full[qs], (r / C::QST) & 1, wc);
                     if (ok && lane == 0) mbar_arrive(q_free);
-                    for (int m = x.blk0; ok && m < x.blk1; ++m, ++gp) {
-                        const int s = gp % C::KST, phase = (gp / C::KST) & 1;
+                    for (int m = x.blk0; ok && m < x.blk1; ++m, ++g) {
+                        const int s = g % C::KST, phase = (g / C::KST) & 1;
                         ok = mbar_wait_warp(&ctl.k_full[s], phase, wc) && mbar_wait_warp(&ctl.v_full[s], phase, wc);
                         if (ok && lane == 0) {
                             mbar_arrive(&ctl.k_empty[s]);
@@ -417,12 +394,11 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(con
                     }
                     continue;
                 }
-                ok = mbar_wait_warp(&ctl.q_ready[t], nq++ & 1, wc) && score(dq, gp, min(C::KPS, x.blk1 - x.blk0), x.blk1 - x.blk0 <= C::KPS);
-                for (int m = x.blk0; ok && m < x.blk1; m += C::KPS) {
-                    const int pages = min(C::KPS, x.blk1 - m);
-                    if (m + C::KPS < x.blk1) ok = score(dq, gp + pages, min(C::KPS, x.blk1 - m - C::KPS), m + 2 * C::KPS >= x.blk1);
-                    ok = ok && product(gp, pages, m == x.blk0);
-                    gp += pages;
+                const int np_item = x.blk1 - x.blk0;
+                ok = mbar_wait_warp(&ctl.q_ready[t], nq++ & 1, wc) && score(dq, g, np_item == 1 ? q_free : nullptr);
+                for (int i = 0; ok && i < np_item; ++i, ++g) {
+                    if (i + 1 < np_item) ok = score(dq, g + 1, i + 2 == np_item ? q_free : nullptr);
+                    ok = ok && product(g, i == 0);
                 }
             }
             if (elect_one()) {
@@ -433,8 +409,8 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(con
         }
     } else {
         // ---------------- softmax, one thread per row
-        take_registers<D, TILES>();
-        constexpr int NK = C::KPS * kBN;   // keys of a step
+        take_registers<TILES>();
+        constexpr int NK = kBN;
         const int tile = (warp - C::SOFT0) >> 2, q = warp & 3;
         const int row = q * 32 + lane;                          // of the tile
         const int tok = tile * R + row / a.G, hq = row % a.G;   // of the item
@@ -501,7 +477,7 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(con
             if (lane == 0) mbar_arrive(&ctl.q_ready[tile]);
             return true;
         };
-        int g = 0, gp = 0, np = 0;   // steps, pages, arrivals of P
+        int g = 0, gt = 0;   // pages; the tile's
         Item x, nx;
         bool ok = take_item(0, x);
         for (int r = 1; ok && x.head >= 0; x = nx, ++r) {
@@ -509,63 +485,30 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(con
             const bool valid = tok < x.ntok;
             const bool warp_rows = warp_has_rows(x);
             if (!tile_has_rows(x)) {
-                gp += x.blk1 - x.blk0;
+                g += x.blk1 - x.blk0;
                 if (!take_item(r, nx)) { ok = false; break; }
                 continue;
             }
             const int pos = x.pos0 + tok;
             float m_use = -CUDART_INF_F, l = 0.f;
             float v_ref = 0.f, v_log = 0.f;   // what one of O stands for
-            for (int m = x.blk0; ok && m < x.blk1; m += C::KPS, ++g) {
-                const int pages = min(C::KPS, x.blk1 - m);
-                // last key column of the step that this row sees (< 0: none; none of a page that is not
-                // there).  Rows of no token are never read: they go unmasked.
-                const int lim = valid ? min(min(NK - 1, pos - m * kBN), (x.blk1 - m) * kBN - 1) : NK - 1;
-                if (!mbar_wait_warp(&ctl.sc_full[tile], g & 1, wc)) { ok = false; break; }
-                float4 sc[C::KPS];
-#pragma unroll
-                for (int i = 0; i < C::KPS; ++i) sc[i] = ctl.scale[(gp + (i < pages ? i : 0)) % C::SCALES];
-                gp += pages;
+            for (int m = x.blk0; m < x.blk1; ++m, ++g, ++gt) {
+                // last key column of the page that this row sees (< 0: none).  Rows of no token are never read: they
+                // go unmasked.
+                const int lim = valid ? min(NK - 1, pos - m * kBN) : NK - 1;
+                if (!mbar_wait_warp(&ctl.sc_full[tile], gt & 1, wc)) { ok = false; break; }
+                const float4 sc = ctl.scale[g % C::SCALES];
                 if (m == x.blk0) {
-                    v_log = sc[0].y;
-                    v_ref = sc[0].w;
+                    v_log = sc.y;
+                    v_ref = sc.w;
                 }
-                auto near = [](float v, float ref) { return fabsf(v - ref) <= kScaleRange; };   // logarithms
-                bool move = !near(sc[0].y, v_log);
-                if constexpr (C::KPS == 2) move |= !near(sc[1].y, v_log);
-                // a step whose pages cannot stand under one scale has its product in two parts
-                const bool parts = C::KPS == 2 && move && !near(sc[C::KPS - 1].y, sc[0].y);
-                // P is free once the product before has read it
-                auto p_free = [&] {
-                    if (np >= 1 && !mbar_wait_warp(&ctl.pv_done[tile], (np - 1) & 1, wc)) return false;
-                    tc_fence_after();
-                    return true;
-                };
-                auto p_ready = [&] {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&ctl.p_full[tile]);
-                    ++np;
-                };
-                auto move_to = [&](const float4& v) {   // the factor that O takes
-                    const float by = v_ref * v.z;
-                    v_ref = v.w;
-                    v_log = v.y;
-                    return by;
-                };
+                // P is free, and O another product's no more, once the product before has read and written them
+                auto product_done = [&] { return gt == 0 || mbar_wait_warp(&ctl.pv_done[tile], (gt - 1) & 1, wc); };
                 if (!warp_rows) {
                     if (lane == 0) mbar_arrive(&ctl.sc_free[tile]);
-                    if (parts) {
-#pragma unroll
-                        for (int i = 0; i < C::KPS; ++i)
-                            if (!near(sc[i].y, v_log)) move_to(sc[i]);
-                    } else if (move) {
-                        move_to(sc[0]);
-                    }
-                    for (int i = 0; ok && i <= static_cast<int>(parts); ++i) {
-                        ok = p_free();
-                        if (ok) p_ready();
-                    }
+                    if (!product_done()) { ok = false; break; }
+                    if (lane == 0) mbar_arrive(&ctl.p_full[tile]);
+                    __syncwarp();
                     continue;
                 }
                 tc_fence_after();
@@ -581,33 +524,33 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(con
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&ctl.sc_free[tile]);
-                float cr[C::KPS];
-                if (m * kBN + NK - 1 > x.pos0 + tile * R || pages < C::KPS) {   // some row does not see all of it
+                if (m * kBN + NK - 1 > x.pos0 + tile * R) {   // some row does not see all of it
 #pragma unroll
                     for (int k = 0; k < NK; ++k) xs[k] = k <= lim ? xs[k] : -CUDART_INF_F;
                 }
-                float mb = -CUDART_INF_F;
+                float mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-                for (int i = 0; i < C::KPS; ++i) {
-                    float mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+                for (int k = 0; k < NK; k += 8) {
 #pragma unroll
-                    for (int k = i * kBN; k < (i + 1) * kBN; k += 8) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) mx[j] = max3f(mx[j], xs[k + 2 * j], xs[k + 2 * j + 1]);
-                    }
-                    cr[i] = row_scale * sc[i].x;
-                    mb = fmaxf(mb, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * cr[i]);
+                    for (int j = 0; j < 4; ++j) mx[j] = max3f(mx[j], xs[k + 2 * j], xs[k + 2 * j + 1]);
                 }
-                bool need = valid && mb > m_use + kRescaleThreshold;
+                const float cr = row_scale * sc.x;
+                const float mb = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * cr;
+                const bool need = valid && mb > m_use + kRescaleThreshold;
                 const float m_new = need ? mb : m_use;
                 const float off = m_new == -CUDART_INF_F ? 0.f : -m_new;
                 float factor = need ? (m_use == -CUDART_INF_F ? 0.f : fast_exp2(m_use - m_new)) : 1.f;
                 m_use = m_new;
                 l *= factor;
-                // O to another maximum, or under another value scale: once the product before is done
-                auto rescale = [&](bool change, float by) {
-                    if (!__any_sync(0xffffffffu, change)) return true;
-                    if (!mbar_wait_warp(&ctl.pv_done[tile], (np - 1) & 1, wc)) return false;
+                // O stands under another value scale from here on
+                const bool move = !(fabsf(sc.y - v_log) <= kScaleRange);
+                if (move) {
+                    factor *= v_ref * sc.z;
+                    v_ref = sc.w;
+                    v_log = sc.y;
+                }
+                if (m > x.blk0 && __any_sync(0xffffffffu, need || move)) {
+                    if (!product_done()) { ok = false; break; }
                     tc_fence_after();
 #pragma unroll 1
                     for (int cc = 0; cc < D / 32; ++cc) {
@@ -615,68 +558,42 @@ __global__ void __launch_bounds__(256 * TILES, 2 / TILES) chunk8_tile_kernel(con
                         tmem_ld32(lane_addr + C::TMEM_O + cc * 32, o);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
                         tmem_st32(lane_addr + C::TMEM_O + cc * 32, o);
                     }
                     tmem_wait_st();
-                    return true;
-                };
-                // P = 2^(z - m) of page i, times its value scale over O's; the row's sum
-                auto weights = [&](int i, uint32_t (&pk)[32]) {
-                    const float by = off + (sc[i].y - v_log);
-                    const uint64_t scale2 = f32x2(cr[i], cr[i]), off2 = f32x2(by, by);
+                }
+                // P = 2^(z - m) times the page's value scale over O's; the row's sum without it
+                uint32_t pk[32];
+                {
+                    const float by = off + (sc.y - v_log);
+                    const uint64_t scale2 = f32x2(cr, cr), off2 = f32x2(by, by);
                     uint64_t acc[4] = {0, 0, 0, 0};
 #pragma unroll
-                    for (int k = 0; k < kBN; k += 2) {
+                    for (int k = 0; k < NK; k += 2) {
                         float a0, a1;
-                        f32x2_split(fma_f32x2(f32x2(xs[i * kBN + k], xs[i * kBN + k + 1]), scale2, off2), a0, a1);
+                        f32x2_split(fma_f32x2(f32x2(xs[k], xs[k + 1]), scale2, off2), a0, a1);
                         const float e0 = fast_exp2(a0), e1 = fast_exp2(a1);
                         acc[(k >> 1) & 3] = add_f32x2(acc[(k >> 1) & 3], f32x2(e0, e1));
                         pk[k >> 1] = pack_f16x2(e0, e1);
                     }
                     float s0, s1;
                     f32x2_split(add_f32x2(add_f32x2(acc[0], acc[1]), add_f32x2(acc[2], acc[3])), s0, s1);
-                    l = fmaf(s0 + s1, sc[i].z * v_ref, l);
-                };
-                if (parts) {
-                    // rare: a page at a time, the other one's weights zero
-#pragma unroll
-                    for (int i = 0; i < C::KPS; ++i) {
-                        const bool moves = !near(sc[i].y, v_log);
-                        if (moves) factor *= move_to(sc[i]);
-                        uint32_t pk[32];
-                        if ((m > x.blk0 || i > 0) && !rescale(need || moves, factor)) { ok = false; break; }
-                        weights(i, pk);
-                        if (!p_free()) { ok = false; break; }
-                        tmem_st32(lane_addr + C::TMEM_P + i * 32, pk);
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) pk[k] = 0;
-                        tmem_st32(lane_addr + C::TMEM_P + (1 - i) * 32, pk);
-                        tmem_wait_st();
-                        if (q == 0 && lane == 0) ctl.again[tile] = i == 0;   // a tile's first warp has rows whenever it has any
-                        p_ready();
-                        factor = 1.f;
-                        need = false;
-                    }
-                    if (!ok) break;
-                    continue;
+                    l = fmaf(s0 + s1, sc.z * v_ref, l);
                 }
-                if (move) factor *= move_to(sc[0]);
-                if (m > x.blk0 && !rescale(need || move, factor)) { ok = false; break; }
-                uint32_t pk[C::KPS][32];
-#pragma unroll
-                for (int i = 0; i < C::KPS; ++i) weights(i, pk[i]);
-                if (!p_free()) { ok = false; break; }
-#pragma unroll
-                for (int i = 0; i < C::KPS; ++i) tmem_st32(lane_addr + C::TMEM_P + i * 32, pk[i]);
+                if (!product_done()) { ok = false; break; }
+                tc_fence_after();
+                tmem_st32(lane_addr + C::TMEM_P, pk);
                 tmem_wait_st();
-                p_ready();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl.p_full[tile]);
             }
             // the next item's Q goes ahead of this one's epilogue: its first product runs during it
             if (!ok || !take_item(r, nx)) { ok = false; break; }
             // The next item's first PV overwrites O only after this warp's next arrival on
             // p_full, which follows the reads below.
-            if (!mbar_wait_warp(&ctl.pv_done[tile], (np - 1) & 1, wc)) { ok = false; break; }
+            if (!mbar_wait_warp(&ctl.pv_done[tile], (gt - 1) & 1, wc)) { ok = false; break; }
             tc_fence_after();
             const size_t orow = (static_cast<size_t>(x.tok0) + tok) * a.Hq + static_cast<size_t>(x.head) * a.G + hq;
             if (x.part < 0) {
