@@ -5,9 +5,9 @@
 // The tensor core takes 8-bit numbers only beside 8-bit numbers, and rounding queries and
 // weights to 8 bits would show.  So the pages' numbers become f16, exactly, in shared memory:
 //   * warp 0 takes work items, publishes them and loads their Q by TMA;
-//   * four warps load pages, a quarter of a page's rows each and one or two pages ahead in
-//     registers, and convert them into rings of f16 tiles in the tensor core's layout, value rows of no key
-//     as zero;
+//   * four warps load pages into registers, two of them keys and two values, each every other
+//     page or half of every page, one ahead, and convert them into rings of f16 tiles in the tensor
+//     core's layout, value rows of no key as zero;
 //   * a warp a tile issues S = Q K^T and O += P V (P read from tensor memory);
 //   * four warps a tile, a thread per row: Q as f16 under a power of two of the row's own
 //     (k_chunk8.cu), mask, online softmax in the log2 domain, P as f16 pairs into tensor memory,
@@ -42,6 +42,7 @@ struct Cfg {
     static constexpr bool QT = D == 128;
     static constexpr int THREADS = 256 + 128 * TILES;
     static constexpr int CONV0 = 4, CONV = 4;                   // the warps that convert
+    static constexpr int SHARES = D == 128 && TILES == 1 ? 2 : 1;   // of a page's keys or values: as registers allow
     static constexpr int SOFT0 = 8;                             // the softmax warps, four a tile
     static constexpr int READERS = TILES + CONV + 4 * TILES;   // of an item
     static constexpr int Q_BYTES = kBM * D * 2;      // of a tile
@@ -49,9 +50,9 @@ struct Cfg {
     static constexpr int KV_BYTES = kBN * D * 2;
     static constexpr int PAGE = kBN * D;
     static constexpr int KST = D == 64 ? 4 : (TILES == 2 ? 4 : 2);   // f16 pages of a ring
-    static constexpr int AHEAD = TILES == 2 ? 2 : 1;   // pages in registers on their way to conversion
-    static constexpr int SCALES = 16;                // pages' scales: the loads are AHEAD + KST + 2 pages ahead of the softmax at most
-    static_assert(AHEAD + KST + 2 <= SCALES, "scales");
+    static_assert(SHARES == 2 || KST % 2 == 0, "a place of the rings is one warp's: see k_chunk8.cu");
+    static constexpr int SCALES = 16;                // pages' scales: the loads are KST + 4 pages ahead of the softmax at most
+    static_assert(KST + 4 <= SCALES, "scales");
     static constexpr int OFF_K = QST * TILES * Q_BYTES;
     static constexpr int OFF_V = OFF_K + KST * KV_BYTES;
     static constexpr int OFF_CTL = OFF_V + KST * KV_BYTES;
@@ -68,16 +69,15 @@ struct Cfg {
 };
 
 // Moves registers between the block's warpgroups (the sum stays within what it was launched
-// with: 128 x (40 + 72 + 128) = 128 x (56 + 56 + 128) = 384 x 80, 128 x (56 + 120 + 2 x 168) = 512 x 128).
+// with: 128 x (40 + 72 + 128) = 384 x 80, 128 x (56 + 120 + 2 x 168) = 512 x 128).
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int D, int TILES>
+template <int TILES>
 __device__ __forceinline__ void give_registers() {
-    constexpr bool two_pages = D == 128 && TILES == 1;   // of a lane's registers, 32 are on their way
-    if (warp_id() < 4) fewer_registers<two_pages ? 40 : 56>();
-    else fewer_registers<TILES == 2 ? 120 : two_pages ? 72 : 56>();
+    if (warp_id() < 4) fewer_registers<TILES == 1 ? 40 : 56>();
+    else fewer_registers<TILES == 1 ? 72 : 120>();
 }
 template <int TILES>
 __device__ __forceinline__ void take_registers() {
@@ -180,8 +180,8 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
     const uint32_t warp = warp_id(), lane = lane_id();
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::QST; ++s) { mbar_init(&ctl.q_full[s], 1); mbar_init(&ctl.q_empty[s], TILES); }
-        for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.k_full[s], C::CONV); mbar_init(&ctl.k_empty[s], TILES); }
-        for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.v_full[s], C::CONV); mbar_init(&ctl.v_empty[s], TILES); }
+        for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.k_full[s], C::SHARES); mbar_init(&ctl.k_empty[s], TILES); }
+        for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.v_full[s], C::SHARES); mbar_init(&ctl.v_empty[s], TILES); }
         for (int t = 0; t < TILES; ++t) {
             mbar_init(&ctl.sc_full[t], 1);
             mbar_init(&ctl.sc_free[t], 4);
@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
     // Every role walks the same items and counts pages over all of them (g): ring slots, score
     // buffers and barrier phases follow g across item boundaries.
     if (warp < C::SOFT0) {
-        give_registers<D, TILES>();
+        give_registers<TILES>();
         if (warp == 0) {
             // ---------------- items and their Q
             if (lane == 0) tma_prefetch_desc(&mapQ);
@@ -252,73 +252,59 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
             }
         } else if (warp >= C::CONV0) {
             // ---------------- pages to f16 tiles
-            const int share = warp - C::CONV0;
+            const bool keys = warp < C::CONV0 + 2;
+            const int mine = warp & 1, share = C::SHARES == 2 ? mine : 0;
+            constexpr int STEP = 3 - C::SHARES;   // pages from one of this warp's to the next
+            const uint8_t* const cache = keys ? a.K8 : a.V8;
+            uint8_t* const ring = smem + (keys ? C::OFF_K : C::OFF_V);
+            uint64_t* const full = keys ? ctl.k_full : ctl.v_full;
+            uint64_t* const empty = keys ? ctl.k_empty : ctl.v_empty;
             int g = 0;
             bool ok = true;
             for (int r = 0; ok; ++r) {
                 Item x;
                 if (!read_item(ctl, r, wc, x)) { ok = false; break; }
                 if (x.head < 0) break;
-                const int end = x.pos0 + x.ntok;   // keys from here on belong to no row of the item
-                const int none = a.num_pages * a.Hkv;
-                int rows = 0;              // of 32 pages, a lane each
+                const int np = x.blk1 - x.blk0, none = a.num_pages * a.Hkv;
+                const int end = keys ? kBN * 32768 : x.pos0 + x.ntok - x.blk0 * kBN;   // values from here on are no row's
+                int rows = 0, batch = -1;  // of 32 pages, a lane each
                 float4 sc = make_float4(1.f, 0.f, 1.f, 1.f);
-                Piece<D, C::CONV> k[C::AHEAD], v[C::AHEAD];
-                int row = none;
-                // Page i of the item: where it is, its scales, the pages behind it into L2.
-                auto locate = [&](int i) {
-                    const int m = x.blk0 + i, j = i & 31;
-                    if (j == 0) {
+                Piece<D, C::SHARES> piece;
+                // Page i of the item into registers, the scales to the softmax, the pages behind it into L2.
+                auto fetch = [&](int i) {
+                    const int j = i & 31;
+                    if (i >> 5 != batch) {
+                        batch = i >> 5;
+                        const int m = x.blk0 + batch * 32;
                         rows = page_row(a, x, m, lane);
                         sc = make_float4(1.f, 0.f, 1.f, 1.f);
                         if (m + static_cast<int>(lane) < x.blk1 && rows < none) {
-                            if (share == 0) {
+                            if (keys) {
                                 const float vs = load(a.v_scale + rows);
                                 sc = make_float4(load(a.k_scale + rows), log2f(vs), 1.f / vs, vs);
                             }
-                            if (lane < kAhead && share < 2) prefetch_page((share == 0 ? a.K8 : a.V8) + static_cast<size_t>(rows) * C::PAGE, C::PAGE);
+                            if (lane < kAhead && (lane & (STEP - 1)) == (j & (STEP - 1)))
+                                prefetch_page(cache + static_cast<size_t>(rows) * C::PAGE, C::PAGE);
                         }
                     }
-                    row = __shfl_sync(0xffffffffu, rows, j);
-                    if (share < 2) {
-                        const int far = __shfl_sync(0xffffffffu, rows, (j + kAhead) & 31);
-                        if (lane == 0 && j + kAhead < 32 && m + kAhead < x.blk1 && far < none)
-                            prefetch_page((share == 0 ? a.K8 : a.V8) + static_cast<size_t>(far) * C::PAGE, C::PAGE);
-                    }
-                    if (share == 0 && static_cast<int>(lane) == j) ctl.scale[(g + i) % C::SCALES] = sc;
+                    const int row = __shfl_sync(0xffffffffu, rows, j), far = __shfl_sync(0xffffffffu, rows, (j + kAhead) & 31);
+                    if (lane == 0 && share == 0 && j + kAhead < 32 && i + kAhead < np && far < none)
+                        prefetch_page(cache + static_cast<size_t>(far) * C::PAGE, C::PAGE);
+                    if (keys && share == 0 && static_cast<int>(lane) == j) ctl.scale[(g + i) % C::SCALES] = sc;
+                    piece.fetch(cache + static_cast<size_t>(row) * C::PAGE, row < none, share, lane);
                 };
-                const int np = x.blk1 - x.blk0;
-#pragma unroll
-                for (int d = 0; d < C::AHEAD; ++d) {
-                    if (d >= np) break;
-                    locate(d);
-                    k[d].fetch(a.K8 + static_cast<size_t>(row) * C::PAGE, row < none, share, lane);
-                    v[d].fetch(a.V8 + static_cast<size_t>(row) * C::PAGE, row < none, share, lane);
-                }
-                for (int i0 = 0; ok && i0 < np; i0 += C::AHEAD) {
-#pragma unroll
-                    for (int d = 0; d < C::AHEAD; ++d) {
-                        const int i = i0 + d, s = (g + i) % C::KST;
-                        if (i >= np) break;
-                        const uint32_t phase = (((g + i) / C::KST) & 1) ^ 1u;
-                        const bool more = i + C::AHEAD < np;
-                        if (more) locate(i + C::AHEAD);
-                        if (!mbar_wait_warp(&ctl.k_empty[s], phase, wc)) { ok = false; break; }
-                        k[d].convert(smem + C::OFF_K + s * C::KV_BYTES, share, lane, kBN);   // late keys may be anything
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&ctl.k_full[s]);
-                        __syncwarp();
-                        if (more) k[d].fetch(a.K8 + static_cast<size_t>(row) * C::PAGE, row < none, share, lane);
-                        if (!mbar_wait_warp(&ctl.v_empty[s], phase, wc)) { ok = false; break; }
-                        // P is 0 past the end, and 0 times a stale NaN is NaN: such value rows become zero
-                        v[d].convert(smem + C::OFF_V + s * C::KV_BYTES, share, lane, end - (x.blk0 + i) * kBN);
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&ctl.v_full[s]);
-                        __syncwarp();
-                        if (more) v[d].fetch(a.V8 + static_cast<size_t>(row) * C::PAGE, row < none, share, lane);
-                    }
+                int i = STEP == 2 ? (g ^ mine) & 1 : 0;
+                if (i < np) fetch(i);
+                for (; i < np; i += STEP) {
+                    const int s = (g + i) % C::KST;
+                    if (!mbar_wait_warp(&empty[s], (((g + i) / C::KST) & 1) ^ 1u, wc)) { ok = false; break; }
+                    // P is 0 past the end, and 0 times a stale NaN is NaN: such value rows become zero
+                    piece.convert(ring + s * C::KV_BYTES, share, lane, end - i * kBN);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&full[s]);
+                    __syncwarp();
+                    if (i + STEP < np) fetch(i + STEP);
                 }
                 g += np;
             }
