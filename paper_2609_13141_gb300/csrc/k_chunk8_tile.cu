@@ -8,7 +8,8 @@
 //   * four warps load pages into registers, two of them keys and two values, each every other
 //     page or half of every page, one ahead, and convert them into rings of f16 tiles in the tensor
 //     core's layout, value rows of no key as zero;
-//   * a warp a tile issues S = Q K^T and O += P V (P read from tensor memory);
+//   * two warps issue the products, S = Q K^T and O += P V (P read from tensor memory): one each of a
+//     block's one tile, or one tile each of two;
 //   * four warps a tile, a thread per row: Q as f16 under a power of two of the row's own
 //     (k_chunk8.cu), mask, online softmax in the log2 domain, P as f16 pairs into tensor memory,
 //     O rescaled only when the maximum grows by 2^8, or where a page's value scale leaves 2^-6 ..
@@ -33,10 +34,11 @@ constexpr int kItemSlots = 4;     // work items in flight between warp 0 and the
 constexpr int kStatusLayout = 3;
 constexpr long long kTwoTiles = 192;   // rows of a request on average
 
-// As in k_chunk.cu, half of Q is in tensor memory at d = 128.  A step is one page: the second
-// page of a step, which helps bf16 pages at d = 64, would need the registers that two more
-// converting warps take here (2 of them set the pace: 2200 cycles a page, 154 us for a ragged
-// batch of 2626 tokens and 24 heads of 64).
+// As in k_chunk.cu, half of Q is in tensor memory at d = 128.  A step is one page, with the next
+// one's scores made ahead at d = 64.  Two pages a step, which helps bf16 pages at d = 64, would
+// need registers that the converting warps hold here; with the second page's scores read twice
+// instead, and no scores ahead, a ragged batch of 2626 tokens and 24 heads of 64 takes 144 us
+// instead of 128.
 template <int D, int TILES>
 struct Cfg {
     static constexpr bool QT = D == 128;
@@ -44,7 +46,8 @@ struct Cfg {
     static constexpr int CONV0 = 4, CONV = 4;                   // the warps that convert
     static constexpr int SHARES = D == 128 && TILES == 1 ? 2 : 1;   // of a page's keys or values: as registers allow
     static constexpr int SOFT0 = 8;                             // the softmax warps, four a tile
-    static constexpr int READERS = TILES + CONV + 4 * TILES;   // of an item
+    static constexpr bool SPLIT = TILES == 1;                   // a warp for scores and one for P V
+    static constexpr int READERS = 2 + CONV + 4 * TILES;       // of an item
     static constexpr int Q_BYTES = kBM * D * 2;      // of a tile
     static constexpr int QST = D == 64 ? 2 : 1;      // Q of the item at work, and the next one's
     static constexpr int KV_BYTES = kBN * D * 2;
@@ -61,7 +64,8 @@ struct Cfg {
     static constexpr int TMEM_COLS = 256;               // of a tile
     static constexpr int TMEM_O = 0;
     static constexpr int TMEM_S = D;
-    static constexpr int TMEM_P = TMEM_S + kBN;         // keys packed in pairs
+    static constexpr int NS = D == 64 ? 2 : 1;          // scores of a page at work, and the next one's
+    static constexpr int TMEM_P = TMEM_S + NS * kBN;    // keys packed in pairs
     static constexpr int TMEM_Q = TMEM_P + 32;          // the row's first 64 dims packed in pairs
     static_assert(TMEM_Q + (QT ? 32 : 0) <= TMEM_COLS, "tensor memory");
     static constexpr uint32_t IDESC_S = idesc_f16(kBM, kBN, 0, 0);
@@ -87,7 +91,7 @@ __device__ __forceinline__ void take_registers() {
 template <class C, int TILES>
 struct Ctl {
     uint64_t q_full[C::QST], q_empty[C::QST], k_full[C::KST], k_empty[C::KST], v_full[C::KST], v_empty[C::KST];
-    uint64_t sc_full[TILES], sc_free[TILES], p_full[TILES], pv_done[TILES], q_ready[TILES], drain_bar;
+    uint64_t sc_full[TILES][C::NS], sc_free[TILES][C::NS], p_full[TILES], pv_done[TILES], q_ready[TILES], drain_bar;
     uint64_t item_full[kItemSlots], item_empty[kItemSlots];
     float4 scale[C::SCALES];   // of page g at g % SCALES: the keys', the values' log2, inverse and itself
     Item item[kItemSlots];
@@ -183,13 +187,12 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
         for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.k_full[s], C::SHARES); mbar_init(&ctl.k_empty[s], TILES); }
         for (int s = 0; s < C::KST; ++s) { mbar_init(&ctl.v_full[s], C::SHARES); mbar_init(&ctl.v_empty[s], TILES); }
         for (int t = 0; t < TILES; ++t) {
-            mbar_init(&ctl.sc_full[t], 1);
-            mbar_init(&ctl.sc_free[t], 4);
+            for (int s = 0; s < C::NS; ++s) { mbar_init(&ctl.sc_full[t][s], 1); mbar_init(&ctl.sc_free[t][s], 4); }
             mbar_init(&ctl.pv_done[t], 1);
             mbar_init(&ctl.p_full[t], 4);
             mbar_init(&ctl.q_ready[t], 4);
         }
-        mbar_init(&ctl.drain_bar, TILES);
+        mbar_init(&ctl.drain_bar, 2);
         for (int s = 0; s < kItemSlots; ++s) {
             mbar_init(&ctl.item_full[s], 1);
             mbar_init(&ctl.item_empty[s], C::READERS);
@@ -308,10 +311,11 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
                 }
                 g += np;
             }
-        } else if (warp <= TILES) {
-            // ---------------- products of a tile: S of a step, then P V of the one before.  A warp a tile: it waits
-            // while its products are at work, and its own waits and commits cost as much again.
-            const int t = warp - 1;
+        } else if (warp <= 2) {
+            // ---------------- products: a warp for the scores and one for P V, or, of two tiles, a warp a tile for both, S
+            // of a step, then P V of the one before
+            const int t = C::SPLIT ? 0 : warp - 1;
+            const bool scores = !C::SPLIT || warp == 1, products = !C::SPLIT || warp == 2;
             const uint32_t tile = tmem_base + t * C::TMEM_COLS;
             const uint64_t dq0 = smem_desc_sw128(smem_u32(smem + t * C::Q_BYTES), 16, 1024);
             const uint64_t dk0 = smem_desc_sw128(smem_u32(smem + C::OFF_K), 16, 1024);
@@ -338,8 +342,10 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
             auto score = [&](uint64_t dq, int g, uint64_t* q_free) {   // q_free: Q's place is free after it
                 const int s = g % C::KST;
                 if (!mbar_wait_warp(&ctl.k_full[s], (g / C::KST) & 1, wc)) return false;
-                if (ns >= 1 && !mbar_wait_warp(&ctl.sc_free[t], (ns - 1) & 1, wc)) return false;
+                const int buf = ns % C::NS;
+                if (ns >= C::NS && !mbar_wait_warp(&ctl.sc_free[t][buf], (ns / C::NS - 1) & 1, wc)) return false;
                 ++ns;
+                const uint32_t to = tile + C::TMEM_S + buf * kBN;
                 tc_fence_after();
                 if (elect_one()) {
                     const uint64_t dk = dk0 + static_cast<uint64_t>((s * C::KV_BYTES) >> 4);
@@ -348,12 +354,12 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
                         const uint32_t off_q = (k >> 2) * (kBM * 128) + (k & 3) * 32;
                         const uint32_t off_k = (k >> 2) * (kBN * 128) + (k & 3) * 32;
                         if (C::QT && k < 4)
-                            umma_bf16_ta(tile + C::TMEM_S, tile + C::TMEM_Q + k * 8, dk + (off_k >> 4), C::IDESC_S, k > 0);
+                            umma_bf16_ta(to, tile + C::TMEM_Q + k * 8, dk + (off_k >> 4), C::IDESC_S, k > 0);
                         else
-                            umma_bf16(tile + C::TMEM_S, dq + (off_q >> 4), dk + (off_k >> 4), C::IDESC_S, k > 0);
+                            umma_bf16(to, dq + (off_q >> 4), dk + (off_k >> 4), C::IDESC_S, k > 0);
                     }
                     umma_commit(&ctl.k_empty[s]);
-                    umma_commit(&ctl.sc_full[t]);
+                    umma_commit(&ctl.sc_full[t][buf]);
                     if (q_free != nullptr) umma_commit(q_free);
                 }
                 __syncwarp();
@@ -367,7 +373,7 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
                 const int qs = r % C::QST;
                 const uint64_t dq = dq0 + static_cast<uint64_t>((qs * TILES * C::Q_BYTES) >> 4);
                 uint64_t* const q_free = &ctl.q_empty[qs];
-                if (t * R >= x.ntok) {   // nothing to do but to let all go, once it is there: arrivals of these phases
+                if (!C::SPLIT && t * R >= x.ntok) {   // nothing to do but to let all go, once it is there: arrivals of these phases
                     ok = mbar_wait_warp(&ctl.q_full[qs], (r / C::QST) & 1, wc);
                     if (ok && lane == 0) mbar_arrive(q_free);
                     for (int m = x.blk0; ok && m < x.blk1; ++m, ++g) {
@@ -381,10 +387,10 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
                     continue;
                 }
                 const int np_item = x.blk1 - x.blk0;
-                ok = mbar_wait_warp(&ctl.q_ready[t], nq++ & 1, wc) && score(dq, g, np_item == 1 ? q_free : nullptr);
+                if (scores) ok = mbar_wait_warp(&ctl.q_ready[t], nq++ & 1, wc) && score(dq, g, np_item == 1 ? q_free : nullptr);
                 for (int i = 0; ok && i < np_item; ++i, ++g) {
-                    if (i + 1 < np_item) ok = score(dq, g + 1, i + 2 == np_item ? q_free : nullptr);
-                    ok = ok && product(g, i == 0);
+                    if (scores && i + 1 < np_item) ok = score(dq, g + 1, i + 2 == np_item ? q_free : nullptr);
+                    if (products) ok = ok && product(g, i == 0);
                 }
             }
             if (elect_one()) {
@@ -482,7 +488,8 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
                 // last key column of the page that this row sees (< 0: none).  Rows of no token are never read: they
                 // go unmasked.
                 const int lim = valid ? min(NK - 1, pos - m * kBN) : NK - 1;
-                if (!mbar_wait_warp(&ctl.sc_full[tile], gt & 1, wc)) { ok = false; break; }
+                const int buf = gt % C::NS;
+                if (!mbar_wait_warp(&ctl.sc_full[tile][buf], (gt / C::NS) & 1, wc)) { ok = false; break; }
                 const float4 sc = ctl.scale[g % C::SCALES];
                 if (m == x.blk0) {
                     v_log = sc.y;
@@ -491,7 +498,7 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
                 // P is free, and O another product's no more, once the product before has read and written them
                 auto product_done = [&] { return gt == 0 || mbar_wait_warp(&ctl.pv_done[tile], (gt - 1) & 1, wc); };
                 if (!warp_rows) {
-                    if (lane == 0) mbar_arrive(&ctl.sc_free[tile]);
+                    if (lane == 0) mbar_arrive(&ctl.sc_free[tile][buf]);
                     if (!product_done()) { ok = false; break; }
                     if (lane == 0) mbar_arrive(&ctl.p_full[tile]);
                     __syncwarp();
@@ -502,14 +509,14 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
                 {
                     uint32_t u[NK / 32][32];
 #pragma unroll
-                    for (int c = 0; c < NK / 32; ++c) tmem_ld32(lane_addr + C::TMEM_S + c * 32, u[c]);
+                    for (int c = 0; c < NK / 32; ++c) tmem_ld32(lane_addr + C::TMEM_S + buf * kBN + c * 32, u[c]);
                     tmem_wait_ld();
 #pragma unroll
                     for (int k = 0; k < NK; ++k) xs[k] = __uint_as_float(u[k / 32][k % 32]);
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&ctl.sc_free[tile]);
+                if (lane == 0) mbar_arrive(&ctl.sc_free[tile][buf]);
                 if (m * kBN + NK - 1 > x.pos0 + tile * R) {   // some row does not see all of it
 #pragma unroll
                     for (int k = 0; k < NK; ++k) xs[k] = k <= lim ? xs[k] : -CUDART_INF_F;
