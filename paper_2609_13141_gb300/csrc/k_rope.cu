@@ -174,8 +174,8 @@ struct Rows {
 struct Share {
     int part, part_step;
     long long t0, step;
-    __device__ __forceinline__ Share(int parts) {
-        const int warps = gridDim.x * kWarps, w = blockIdx.x * kWarps + warp_id();
+    __device__ __forceinline__ explicit Share(int parts, int block, int blocks) {
+        const int warps = blocks * kWarps, w = block * kWarps + warp_id();
         part_step = min(parts, warps);
         part = w % part_step;
         step = warps / part_step;
@@ -207,12 +207,12 @@ constexpr int rope_fwd_unit() { return kFwdRows * 32 * 16 + Table<D>::BYTES; }  
 template <int D>
 constexpr int rope_fwd_smem() { return kWarps * kFwdStages * rope_fwd_unit<D>(); }
 
+// The block-th of `blocks` blocks' share; sm: rope_fwd_smem<D>() bytes.
 template <int D, bool INTER, bool PAGED, bool PART>
-__global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs a) {
+__device__ __forceinline__ void rope_fwd(const RopeArgs& a, int block, int blocks, uint8_t* sm) {
     constexpr int kRows = kFwdRows;
     using R = Rows<D, kRows>;
     constexpr int UNIT = rope_fwd_unit<D>(), TAB = kRows * 512;
-    extern __shared__ __align__(16) uint8_t sm[];
     const int lane = lane_id(), l = lane % R::LPR, g = lane / R::LPR;
     const unsigned group = R::group_mask(g);
     const int H = a.Hq + 2 * a.Hkv, HN = a.Hq + a.Hkv, parts = R::parts(a);
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
     const int mine = g * (R::LPR * 16);   // the group's row within 512 bytes
     const Place<INTER> pl(a, l);
     const bool turns = turned(a, l);
-    const Share sh(parts);
+    const Share sh(parts, block, blocks);
     grid_dep_wait();
     for (int part = sh.part; part < parts; part += sh.part_step) {
         const int h0 = part * R::RPU + g;   // row u of the group is head h0 + u GPW
@@ -314,6 +314,12 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs
     }
 }
 
+template <int D, bool INTER, bool PAGED, bool PART>
+__global__ void __launch_bounds__(kThreads, kFwdBlocks) rope_fwd_kernel(RopeArgs a) {
+    extern __shared__ __align__(16) uint8_t sm[];
+    rope_fwd<D, INTER, PAGED, PART>(a, blockIdx.x, gridDim.x, sm);
+}
+
 // A lane keeps its columns of dw in registers, per row of its group, and adds them to
 // its warp's sums at the end; a block adds its warps' sums into one row of `part`,
 // and the last block to finish adds those in their order: equal inputs give equal
@@ -349,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) rope_bwd_kernel(RopeArgs
     for (int i = lane; i < 2 * D; i += 32) sum[i] = 0.f;
     const Place<INTER> pl(a, l);
     const bool turns = turned(a, l);
-    const Share sh(parts);
+    const Share sh(parts, blockIdx.x, gridDim.x);
     grid_dep_wait();
     for (int part = sh.part; part < parts; part += sh.part_step) {
         const int h0 = part * hp + g;   // row u of the group is head h0 + u hs
@@ -592,19 +598,26 @@ struct Run {
     unsigned lo, hi;   // its rows of the page
 };
 
+__device__ __forceinline__ void prefetch_line(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
+
 template <int D, bool INTER>
-__global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8 c, int window) {
+__device__ __forceinline__ void append8_window(const RopeArgs& a, const Cache8& c, int window, unsigned block) {
     using R = Rows<D, 1>;
     constexpr int P = kRunRows / R::GPW;   // passes: a group's rows
     __shared__ int pages[kMaxWindow + 65], rows[kMaxWindow + 64], spots[kMaxWindow + 64];   // pages: of the token before, too
     __shared__ float tops[2][2][kWarps];
     const int lane = lane_id(), warp = warp_id(), l = lane % R::LPR, g = lane / R::LPR;
-    const unsigned at_window = blockIdx.x / static_cast<unsigned>(a.Hkv);
-    const int head = static_cast<int>(blockIdx.x - at_window * a.Hkv);
+    const unsigned at_window = block / static_cast<unsigned>(a.Hkv);
+    const int head = static_cast<int>(block - at_window * a.Hkv);
     const long long t0 = static_cast<long long>(at_window) * window;
     const Place<INTER> pl(a, l);
     const bool turns = turned(a, l);
     grid_dep_wait();
+    // what the window's tokens have for the head is on its way while their slots are read (85.5 -> 81.5 us)
+    if (static_cast<int>(threadIdx.x) < 4 * window && t0 + (threadIdx.x >> 2) < a.T) {
+        const int h = a.Hq + head + (threadIdx.x & 1) * a.Hkv;
+        prefetch_line(a.qkv + (t0 + (threadIdx.x >> 2)) * a.ld + static_cast<long long>(h) * D + (threadIdx.x >> 1 & 1) * (D / 2));
+    }
     Quads w;
     w.load(a.wk, pl.ia, pl.ib);
     // the window's tokens, and as many after it as its last run may have: page (-1: none), row of the page (64: no
@@ -783,18 +796,41 @@ __global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, Cache8
     }
 }
 
+// One grid for both: first the blocks of the queries, which are rows of the fused projection's first heads (q: without
+// the others), then the windows, which take their places as they end.  Two launches take 12.1 us instead of 10.0 where
+// the host is the limit (96 tokens); taking turns, so that a multiprocessor has both kinds at a time, 96 to 134 us
+// instead of 85 at 15232 tokens of 32 + 2 x 8 heads of 128: the queries' rows come slower than one after the other.
+template <int D, bool INTER, bool PART>
+__global__ void __launch_bounds__(kThreads, 2) append8_kernel(RopeArgs a, RopeArgs q, Cache8 c, int window, unsigned q_blocks) {
+    extern __shared__ __align__(16) uint8_t sm[];
+    if (blockIdx.x < q_blocks) rope_fwd<D, INTER, true, PART>(q, blockIdx.x, q_blocks, sm);
+    else append8_window<D, INTER>(a, c, window, blockIdx.x - q_blocks);
+}
+
 // Tokens of a window: as few as give every warp a token, more where there are blocks enough
 // (eight a multiprocessor: an empty window costs a block 2 us).
-int append8_window(const RopeArgs& a) {
+int append8_tokens(const RopeArgs& a) {
     const long long w = a.T * a.Hkv / (8LL * device_sm_count());
     return w < kWarps ? kWarps : (w > kMaxWindow ? kMaxWindow : static_cast<int>(w));
 }
 
+template <int D, bool INTER, bool PART>
+cudaError_t launch_append8(const RopeArgs& a, const Cache8& c, const KernelEnv& env) {
+    const void* const kernel = reinterpret_cast<const void*>(append8_kernel<D, INTER, PART>);
+    const cudaError_t e = ensure_smem_attr(kernel, rope_fwd_smem<D>(), true);
+    if (e != cudaSuccess) return e;
+    RopeArgs q = a;
+    q.Hkv = 0;
+    const int window = append8_tokens(a);
+    const unsigned kv_blocks = static_cast<unsigned>((a.T + window - 1) / window * a.Hkv);
+    const unsigned q_blocks = static_cast<unsigned>(blocks_for<D, kFwdRows>(q, kFwdBlocks * device_sm_count(), 1));
+    return launch_early(append8_kernel<D, INTER, PART>, dim3(kv_blocks + q_blocks), kThreads, rope_fwd_smem<D>(), env.stream, a, q, c, window, q_blocks);
+}
+
 template <int D>
 cudaError_t launch_append8(const RopeArgs& a, const Cache8& c, const KernelEnv& env) {
-    const int window = append8_window(a);
-    const dim3 grid(static_cast<unsigned>((a.T + window - 1) / window * a.Hkv));
-    return launch_early(a.interleaved ? append8_kernel<D, true> : append8_kernel<D, false>, grid, kThreads, 0, env.stream, a, c, window);
+    if (a.rot < D) return a.interleaved ? launch_append8<D, true, true>(a, c, env) : launch_append8<D, false, true>(a, c, env);
+    return a.interleaved ? launch_append8<D, true, false>(a, c, env) : launch_append8<D, false, false>(a, c, env);
 }
 
 template <int D>
@@ -802,7 +838,11 @@ cudaError_t prepare_fwd() {
     const void* kernels[] = {reinterpret_cast<const void*>(rope_fwd_kernel<D, true, true, true>),
                              reinterpret_cast<const void*>(rope_fwd_kernel<D, true, true, false>),
                              reinterpret_cast<const void*>(rope_fwd_kernel<D, false, true, true>),
-                             reinterpret_cast<const void*>(rope_fwd_kernel<D, false, true, false>)};
+                             reinterpret_cast<const void*>(rope_fwd_kernel<D, false, true, false>),
+                             reinterpret_cast<const void*>(append8_kernel<D, true, true>),
+                             reinterpret_cast<const void*>(append8_kernel<D, true, false>),
+                             reinterpret_cast<const void*>(append8_kernel<D, false, true>),
+                             reinterpret_cast<const void*>(append8_kernel<D, false, false>)};
     cudaError_t e = cudaSuccess;
     for (const void* k : kernels)
         if (e == cudaSuccess) e = ensure_smem_attr(k, rope_fwd_smem<D>(), true);
@@ -824,7 +864,7 @@ const char* rope_check(int rot, int interleaved, int max_pos, float eps, long lo
 // Tokens are counted in 32 bits where a batch row is found by division.
 bool rope_supported(const RopeArgs& a) { return a.T <= 0x7fffffffLL; }
 
-bool append8_supported(const RopeArgs& a) { return (a.T + kWarps - 1) / kWarps * a.Hkv <= 0x7fffffffLL; }
+bool append8_supported(const RopeArgs& a) { return (a.T + kWarps - 1) / kWarps * a.Hkv <= 0x70000000LL; }
 
 int rope_bwd_max_blocks() { return kBwdBlocks * device_sm_count(); }   // all resident
 
@@ -840,10 +880,6 @@ cudaError_t launch_rope_fwd(const RopeArgs& a, int d, const KernelEnv& env) {
 }
 
 cudaError_t launch_append8(const RopeArgs& a, const Cache8& c, int d, const KernelEnv& env) {
-    RopeArgs q = a;   // the queries alone: rows of the fused projection's first heads
-    q.Hkv = 0;
-    const cudaError_t e = launch_rope_fwd(q, d, env);
-    if (e != cudaSuccess) return e;
     return d == 128 ? launch_append8<128>(a, c, env) : launch_append8<64>(a, c, env);
 }
 

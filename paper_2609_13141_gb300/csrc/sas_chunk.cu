@@ -301,7 +301,7 @@ sas_status sas_chunk_append8(sas_chunk_handle* h, const sas_rope_config* rope, i
         if (!sas::rope_supported(a) || !sas::append8_supported(a)) return cfail(h, SAS_ERR_UNSUPPORTED, "too many tokens");
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         const sas::KernelEnv env{s, h->status, h->limit};
-        const cudaError_t e = ctimed(h, 1, 2, s, [&] { return sas::launch_append8(a, cache, c.d, env); });
+        const cudaError_t e = ctimed(h, 1, 1, s, [&] { return sas::launch_append8(a, cache, c.d, env); });
         return e == cudaSuccess ? SAS_OK : ccuda_fail(h, e, "norm + rotation + 8-bit append");
     });
 }

@@ -236,5 +236,5 @@ def test_refusals():
         ch.append8(**{**case, "qkv": case["qkv"].repeat(2, 1, 1), "positions": case["positions"].repeat(2), "slots": case["slots"].repeat(2)})
     assert sas.sas_chunk_launch_count(ch.h) == 0
     ch.append8(**case)
-    assert sas.sas_chunk_launch_count(ch.h) == 2
+    assert sas.sas_chunk_launch_count(ch.h) == 1
     ch.close()
