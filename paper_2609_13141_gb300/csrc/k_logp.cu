@@ -10,17 +10,22 @@
 //
 // Bound: HBM, a read of the logits (and a write of as much for the gradient); the
 // exponential unit and the arithmetic take about half of that time.  So: 16-byte loads, four a
-// thread in flight, a row a block, or a warp where rows are short, and where there are fewer
-// rows than places for blocks a row in several parts, whose last block to end joins them.
+// thread in flight and two rounds more on their way into L2, a row a block, or a warp where rows
+// are short, and where there are fewer rows than places for blocks a row in several parts, whose
+// last block to end joins them.  8192 bf16 rows of 151936: 348 us, 7.2 TB/s (without the rounds
+// ahead 371), their gradient 739 us.
 //
 // The likeliest columns come along in the same pass: a column is a candidate while its key
 // (order of the value, then of the index) is above a bar that k columns reach.  The bar is the
-// k-th largest of the threads' maxima so far, taken after rounds 1, 2, 4, ..., so that about k
-// columns pass it from one of these to the next.  Each warp keeps its candidates in shared memory
-// (a block's warps need not wait for one another: a maximum that has moved on since it was read
-// only makes the bar too low), its lanes look together at the columns of a lane whose maximum
-// passes, and cuts them down to the best k where they are many.  A bar from the first columns
-// alone, and each lane at its own columns: 122 us for 640 rows of 151936 and 20 columns.
+// k-th largest of the threads' maxima so far, taken in rounds 0, 2, 8, 26, ...: about 2 k columns
+// pass it from one of these to the next.  (A bar takes a warp 150 instructions, a candidate 100:
+// rounds 0, 1, 3, 7, ... are slower for few columns, 435 against 417 us at 8192 rows of 151936 and
+// one column, and faster for many, 542 against 557 with 20.)  Each warp keeps its candidates in
+// shared memory (a block's warps need not wait for one another: a maximum that has moved on since
+// it was read only makes the bar too low), its lanes look together at the columns of a lane whose
+// maximum passes, and cuts them down to the best k where they are many.  What bounds it then is
+// the instructions: 640 rows of 151936 take 38.5 us alone, 49 with one column and 64 with 20.  A
+// bar from the first columns alone, and each lane at its own columns, took 122 us.
 #include <cmath>
 
 #include <math_constants.h>
@@ -34,9 +39,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBlocks = 4;            // a multiprocessor, as many as their registers allow
 constexpr int kMaxParts = 32;         // of a row: a lane each at the join
+constexpr int kAhead = 3;             // rounds of a block's from its loads to its farthest prefetch (2 or 4: within 2%, 6 slower)
+constexpr int kBarStep = 3;           // from a bar's round to the next one's
 constexpr int kWaves = 2;             // of blocks, where rows come in parts (640 rows of 32000: 13 us, with four waves 26)
-constexpr int kMinPart = 4096;        // columns
-constexpr int kSmallRow = 4096;       // columns of rows that a warp takes
+constexpr int kMinPart = 4096;        // columns: a round of fp32
+// Columns of rows that a warp takes, for the gradient: 16384 bf16 rows of 4096 take 46 us by warps and 60 by blocks,
+// of 16384 182 and 171, 152 rows of 16384 19 and 9.
+constexpr int kSmallRow = 4096;
 constexpr int kStatusBadInput = 1;    // == SAS_ERR_INVALID_ARG
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.69314718055994531f;
@@ -67,6 +76,7 @@ struct Vec<bf16> {
     __device__ __forceinline__ static uint4 pack(const float* f) {
         return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
     }
+    __device__ __forceinline__ static uint4 nothing() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
     // The largest number, NaN passed over (-infinity if there is no other).
     __device__ __forceinline__ static uint32_t max2(uint32_t a, uint32_t b) {
         uint32_t d;
@@ -95,6 +105,7 @@ struct Vec<float> {
     __device__ __forceinline__ static uint4 pack(const float* f) {
         return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
     }
+    __device__ __forceinline__ static uint4 nothing() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
     template <int U>
     __device__ __forceinline__ static float top(const uint4 (&u)[U]) {
         float m = -CUDART_INF_F;
@@ -160,7 +171,7 @@ __device__ __forceinline__ Sums shfl_xor(const Sums& x, int o) {
 // The same in every lane: which of two joined sums is the left one must not matter, so both
 // lanes of a pair add them in lane order.
 template <int LANES = 32>
-__device__ __forceinline__ Sums warp_join(Sums x) {   // of the first LANES
+__device__ __forceinline__ Sums warp_join(Sums x) {   // of every LANES neighbours
 #pragma unroll
     for (int o = 1; o < LANES; o <<= 1) {
         const Sums y = shfl_xor(x, o);
@@ -186,7 +197,7 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
 }
 __device__ __forceinline__ int key_index(unsigned long long k) { return static_cast<int>(0xffffffffu - static_cast<uint32_t>(k)); }
 
-constexpr int kMaxTop = 32;
+constexpr int kMaxTop = 32;    // a warp's lanes put them out
 constexpr int kCand = 128;     // candidates of a warp
 constexpr int kCut = 64;       // cut down at the end of a round that leaves this many
 constexpr int kJoin = 512;     // candidates that the block joins at a time
@@ -227,6 +238,10 @@ __device__ __forceinline__ int cut(unsigned long long* key, unsigned long long* 
     return n;
 }
 
+__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
+
 // What a row gives, by one thread.
 __device__ __forceinline__ void put_row(const LogpArgs& a, int row, const Sums& x, float zx) {
     const float ll = logf(x.l);
@@ -241,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
     using V = Vec<E>;
     constexpr int N = V::N, U = V::UNROLL, ROUND = TEAM * U, TEAMS = kThreads / TEAM;
     static_assert(N * U <= 32, "a thread's columns of a round, a lane each");
-    static_assert(kMaxTop + 32 <= kCut && kCut + 32 <= kCand, "room for a lane's columns after a cut");
+    static_assert(kMaxTop < kCut && kCut + 32 <= kCand, "room for a lane's columns");
     __shared__ Cand cands[TOP ? kThreads / 32 : 1];
     __shared__ unsigned long long all[TOP && TEAM == kThreads ? kJoin : 1], all_top[kMaxTop];
     __shared__ uint4 seen[TOP ? U * kThreads : 1];
@@ -285,7 +300,43 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
     const int late = rounds * ROUND + head, others = sp.count - late + head;   // where they begin, how many
     const int all_rounds = rounds + (others + ROUND - 1) / ROUND;
     const E* from = z + sp.column(head + rank);
+    // whole rounds, on their way into L2
+    auto prefetch = [&](int r) {
+        if (TEAM == kThreads && rank == 0 && r < rounds) prefetch_l2(z + sp.column(head) + static_cast<size_t>(r) * (ROUND * N), ROUND * 16);
+    };
+    for (int r = 1; r < kAhead; ++r) prefetch(r);
+    // The bar: the k-th largest of the maxima of four threads each (k columns are no smaller), down to the upper 16 bits of its order: the
+    // largest such number that k of them reach.
+    auto put_max = [&] {   // of a block
+        float v = fmaxf(t.m, __shfl_xor_sync(0xffffffffu, t.m, 1));
+        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+        if (rank % 4 == 0) tops[rank / 4] = v;
+    };
+    auto raise_bar = [&] {
+        constexpr int M = TEAM == 32 ? 1 : kGroups / 32;
+        uint32_t o[M], low = 0xffffffffu, high = 0;
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            o[i] = order_of(TEAM == 32 ? t.m : *static_cast<volatile float*>(&tops[i * 32 + lane_id()]));
+            low = min(low, o[i]);
+            high = max(high, o[i]);
+        }
+        low = __reduce_min_sync(0xffffffffu, low);
+        high = __reduce_max_sync(0xffffffffu, high);
+        uint32_t bit = 0x80000000u >> __clz((low ^ high) | 1u);   // the first that is not the same in all
+        uint32_t at = high & ~(2 * bit - 1) & 0xffff0000u;
+#pragma unroll 1
+        for (; bit >= 0x10000u; bit >>= 1) {
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < M; ++i) n += o[i] >= (at | bit);
+            if (__reduce_add_sync(0xffffffffu, n) >= a.k) at |= bit;
+        }
+        if (at > order_of(-CUDART_INF_F)) bar_value = fmaxf(bar_value, value_of(at));
+    };
+    int next_bar = 0;
     for (int round = 0; round < all_rounds; ++round) {
+        prefetch(round + kAhead);
         // this thread's u-th vector
         auto vector = [&](int u, int rank) {
             const int q = (round < rounds ? round : round - rounds) * ROUND + u * TEAM + rank;
@@ -300,12 +351,14 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int j = vector(u, rank), v = sp.column(j);
-                if (j < sp.count && sp.whole(j)) {
+                raw[u] = V::nothing();
+                if (j >= sp.count) continue;
+                if (sp.whole(j)) {
                     raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + v));
                 } else {   // columns of the row alone, -infinity for the others
                     float f[N];
 #pragma unroll
-                    for (int e = 0; e < N; ++e) f[e] = j < sp.count && v + e >= sp.v0 && v + e < sp.v1 ? V::one(z + v + e) : -CUDART_INF_F;
+                    for (int e = 0; e < N; ++e) f[e] = v + e >= sp.v0 && v + e < sp.v1 ? V::one(z + v + e) : -CUDART_INF_F;
                     raw[u] = V::pack(f);
                 }
             }
@@ -313,8 +366,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
         const float top = V::top(raw);
         if (top > t.m) t.move(top);
         const float m = t.m == -CUDART_INF_F ? 0.f : t.m;
-        float l, s;
-        {
+        float l = 0.f, s = CUDART_NAN_F;
+        if (round < rounds) {
             const uint64_t scale2 = f32x2(kLog2e, kLog2e), off2 = f32x2(-m, -m);
             uint64_t l2[2] = {0, 0}, s2[2] = {0, 0};
 #pragma unroll
@@ -341,6 +394,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
             l = s = 0.f;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (vector(u, rank - static_cast<int>(lane_id())) >= sp.count) continue;   // none of the warp's
                 float f[N];
                 V::unpack(raw[u], f);
 #pragma unroll
@@ -355,31 +409,14 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
         t.l += l;
         t.s += s;
         if constexpr (TOP) {
-            if ((round & (round - 1)) == 0) {
-                // The k-th largest of the maxima (k columns are no smaller), down to the upper 16 bits of its order:
-                // the largest such number that k of them reach.
-                constexpr int M = TEAM == 32 ? 1 : kGroups / 32;
-                uint32_t o[M];
+            if (round == next_bar) {
+                next_bar = kBarStep * next_bar + kBarStep - 1;
                 if constexpr (TEAM == kThreads) {
-                    float v = fmaxf(t.m, __shfl_xor_sync(0xffffffffu, t.m, 1));
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
-                    if (rank % 4 == 0) tops[rank / 4] = v;
+                    put_max();
                     if (round == 0) __syncthreads();
                     else __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < M; ++i) o[i] = order_of(*static_cast<volatile float*>(&tops[i * 32 + lane_id()]));
-                } else {
-                    o[0] = order_of(t.m);
                 }
-                uint32_t at = 0;
-#pragma unroll 1
-                for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
-                    int n = 0;
-#pragma unroll
-                    for (int i = 0; i < M; ++i) n += o[i] >= (at | bit);
-                    if (__reduce_add_sync(0xffffffffu, n) >= a.k) at |= bit;
-                }
-                if (at > order_of(-CUDART_INF_F)) bar_value = fmaxf(bar_value, value_of(at));
+                raise_bar();
             }
             unsigned pass = __ballot_sync(0xffffffffu, top >= bar_value);   // lanes with a candidate, maybe
             if (pass != 0) {
@@ -388,29 +425,27 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
                     for (int u = 0; u < U; ++u) seen[u * kThreads + threadIdx.x] = raw[u];
                 }
                 __syncwarp();
+                const int i = lane_id(), u = i / N, e = i % N;   // a lane's N U columns, one of them each
+                const E* const column = reinterpret_cast<const E*>(seen + (u < U ? u : 0) * kThreads + threadIdx.x - i) + e;
+#pragma unroll 1
                 for (; pass != 0; pass &= pass - 1) {
-                    // a lane's N U columns, one of them each
-                    const int at = __ffs(pass) - 1, i = lane_id(), u = i / N;
-                    const int j = vector(u, rank - i + at), v = sp.column(j) + i % N;
-                    const bool there = u < U && j < sp.count && v >= sp.v0 && v < sp.v1;
-                    const float f = there ? V::one(reinterpret_cast<const E*>(seen + u * kThreads + threadIdx.x - i + at) + i % N) : 0.f;
-                    const unsigned long long key = key_of(f, v);
-                    auto candidate = [&] { return there && f >= bar_value && key > bar; };
-                    auto raise = [&] {
+                    const int at = __ffs(pass) - 1;
+                    const float f = u < U ? V::one(column + at * N) : CUDART_NAN_F;
+                    unsigned who = __ballot_sync(0xffffffffu, f >= bar_value);
+                    if (who == 0) continue;   // it has moved
+                    const int j = vector(u, rank - i + at), v = sp.column(j) + e;
+                    if (bar != 0 || bar_value == -CUDART_INF_F)   // (what is no column has come as -infinity)
+                        who = __ballot_sync(0xffffffffu, f >= bar_value && key_of(f, v) > bar && j < sp.count && v >= sp.v0 && v < sp.v1);
+                    if (who >> i & 1u) c.key[held + __popc(who & ((1u << i) - 1))] = key_of(f, v);
+                    held += __popc(who);
+                    if (held >= kCut) {
                         __syncwarp();
                         held = cut<32>(c.key, c.top, held, a.k);
-                        if (held < a.k) return;
-                        bar = c.key[a.k - 1];
-                        bar_value = fmaxf(bar_value, key_value(bar));
-                    };
-                    unsigned who = __ballot_sync(0xffffffffu, candidate());
-                    if (held + __popc(who) > kCand) {
-                        raise();
-                        who = __ballot_sync(0xffffffffu, candidate());
+                        if (held == a.k) {
+                            bar = c.key[a.k - 1];
+                            bar_value = fmaxf(bar_value, key_value(bar));
+                        }
                     }
-                    if (who >> i & 1u) c.key[held + __popc(who & ((1u << i) - 1))] = key;
-                    held += __popc(who);
-                    if (held >= kCut) raise();
                 }
                 __syncwarp();   // before other columns are put there
             }
@@ -420,14 +455,28 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
     if constexpr (TEAM == kThreads) {
         if (lane_id() == 0) joined[warp_id()] = make_float3(t.m, t.l, t.s);
         __syncthreads();
-        t = Sums();
-        if (lane_id() < kThreads / 32) t = Sums(joined[lane_id()].x, joined[lane_id()].y, joined[lane_id()].z);
-        t = warp_join<kThreads / 32>(t);
+        if (warp_id() == 0) {   // whose alone are a row's and a part's results
+            const float3 q = joined[lane_id() % (kThreads / 32)];   // in every lane: each may put out a column
+            t = warp_join<kThreads / 32>(Sums(q.x, q.y, q.z));
+        }
     }
     unsigned long long* best = c.key;   // the best k, and how many of them are columns
     if constexpr (TOP) {
         __syncwarp();
-        held = cut<32>(c.key, c.top, held, a.k);
+        if constexpr (TEAM == kThreads) {   // what is still above the bar, most often a few
+            int kept = 0;
+            for (int i0 = 0; i0 < held; i0 += 32) {
+                const int i = i0 + static_cast<int>(lane_id());
+                const unsigned long long key = i < held ? c.key[i] : 0ull;
+                const bool stays = i < held && key_value(key) >= bar_value;
+                const unsigned who = __ballot_sync(0xffffffffu, stays);
+                if (stays) c.key[kept + __popc(who & ((1u << lane_id()) - 1))] = key;
+                kept += __popc(who);
+                __syncwarp();
+            }
+            held = kept;
+        }
+        if (TEAM == 32 || held > a.k) held = cut<32>(c.key, c.top, held, a.k);
         if constexpr (TEAM == kThreads) {
             best = all;
             if (lane_id() == 0) sh_held[warp_id()] = held;
@@ -458,12 +507,14 @@ __global__ void __launch_bounds__(kThreads, kBlocks) logp_kernel(LogpArgs a) {
         __threadfence();
         if (rank == 0) a.count[row] = 0;
         const size_t row0 = static_cast<size_t>(row) * a.parts;
-        t = Sums();
-        if (static_cast<int>(lane_id()) < a.parts) {
-            const float4 q = __ldcg(a.part + row0 + lane_id());
-            t = Sums(q.x, q.y, q.z);
+        if (warp_id() == 0) {
+            t = Sums();
+            if (static_cast<int>(lane_id()) < a.parts) {
+                const float4 q = __ldcg(a.part + row0 + lane_id());
+                t = Sums(q.x, q.y, q.z);
+            }
+            t = warp_join(t);
         }
-        t = warp_join(t);
         if constexpr (TOP) {
             held = 0;
             const int step = (kJoin - kMaxTop) / kMaxTop;   // parts whose candidates fit beside the best so far
@@ -565,9 +616,31 @@ void split_rows(int rows, int V, int places, int& parts, int& chunk) {
     parts = (V + chunk - 1) / chunk;
 }
 
+// Whether a warp takes a row.  A block's row costs 3 us whatever its length, a warp's waits for one load after the
+// other, and for its k columns more than all.  By a warp and by a block, us (k columns of bf16 rows):
+//                          columns 1024       4096         8192         16384        32000
+//   608 rows    k = 0        8.0, 8.2    7.8, 7.6    7.6, 12.8   11.3, 12.5   27.8, 16.8
+//               k = 5       10.8, 9.6   11.9, 9.0   17.2, 21.3   24.3, 20.3   42.8, 26.0
+//               k = 20      9.3, 10.9  23.4, 10.4   32.9, 23.4   46.6, 22.8   72.2, 30.8
+//   2432 rows   k = 0       7.4, 13.4   9.9, 15.9   10.6, 15.7   17.4, 21.5   33.3, 34.2
+//               k = 5       8.6, 26.6  13.5, 26.8   20.9, 26.5   31.6, 35.1   50.6, 53.7
+//               k = 20     10.4, 33.8  27.7, 31.7   40.7, 31.3   57.7, 43.8   82.7, 65.1
+//   4864 rows   k = 0       7.9, 24.4   8.7, 29.9   14.2, 30.7   25.5, 39.6   48.0, 63.2
+//               k = 5       9.3, 50.2  18.9, 51.2   29.8, 51.1   42.3, 64.9   70.5, 100
+//               k = 20     15.7, 64.1  42.9, 60.4   62.1, 60.4   87.9, 81.5    125, 123
+//   16384 rows  k = 0      12.1, 77.3  27.6, 97.3   47.2, 93.8  89.9, 123.7   165, 203
+//               k = 5      25.3, 162   55.2, 167    84.9, 161    130, 206     221, 321
+//               k = 20     46.0, 205    128, 196     189, 190    267, 259     382, 393
+// and for 2432 rows of 65536 without any 62, 56.  (Not by k: a row's numbers are the same with and without
+// alternatives.)
+bool row_by_warp(const LogpArgs& a) {
+    const int per_sm = a.rows / device_sm_count();
+    return a.V <= (per_sm >= 32 ? 32768 : per_sm >= 16 ? 4096 : 1024);
+}
+
 template <class E>
 cudaError_t launch_fwd(LogpArgs a, const KernelEnv& env) {
-    const bool small = a.V <= kSmallRow;
+    const bool small = row_by_warp(a);
     a.parts = 1;
     a.chunk = a.V;
     if (!small) split_rows(a.rows, a.V, logp_max_splits(), a.parts, a.chunk);

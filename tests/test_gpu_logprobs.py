@@ -92,6 +92,27 @@ def test_rows(T, V, pad, shift, dtype):
     assert again is s and all(torch.equal(a, b) for a, b in zip(again, ch.logprobs(z, tokens, k)))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("per_sm,V", [(16, 4095), (16, 4097), (32, 4500), (32, 20011), (32, 32769)])
+def test_many_rows(per_sm, V, dtype):
+    # so many that a warp takes each, up to a length; hard rows among them
+    T = per_sm * torch.cuda.get_device_properties(0).multi_processor_count + 3
+    z, tokens = _logits(T, V, dtype, T + V, pad=3)
+    z[0], z[2], z[3] = 0.25, -math.inf, torch.arange(V, device=DEV) % 5
+    z[2, V - 1] = 1.0
+    z[4, 7:V - 4] = math.nan
+    z[5, : V - 3] = -math.inf
+    tokens[1] = -1
+    s = _chunk(T).logprobs(z, tokens, 32)
+    r = _layer().token_logprobs(z, tokens)
+    assert all(torch.equal(a, b) or torch.equal(a.isnan(), b.isnan()) and torch.equal(a[~a.isnan()], b[~b.isnan()]) for a, b in zip(r[:3], s[:3]))
+    rows = [0, 2, 3, 5, 6, 7, 8, T // 2, T - 2, T - 1]
+    _check_rows(z, tokens, r, rows)
+    _check_top(z, s, 32, rows)
+    few = _chunk(6).logprobs(z[:6], tokens[:6], 32)
+    assert torch.equal(few.top_index, s.top_index[:6])
+
+
 @pytest.mark.parametrize("V", [40, 500, 4500, 40000])
 @pytest.mark.parametrize("k", [1, 2, 31, 32])
 def test_alternatives_of_hard_rows(V, k):
