@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
                 const uint64_t dq = dq0 + static_cast<uint64_t>((qs * TILES * C::Q_BYTES) >> 4);
                 uint64_t* const q_free = &ctl.q_empty[qs];
                 if (!C::SPLIT && t * R >= x.ntok) {   // nothing to do but to let all go, once it is there: arrivals of these phases
-                    ok = mbar_wait_warp(&ctl.q_full[qs], (r / C::QST) & 1, wc);
+                    ok = mbar_wait_warp(&ctl.q_ready[t], nq++ & 1, wc);
                     if (ok && lane == 0) mbar_arrive(q_free);
                     for (int m = x.blk0; ok && m < x.blk1; ++m, ++g) {
                         const int s = g % C::KST, phase = (g / C::KST) & 1;
@@ -411,11 +411,12 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
         auto warp_has_rows = [&](const Item& x) { return tile * R * a.G + q * 32 < x.ntok * a.G; };
         auto tile_has_rows = [&](const Item& x) { return tile * R < x.ntok; };
         float row_scale = 0.f, next_scale = 0.f;
-        // the r-th item, and its rows as f16, in place; the first 64 dims of 128 into tensor memory (the products
+        // the r-th item, and its rows as f16, in place (a tile without rows waits and arrives all the same: a barrier
+        // that is passed over one phase does not tell the next one); the first 64 dims of 128 into tensor memory (the products
         // of the item before, which read the ones there, are done: this warp has seen their scores)
         auto take_item = [&](int r, Item& x) {
             if (!read_item(ctl, r, wc, x)) return false;
-            if (x.head < 0 || !tile_has_rows(x)) return true;
+            if (x.head < 0) return true;
             const int qs = r % C::QST;
             if (!mbar_wait_warp(&ctl.q_full[qs], (r / C::QST) & 1, wc)) return false;
             if (warp_has_rows(x)) {

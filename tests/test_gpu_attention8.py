@@ -157,6 +157,23 @@ def test_splits_and_mixed_batches(G, Hkv, d, lens):
     _run(lens, G * Hkv, Hkv, d, seed=len(lens))
 
 
+@pytest.mark.parametrize("G,Hkv,lens", [(1, 4, [(9000, 1300)]), (2, 4, [(9000, 2195)]), (4, 8, [(9000, 1500)]), (8, 4, [(5000, 715)]),
+                                        (4, 4, [(3000, 411), (5000, 400), (700, 1), (4000, 285)])])
+def test_last_tiles_of_half_a_pair(G, Hkv, lens):
+    # requests whose last unit fills one of a block's two tiles at most, taken ahead of a split that has both;
+    # what another batch left in the block's memory shows nowhere
+    case, other = (_case(lens, G * Hkv, Hkv, 128, seed=k) for k in (5, 6))
+    ch = _chunk(case)
+    first = None
+    for _ in range(3):
+        ch.attention8(*other)
+        O, LSE = ch.attention8(*case)
+        first = first or (O, LSE)
+        assert torch.equal(O, first[0]) and torch.equal(LSE, first[1])
+    _compare(O, LSE, case, 1 / math.sqrt(128))
+    assert sas.sas_chunk_get_device_status(ch.h) == 0
+
+
 def test_many_sequences():
     rng = np.random.default_rng(7)
     _run([(int(c), int(n)) for c, n in zip(rng.integers(0, 90, 1500), rng.integers(0, 3, 1500))], 2, 1, 64, seed=1)
