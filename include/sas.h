@@ -705,8 +705,8 @@ sas_status sas_chunk_append(sas_chunk_handle* h, const sas_rope_config* rope, in
  * row 0 is written.  Rounding is to nearest; what is not finite has no say in the scale
  * and is stored as NaN.
  * The new tokens of a page must stand next to each other in the batch (as sas_chunk_plan
- * lists them, any order within the page).  Tokens are skipped as in sas_chunk_append.  Two
- * launches. */
+ * lists them, any order within the page).  Tokens are skipped as in sas_chunk_append.  One
+ * launch. */
 sas_status sas_chunk_append8(sas_chunk_handle* h, const sas_rope_config* rope, int32_t T, const void* qkv, int64_t ld,
                              const void* wq, const void* wk, const float* cos, const float* sin,
                              const int32_t* positions, const int64_t* slots, void* Q, void* K_cache, void* V_cache,

@@ -5,23 +5,24 @@
 // j over the tokens of the request up to i, s_K(j) and s_V(j) the scales of j's page.
 //
 // Work is cut as chunk_work.cuh says.  A tile has few rows here (8 or 16: R tokens times the G
-// heads of a KV group), and each of four teams of warps takes whole pages of the item, each warp
-// a share of the keys, with a running maximum, sum and output of its own, which the block joins
-// at the item's end.  A warp alone converts a number in 2.5 times the cycles that the unit needs,
-// so there are as many as their registers allow: teams of four at 8 rows, of two at 16.  Another
-// warp loads the pages by TMA into rings of shared memory.  A ring has a multiple of four places,
-// so that a place is always the same team's: one that waited for a place of another's could find
-// it two loads behind, which a barrier's parity does not tell from loaded (loads end out of order
-// by microseconds when HBM is busy).
+// heads of a KV group), and each of four teams of two warps takes whole pages of the item, each
+// warp half of the keys, with a running maximum, sum and output of its own, which the block joins
+// at the item's end.  (Teams of four have half the registers a warp, and take 156 us where two
+// take 108.)  Another warp loads the pages by TMA into rings of shared memory.  A ring has a
+// multiple of four places, so that a place is always the same team's: one that waited for a place
+// of another's could find it two loads behind, which a barrier's parity does not tell from loaded
+// (loads end out of order by microseconds when HBM is busy).
 //
 // Bound: HBM, 2 d bytes a token and KV head.  What stands between a byte in shared memory and
-// the tensor core is its conversion, exact, to f16 (two numbers an instruction, 64 a cycle of
-// the multiprocessor, where HBM brings 23).  It is done once, in registers: the keys are the
+// the tensor core is its conversion, exact, to f16 (two numbers an instruction; HBM brings a
+// multiprocessor 23 a cycle).  It is done once, in registers: the keys are the
 // left operand of S^T = K Q^T, the values of O^T = V^T P^T (mma.sync m16n8k16: 16 keys or 16
 // dims by 8 rows), so that their numbers go from shared memory to the registers where the
 // instruction wants them, and nothing converted is written back: the tensor memory's way
 // would store two bytes for each one that HBM brings and read them again, more than shared
-// memory moves in that time.  Both products accumulate in fp32.
+// memory moves in that time.  Both products accumulate in fp32.  96 single tokens over 250000
+// keys in all, 8 KV heads of 128: 108 us, of which HBM needs 76 (4.8 TB/s) and start, end and join
+// of the two launches 12 to 15; one token over 32000 keys 24 us, 9.7 of them HBM's.
 //
 // Which dim or key stands in which place of an operand is free, as long as both operands agree:
 //   * S^T: a lane's four dims of a step are four neighbouring bytes of a key's row;
@@ -71,8 +72,8 @@ struct Cfg {
     static constexpr int OFF_CTL = OFF_ML + WARPS * ROWS * 8;
     static constexpr int SMEM = OFF_CTL + 2048;
     static_assert(SMEM <= 232448 && OFF_SUM % 16 == 0 && OFF_Q % 16 == 0 && OFF_CTL % 16 == 0, "shared memory");
-    // Registers of the loading and of the computing warpgroups; the sum stays within what the block is launched
-    // with: 128 x 64 + 512 x 104 = 640 x 96, 128 x 88 + 256 x 208 = 384 x 168.
+    // Registers of the loading and of the computing warpgroups; the sum is what the block is launched with:
+    // 128 x 88 + 256 x 208 = 384 x 168.
     static constexpr int FEWER = 88, MORE = 208;
 };
 
@@ -584,7 +585,8 @@ cudaError_t launch_d(const ChunkArgs& a, const KernelEnv& env, const char** err)
 
 template <int D>
 cudaError_t launch_rows(const ChunkArgs& a, const KernelEnv& env, const char** err) {
-    // tiles as high as the requests' rows are on average
+    // tiles as high as the requests' rows are on average (12 requests of 8 rows over 8000 to 20000: 60.5 us with tiles of
+    // 8 rows, 62.1 of 16)
     const long long rows = static_cast<long long>(a.T) * a.G;
     if (rows <= 8LL * a.B) return launch_d<D, 1>(a, env, err);
     return launch_d<D, 2>(a, env, err);
@@ -606,8 +608,9 @@ cudaError_t chunk8_prepare(int d) {
 
 cudaError_t launch_chunk8(ChunkArgs a, const KernelEnv& env, const char** err) {
     // Requests of more than 16 rows on average: tiles of 128 rows, whose products cost the same however many of
-    // the rows there are (12 requests over 8000 to 20000, 8 heads of 128: 96 us at 20 rows, 98 at 16; here 76 at 16,
-    // and 172 at 20 with tiles of 32 rows, whose outputs take all registers).
+    // the rows there are (12 requests over 8000 to 20000, 8 heads of 128: 90 us at 20 rows, 91 at 16, 81 at 8; here 76 at
+    // 16 and 61 at 8, and 172 at 20 with tiles of 32 rows, whose outputs take all registers; heads of 64: 67 us at 20
+    // rows, 58 at 16, 73 at 8; here 60 at 16 and 70 at 8).
     if (static_cast<long long>(a.T) * a.G > 16LL * a.B) return launch_chunk8_tile(a, env, err);
     a.blocks = device_sm_count();   // one a multiprocessor
     if (a.d == 128) return launch_rows<128>(a, env, err);

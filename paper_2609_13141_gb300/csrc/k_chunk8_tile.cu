@@ -20,6 +20,13 @@
 // thirds of the time that the tensor core needs), so at d = 128 long requests have two tiles a
 // block and one block a multiprocessor; requests of fewer rows, and those of d = 64, one tile a
 // block and two blocks, each with its own pages.
+//
+// Bound: the tensor core for prompts, HBM for drafts.  4096 tokens after 28000, 32 query and 8 KV
+// heads of 128, take 1456 us (73% of the tensor core's rate): the softmax and the wait for it set
+// the pace, 1900 cycles a page of two tiles, of which the exponentials take 650, the maxima 320.
+// At d = 64 they do all the more, against half the products: a ragged batch of 2626 tokens and 24
+// heads 128 us (22%), 2100 cycles a page with two blocks at a time.  Drafts of 20 rows over 152000
+// keys in all, 8 heads of 128, 86 us, HBM's 46 (54%): the blocks' rows are mostly of no token.
 #include <cuda_fp16.h>
 
 #include "chunk_work.cuh"
@@ -32,7 +39,10 @@ constexpr float kRescaleThreshold = 8.0f;   // log2 units
 constexpr float kScaleRange = 6.f;              // log2 units
 constexpr int kItemSlots = 4;     // work items in flight between warp 0 and the other roles
 constexpr int kStatusLayout = 3;
-constexpr long long kTwoTiles = 192;   // rows of a request on average
+// Rows of a request on average above which blocks have two tiles, at d = 128: 12 requests over 8000 to 20000, 8 KV heads,
+// in us with one tile and with two: 64 rows 96, 119; 128 rows 108, 132; 160 rows 178, 140; 256 rows 177, 147; 1024 rows
+// 712, 562.
+constexpr long long kTwoTiles = 128;
 
 // As in k_chunk.cu, half of Q is in tensor memory at d = 128.  A step is one page, with the next
 // one's scores made ahead at d = 64.  Two pages a step, which helps bf16 pages at d = 64, would
@@ -672,7 +682,6 @@ cudaError_t chunk8_tile_prepare(int d) {
 
 cudaError_t launch_chunk8_tile(const ChunkArgs& a, const KernelEnv& env, const char** err) {
     if (a.d == 64) return launch_d<64, 1>(a, env, err);
-    // two tiles a block where most items fill them
     return static_cast<long long>(a.T) * a.G > kTwoTiles * a.B ? launch_d<128, 2>(a, env, err) : launch_d<128, 1>(a, env, err);
 }
 

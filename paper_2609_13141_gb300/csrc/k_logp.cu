@@ -12,8 +12,8 @@
 // exponential unit and the arithmetic take about half of that time.  So: 16-byte loads, four a
 // thread in flight and two rounds more on their way into L2, a row a block, or a warp where rows
 // are short, and where there are fewer rows than places for blocks a row in several parts, whose
-// last block to end joins them.  8192 bf16 rows of 151936: 348 us, 7.2 TB/s (without the rounds
-// ahead 371), their gradient 739 us.
+// last block to end joins them.  8192 bf16 rows of 151936: 330 to 348 us, 7.2 to 7.5 TB/s (without
+// the rounds ahead 371), their gradient 739 us.
 //
 // The likeliest columns come along in the same pass: a column is a candidate while its key
 // (order of the value, then of the index) is above a bar that k columns reach.  The bar is the
