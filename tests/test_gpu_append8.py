@@ -238,3 +238,53 @@ def test_refusals():
     ch.append8(**case)
     assert sas.sas_chunk_launch_count(ch.h) == 1
     ch.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(8, 8, 64), (16, 8, 128)])
+def test_batches_of_wide_windows(Hq, Hkv, d):
+    """So many tokens that a block looks at more than eight at a time: the bits of the same requests a few at a time."""
+    rng = np.random.default_rng(d)
+    lens = [(int(rng.integers(0, 200)), n) for n in [1] * 900 + [5, 9, 64, 65, 130] * 4 + [1000, 777, 2000, 1500] + [1] * 70]
+    case = _case(lens, Hq, Hkv, d, d)
+    T, pages = case["qkv"].shape[0], case["K_scale"].shape[0]
+    assert T * Hkv > 40 * 8 * torch.cuda.get_device_properties(0).multi_processor_count
+    few = {k: v.clone() for k, v in case.items()}
+    ch = sas.SasChunk(len(lens), Hq, Hkv, d, 64, pages, T)
+    Q = ch.append8(**case)
+    at, parts = 0, []
+    while at < T:          # whole requests
+        n, t = at, 0
+        for _, new in lens:
+            if t >= at and t + new - at <= max(400, new):
+                n = t + new
+            t += new
+        part = {k: v[at:n] if k in ("qkv", "positions", "slots") else v for k, v in few.items()}
+        parts.append(ch.append8(**part))
+        at = n
+    assert len(parts) > 5 and torch.equal(torch.cat(parts), Q)
+    assert all(torch.equal(few[k].view(torch.uint8), case[k].view(torch.uint8)) for k in ("K_cache", "V_cache"))
+    live = (case["slots"] // 64).unique()
+    assert all(torch.equal(few[k][live], case[k][live]) for k in ("K_scale", "V_scale"))
+    assert sas.sas_chunk_get_device_status(ch.h) == sas.SAS_OK
+
+
+def test_captured_and_on_another_stream():
+    case = _case([(0, 70), (5, 1), (64, 9), (10, 1)], 4, 2, 128, 128)
+    start = {k: v.clone() for k, v in case.items()}
+    ch = sas.SasChunk(4, 4, 2, 128, 64, case["K_scale"].shape[0], 81)
+    want = {k: v.clone() for k, v in case.items()}
+    Q = ch.append8(**want)
+    out, side = torch.empty_like(Q), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        ch.append8(**case, out=out)
+    for _ in range(2):
+        for k in ("K_cache", "V_cache", "K_scale", "V_scale"):
+            case[k].copy_(start[k])
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, Q)
+        for k in ("K_cache", "V_cache", "K_scale", "V_scale"):
+            assert torch.equal(case[k].contiguous().view(torch.uint8), want[k].contiguous().view(torch.uint8)), k
