@@ -653,7 +653,10 @@ cudaError_t launch_bwd(LogpBwdArgs a, const KernelEnv& env) {
     const bool small = a.V <= kSmallRow;
     a.parts = 1;
     a.chunk = a.V;
-    if (!small) split_rows(a.rows, a.V, 4 * 8 * device_sm_count(), a.parts, a.chunk);
+    // several waves of blocks, which have nothing to join at their end, in parts of as many bytes for either type (us, of
+    // 777 rows of 32003: fp32 with 32 places a multiprocessor 32.9, with 6 37.7; bf16 with 16 21.3, with 32 22.6)
+    const int places = 8 * static_cast<int>(sizeof(E)) * device_sm_count();
+    if (!small) split_rows(a.rows, a.V, places, a.parts, a.chunk);
     const dim3 grid(small ? (a.rows + kThreads / 32 - 1) / (kThreads / 32) : a.rows * a.parts);
     return launch_early(small ? logp_bwd_kernel<E, 32> : logp_bwd_kernel<E, kThreads>, grid, kThreads, 0, env.stream, a);
 }
