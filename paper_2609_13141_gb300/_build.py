@@ -21,7 +21,7 @@ LIB_PATH = os.path.join(HERE, "libsas.so")
 
 SOURCES = ["sas_api.cu", "k_gemm.cu", "k_pool.cu", "k_select.cu", "k_attn.cu", "sas_noalloc.cu", "k_decode.cu",
            "sas_decode.cu", "k_bwd.cu", "k_rope.cu", "k_serve.cu", "k_chunk.cu", "sas_chunk.cu", "k_logp.cu", "k_chunk8.cu", "k_chunk8_tile.cu"]
-HEADERS = ["ptx.cuh", "internal.h", "serve_ptx.cuh", "serve.h", "chunk_work.cuh"]
+HEADERS = ["ptx.cuh", "internal.h", "serve_ptx.cuh", "serve.h", "chunk_work.cuh", "chunk8.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CFLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC",
                  "--expt-relaxed-constexpr", "-I", INCLUDE]

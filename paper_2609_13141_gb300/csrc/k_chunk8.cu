@@ -38,6 +38,7 @@
 // moved where a page's is further off).
 #include <cuda_fp16.h>
 
+#include "chunk8.cuh"
 #include "chunk_work.cuh"
 
 namespace sas {
@@ -378,7 +379,7 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int row = n * 8 + 2 * t + e;
-                    cr[n][e] = ctl.row_scale[row] * ks;
+                    cr[n][e] = score_factor(ctl.row_scale[row], ks);
                     if (late) {
                         const int lim = x.pos0 + (row >> gl) - first;   // its last key of the page
 #pragma unroll

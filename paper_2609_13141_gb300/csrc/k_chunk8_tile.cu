@@ -29,6 +29,7 @@
 // keys in all, 8 heads of 128, 86 us, HBM's 46 (54%): the blocks' rows are mostly of no token.
 #include <cuda_fp16.h>
 
+#include "chunk8.cuh"
 #include "chunk_work.cuh"
 
 namespace sas {
@@ -538,7 +539,7 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
 #pragma unroll
                     for (int j = 0; j < 4; ++j) mx[j] = max3f(mx[j], xs[k + 2 * j], xs[k + 2 * j + 1]);
                 }
-                const float cr = row_scale * sc.x;
+                const float cr = score_factor(row_scale, sc.x);
                 const float mb = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * cr;
                 const bool need = valid && mb > m_use + kRescaleThreshold;
                 const float m_new = need ? mb : m_use;

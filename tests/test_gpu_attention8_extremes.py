@@ -1,0 +1,65 @@
+"""Attention over an 8-bit cache where the scales of pages or the sizes of queries are extreme: the scores' factor (query times
+key scale) outside fp32's range, value scales of one request at either end of what the append writes.  Cases, plain form and
+bounds are test_gpu_attention8's."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_13141_gb300 import sas
+from tests.test_gpu_attention8 import DEV, E4, I32, _case, _chunk, _compare, _plain
+
+pytestmark = pytest.mark.gpu
+
+# heads a KV head, requests: each of the kernels at its heights (8 and 16 rows a tile, one and two 128-row tiles a block), with
+# pages of which rows see a part, requests of one token and requests of many splits
+SHAPES = [(4, [(500, 1), (90, 1), (0, 1), (63, 1)]), (8, [(9000, 1)]), (2, [(500, 5), (3, 5), (700, 4)]), (1, [(7000, 16)]),
+          (2, [(500, 30), (90, 9), (0, 1)]), (1, [(6000, 64)]), (4, [(700, 90), (3, 40), (64, 1)]), (1, [(4000, 300)])]
+
+
+def _dead(case, head):
+    """The keys of a request's last page and of every second one before it become zero, as a step on zeros leaves them."""
+    K, sk, table = case[1], case[3], case[5]
+    for p in (p for row in table.tolist() for p in [p for p in row if p >= 0][::-2]):
+        x = K.view(torch.uint8)[p, head]
+        x[(x & 0x7F) != 0x7F] = 0          # what no token sees stays NaN
+        sk[p, head] = 2.0 ** -64
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,lens", SHAPES)
+def test_zero_and_tiny_queries_over_zero_keys(G, lens, d):
+    """A product of 0 between finite numbers is a score of 0, however small query and scale are."""
+    case = _case(lens, 2 * G, 2, d, seed=G + d)
+    Q = case[0]
+    _dead(case, 0)
+    _dead(case, 1)
+    Q[:, 0] = 0
+    Q[::2, G - 1] *= 2.0 ** -120
+    Q[1::2, G] = 0
+    ch = _chunk(case)
+    O, LSE = ch.attention8(*case)
+    _compare(O, LSE, case, 1 / math.sqrt(d))
+    assert sas.sas_chunk_get_device_status(ch.h) == sas.SAS_OK
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,new", [(4, [1, 1, 3]), (2, [70, 10, 33]), (4, [400, 130])])
+def test_a_step_on_zeros(G, new, d):
+    """append8 of zero rows, attention8 over what it wrote: zeros, and the logarithm of how many."""
+    B, T = len(new), sum(new)
+    table = torch.arange(8 * B, dtype=I32, device=DEV).view(B, 8)
+    ch = sas.SasChunk(B, 2 * G, 2, d, 8, 8 * B, T)
+    K, V = (torch.full((8 * B, 2, 64, d), 0x7F, dtype=torch.uint8, device=DEV).view(E4) for _ in range(2))
+    sk, sv = (torch.full((8 * B, 2), math.nan, device=DEV) for _ in range(2))
+    one, turn = torch.ones(d, device=DEV, dtype=torch.bfloat16), torch.rand(512, d // 2, device=DEV)
+    n = torch.tensor(new, dtype=I32, device=DEV)
+    pos = torch.cat([torch.arange(k, dtype=I32, device=DEV) for k in new])
+    slots = torch.cat([table[b].long().repeat_interleave(64)[:k] * 64 + torch.arange(k, device=DEV) % 64 for b, k in enumerate(new)])
+    cu = torch.cat([torch.zeros(1, dtype=I32, device=DEV), n.cumsum(0, dtype=I32)])
+    Q = ch.append8(torch.zeros(T, 2 * G + 4, d, device=DEV, dtype=torch.bfloat16), one, one, turn.cos(), turn.sin(), pos, slots, K, V, sk, sv)
+    assert (Q == 0).all()
+    O, LSE = ch.attention8(Q, K, V, sk, sv, table, cu, n)
+    assert (O == 0).all()
+    assert ((LSE - (pos + 1).float().log()[:, None]).abs() < 2.0 ** -15).all()
+    assert sas.sas_chunk_get_device_status(ch.h) == sas.SAS_OK
