@@ -63,3 +63,32 @@ def test_a_step_on_zeros(G, new, d):
     assert (O == 0).all()
     assert ((LSE - (pos + 1).float().log()[:, None]).abs() < 2.0 ** -15).all()
     assert sas.sas_chunk_get_device_status(ch.h) == sas.SAS_OK
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,lens", SHAPES)
+def test_scores_below_the_least_number(G, lens, d):
+    """A key whose score is under -2^128 has no weight; its page's other scores are 0, as its zero keys have it."""
+    case = _case(lens, G, 1, d, seed=G + d, poison=False)
+    Q, K, V, sk, sv, table, cu, kv = case
+    K.view(torch.uint8).zero_()
+    Q.zero_()
+    Q[..., 3] = 2.0 ** 60
+    first = table[:, 0].long()
+    K.view(torch.uint8)[first, 0, 0, 3] = 0xB8          # -1
+    sk[first] = 2.0 ** 100
+    ch = _chunk(case)
+    O, LSE = ch.attention8(*case)
+    for b, L in enumerate(kv.tolist()):
+        t0, t1 = int(cu[b]), int(cu[b + 1])
+        pages = table[b, :-(-L // 64)].long()
+        v = (V.view(torch.uint8)[pages, 0].view(E4).double() * sv[pages, 0].double()[:, None, None]).reshape(-1, d)[:L]
+        for t in range(t0, t1):
+            n = L - t1 + t      # keys but the first one
+            if n == 0:
+                continue        # a row of such a key alone: its largest score is -infinity in fp32
+            # uniform weights: fp16 sums of 1 are exact, fp32 sums and the output's rounding are left
+            ref, size = v[1:n + 1].mean(0), v[1:n + 1].abs().mean(0)
+            assert ((O[t].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -16 * size).all(), t
+            assert (LSE[t] - math.log(n)).abs().max() < 2.0 ** -15
+    assert sas.sas_chunk_get_device_status(ch.h) == sas.SAS_OK
