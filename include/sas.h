@@ -734,7 +734,10 @@ sas_status sas_chunk_attention(sas_chunk_handle* h, int32_t num_seqs, int32_t T,
 
 /* sas_chunk_attention over an 8-bit cache (see sas_chunk_append8), the same otherwise: sums
  * and softmax in fp32, the weights rounded to fp16.  A value's NaN reaches earlier rows of
- * its tile as there.  Scales must be positive and finite.  Two launches. */
+ * its tile as there.  Scales must be positive, finite and not subnormal.  Sums of values
+ * stand under a power of two that follows the scales of a request's pages, however far
+ * apart: beside a page of a larger scale they keep what is above 2^-149 of it.  Two
+ * launches. */
 sas_status sas_chunk_attention8(sas_chunk_handle* h, int32_t num_seqs, int32_t T, const void* Q, const void* K_cache,
                                 const void* V_cache, const float* K_scale, const float* V_scale,
                                 const int32_t* block_table, const int32_t* cu_new, const int32_t* kv_lens, void* O,

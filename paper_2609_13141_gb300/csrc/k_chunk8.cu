@@ -35,7 +35,7 @@
 // 2^14: bf16 numbers down to 2^-31 of the row's largest are exact, less is below the sum's own
 // rounding.  P is f16, at most 2^8 (the maximum is moved when a row's sum would pass that) times
 // the page's value scale over that of the accumulator, within 2^-6 .. 2^6 (the accumulator is
-// moved where a page's is further off).
+// moved where a page's is further off; where it cannot follow, chunk8.cuh, P is smaller).
 #include <cuda_fp16.h>
 
 #include "chunk8.cuh"
@@ -308,6 +308,7 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             for (int i = 0; i < MT; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
         }
         float v_ref = 0.f;   // what one of o stands for; 0: nothing yet
+        bool large = false;  // a scale was above kLargeScale
         const int np = x.blk1 - x.blk0;
         for (int i = (static_cast<int>(warp / C::TEAM) - g0) & (kTeams - 1); ok && i < np; i += kTeams) {
             const int g = g0 + i, s = g % C::ST, m = x.blk0 + i;
@@ -321,15 +322,38 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             constexpr int KT = 4 / C::TEAM;   // 16-key steps of a warp's share
             const int share = warp % C::TEAM;
             if (v_ref == 0.f) v_ref = vs;
+            large |= vs > kLargeScale;
             if (!(vs <= kScaleRange * v_ref && vs * kScaleRange >= v_ref)) {
-                const float f = v_ref / vs;
+                float f = v_ref / vs;
+                if (f <= 1.f) {
+                    if (f < kFarRise) {
+                        f = v_ref * kRiseRest / vs;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int y = 0; y < MT; ++y)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[y][n][e] *= kRiseStep;
+                    }
+                    v_ref = vs;
+                } else {
+                    float top = 0.f;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int y = 0; y < MT; ++y)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) top = fmaxf(top, finite_size(o[y][n][e]));
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    f = move_unit(v_ref, vs, top);
+                }
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int y = 0; y < MT; ++y)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[y][n][e] *= f;
-                v_ref = vs;
             }
             const float ratio = vs / v_ref;
             // ---- S^T = K Q^T
@@ -491,6 +515,17 @@ chunk8_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             if (lane == 0) mbar_arrive(&ctl.v_empty[s]);
         }
         g0 += np;
+        if (large) {
+            v_ref *= kShrinkFactor;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    m_use[n][e] += kShrink;
+                    l[n][e] *= kShrinkFactor;
+                }
+            }
+        }
 
         // ---- the warps' results, joined in the warps' order
 #pragma unroll

@@ -38,6 +38,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescaleThreshold = 8.0f;   // log2 units
 constexpr float kScaleRange = 6.f;              // log2 units
+constexpr float kLeast = 1099511627776.f, kLeastLog = 40.f;   // a unit over a page's scale, in P: 2^40
 constexpr int kItemSlots = 4;     // work items in flight between warp 0 and the other roles
 constexpr int kStatusLayout = 3;
 // Rows of a request on average above which blocks have two tiles, at d = 128: 12 requests over 8000 to 20000, 8 KV heads,
@@ -496,16 +497,18 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
             const int pos = x.pos0 + tok;
             float m_use = -CUDART_INF_F, l = 0.f;
             float v_ref = 0.f, v_log = 0.f;   // what one of O stands for
+            bool large = false;               // a scale was above kLargeScale
             for (int m = x.blk0; m < x.blk1; ++m, ++g, ++gt) {
                 // last key column of the page that this row sees (< 0: none).  Rows of no token are never read: they
                 // go unmasked.
                 const int lim = valid ? min(NK - 1, pos - m * kBN) : NK - 1;
                 const int buf = gt % C::NS;
                 if (!mbar_wait_warp(&ctl.sc_full[tile][buf], (gt / C::NS) & 1, wc)) { ok = false; break; }
-                const float4 sc = ctl.scale[g % C::SCALES];
+                float4 sc = ctl.scale[g % C::SCALES];
                 if (m == x.blk0) {
                     v_log = sc.y;
                     v_ref = sc.w;
+                    large = v_ref > kLargeScale;
                 }
                 // P is free, and O another product's no more, once the product before has read and written them
                 auto product_done = [&] { return gt == 0 || mbar_wait_warp(&ctl.pv_done[tile], (gt - 1) & 1, wc); };
@@ -549,14 +552,43 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
                 l *= factor;
                 // O stands under another value scale from here on
                 const bool move = !(fabsf(sc.y - v_log) <= kScaleRange);
-                if (move) {
-                    factor *= v_ref * sc.z;
-                    v_ref = sc.w;
-                    v_log = sc.y;
-                }
                 if (m > x.blk0 && __any_sync(0xffffffffu, need || move)) {
                     if (!product_done()) { ok = false; break; }
                     tc_fence_after();
+                    if (__any_sync(0xffffffffu, move)) {
+                        float fall = v_ref * sc.z;
+                        const bool falls = !(fall <= 1.f), far = move && fall < kFarRise;
+                        if (far) fall = v_ref * kRiseRest * sc.z;
+                        const float step = far ? kRiseStep : 1.f;
+                        float top = 0.f;
+#pragma unroll 1
+                        for (int cc = 0; cc < D / 32; ++cc) {
+                            uint32_t o[32];
+                            tmem_ld32(lane_addr + C::TMEM_O + cc * 32, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                top = fmaxf(top, fabsf(__uint_as_float(o[e])));
+                                o[e] = __float_as_uint(__uint_as_float(o[e]) * step);
+                            }
+                            tmem_st32(lane_addr + C::TMEM_O + cc * 32, o);
+                        }
+                        tmem_wait_st();
+                        if (move) {
+                            v_log = sc.y;
+                            if (falls) fall = move_unit(v_ref, sc.w, top * factor);
+                            else v_ref = sc.w;
+                            factor *= fall;
+                            large |= sc.w > kLargeScale;
+                            if (v_ref != sc.w) {
+                                // under a unit that could not follow, P goes no lower than where nothing is left of it in f16: the row's
+                                // sum needs its exponentials
+                                v_log = log2f(v_ref);
+                                sc.y = fmaxf(sc.y, v_log - kLeastLog);
+                                sc.z = fminf(sc.z, kLeast / v_ref);
+                            }
+                        }
+                    }
 #pragma unroll 1
                     for (int cc = 0; cc < D / 32; ++cc) {
                         uint32_t o[32];
@@ -630,6 +662,11 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, 2 / TILES) chunk8_tile
             // ---- a split: (max, sum) and the unnormalised O of every row in fp32, laid out
             // [quad of columns][row], so that a warp's 32 rows write 512 bytes at a time
             if (warp_rows) {
+                if (large) {
+                    v_ref *= kShrinkFactor;
+                    m_use += kShrink;
+                    l *= kShrinkFactor;
+                }
                 float4* po = reinterpret_cast<float4*>(a.part_o) + (static_cast<size_t>(x.part) * TILES + tile) * (D / 4) * kBM + row;
 #pragma unroll 1
                 for (int cc = 0; cc < D / 32; ++cc) {

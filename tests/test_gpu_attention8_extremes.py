@@ -92,3 +92,62 @@ def test_scores_below_the_least_number(G, lens, d):
             assert ((O[t].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -16 * size).all(), t
             assert (LSE[t] - math.log(n)).abs().max() < 2.0 ** -15
     assert sas.sas_chunk_get_device_status(ch.h) == sas.SAS_OK
+
+
+def _values(case, logs, dead=()):
+    """Scales 2^logs[i] for a request's i-th page of values, over and over; codes of pages from 2^100 on are small, so that
+    their numbers are finite; pages i of `dead` hold zeros."""
+    V, sv, table = case[2], case[4], case[5]
+    for row in table.tolist():
+        for i, p in enumerate([p for p in row if p >= 0]):
+            k = i % len(logs)
+            if logs[k] > 100:
+                V[p] = (V[p].float() / 64).to(E4)
+            if k in dead:
+                V.view(torch.uint8)[p] = 0
+            sv[p] = 2.0 ** logs[k]
+
+
+FAR = [((60, -64), (1,)), ((120, -8, -64, -64), (2, 3)), ((-8, 120, -8), ()), ((120, -126, 60), ()), ((-64, 120, -64, 100, -64), (0, 2, 4)),
+       ((120, 120, 119), ()), ((110, 75, 40, 5, -30, -65, -100), ()), ((120, 85, 50, 15, -20, -55, -64), (6,)), ((120, -8), (0,)), ((-126, -64), ())]
+
+
+@pytest.mark.parametrize("logs,dead", FAR)
+@pytest.mark.parametrize("G,lens,d", [(4, [(500, 1), (90, 1)], 128), (8, [(9000, 1)], 64), (2, [(700, 5)], 128), (2, [(500, 30), (90, 9)], 64),
+                                      (1, [(6000, 64)], 128), (4, [(700, 90)], 128), (1, [(4000, 300)], 128), (1, [(4000, 300)], 64), (2, [(2500, 1)] * 200, 64)])
+def test_value_scales_at_the_ends_of_their_range(G, lens, d, logs, dead):
+    """What a row's output may be off by is in units of its largest values: 2^-25 of them a key (times the spread 64 within which
+    pages share a unit), where its weights are rounded to fp16."""
+    case = _case(lens, G, 1, d, seed=G + d, poison=False)
+    _values(case, logs, dead)
+    ch = _chunk(case)
+    O, LSE = ch.attention8(*case)
+    ref, lse, A, size, U = _plain(*case, 1 / math.sqrt(d))
+    assert (ref.abs() < 2.0 ** 127).all()
+    delta = 2.0 ** -17 * size
+    # the least bf16 number's half, too
+    tol = 2.0 ** -8 * ref.abs() + (2.0 ** -11 + 2.0 ** -16 + 2 * delta[..., None]) * A + 2.0 ** -25 * 64 * U.amax(-1, keepdim=True) + 2.0 ** -134
+    assert O.isfinite().all()
+    assert ((O.double() - ref).abs() <= tol).all(), float(((O.double() - ref).abs() / tol).max())
+    assert ((LSE.double() - lse).abs() <= delta + 2.0 ** -15).all()
+    assert sas.sas_chunk_get_device_status(ch.h) == sas.SAS_OK
+
+
+@pytest.mark.parametrize("G,lens,d", [(4, [(500, 1), (90, 1)], 128), (8, [(9000, 1)], 64), (2, [(700, 5)], 128), (2, [(500, 30)], 64), (4, [(700, 90)], 128),
+                                      (1, [(4000, 300)], 128), (2, [(2500, 1)] * 200, 64), (1, [(2500, 2)] * 100, 128)])
+def test_zero_values_under_any_scale_change_nothing_but_weights(G, lens, d):
+    """Pages of zero values under scales of either end, among ordinary ones: to the precision of the ordinary ones' values."""
+    case = _case(lens, G, 1, d, seed=G + d, poison=False)
+    V, sv, table = case[2], case[4], case[5]
+    for row in table.tolist():
+        for i, p in enumerate([p for p in row if p >= 0]):
+            if i % 3 != 1:
+                V.view(torch.uint8)[p] = 0
+                sv[p] = 2.0 ** (120 if i % 3 == 0 else -64)
+    ch = _chunk(case)
+    O, LSE = ch.attention8(*case)
+    ref, lse, A, size, U = _plain(*case, 1 / math.sqrt(d))
+    delta = 2.0 ** -17 * size
+    tol = 2.0 ** -8 * ref.abs() + (2.0 ** -11 + 2.0 ** -16 + 2 * delta[..., None]) * A + 2.0 ** -25 * 64 * U
+    assert O.isfinite().all() and ((O.double() - ref).abs() <= tol).all()
+    assert ((LSE.double() - lse).abs() <= delta + 2.0 ** -15).all()
