@@ -441,7 +441,9 @@ sas_status sas_token_logprobs(sas_handle* h, int32_t T, int32_t V, const void* l
  *   dlogprob, dentropy  fp32 [T]; dentropy may be NULL (0)                    (in)
  *   dlogits  [T] rows of V, ld_d apart: the logits' own memory (ld_d = ld) or memory
  *            apart from it                                                    (out)
- * Rows that do not count get zeros.  One launch. */
+ * Rows that do not count get zeros.  Results whose rows begin at the same place within 16
+ * bytes as the logits' are written in whole vectors (ld_d = ld will do), others an element
+ * at a time: up to 4 times the time for bf16.  One launch. */
 sas_status sas_token_logprobs_bwd(sas_handle* h, int32_t T, int32_t V, const void* logits, int32_t dtype, int64_t ld,
                                   const int32_t* tokens, const float* lse, const float* entropy, const float* dlogprob,
                                   const float* dentropy, void* dlogits, int64_t ld_d, void* stream);
@@ -618,7 +620,8 @@ int64_t sas_decode_launch_count(const sas_decode_handle* h);
  * prefills before it decodes and has no counterpart of these.)  After a prompt or
  * accepted drafts are in the cache, sas_decode_summarize makes the summaries of the
  * blocks they filled, and sas_decode_step continues on the same cache, block table
- * and lengths.
+ * and lengths.  (Both read bf16 pages; a decode over the 8-bit cache below is the dense
+ * attention of single tokens, sas_chunk_attention8.)
  *
  * Lengths, offsets, slots, page and token indices are read on the device: nothing
  * here synchronises or allocates after sas_chunk_create, and a captured step can be
@@ -736,8 +739,11 @@ sas_status sas_chunk_attention(sas_chunk_handle* h, int32_t num_seqs, int32_t T,
  * and softmax in fp32, the weights rounded to fp16.  A value's NaN reaches earlier rows of
  * its tile as there.  Scales must be positive, finite and not subnormal.  Sums of values
  * stand under a power of two that follows the scales of a request's pages, however far
- * apart: beside a page of a larger scale they keep what is above 2^-149 of it.  Two
- * launches. */
+ * apart: beside a page of a larger scale they keep what is above 2^-149 of it.
+ * Equal inputs give equal bits where T and num_seqs are equal: which kernel runs goes by
+ * rows of a request on average, T Hq / (Hkv num_seqs) (up to 16, up to 128, more), T being
+ * the capacity.  A long prompt chunk is best a call of its own beside many single tokens,
+ * and T no larger than the step needs.  Two launches. */
 sas_status sas_chunk_attention8(sas_chunk_handle* h, int32_t num_seqs, int32_t T, const void* Q, const void* K_cache,
                                 const void* V_cache, const float* K_scale, const float* V_scale,
                                 const int32_t* block_table, const int32_t* cu_new, const int32_t* kv_lens, void* O,

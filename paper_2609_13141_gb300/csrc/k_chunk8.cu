@@ -21,7 +21,7 @@
 // instruction wants them, and nothing converted is written back: the tensor memory's way
 // would store two bytes for each one that HBM brings and read them again, more than shared
 // memory moves in that time.  Both products accumulate in fp32.  96 single tokens over 250000
-// keys in all, 8 KV heads of 128: 108 us, of which HBM needs 76 (4.8 TB/s) and start, end and join
+// keys in all, 8 KV heads of 128: 107 us, of which HBM needs 76 (4.8 TB/s) and start, end and join
 // of the two launches 12 to 15; one token over 32000 keys 24 us, 9.7 of them HBM's.
 //
 // Which dim or key stands in which place of an operand is free, as long as both operands agree:
@@ -646,7 +646,8 @@ cudaError_t launch_chunk8(ChunkArgs a, const KernelEnv& env, const char** err) {
     // Requests of more than 16 rows on average: tiles of 128 rows, whose products cost the same however many of
     // the rows there are (12 requests over 8000 to 20000, 8 heads of 128: 90 us at 20 rows, 91 at 16, 81 at 8; here 76 at
     // 16 and 61 at 8, and 172 at 20 with tiles of 32 rows, whose outputs take all registers; heads of 64: 67 us at 20
-    // rows, 58 at 16, 73 at 8; here 60 at 16 and 70 at 8).
+    // rows, 58 at 16, 73 at 8; here 60 at 16 and 70 at 8).  The average is the batch's: 255 single tokens take 189 us and a
+    // prompt chunk of 2048 tokens 40 (8 heads), but one call of both 488, the chunk in tiles of 16 rows here.
     if (static_cast<long long>(a.T) * a.G > 16LL * a.B) return launch_chunk8_tile(a, env, err);
     a.blocks = device_sm_count();   // one a multiprocessor
     if (a.d == 128) return launch_rows<128>(a, env, err);

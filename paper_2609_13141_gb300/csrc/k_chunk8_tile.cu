@@ -22,11 +22,13 @@
 // block and two blocks, each with its own pages.
 //
 // Bound: the tensor core for prompts, HBM for drafts.  4096 tokens after 28000, 32 query and 8 KV
-// heads of 128, take 1456 us (73% of the tensor core's rate): the softmax and the wait for it set
+// heads of 128, take 1452 to 1482 us (73% of the tensor core's rate): the softmax and the wait for it set
 // the pace, 1900 cycles a page of two tiles, of which the exponentials take 650, the maxima 320.
 // At d = 64 they do all the more, against half the products: a ragged batch of 2626 tokens and 24
-// heads 128 us (22%), 2100 cycles a page with two blocks at a time.  Drafts of 20 rows over 152000
+// heads 130 us (22%), 2100 cycles a page with two blocks at a time.  Drafts of 20 rows over 152000
 // keys in all, 8 heads of 128, 86 us, HBM's 46 (54%): the blocks' rows are mostly of no token.
+// The forms of one tile keep 48 to 56 bytes a thread in local memory: 80 registers at launch do not hold every role.
+// Units that value scales of any distance need (chunk8.cuh) are 1.1 to 1.6% of these times.
 #include <cuda_fp16.h>
 
 #include "chunk8.cuh"

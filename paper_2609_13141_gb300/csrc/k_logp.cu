@@ -567,7 +567,9 @@ __global__ void __launch_bounds__(kThreads) logp_bwd_kernel(LogpBwdArgs a) {
     };
     const int v0 = part * a.chunk;
     const Span<E> sp(z, v0, min(a.V, v0 + a.chunk));
-    // output vectors of the same columns
+    // output vectors of the same columns; where the results' rows lie otherwise within 16 bytes than the logits', stores
+    // of one element (4096 bf16 rows of 32003 out of rows of 32064: 324 us into rows of 32003, 86 into rows of 32064;
+    // fp32 169 and 161)
     const bool same = ((reinterpret_cast<uintptr_t>(dz) ^ reinterpret_cast<uintptr_t>(z)) & 15u) == 0;
     for (int j0 = rank; j0 < sp.count; j0 += U * TEAM) {
         uint4 raw[U];

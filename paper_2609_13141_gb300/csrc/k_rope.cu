@@ -550,8 +550,9 @@ cudaError_t launch_any_bwd(const RopeArgs& a, const KernelEnv& env) {
 // Bound: HBM, a read of the fused rows and a write of the queries and of half as many bytes for
 // keys and values.  15232 tokens of 32 + 2 x 8 heads of 128 take 81.5 us (4.3 TB/s, 64%): the
 // queries' blocks 41, at HBM's rate, the windows' as long, as a block waits for slots, rows,
-// tables, the joint maximum and its stores one after the other, with two blocks of 114 registers
-// a thread at a time (three, with their rows in local memory, 100 us).  96 tokens: 10 us, a launch.
+// tables, the joint maximum and its stores one after the other, with two blocks of 118 registers
+// a thread at a time (106 to 118 by form; three, with their rows in local memory, 100 us).  96
+// tokens: 6.1 us in a captured row of calls, 10 from the host.
 constexpr int kRunRows = 8;                       // of a warp
 constexpr int kMaxWindow = 64;                    // tokens; runs have 64 at most
 static_assert(kWarps * kRunRows >= 64, "a block's longest run is a page");

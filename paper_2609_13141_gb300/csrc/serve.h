@@ -55,8 +55,8 @@ bool rope_supported(const RopeArgs& a);   // the kernels can count this many tok
 int rope_bwd_max_blocks();
 cudaError_t rope_paged_prepare(int d);    // shared-memory limit of the form into cache pages (before any capture)
 cudaError_t launch_rope_fwd(const RopeArgs& a, int d, const KernelEnv& env);
-bool append8_supported(const RopeArgs& a);   // one block a head and 8 tokens
-// Queries to a.Q, keys and values into an 8-bit cache (a.K and a.V are not used): two launches.
+bool append8_supported(const RopeArgs& a);   // blocks of windows: at most one for a head and 8 tokens
+// Queries to a.Q, keys and values into an 8-bit cache (a.K and a.V are not used): one launch.
 cudaError_t launch_append8(const RopeArgs& a, const Cache8& c, int d, const KernelEnv& env);
 cudaError_t launch_rope_bwd(const RopeArgs& a, int d, const KernelEnv& env);
 

@@ -677,7 +677,8 @@ class SasLayer:
         return out
 
     def token_logprobs_bwd(self, logits, tokens, lse, entropy, dlogprob, dentropy=None, out=None, stream=None):
-        """Returns dlogits [T, V] in the logits' type; out reuses the caller's (the logits themselves, for one)."""
+        """Returns dlogits [T, V] in the logits' type; out reuses the caller's (the logits themselves, for one).  For logits that
+        are a view of wider rows, out had best be a view of as wide ones: rows that lie alike are written faster."""
         if out is None:
             with _on(stream):
                 out = torch.empty(logits.shape, device=logits.device, dtype=logits.dtype)
@@ -1011,7 +1012,7 @@ class SasChunk:
 
     Owns one handle; allocates the outputs (on the stream the call runs on) unless the caller
     passes its own, as a captured graph needs.  K_cache, V_cache [num_pages, Hkv, 64, d] and
-    block_table [requests, max_blocks] are those of SasDecoder."""
+    block_table [requests, max_blocks] are those of SasDecoder (which has no 8-bit form)."""
 
     def __init__(self, max_seqs, Hq, Hkv, d, max_blocks, num_pages, max_tokens, sm_scale=0.0):
         self.Hq, self.Hkv, self.d, self.max_blocks = Hq, Hkv, d, max_blocks
@@ -1067,7 +1068,8 @@ class SasChunk:
         return out
 
     def attention8(self, Q, K_cache, V_cache, K_scale, V_scale, block_table, cu_new, kv_lens, out=None, stream=None):
-        """attention over an 8-bit cache (append8).  Returns (O [T, Hq, d], LSE [T, Hq]); out as in attention."""
+        """attention over an 8-bit cache (append8).  Returns (O [T, Hq, d], LSE [T, Hq]); out as in attention.  Its kernel goes by
+        the rows that requests have on average: a long chunk beside many single tokens had best be a call of its own."""
         if out is None:
             with _on(stream):
                 out = (torch.empty_like(Q), torch.empty(Q.shape[:2], device=Q.device, dtype=torch.float32))
